@@ -53,9 +53,16 @@ extern "C" {
 #define SPD_MAX_ROWS         64    /* rows (n_seqs * M) per forward call          */
 #define SPD_MAX_M             8    /* new tokens per sequence per forward call    */
 
+#define SPD_MAX_TOP          32    /* alternatives per row of spd_token_logprobs      */
+
 /* flags of spd_speculative_accept */
 #define SPD_TARGET_IS_PROBS  1u    /* target rows are probabilities, not logits   */
 #define SPD_DRAFT_IS_PROBS   2u    /* draft rows are probabilities, not logits    */
+
+/* flags of spd_token_logprobs, spd_q4_quantize / spd_q4_dequantize, spd_q4_matmul */
+#define SPD_ROWS_ARE_PROBS   1u    /* rows are probabilities, not logits          */
+#define SPD_W_IS_BF16        1u    /* weights bfloat16, else float32              */
+#define SPD_X_IS_BF16        1u    /* activations bfloat16, else float32          */
 
 typedef struct spd_model spd_model;
 
@@ -88,6 +95,27 @@ typedef struct {
     const void  *const *w_down;      /* bf16 [d_model, d_ffn]                      */
 } spd_weights;
 
+/* A matrix [out_features N, in_features K] in 4 bits: W[n][k] = scale[n][k / group] * q[n][k].
+ *   q       uint8 [N, ceil(K / 2)]: integers -8..7 in two's complement, even columns in the low half of their byte
+ *   scales  bfloat16 [N, ceil(K / group)]; group is 32, 64 or 128, the last group of a row may be shorter
+ * Both device memory.  spd_q4_quantize makes them; any other quantiser's in this form will do. */
+typedef struct {
+    const void *q, *scales;
+} spd_q4_matrix;
+
+/* Weights of a model whose matrices are in 4 bits (shapes as in spd_weights; embedding table bfloat16, gains float32).
+ * lm_head is always given, also with tied embeddings. */
+typedef struct {
+    int32_t       group;
+    const void   *embed;
+    spd_q4_matrix lm_head;
+    const float  *final_norm;
+    const float *const *attn_norm;                    /* per layer, as in spd_weights */
+    const spd_q4_matrix *wq, *wk, *wv, *wo;
+    const float *const *mlp_norm;
+    const spd_q4_matrix *w_gate, *w_up, *w_down;
+} spd_weights_q4;
+
 /* Description of the last error on this thread ("" if none).  Host pointer,
  * valid until the next failing call on the same thread. */
 const char *spd_last_error(void);
@@ -108,6 +136,18 @@ int32_t spd_model_create(const spd_model_config *h_cfg, const spd_weights *h_wei
                          void *packed, size_t packed_bytes, void *kv_cache, size_t kv_bytes,
                          void *workspace, size_t workspace_bytes, void *stream,
                          spd_model **h_out);
+
+/* The same for a model whose matrices stay in 4 bits (spd_weights_q4): 3.8 times fewer bytes per step at groups of 128.  All
+ * calls on such a model are those of any other; its products are as exact as the bf16 model's (float32 activations and sums),
+ * so it differs from a bf16 model of the dequantised weights by float32 rounding only.  A row of activations with a
+ * value that is not finite gives NaN.  Prompts run in passes of 64 rows; of spd_tuning only the attention's fields and
+ * wait_spin_limit have an effect.  Errors as spd_model_create, SPD_ERR_SHAPE for another group. */
+int32_t spd_model_bytes_q4(const spd_model_config *h_cfg, int32_t group, size_t *h_packed_bytes,
+                           size_t *h_kv_bytes, size_t *h_workspace_bytes);
+int32_t spd_model_create_q4(const spd_model_config *h_cfg, const spd_weights_q4 *h_weights,
+                            void *packed, size_t packed_bytes, void *kv_cache, size_t kv_bytes,
+                            void *workspace, size_t workspace_bytes, void *stream,
+                            spd_model **h_out);
 
 int32_t spd_model_destroy(spd_model *model);
 
@@ -242,6 +282,54 @@ int32_t spd_speculative_accept_static(const float *target, const float *draft, c
                                       const float *u, int32_t n_seqs, int32_t gamma, int32_t vocab,
                                       float temperature, uint32_t flags, int32_t *n_accepted_out,
                                       int32_t *next_token_out, float *accept_prob_out, void *stream);
+
+/* Log probabilities of given tokens, entropy and the most likely alternatives of rows: what a serving program returns
+ * with a token, and how sure a draft is.  Rows may be those of spd_verify_forward, or (SPD_ROWS_ARE_PROBS) of spd_draft_step.
+ *   rows    float32 [n_rows, vocab], row_stride elements apart: logits, or probabilities
+ *   tokens  int32 [n_rows]; NULL if neither logprob_out nor rank_out is wanted
+ *   logprob_out       float32 [n_rows] or NULL: lp(x) = z_x - log(sum exp z) of z = logits / temperature, or log(row[x])
+ *   entropy_out       float32 [n_rows] or NULL: -sum p lp, in nats
+ *   rank_out          int32 [n_rows] or NULL: entries before the token in descending order, equal ones by index (0: the first)
+ *   top_tokens_out    int32, top_logprobs_out float32 [n_rows, n_top]: the first n_top entries in that order (0 <= n_top <= SPD_MAX_TOP)
+ *   workspace         scratch of spd_logprobs_workspace_bytes bytes (which may be 0; then it may be NULL), 16-byte aligned; it may hold
+ *                     anything before the call and nothing in it has to survive it.  Calls that share one must not overlap.
+ * temperature > 0 (temperature 0 leaves no log probabilities: ask for those at 1); ignored for probabilities.
+ * Entries at -infinity (probability 0) weigh nothing and are no alternatives: places they leave hold token -1 and -infinity.  A
+ * row of nothing else: log probability -infinity, entropy 0.  A token outside 0..vocab-1: -infinity, rank vocab.  A row with a NaN or
+ * +infinity (probabilities: a negative or infinite one or a NaN) has no distribution: NaN, rank and alternatives -1.
+ * Errors: SPD_ERR_INVALID_ARG, SPD_ERR_CAPACITY (workspace too small). */
+int32_t spd_logprobs_workspace_bytes(int32_t n_rows, int32_t vocab, int32_t n_top, size_t *h_bytes);
+int32_t spd_token_logprobs(const float *rows, size_t row_stride, const int32_t *tokens, int32_t n_rows, int32_t vocab,
+                           float temperature, uint32_t flags, float *logprob_out, float *entropy_out, int32_t *rank_out,
+                           int32_t n_top, int32_t *top_tokens_out, float *top_logprobs_out,
+                           void *workspace, size_t workspace_bytes, void *stream);
+
+/* ---- weights in 4 bits (format: spd_q4_matrix) -----------------------------------------------------
+ * spd_q4_quantize: a = the largest magnitude of a group, scale = a / 7 rounded to bfloat16, q = w / scale rounded to the nearest
+ * integer (even on ties), limited to -8..7; 0 where the scale is 0.  A group with a value that is not finite: scale NaN, q 0.
+ * w: float32, or bfloat16 with SPD_W_IS_BF16, [N, K] with w_stride elements between rows.
+ * spd_q4_dequantize: the values that q and scales stand for (rounded once if bfloat16).
+ * spd_q4_pack: re-tiles a matrix for the matrix cores into `packed` (spd_q4_bytes bytes, 256-byte aligned), which spd_q4_matmul reads.
+ * Errors: SPD_ERR_INVALID_ARG, SPD_ERR_SHAPE (N or K < 1, another group), SPD_ERR_CAPACITY. */
+int32_t spd_q4_bytes(int32_t N, int32_t K, int32_t group, size_t *h_packed_bytes);
+int32_t spd_q4_quantize(const void *w, size_t w_stride, uint32_t flags, int32_t N, int32_t K, int32_t group,
+                        void *q_out, void *scales_out, void *stream);
+int32_t spd_q4_dequantize(const void *q, const void *scales, int32_t N, int32_t K, int32_t group,
+                          void *w_out, size_t w_stride, uint32_t flags, void *stream);
+int32_t spd_q4_pack(const void *q, const void *scales, int32_t N, int32_t K, int32_t group,
+                    void *packed, size_t packed_bytes, void *stream);
+
+/* y[r][n] = sum over k of x[r][k] W[n][k] for rows <= SPD_MAX_ROWS rows: x float32, or bfloat16 with SPD_X_IS_BF16, x_stride
+ * elements between rows, y float32, y_stride between rows.  Exact products, float32 sums; x counts with 30 bits below the
+ * largest magnitude of its row (float32 keeps 24 below each), and magnitudes below 2^-90 with fewer.  A row with a value that
+ * is not finite gives NaN.  y must not overlap x.
+ * workspace: spd_q4_matmul_workspace_bytes bytes (which may be 0; then it may be NULL), 256-byte aligned; it may hold anything before the
+ * call and nothing in it has to survive it.  Calls that share one must not overlap.
+ * Errors: SPD_ERR_INVALID_ARG, SPD_ERR_SHAPE, SPD_ERR_CAPACITY (workspace too small). */
+int32_t spd_q4_matmul_workspace_bytes(int32_t rows, int32_t N, int32_t K, size_t *h_bytes);
+int32_t spd_q4_matmul(const void *packed, int32_t N, int32_t K, int32_t group, const void *x, size_t x_stride,
+                      uint32_t flags, int32_t rows, float *y, size_t y_stride,
+                      void *workspace, size_t workspace_bytes, void *stream);
 
 /* ---- the block loop without the host (Section 2.1, one block = gamma draft steps, one
  * target call, accept / resample, commit) ---------------------------------------------

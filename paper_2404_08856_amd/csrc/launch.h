@@ -236,4 +236,51 @@ hipError_t launch_softmax_sample(const float *logits, size_t row_stride, int n_s
                                  float temperature, const float *u, int u_stride, float *probs_out,
                                  size_t probs_stride, int32_t *token_out, int token_stride, hipStream_t stream);
 
+// ---- log probabilities of tokens (logprobs.hip) ------------------------------------
+struct LogprobArgs {
+    const float *rows;       // [n_rows][vocab], row_stride elements apart: logits, or (probs) probabilities
+    size_t row_stride;
+    const int32_t *tokens;   // [n_rows] or NULL
+    int n_rows, vocab, n_top;
+    bool probs;
+    float inv_temp;
+    float *logprob, *entropy;        // [n_rows], may be NULL
+    int32_t *rank;
+    int32_t *top_tokens;             // [n_rows][n_top]
+    float *top_logprobs;
+    void *workspace;                 // logprobs_workspace_bytes
+};
+size_t logprobs_workspace_bytes(int n_rows, int vocab, int n_top);
+hipError_t launch_logprobs(const LogprobArgs &a, hipStream_t stream);
+
+// ---- weights in 4 bits (q4.hip) ----------------------------------------------------
+bool q4_group_ok(int G);
+size_t q4_packed_bytes(int N, int K, int G);
+// row-major: q [N][ceil(K / 2)], scales bf16 [N][ceil(K / G)], W float32 or bf16, ldw elements between rows
+hipError_t launch_q4_quantize(const void *W, bool bf16, size_t ldw, int N, int K, int G, void *q, void *scales, hipStream_t stream);
+hipError_t launch_q4_dequantize(const void *q, const void *scales, int N, int K, int G, void *W, bool bf16, size_t ldw, hipStream_t stream);
+// sources and modes as in launch_pack_weight
+hipError_t launch_q4_pack(const void *const (&q)[3], const void *const (&scales)[3], int mode, int N, int K, int G, void *packed, hipStream_t stream);
+enum Q4Activations { Q4_X_F32 = 0, Q4_X_BF16 = 1, Q4_X_PACKED = 2 };
+struct Q4GemmArgs {
+    const void *W;            // packed
+    int N, K, group, rows;    // rows <= 64
+    const void *X;            // row-major, ldx elements between rows, or the packed operand of GemmArgs
+    int x_kind;
+    size_t ldx;
+    float *Y;                 // the rest as in GemmArgs (N % 16 == 0 but for STORE)
+    size_t ldy;
+    const float *ssq_in;
+    int ssq_in_parts;
+    float eps;
+    const float *gain_next;
+    void *Xnext;
+    float *ssq_out;
+    void *Xout;
+    int K_out;
+    void *workspace;          // q4_workspace_bytes
+};
+size_t q4_workspace_bytes(int rows, int N, int K);
+hipError_t launch_q4_gemm(const Q4GemmArgs &a, int epilogue, hipStream_t stream);
+
 }  // namespace spd

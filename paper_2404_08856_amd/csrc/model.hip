@@ -73,20 +73,22 @@ int32_t check_shape(const spd_model_config &c) {
     return SPD_OK;
 }
 
-void make_layout(const spd_model_config &c, Layout &L) {
+// q4_group: 0 for matrices in bf16, else the group size of matrices in 4 bits
+void make_layout(const spd_model_config &c, int q4_group, Layout &L) {
+    auto matrix_bytes = [&](int N, int K) { return q4_group ? q4_packed_bytes(N, K, q4_group) : packed_matrix_bytes(N, K); };
     const int d = c.d_model, HD = c.n_heads * c.head_dim, F = c.d_ffn, V = c.vocab;
     size_t off = 0;
     auto take = [&](size_t bytes) { size_t o = off; off = align_up(off + bytes, 256); return o; };
     L.embed = take((size_t)V * d * 2);
-    L.lm_head = take(packed_matrix_bytes(V, d));
+    L.lm_head = take(matrix_bytes(V, d));
     L.final_norm = take((size_t)d * 4);
     for (int l = 0; l < c.n_layers; ++l) {
         L.attn_norm.push_back(take((size_t)d * 4));
-        L.wqkv.push_back(take(packed_matrix_bytes(3 * HD, d)));
-        L.wo.push_back(take(packed_matrix_bytes(d, HD)));
+        L.wqkv.push_back(take(matrix_bytes(3 * HD, d)));
+        L.wo.push_back(take(matrix_bytes(d, HD)));
         L.mlp_norm.push_back(take((size_t)d * 4));
-        L.wgu.push_back(take(packed_matrix_bytes(2 * F, d)));
-        L.wdown.push_back(take(packed_matrix_bytes(d, F)));
+        L.wgu.push_back(take(matrix_bytes(2 * F, d)));
+        L.wdown.push_back(take(matrix_bytes(d, F)));
     }
     L.packed_total = off;
 
@@ -115,6 +117,10 @@ void make_layout(const spd_model_config &c, Layout &L) {
     for (size_t b : {gemm_batch_scratch_bytes(3 * HD, d), gemm_batch_scratch_bytes(d, HD), gemm_batch_scratch_bytes(2 * F, d),
                      gemm_batch_scratch_bytes(d, F), gemm_batch_scratch_bytes(V, d)})
         pb = b > pb ? b : pb;
+    if (q4_group)
+        for (size_t b : {q4_workspace_bytes(kMaxRows, 3 * HD, d), q4_workspace_bytes(kMaxRows, d, HD), q4_workspace_bytes(kMaxRows, 2 * F, d),
+                         q4_workspace_bytes(kMaxRows, d, F), q4_workspace_bytes(kMaxRows, V, d)})
+            pb = b > pb ? b : pb;
     L.part = take(pb);
     L.arrive = take((size_t)kBatchMaxTileGroups * 4);
     L.zero = take(1024);
@@ -185,6 +191,7 @@ struct spd_model {
     bool fuse_qa2 = false;             // ... also for 6..8 rows of one sequence
     int chain = 0, chain_ok = 0;       // rows up to which all layers are one launch: as it is, and what shape and device allow
     bool fuse_qa_ok = false, fuse_qa2_ok = false;   // what the shape and the device allow (checked at creation)
+    int q4_group = 0;                  // > 0: the matrices are held in 4 bits, with scales per group of so many columns
     int attn_slices = 0;               // workgroups per head of the stand-alone attention kernel (0: chosen by batch size)
     unsigned spin_limit = 1u << 22;    // polls before a wait between workgroups gives up
     std::vector<float> rope_host;
@@ -244,12 +251,26 @@ enum ProfKind { PK_QKV = 0, PK_O, PK_GATE_UP, PK_DOWN, PK_LM_HEAD, PK_ATTENTION,
         }                                                                                      \
     } while (0)
 
-// a projection over one row group is a single kernel; more rows may take several passes
-#define PROF_GEMM(kind, expr)                                                                  \
+// A projection.  Over one row group of a bf16 matrix it is a single kernel; more rows may take several passes.
+#define PROF_GEMM(kind, g, epi, tuning)                                                        \
     do {                                                                                       \
-        if (rows <= kGroupRows) PROF_KERNEL(kind, expr);                                       \
-        else PROF_TRY(kind, expr);                                                             \
+        if (m->q4_group) PROF_TRY(kind, project_q4(m, g, epi, st));                            \
+        else if (rows <= kGroupRows) PROF_KERNEL(kind, launch_gemm(g, epi, tuning, st));       \
+        else PROF_TRY(kind, launch_gemm(g, epi, tuning, st));                                  \
     } while (0)
+
+// the projection that `g` describes, its matrix held in 4 bits
+hipError_t project_q4(const spd_model *m, const GemmArgs &g, Epilogue epi, hipStream_t st) {
+    Q4GemmArgs a{};
+    a.W = g.W; a.N = g.N; a.K = g.K; a.group = m->q4_group; a.rows = g.rows;
+    a.X = g.X; a.x_kind = Q4_X_PACKED;
+    a.Y = g.Y; a.ldy = g.ldy;
+    a.ssq_in = g.ssq_in; a.ssq_in_parts = g.ssq_in_parts; a.eps = g.eps;
+    a.gain_next = g.gain_next; a.Xnext = g.Xnext; a.ssq_out = g.ssq_out;
+    a.Xout = g.Xout; a.K_out = g.K_out;
+    a.workspace = m->ws + m->L.part;
+    return launch_q4_gemm(a, epi, st);
+}
 }  // namespace
 
 
@@ -258,35 +279,44 @@ extern "C" {
 
 const char *spd_last_error(void) { return g_err; }
 
-int32_t spd_model_bytes(const spd_model_config *cfg, size_t *packed_bytes, size_t *kv_bytes,
-                        size_t *workspace_bytes) {
+}  // extern "C"
+
+namespace {
+
+int32_t model_bytes(const spd_model_config *cfg, int q4_group, size_t *packed_bytes, size_t *kv_bytes, size_t *workspace_bytes) {
     if (!cfg) return fail(SPD_ERR_INVALID_ARG, "NULL config");
     int32_t rc = check_shape(*cfg);
     if (rc) return rc;
     Layout L;
-    make_layout(*cfg, L);
+    make_layout(*cfg, q4_group, L);
     if (packed_bytes) *packed_bytes = L.packed_total;
     if (kv_bytes) *kv_bytes = L.kv_total;
     if (workspace_bytes) *workspace_bytes = L.ws_total;
     return SPD_OK;
 }
 
-int32_t spd_model_create(const spd_model_config *cfg, const spd_weights *w, void *packed,
-                         size_t packed_bytes, void *kv_cache, size_t kv_bytes, void *workspace,
-                         size_t workspace_bytes, void *stream, spd_model **out) {
-    if (!cfg || !w || !packed || !kv_cache || !workspace || !out)
-        return fail(SPD_ERR_INVALID_ARG, "NULL argument to spd_model_create");
+bool complete(const spd_q4_matrix *w) { return w && w->q && w->scales; }
+
+// Exactly one of w (matrices in bf16) and w4 (in 4 bits) is given.
+int32_t create_model(const spd_model_config *cfg, const spd_weights *w, const spd_weights_q4 *w4, void *packed,
+                     size_t packed_bytes, void *kv_cache, size_t kv_bytes, void *workspace,
+                     size_t workspace_bytes, void *stream, spd_model **out) {
     int32_t rc = check_shape(*cfg);
     if (rc) return rc;
     if (((uintptr_t)packed | (uintptr_t)kv_cache | (uintptr_t)workspace) & 255)
         return fail(SPD_ERR_INVALID_ARG, "buffers must be 256-byte aligned");
-    if (!w->embed || !w->final_norm || !w->attn_norm || !w->wq || !w->wk || !w->wv || !w->wo ||
-        !w->mlp_norm || !w->w_gate || !w->w_up || !w->w_down || (!cfg->tied_embeddings && !w->lm_head))
+    if (w && (!w->embed || !w->final_norm || !w->attn_norm || !w->wq || !w->wk || !w->wv || !w->wo ||
+              !w->mlp_norm || !w->w_gate || !w->w_up || !w->w_down || (!cfg->tied_embeddings && !w->lm_head)))
         return fail(SPD_ERR_INVALID_ARG, "NULL weight pointer");
+    if (w4 && (!w4->embed || !w4->final_norm || !w4->attn_norm || !w4->wq || !w4->wk || !w4->wv || !w4->wo ||
+               !w4->mlp_norm || !w4->w_gate || !w4->w_up || !w4->w_down || !complete(&w4->lm_head)))
+        return fail(SPD_ERR_INVALID_ARG, "NULL weight pointer");
+    if (w4 && !q4_group_ok(w4->group)) return fail(SPD_ERR_SHAPE, "group %d must be 32, 64 or 128", w4->group);
     spd_model *m = new (std::nothrow) spd_model;
     if (!m) return fail(SPD_ERR_INVALID_ARG, "out of host memory");
     m->cfg = *cfg;
-    make_layout(*cfg, m->L);
+    m->q4_group = w4 ? w4->group : 0;
+    make_layout(*cfg, m->q4_group, m->L);
     const Layout &L = m->L;
     if (packed_bytes < L.packed_total || kv_bytes < L.kv_total || workspace_bytes < L.ws_total) {
         delete m;
@@ -308,11 +338,30 @@ int32_t spd_model_create(const spd_model_config *cfg, const spd_weights *w, void
         }                                                                                      \
     } while (0)
 
-    CREATE_TRY(hipMemcpyAsync(m->packed + L.embed, w->embed, (size_t)V * d * 2, hipMemcpyDeviceToDevice, st));
-    CREATE_TRY(launch_pack_weight(cfg->tied_embeddings ? w->embed : w->lm_head, nullptr, nullptr, PACK_PLAIN,
-                                  V, d, m->packed + L.lm_head, st));
-    CREATE_TRY(hipMemcpyAsync(m->packed + L.final_norm, w->final_norm, (size_t)d * 4, hipMemcpyDeviceToDevice, st));
-    for (int l = 0; l < cfg->n_layers; ++l) {
+    CREATE_TRY(hipMemcpyAsync(m->packed + L.embed, w ? w->embed : w4->embed, (size_t)V * d * 2, hipMemcpyDeviceToDevice, st));
+    auto pack4 = [&](int mode, const spd_q4_matrix &a, const spd_q4_matrix &b, const spd_q4_matrix &c, int N, int K, size_t off) {
+        const void *const q[3] = {a.q, b.q, c.q}, *const s[3] = {a.scales, b.scales, c.scales};
+        return launch_q4_pack(q, s, mode, N, K, m->q4_group, m->packed + off, st);
+    };
+    const spd_q4_matrix none{nullptr, nullptr};
+    if (w4) CREATE_TRY(pack4(PACK_PLAIN, w4->lm_head, none, none, V, d, L.lm_head));
+    else CREATE_TRY(launch_pack_weight(cfg->tied_embeddings ? w->embed : w->lm_head, nullptr, nullptr, PACK_PLAIN,
+                                       V, d, m->packed + L.lm_head, st));
+    CREATE_TRY(hipMemcpyAsync(m->packed + L.final_norm, w ? w->final_norm : w4->final_norm, (size_t)d * 4, hipMemcpyDeviceToDevice, st));
+    for (int l = 0; w4 && l < cfg->n_layers; ++l) {
+        if (!w4->attn_norm[l] || !w4->mlp_norm[l] || !complete(&w4->wq[l]) || !complete(&w4->wk[l]) || !complete(&w4->wv[l]) ||
+            !complete(&w4->wo[l]) || !complete(&w4->w_gate[l]) || !complete(&w4->w_up[l]) || !complete(&w4->w_down[l])) {
+            delete m;
+            return fail(SPD_ERR_INVALID_ARG, "NULL weight pointer in layer %d", l);
+        }
+        CREATE_TRY(hipMemcpyAsync(m->packed + L.attn_norm[l], w4->attn_norm[l], (size_t)d * 4, hipMemcpyDeviceToDevice, st));
+        CREATE_TRY(hipMemcpyAsync(m->packed + L.mlp_norm[l], w4->mlp_norm[l], (size_t)d * 4, hipMemcpyDeviceToDevice, st));
+        CREATE_TRY(pack4(PACK_CONCAT3, w4->wq[l], w4->wk[l], w4->wv[l], 3 * HD, d, L.wqkv[l]));
+        CREATE_TRY(pack4(PACK_PLAIN, w4->wo[l], none, none, d, HD, L.wo[l]));
+        CREATE_TRY(pack4(PACK_GATE_UP, w4->w_gate[l], w4->w_up[l], none, 2 * F, d, L.wgu[l]));
+        CREATE_TRY(pack4(PACK_PLAIN, w4->w_down[l], none, none, d, F, L.wdown[l]));
+    }
+    for (int l = 0; w && l < cfg->n_layers; ++l) {
         if (!w->attn_norm[l] || !w->wq[l] || !w->wk[l] || !w->wv[l] || !w->wo[l] || !w->mlp_norm[l] ||
             !w->w_gate[l] || !w->w_up[l] || !w->w_down[l]) {
             delete m;
@@ -348,14 +397,46 @@ int32_t spd_model_create(const spd_model_config *cfg, const spd_weights *w, void
     m->t_down = default_tuning(d, F);
     m->t_lm = default_tuning(V, d);
     // QKV projection + attention as one kernel where the shape and the device allow it
-    m->fuse_qa_ok = qkv_attention_supported(cfg->d_model, cfg->n_heads, cfg->head_dim, 1, 1, 1);
+    // (these and the launch of all layers read weights in bf16)
+    m->fuse_qa_ok = w && qkv_attention_supported(cfg->d_model, cfg->n_heads, cfg->head_dim, 1, 1, 1);
     m->fuse_qa2_ok = m->fuse_qa_ok && qkv_attention_supported(cfg->d_model, cfg->n_heads, cfg->head_dim, 8, 1, 8);
     m->fuse_qa = m->fuse_qa_ok;
     m->fuse_qa2 = m->fuse_qa2_ok;
     // (a layer has to fit the L2s: with more weights a launch per projection keeps the memory busier)
-    m->chain = m->chain_ok = layer_weight_bytes(*cfg) <= kSmallLayer && chain_supported(d, HD, F, cfg->head_dim) ? chain_rows(d, HD, F) : 0;
+    m->chain = m->chain_ok = w && layer_weight_bytes(*cfg) <= kSmallLayer && chain_supported(d, HD, F, cfg->head_dim) ? chain_rows(d, HD, F) : 0;
     *out = m;
     return SPD_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+int32_t spd_model_bytes(const spd_model_config *cfg, size_t *packed_bytes, size_t *kv_bytes,
+                        size_t *workspace_bytes) {
+    return model_bytes(cfg, 0, packed_bytes, kv_bytes, workspace_bytes);
+}
+
+int32_t spd_model_bytes_q4(const spd_model_config *cfg, int32_t group, size_t *packed_bytes, size_t *kv_bytes,
+                           size_t *workspace_bytes) {
+    if (!q4_group_ok(group)) return fail(SPD_ERR_SHAPE, "group %d must be 32, 64 or 128", group);
+    return model_bytes(cfg, group, packed_bytes, kv_bytes, workspace_bytes);
+}
+
+int32_t spd_model_create(const spd_model_config *cfg, const spd_weights *w, void *packed,
+                         size_t packed_bytes, void *kv_cache, size_t kv_bytes, void *workspace,
+                         size_t workspace_bytes, void *stream, spd_model **out) {
+    if (!cfg || !w || !packed || !kv_cache || !workspace || !out)
+        return fail(SPD_ERR_INVALID_ARG, "NULL argument to spd_model_create");
+    return create_model(cfg, w, nullptr, packed, packed_bytes, kv_cache, kv_bytes, workspace, workspace_bytes, stream, out);
+}
+
+int32_t spd_model_create_q4(const spd_model_config *cfg, const spd_weights_q4 *w, void *packed,
+                            size_t packed_bytes, void *kv_cache, size_t kv_bytes, void *workspace,
+                            size_t workspace_bytes, void *stream, spd_model **out) {
+    if (!cfg || !w || !packed || !kv_cache || !workspace || !out)
+        return fail(SPD_ERR_INVALID_ARG, "NULL argument to spd_model_create_q4");
+    return create_model(cfg, nullptr, w, packed, packed_bytes, kv_cache, kv_bytes, workspace, workspace_bytes, stream, out);
 }
 
 int32_t spd_model_set_tuning(spd_model *m, const spd_tuning *t) {
@@ -479,7 +560,7 @@ int32_t run_lm_head(spd_model *m, int rows, float *logits_out, hipStream_t st) {
     g.batch_partials = (float *)(m->ws + L.part); g.batch_arrive = (unsigned *)(m->ws + L.arrive); g.batch_zero = m->ws + L.zero;
     g.W = m->packed + L.lm_head; g.X = m->ws + L.xn; g.N = c.vocab; g.K = c.d_model; g.rows = rows; g.Y = logits_out; g.ldy = c.vocab;
     g.ssq_in = (float *)(m->ws + L.ssq_b); g.ssq_in_parts = c.d_model / 16; g.eps = c.rms_eps;
-    PROF_GEMM(PK_LM_HEAD, launch_gemm(g, EPI_STORE, m->t_lm, st));
+    PROF_GEMM(PK_LM_HEAD, g, EPI_STORE, m->t_lm);
     return SPD_OK;
 }
 
@@ -533,7 +614,7 @@ int32_t run_layers(spd_model *m, int first, AttnArgs &at, int seq0, int n_seqs, 
 
     // Small models, few rows: a projection lasts about as long as its first loads take, so the weights of the next ones are
     // brought into L2 meanwhile.
-    const bool prefetch = rows <= 2 * kGroupRows && layer_weight_bytes(c) <= kSmallLayer;
+    const bool prefetch = !m->q4_group && rows <= 2 * kGroupRows && layer_weight_bytes(c) <= kSmallLayer;
     const bool fused = m->fuse_qa && n_seqs == 1 && (rows <= kGroupRows || (rows <= 8 && m->fuse_qa2));   // shapes checked at creation
     for (int l = first; l < c.n_layers; ++l) {
         // RMSNorm is folded into the projections: the producer of h (input rows / O / down
@@ -557,7 +638,7 @@ int32_t run_layers(spd_model *m, int first, AttnArgs &at, int seq0, int n_seqs, 
         } else {
             g.W = m->packed + L.wqkv[l]; g.X = xn; g.N = at.row_cached ? HD : 3 * HD; g.K = d; g.rows = rows; g.Y = qkv; g.ldy = 3 * HD;
             g.ssq_in = ssq_b; g.ssq_in_parts = l == first ? 1 : d_tiles; g.eps = c.rms_eps;
-            PROF_GEMM(PK_QKV, launch_gemm(g, EPI_STORE, m->t_qkv, st));
+            PROF_GEMM(PK_QKV, g, EPI_STORE, m->t_qkv);
             WeightPrefetch pf{};
             if (prefetch) {
                 auto add = [&](size_t off, int N, int K) { pf.m[pf.n].w = m->packed + off; pf.m[pf.n].tiles = N / 16; pf.m[pf.n++].tile_bytes = (K + 31) / 32 * 1024; };
@@ -575,17 +656,17 @@ int32_t run_layers(spd_model *m, int first, AttnArgs &at, int seq0, int n_seqs, 
         g.batch_partials = (float *)(m->ws + L.part); g.batch_arrive = (unsigned *)(m->ws + L.arrive); g.batch_zero = m->ws + L.zero; g.fold = kv_cached;
         g.W = m->packed + L.wo[l]; g.X = xo; g.N = d; g.K = HD; g.rows = rows; g.Y = h; g.ldy = d;
         g.gain_next = gain_of(L.mlp_norm[l]); g.Xnext = xn; g.ssq_out = ssq_a;
-        PROF_GEMM(PK_O, launch_gemm(g, EPI_RESIDUAL, m->t_o, st));
+        PROF_GEMM(PK_O, g, EPI_RESIDUAL, m->t_o);
         g = GemmArgs{};
         g.batch_partials = (float *)(m->ws + L.part); g.batch_arrive = (unsigned *)(m->ws + L.arrive); g.batch_zero = m->ws + L.zero; g.fold = kv_cached;
         g.W = m->packed + L.wgu[l]; g.X = xn; g.N = 2 * F; g.K = d; g.rows = rows; g.Xout = xf; g.K_out = F;
         g.ssq_in = ssq_a; g.ssq_in_parts = d_tiles; g.eps = c.rms_eps;
-        PROF_GEMM(PK_GATE_UP, launch_gemm(g, EPI_SWIGLU, m->t_gu, st));
+        PROF_GEMM(PK_GATE_UP, g, EPI_SWIGLU, m->t_gu);
         g = GemmArgs{};
         g.batch_partials = (float *)(m->ws + L.part); g.batch_arrive = (unsigned *)(m->ws + L.arrive); g.batch_zero = m->ws + L.zero; g.fold = kv_cached;
         g.W = m->packed + L.wdown[l]; g.X = xf; g.N = d; g.K = F; g.rows = rows; g.Y = h; g.ldy = d;
         g.gain_next = gain_of(l + 1 < c.n_layers ? L.attn_norm[l + 1] : L.final_norm); g.Xnext = xn; g.ssq_out = ssq_b;
-        PROF_GEMM(PK_DOWN, launch_gemm(g, EPI_RESIDUAL, m->t_down, st));
+        PROF_GEMM(PK_DOWN, g, EPI_RESIDUAL, m->t_down);
     }
     return logits_out ? run_lm_head(m, rows, logits_out, st) : SPD_OK;
 }
@@ -718,8 +799,8 @@ int32_t prefill_common(spd_model *m, int32_t seq, const float *embeds, const int
         return fail(SPD_ERR_CAPACITY, "KV cache overflow in prefill: %d + %d > %d", m->lens[seq], n_rows, m->cfg.max_positions);
     float *scratch = (float *)(m->ws + m->L.logits);
     if (m->dev_lens) m->lens_least[seq] = std::min(m->lens_least[seq] + n_rows, m->cfg.max_positions);
-    // passes through the prefill kernels, unless a kernel family was asked for (batch_kernel = 1 or 2)
-    if (!m->t_qkv.no_batch && !m->t_qkv.force_batch) {
+    // passes through the prefill kernels, unless a kernel family was asked for (batch_kernel = 1 or 2); they read matrices in bf16
+    if (!m->q4_group && !m->t_qkv.no_batch && !m->t_qkv.force_batch) {
         const int min_rows = prefill_min_rows(m->cfg.d_model);
         while (n_rows >= min_rows) {
             const int M = std::min(n_rows, m->L.prefill_rows);
@@ -923,6 +1004,120 @@ int32_t spd_block_finish(spd_model *target, spd_model *draft, const float *targe
     // host bounds: at most gamma + 1 positions per sequence were added by the verify call and stay, at least one did
     for (spd_model *m : {target, draft})
         for (int s = 0; s < n_seqs; ++s) m->lens_least[s] = std::min(m->lens_least[s] + 1, m->cfg.max_positions);
+    return SPD_OK;
+}
+
+}  // extern "C"
+
+// ---- weights in 4 bits -------------------------------------------------------------------------
+namespace {
+int32_t check_q4(const char *what, int32_t N, int32_t K, int32_t group) {
+    if (N < 1 || K < 1) return fail(SPD_ERR_SHAPE, "%s: N = %d and K = %d must be positive", what, N, K);
+    if (!q4_group_ok(group)) return fail(SPD_ERR_SHAPE, "%s: group %d must be 32, 64 or 128", what, group);
+    if ((int64_t)((N + 15ll) / 16) * ((K + 127ll) / 128) > (int64_t)1 << 31) return fail(SPD_ERR_SHAPE, "%s: %d x %d is more than 2^42 weights", what, N, K);
+    return SPD_OK;
+}
+constexpr uint32_t kTypeFlags = SPD_W_IS_BF16;
+}  // namespace
+
+extern "C" {
+
+int32_t spd_q4_bytes(int32_t N, int32_t K, int32_t group, size_t *bytes) {
+    if (!bytes) return fail(SPD_ERR_INVALID_ARG, "NULL argument to spd_q4_bytes");
+    const int32_t rc = check_q4("spd_q4_bytes", N, K, group);
+    if (rc) return rc;
+    *bytes = q4_packed_bytes(N, K, group);
+    return SPD_OK;
+}
+
+int32_t spd_q4_quantize(const void *w, size_t w_stride, uint32_t flags, int32_t N, int32_t K, int32_t group, void *q_out, void *scales_out, void *stream) {
+    if (!w || !q_out || !scales_out) return fail(SPD_ERR_INVALID_ARG, "NULL argument to spd_q4_quantize");
+    const int32_t rc = check_q4("spd_q4_quantize", N, K, group);
+    if (rc) return rc;
+    if (flags & ~kTypeFlags) return fail(SPD_ERR_INVALID_ARG, "unknown flag bits");
+    if (w_stride < (size_t)K) return fail(SPD_ERR_INVALID_ARG, "w_stride must cover a row");
+    HIP_TRY(launch_q4_quantize(w, flags & SPD_W_IS_BF16, w_stride, N, K, group, q_out, scales_out, (hipStream_t)stream));
+    return SPD_OK;
+}
+
+int32_t spd_q4_dequantize(const void *q, const void *scales, int32_t N, int32_t K, int32_t group, void *w_out, size_t w_stride, uint32_t flags, void *stream) {
+    if (!q || !scales || !w_out) return fail(SPD_ERR_INVALID_ARG, "NULL argument to spd_q4_dequantize");
+    const int32_t rc = check_q4("spd_q4_dequantize", N, K, group);
+    if (rc) return rc;
+    if (flags & ~kTypeFlags) return fail(SPD_ERR_INVALID_ARG, "unknown flag bits");
+    if (w_stride < (size_t)K) return fail(SPD_ERR_INVALID_ARG, "w_stride must cover a row");
+    HIP_TRY(launch_q4_dequantize(q, scales, N, K, group, w_out, flags & SPD_W_IS_BF16, w_stride, (hipStream_t)stream));
+    return SPD_OK;
+}
+
+int32_t spd_q4_pack(const void *q, const void *scales, int32_t N, int32_t K, int32_t group, void *packed, size_t packed_bytes, void *stream) {
+    if (!q || !scales || !packed) return fail(SPD_ERR_INVALID_ARG, "NULL argument to spd_q4_pack");
+    const int32_t rc = check_q4("spd_q4_pack", N, K, group);
+    if (rc) return rc;
+    if ((uintptr_t)packed & 255) return fail(SPD_ERR_INVALID_ARG, "packed must be 256-byte aligned");
+    if (packed_bytes < q4_packed_bytes(N, K, group)) return fail(SPD_ERR_CAPACITY, "buffer smaller than spd_q4_bytes reports");
+    const void *const qs[3] = {q, nullptr, nullptr}, *const ss[3] = {scales, nullptr, nullptr};
+    HIP_TRY(launch_q4_pack(qs, ss, PACK_PLAIN, N, K, group, packed, (hipStream_t)stream));
+    return SPD_OK;
+}
+
+int32_t spd_q4_matmul_workspace_bytes(int32_t rows, int32_t N, int32_t K, size_t *bytes) {
+    if (!bytes) return fail(SPD_ERR_INVALID_ARG, "NULL argument to spd_q4_matmul_workspace_bytes");
+    if (rows < 1 || rows > SPD_MAX_ROWS) return fail(SPD_ERR_SHAPE, "rows = %d must be in 1..%d", rows, SPD_MAX_ROWS);
+    const int32_t rc = check_q4("spd_q4_matmul_workspace_bytes", N, K, 32);
+    if (rc) return rc;
+    *bytes = q4_workspace_bytes(rows, N, K);
+    return SPD_OK;
+}
+
+int32_t spd_q4_matmul(const void *packed, int32_t N, int32_t K, int32_t group, const void *x, size_t x_stride, uint32_t flags, int32_t rows,
+                      float *y, size_t y_stride, void *workspace, size_t workspace_bytes, void *stream) {
+    if (!packed || !x || !y) return fail(SPD_ERR_INVALID_ARG, "NULL argument to spd_q4_matmul");
+    const int32_t rc = check_q4("spd_q4_matmul", N, K, group);
+    if (rc) return rc;
+    if (rows < 1 || rows > SPD_MAX_ROWS) return fail(SPD_ERR_SHAPE, "rows = %d must be in 1..%d", rows, SPD_MAX_ROWS);
+    if (flags & ~SPD_X_IS_BF16) return fail(SPD_ERR_INVALID_ARG, "unknown flag bits");
+    if (x_stride < (size_t)K || y_stride < (size_t)N) return fail(SPD_ERR_INVALID_ARG, "strides must cover a row");
+    if (((uintptr_t)packed & 255) || ((uintptr_t)workspace & 255)) return fail(SPD_ERR_INVALID_ARG, "packed and workspace must be 256-byte aligned");
+    const size_t need = q4_workspace_bytes(rows, N, K);
+    if (need && (!workspace || workspace_bytes < need)) return fail(SPD_ERR_CAPACITY, "workspace smaller than spd_q4_matmul_workspace_bytes reports");
+    Q4GemmArgs a{};
+    a.W = packed; a.N = N; a.K = K; a.group = group; a.rows = rows;
+    a.X = x; a.x_kind = flags & SPD_X_IS_BF16 ? Q4_X_BF16 : Q4_X_F32; a.ldx = x_stride;
+    a.Y = y; a.ldy = y_stride;
+    a.workspace = workspace;
+    HIP_TRY(launch_q4_gemm(a, EPI_STORE, (hipStream_t)stream));
+    return SPD_OK;
+}
+
+// ---- log probabilities -------------------------------------------------------------------------
+int32_t spd_logprobs_workspace_bytes(int32_t n_rows, int32_t vocab, int32_t n_top, size_t *bytes) {
+    if (!bytes || n_rows < 1 || vocab < 1 || n_top < 0 || n_top > SPD_MAX_TOP) return fail(SPD_ERR_INVALID_ARG, "bad argument to spd_logprobs_workspace_bytes");
+    *bytes = logprobs_workspace_bytes(n_rows, vocab, n_top);
+    return SPD_OK;
+}
+
+int32_t spd_token_logprobs(const float *rows, size_t row_stride, const int32_t *tokens, int32_t n_rows, int32_t vocab, float temperature, uint32_t flags,
+                           float *logprob_out, float *entropy_out, int32_t *rank_out, int32_t n_top, int32_t *top_tokens_out, float *top_logprobs_out,
+                           void *workspace, size_t workspace_bytes, void *stream) {
+    if (!rows || (!tokens && (logprob_out || rank_out)) || (n_top > 0 && (!top_tokens_out || !top_logprobs_out)))
+        return fail(SPD_ERR_INVALID_ARG, "NULL argument to spd_token_logprobs");
+    if (n_rows < 1 || vocab < 1) return fail(SPD_ERR_INVALID_ARG, "n_rows, vocab >= 1 required");
+    if (n_top < 0 || n_top > SPD_MAX_TOP) return fail(SPD_ERR_INVALID_ARG, "n_top = %d must be in 0..%d", n_top, SPD_MAX_TOP);
+    if (row_stride < (size_t)vocab) return fail(SPD_ERR_INVALID_ARG, "row_stride must cover a row");
+    if (flags & ~SPD_ROWS_ARE_PROBS) return fail(SPD_ERR_INVALID_ARG, "unknown flag bits");
+    const bool probs = flags & SPD_ROWS_ARE_PROBS;
+    if (!probs && !(temperature > 0.f && 1.0f / temperature < INFINITY && 1.0f / temperature > 0.f)) return fail(SPD_ERR_INVALID_ARG, "temperature must be positive and finite");
+    if ((uintptr_t)workspace & 15) return fail(SPD_ERR_INVALID_ARG, "workspace must be 16-byte aligned");
+    const size_t need = logprobs_workspace_bytes(n_rows, vocab, n_top);
+    if (need && (!workspace || workspace_bytes < need)) return fail(SPD_ERR_CAPACITY, "workspace smaller than spd_logprobs_workspace_bytes reports");
+    if (!logprob_out && !entropy_out && !rank_out && n_top == 0) return SPD_OK;
+    LogprobArgs a;
+    a.rows = rows; a.row_stride = row_stride; a.tokens = tokens; a.n_rows = n_rows; a.vocab = vocab; a.n_top = n_top;
+    a.probs = probs; a.inv_temp = probs ? 1.0f : 1.0f / temperature;
+    a.logprob = logprob_out; a.entropy = entropy_out; a.rank = rank_out; a.top_tokens = top_tokens_out; a.top_logprobs = top_logprobs_out;
+    a.workspace = workspace;
+    HIP_TRY(launch_logprobs(a, (hipStream_t)stream));
     return SPD_OK;
 }
 

@@ -1,0 +1,485 @@
+// Weights in 4 bits: the quantiser, its inverse, the re-tiling and the product  Y[rows, N] = X[rows, K] W[N, K]^T  for up
+// to 64 rows, with the epilogues of the decoder's projections.
+//
+//   W[n][k] = scale[n][k / G] * q[n][k],   q in -8 .. 7,   scale bfloat16,   G = 32, 64 or 128
+//
+// The product is made of integers.  The values of an activation row in a block of 128 columns share the exponent E of their
+// largest magnitude: x = v * 2^(E - 30) with a 31-bit integer v (what is cut off is below 2^-30 of the largest one, where
+// float32 itself keeps 2^-24 of each), and v is four signed base-256 digits.  Four rows x four digits are the 16
+// columns of v_mfma_i32_16x16x64_i8; a nibble in the upper half of a byte is 16 q as an 8-bit integer, so the weights need
+// one mask (and every other one a shift) per 4 of them and no zero point.  A group's sum is exact in 32 bits (at most
+// 128 * 128 * 128 = 2^21) and in the float32 it is turned into; then one fused multiply-add with scale * 2^(E - 34 + 8 digit),
+// which is exact too, adds it to the float32 sum of the row.  So a product rounds once per group, in float32.
+// A row with a value that is not finite gives NaN; a block whose largest magnitude is below 2^-90 keeps less than 31 bits.
+#include <algorithm>
+
+#include "launch.h"
+
+namespace spd {
+
+typedef __attribute__((ext_vector_type(4))) int i32x4_t;
+
+constexpr int kQ4Block = 128;             // columns of a block: 16 bytes per lane of a 16-row tile
+constexpr int kQ4Rows = 4;                // activation rows of a row group
+
+// ---------------------------------------------------------------------------------
+// quantiser and its inverse, row-major
+// ---------------------------------------------------------------------------------
+struct __attribute__((packed, aligned(4))) FloatQuad { float v[4]; };
+struct __attribute__((packed, aligned(2))) HalfOct { uint32_t v[4]; };
+struct __attribute__((packed, aligned(1))) ByteQuad { uint32_t v; };
+
+// values k0 .. k0 + 7 of a row of K, zeros behind its end
+__device__ __forceinline__ void load8(const float *row, size_t k0, int K, float (&v)[8]) {
+    if (k0 + 8 <= (size_t)K) {
+        const FloatQuad a = *reinterpret_cast<const FloatQuad *>(row + k0), b = *reinterpret_cast<const FloatQuad *>(row + k0 + 4);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) { v[e] = a.v[e]; v[4 + e] = b.v[e]; }
+    } else {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] = k0 + e < (size_t)K ? row[k0 + e] : 0.f;
+    }
+}
+__device__ __forceinline__ void load8(const uint16_t *row, size_t k0, int K, float (&v)[8]) {
+    if (k0 + 8 <= (size_t)K) {
+        const HalfOct a = *reinterpret_cast<const HalfOct *>(row + k0);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) { v[2 * e] = bf16_lo(a.v[e]); v[2 * e + 1] = bf16_hi(a.v[e]); }
+    } else {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] = k0 + e < (size_t)K ? bf16_bits_to_f32(row[k0 + e]) : 0.f;
+    }
+}
+
+// A wave per 512 columns of a row, 8 per lane; a group is 4, 8 or 16 neighbouring lanes.
+template <class T, int G>
+__global__ __launch_bounds__(256) void q4_quantize_kernel(const T *__restrict__ W, size_t ldw, int N, int K, uint8_t *__restrict__ q, uint16_t *__restrict__ scales) {
+    const int per_row = (K + 511) / 512, lane = threadIdx.x & 63;
+    const size_t unit = (size_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+    if (unit >= (size_t)N * per_row) return;
+    const size_t n = unit / per_row, k0 = (unit - n * per_row) * 512 + lane * 8;
+    float v[8];
+    load8(W + n * ldw, k0, K, v);
+    float m = 0.f;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) m = __builtin_elementwise_maximum(m, fabsf(v[e]));        // NaN stays
+    m = __builtin_elementwise_maximum(m, lane_xor<1>(m));
+    m = __builtin_elementwise_maximum(m, lane_xor<2>(m));
+    if (G >= 64) m = __builtin_elementwise_maximum(m, lane_xor<4>(m));
+    if (G >= 128) m = __builtin_elementwise_maximum(m, lane_xor<8>(m));
+    const bool finite = m < INFINITY;
+    const uint16_t s16 = finite ? f32_to_bf16_bits(m / 7.0f) : (uint16_t)0x7fc0;
+    const float s = bf16_bits_to_f32(s16);
+    uint32_t bytes = 0;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+        const int i = finite && s != 0.f ? (int)fminf(fmaxf(rintf(v[e] / s), -8.f), 7.f) : 0;
+        bytes |= (uint32_t)(i & 15) << (4 * e);                // even columns in the low halves
+    }
+    if (k0 >= (size_t)K) return;
+    if (k0 % G == 0) scales[n * ((K + G - 1) / G) + k0 / G] = s16;
+    const size_t row_bytes = ((size_t)K + 1) / 2;
+    uint8_t *dst = q + n * row_bytes + k0 / 2;
+    if (k0 + 8 <= (size_t)K) reinterpret_cast<ByteQuad *>(dst)->v = bytes;
+    else
+        for (size_t e = 0; k0 / 2 + e < row_bytes; ++e) dst[e] = (uint8_t)(bytes >> (8 * e));
+}
+
+// 8 columns per thread
+template <class T, int G>
+__global__ __launch_bounds__(256) void q4_dequantize_kernel(const uint8_t *__restrict__ q, const uint16_t *__restrict__ scales, int N, int K, T *__restrict__ W, size_t ldw) {
+    const int per_row = (K + 511) / 512, lane = threadIdx.x & 63;
+    const size_t unit = (size_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+    if (unit >= (size_t)N * per_row) return;
+    const size_t n = unit / per_row, k0 = (unit - n * per_row) * 512 + lane * 8;
+    if (k0 >= (size_t)K) return;
+    const size_t row_bytes = ((size_t)K + 1) / 2;
+    const uint8_t *src = q + n * row_bytes + k0 / 2;
+    uint32_t bytes = 0;
+    if (k0 + 8 <= (size_t)K) bytes = reinterpret_cast<const ByteQuad *>(src)->v;
+    else
+        for (size_t e = 0; k0 / 2 + e < row_bytes; ++e) bytes |= (uint32_t)src[e] << (8 * e);
+    const float s = bf16_bits_to_f32(scales[n * ((K + G - 1) / G) + k0 / G]);
+    float v[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] = (float)((int)(bytes << (28 - 4 * e)) >> 28) * s;
+    T *dst = W + n * ldw + k0;
+    if (k0 + 8 <= (size_t)K) {
+        if constexpr (sizeof(T) == 4) {
+            *reinterpret_cast<FloatQuad *>(dst) = FloatQuad{{v[0], v[1], v[2], v[3]}};
+            *reinterpret_cast<FloatQuad *>(dst + 4) = FloatQuad{{v[4], v[5], v[6], v[7]}};
+        } else {
+            HalfOct o;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) o.v[e] = f32_to_bf16_bits(v[2 * e]) | (uint32_t)f32_to_bf16_bits(v[2 * e + 1]) << 16;
+            *reinterpret_cast<HalfOct *>(dst) = o;
+        }
+    } else {
+        for (size_t e = 0; k0 + e < (size_t)K; ++e) {
+            if constexpr (sizeof(T) == 4) dst[e] = v[e];
+            else dst[e] = f32_to_bf16_bits(v[e]);
+        }
+    }
+}
+
+bool q4_group_ok(int G) { return G == 32 || G == 64 || G == 128; }
+
+template <class F>
+static hipError_t with_group(int G, F f) {
+    switch (G) {
+        case 32: f(std::integral_constant<int, 32>()); break;
+        case 64: f(std::integral_constant<int, 64>()); break;
+        case 128: f(std::integral_constant<int, 128>()); break;
+        default: return hipErrorInvalidValue;
+    }
+    return hipGetLastError();
+}
+
+static unsigned unit_grid(int N, int K) { return (unsigned)(((size_t)N * ((K + 511) / 512) + 3) / 4); }
+
+hipError_t launch_q4_quantize(const void *W, bool bf16, size_t ldw, int N, int K, int G, void *q, void *scales, hipStream_t stream) {
+    return with_group(G, [&](auto g) {
+        if (bf16) hipLaunchKernelGGL((q4_quantize_kernel<uint16_t, g()>), dim3(unit_grid(N, K)), dim3(256), 0, stream, (const uint16_t *)W, ldw, N, K, (uint8_t *)q, (uint16_t *)scales);
+        else hipLaunchKernelGGL((q4_quantize_kernel<float, g()>), dim3(unit_grid(N, K)), dim3(256), 0, stream, (const float *)W, ldw, N, K, (uint8_t *)q, (uint16_t *)scales);
+    });
+}
+
+hipError_t launch_q4_dequantize(const void *q, const void *scales, int N, int K, int G, void *W, bool bf16, size_t ldw, hipStream_t stream) {
+    return with_group(G, [&](auto g) {
+        if (bf16) hipLaunchKernelGGL((q4_dequantize_kernel<uint16_t, g()>), dim3(unit_grid(N, K)), dim3(256), 0, stream, (const uint8_t *)q, (const uint16_t *)scales, N, K, (uint16_t *)W, ldw);
+        else hipLaunchKernelGGL((q4_dequantize_kernel<float, g()>), dim3(unit_grid(N, K)), dim3(256), 0, stream, (const uint8_t *)q, (const uint16_t *)scales, N, K, (float *)W, ldw);
+    });
+}
+
+// ---------------------------------------------------------------------------------
+// re-tiling
+// ---------------------------------------------------------------------------------
+// Tiles of 16 rows, blocks of 128 columns: block (t, b) at index t * KB + b is 1 KiB, lane l = r + 16 g holds row 16 t + r in its
+// 16 bytes: word j < 4 has columns 128 b + 32 j + 8 g + e (e < 4) in the upper halves of its bytes and + 4 + e in the lower
+// ones.  Two masks make of words 2 s, 2 s + 1 the operand of matrix-core step s (64 columns, in an order that the activations follow).
+// Behind the blocks the scales, [t][b][g][128 / G][4] for rows 16 t + 4 g + i: what the lane that ends with these rows' sums reads at once.
+// Rows and columns beyond the matrix are zero.
+size_t q4_scales_offset(int N, int K) { return ((size_t)((N + 15) / 16) * ((K + kQ4Block - 1) / kQ4Block) * 1024 + 255) / 256 * 256; }
+size_t q4_packed_bytes(int N, int K, int G) {
+    return (q4_scales_offset(N, K) + (size_t)((N + 15) / 16) * ((K + kQ4Block - 1) / kQ4Block) * (4096 / G) + 255) / 256 * 256;
+}
+
+struct Q4PackArgs {
+    const uint8_t *q[3];
+    const uint16_t *s[3];
+    int mode, N, K, KB, G;
+    uint4 *blocks;
+    uint16_t *scales;
+};
+// source matrix and row of packed row p; false beyond the matrix
+__device__ __forceinline__ bool source_row(const Q4PackArgs &a, int p, int &which, int &row) {
+    which = 0; row = p;
+    if (a.mode == PACK_CONCAT3) {
+        const int third = a.N / 3;
+        which = min(p / third, 2);
+        row = p - which * third;
+    } else if (a.mode == PACK_GATE_UP) {
+        which = (p & 15) >= 8;
+        row = (p >> 4) * 8 + (p & 7);
+    }
+    return p < a.N;
+}
+__global__ __launch_bounds__(256) void q4_pack_kernel(Q4PackArgs a) {
+    const size_t id = (size_t)blockIdx.x * 4 + (threadIdx.x >> 6), tiles = (size_t)(a.N + 15) / 16;
+    if (id >= tiles * a.KB) return;
+    const int lane = threadIdx.x & 63, r = lane & 15, g = lane >> 4;
+    const int t = (int)(id / a.KB), b = (int)(id - (size_t)t * a.KB);
+    int which, row;
+    const size_t row_bytes = ((size_t)a.K + 1) / 2;
+    uint32_t w[4] = {0, 0, 0, 0};
+    if (source_row(a, 16 * t + r, which, row)) {
+        const uint8_t *src = a.q[which] + (size_t)row * row_bytes;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const int k0 = kQ4Block * b + 32 * j + 8 * g;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                const int k = k0 + e;
+                const uint32_t v = k < a.K ? (src[k >> 1] >> (4 * (k & 1))) & 15u : 0u;
+                w[j] |= v << (8 * (e & 3) + (e < 4 ? 4 : 0));
+            }
+        }
+    }
+    a.blocks[id * 64 + lane] = uint4{w[0], w[1], w[2], w[3]};
+    const int per = kQ4Block / a.G, groups = (a.K + a.G - 1) / a.G;      // scales of the block: 16 rows x per
+    for (int i = lane; i < 16 * per; i += 64) {                          // [g][per][4]
+        const int gg = i / (4 * per), gi = (i / 4) % per, group = b * per + gi;
+        uint16_t v = 0;
+        if (group < groups && source_row(a, 16 * t + 4 * gg + (i & 3), which, row)) v = a.s[which][(size_t)row * groups + group];
+        a.scales[id * (16 * per) + i] = v;
+    }
+}
+
+hipError_t launch_q4_pack(const void *const (&q)[3], const void *const (&scales)[3], int mode, int N, int K, int G, void *packed, hipStream_t stream) {
+    if (!q4_group_ok(G)) return hipErrorInvalidValue;
+    Q4PackArgs a;
+    for (int i = 0; i < 3; ++i) { a.q[i] = (const uint8_t *)q[i]; a.s[i] = (const uint16_t *)scales[i]; }
+    a.mode = mode; a.N = N; a.K = K; a.KB = (K + kQ4Block - 1) / kQ4Block; a.G = G;
+    a.blocks = (uint4 *)packed;
+    a.scales = (uint16_t *)((char *)packed + q4_scales_offset(N, K));
+    const size_t blocks = (size_t)((N + 15) / 16) * a.KB;
+    hipLaunchKernelGGL(q4_pack_kernel, dim3((unsigned)((blocks + 3) / 4)), dim3(256), 0, stream, a);
+    return hipGetLastError();
+}
+
+// ---------------------------------------------------------------------------------
+// the product
+// ---------------------------------------------------------------------------------
+struct Q4Kernel {
+    const uint4 *W;
+    const uint16_t *S;
+    int N, K, KB, tiles;
+    const void *X;
+    int x_kind;               // Q4_X_F32, Q4_X_BF16 (row-major, ldx elements apart) or Q4_X_PACKED (three bf16 terms, KS blocks a row group)
+    size_t ldx;
+    int KS, row0, rows;       // rows of the call; this launch starts at row0
+    float *Y;
+    size_t ldy;
+    const float *ssq_in;      // the rest as in GemmArgs
+    int ssq_in_parts;
+    float inv_d, eps;
+    const float *gain_next;
+    uint16_t *Xnext;
+    float *ssq_out;
+    uint16_t *Xout;
+    int KS_out, epilogue;
+};
+
+// Values k0 .. k0 + 7 (k0 % 8 == 0) of an activation row, zeros beyond the matrix
+__device__ __forceinline__ void load_x8(const Q4Kernel &a, int row, int k0, float (&v)[8]) {
+    if (row >= a.rows || k0 >= a.K) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] = 0.f;
+    } else if (a.x_kind == Q4_X_F32) {
+        load8((const float *)a.X + (size_t)row * a.ldx, k0, a.K, v);
+    } else if (a.x_kind == Q4_X_BF16) {
+        load8((const uint16_t *)a.X + (size_t)row * a.ldx, k0, a.K, v);
+    } else {                                                   // the sum of the terms is the float32 value they were made of
+        const uint16_t *X = (const uint16_t *)a.X;
+        uint4 t[kTerms];
+#pragma unroll
+        for (int i = 0; i < kTerms; ++i) t[i] = *reinterpret_cast<const uint4 *>(X + xpack_index(row, k0, a.KS, i));
+        const uint32_t *p0 = &t[0].x, *p1 = &t[1].x, *p2 = &t[2].x;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            v[2 * e] = bf16_lo(p0[e]) + (bf16_lo(p1[e]) + bf16_lo(p2[e]));
+            v[2 * e + 1] = bf16_hi(p0[e]) + (bf16_hi(p1[e]) + bf16_hi(p2[e]));
+        }
+    }
+}
+
+__device__ __forceinline__ uint32_t byte_perm(uint32_t hi, uint32_t lo, uint32_t sel) { return __builtin_amdgcn_perm(hi, lo, sel); }
+
+// Digits of a block of 128 columns for a row group.  Lane l = (4 c + t) + 16 g brings columns 32 t + 8 g .. + 7 of row c
+// and leaves with digit t (t = 3: the leading one) of columns 32 j + 8 g .. + 7, j < 4, of the row: B[2 j], B[2 j + 1].
+// exponent: of the largest magnitude among what the lane's row has in the block (biased, at least 36, 255: not finite).
+__device__ __forceinline__ int block_exponent(const float (&v)[8]) {
+    float m = 0.f;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) m = __builtin_elementwise_maximum(m, fabsf(v[e]));        // NaN stays
+    m = __builtin_elementwise_maximum(m, lane_xor<1>(m));
+    m = __builtin_elementwise_maximum(m, lane_xor<2>(m));
+    m = __builtin_elementwise_maximum(m, lane_xor<16>(m));
+    m = __builtin_elementwise_maximum(m, lane_xor<32>(m));
+    return max((int)(__float_as_uint(m) >> 23 & 255u), 36);
+}
+// what a digit-t sum of 16 q * digit is worth
+__device__ __forceinline__ float digit_factor(int exponent, int t) {
+    return exponent == 255 ? __uint_as_float(0x7fc00000u) : __uint_as_float((unsigned)(exponent - 33 + 8 * t) << 23);
+}
+__device__ __forceinline__ void block_digits(const float (&v)[8], int exponent, uint32_t (&B)[8]) {
+    const float up = __uint_as_float((unsigned)(283 - exponent) << 23);       // 2^(30 - E): |v| stays below 2^30
+    uint32_t z[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) z[e] = ((uint32_t)(int)(v[e] * up) + 0x00808080u) ^ 0x00808080u;   // its bytes are the digits
+    uint32_t a[4][2];
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {                              // bytes of 4 columns by digit
+        const uint32_t p0 = byte_perm(z[4 * h + 1], z[4 * h], 0x05010400u), p1 = byte_perm(z[4 * h + 1], z[4 * h], 0x07030602u);
+        const uint32_t q0 = byte_perm(z[4 * h + 3], z[4 * h + 2], 0x05010400u), q1 = byte_perm(z[4 * h + 3], z[4 * h + 2], 0x07030602u);
+        a[0][h] = byte_perm(q0, p0, 0x05040100u);
+        a[1][h] = byte_perm(q0, p0, 0x07060302u);
+        a[2][h] = byte_perm(q1, p1, 0x05040100u);
+        a[3][h] = byte_perm(q1, p1, 0x07060302u);
+    }
+    const bool odd = threadIdx.x & 1, upper = threadIdx.x & 2;
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {                              // 4 x 4 transpose over the lanes t of a row
+#pragma unroll
+        for (int d = 0; d < 4; d += 2) {
+            const uint32_t x = lane_xor<1>(a[d + 1][h]), y = lane_xor<1>(a[d][h]);
+            a[d][h] = odd ? x : a[d][h];
+            a[d + 1][h] = odd ? a[d + 1][h] : y;
+        }
+#pragma unroll
+        for (int d = 0; d < 2; ++d) {
+            const uint32_t x = lane_xor<2>(a[d + 2][h]), y = lane_xor<2>(a[d][h]);
+            a[d][h] = upper ? x : a[d][h];
+            a[d + 2][h] = upper ? a[d + 2][h] : y;
+        }
+    }
+#pragma unroll
+    for (int j = 0; j < 4; ++j) { B[2 * j] = a[j][0]; B[2 * j + 1] = a[j][1]; }
+}
+
+__device__ __forceinline__ uint32_t upper_nibbles(uint32_t w) { return w & 0xf0f0f0f0u; }
+__device__ __forceinline__ uint32_t lower_nibbles(uint32_t w) { return (w << 4) & 0xf0f0f0f0u; }
+
+// sum += a block of a tile (w: its words, sc: scales of the lane's 4 rows) times a row group's digits
+template <int G>
+__device__ __forceinline__ void block_product(const uint4 &w, const float (&sc)[kQ4Block / G][4], const uint32_t (&B)[8], float f, f32x4_t &sum) {
+    const uint32_t words[4] = {w.x, w.y, w.z, w.w};
+    const i32x4_t none = {0, 0, 0, 0};
+    auto add = [&](const i32x4_t &acc, int gi) __attribute__((always_inline)) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) sum[i] = __builtin_fmaf((float)acc[i], sc[gi][i] * f, sum[i]);
+    };
+    if constexpr (G == 32) {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const long A = (long)((unsigned long)lower_nibbles(words[j]) << 32 | upper_nibbles(words[j]));
+            const long b = (long)((unsigned long)B[2 * j + 1] << 32 | B[2 * j]);
+            add(__builtin_amdgcn_mfma_i32_16x16x32_i8(A, b, none, 0, 0, 0), j);
+        }
+    } else {
+        i32x4_t acc = none;
+#pragma unroll
+        for (int s = 0; s < 2; ++s) {
+            const i32x4_t A = {(int)upper_nibbles(words[2 * s]), (int)lower_nibbles(words[2 * s]), (int)upper_nibbles(words[2 * s + 1]), (int)lower_nibbles(words[2 * s + 1])};
+            const i32x4_t b = {(int)B[4 * s], (int)B[4 * s + 1], (int)B[4 * s + 2], (int)B[4 * s + 3]};
+            acc = __builtin_amdgcn_mfma_i32_16x16x64_i8(A, b, G == 64 ? none : acc, 0, 0, 0);
+            if (G == 64) add(acc, s);
+        }
+        if (G == 128) add(acc, 0);
+    }
+}
+
+template <int G>
+__device__ __forceinline__ void load_scales(const uint16_t *S, size_t block, int g, float (&sc)[kQ4Block / G][4]) {
+    constexpr int per = kQ4Block / G;
+    const uint2 *p = reinterpret_cast<const uint2 *>(S + (block * 4 + g) * (4 * per));
+#pragma unroll
+    for (int gi = 0; gi < per; ++gi) {
+        const uint2 v = p[gi];
+        sc[gi][0] = bf16_lo(v.x); sc[gi][1] = bf16_hi(v.x); sc[gi][2] = bf16_lo(v.y); sc[gi][3] = bf16_hi(v.y);
+    }
+}
+
+// The value (gate, up: of the two halves of a tile) of row `row`, column n of tile t into place; the 16 columns of a row sit in 16 neighbouring lanes
+__device__ __forceinline__ void finish(const Q4Kernel &a, bool active, int row, int t, int n, float sum, float up, float inv) {
+    const int col = t * 16 + n;
+    if (a.epilogue == EPI_SWIGLU) {
+        if (!active || n >= 8) return;
+        const float gate = sum * inv;
+        uint16_t t3[kTerms];
+        split3(gate / (1.0f + expf(-gate)) * (up * inv), t3);
+#pragma unroll
+        for (int q = 0; q < kTerms; ++q) a.Xout[xpack_index(row, t * 8 + n, a.KS_out, q)] = t3[q];
+    } else if (a.epilogue == EPI_STORE) {
+        if (active && col < a.N) a.Y[(size_t)row * a.ldy + col] = sum * inv;
+    } else {
+        float hnew = 0.f;
+        if (active) {
+            hnew = a.Y[(size_t)row * a.ldy + col] + sum;
+            a.Y[(size_t)row * a.ldy + col] = hnew;
+            if (a.gain_next) {
+                uint16_t t3[kTerms];
+                split3(hnew * a.gain_next[col], t3);
+#pragma unroll
+                for (int q = 0; q < kTerms; ++q) a.Xnext[xpack_index(row, col, a.tiles / 2, q)] = t3[q];
+            }
+        }
+        const float sq = row_sum(hnew * hnew);
+        if (a.ssq_out && n == 0 && active) a.ssq_out[(size_t)row * a.tiles + t] = sq;
+    }
+}
+
+// A workgroup takes tiles of 16 outputs; its 8 waves take the blocks of a tile's row in turn and meet in LDS.
+constexpr int kQ4Waves = 8;
+template <int NG, int G>
+__global__ __launch_bounds__(kQ4Waves * 64) void q4_gemm_kernel(Q4Kernel a) {
+    const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int g = lane >> 4, t = lane & 3, c = (lane & 15) >> 2;
+    __shared__ float red[2][kQ4Waves][NG][16][kQ4Rows];
+    __shared__ float inv_s[kMaxRows];
+    const int last = min(a.rows, a.row0 + NG * kQ4Rows);
+    if (a.ssq_in) {
+        for (int r = a.row0 + w; r < last; r += kQ4Waves) {
+            float sum = 0.f;
+            for (int p = lane; p < a.ssq_in_parts; p += 64) sum += a.ssq_in[(size_t)r * (a.K / 16) + p];
+            sum = wave_sum(sum);
+            if (lane == 0) inv_s[r] = 1.0f / sqrtf(sum * a.inv_d + a.eps);
+        }
+    } else if (threadIdx.x < kMaxRows) {
+        inv_s[threadIdx.x] = 1.0f;
+    }
+    int parity = 0;
+    for (int tile = blockIdx.x; tile < a.tiles; tile += gridDim.x, parity ^= 1) {
+        f32x4_t sum[NG];
+#pragma unroll
+        for (int i = 0; i < NG; ++i) sum[i] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+        for (int b = w; b < a.KB; b += kQ4Waves) {
+            const size_t block = (size_t)tile * a.KB + b;
+            const uint4 words = a.W[block * 64 + lane];
+            float sc[kQ4Block / G][4];
+            load_scales<G>(a.S, block, g, sc);
+#pragma unroll
+            for (int i = 0; i < NG; ++i) {
+                float v[8];
+                uint32_t B[8];
+                load_x8(a, a.row0 + kQ4Rows * i + c, kQ4Block * b + 32 * t + 8 * g, v);
+                const int e = block_exponent(v);
+                block_digits(v, e, B);
+                block_product<G>(words, sc, B, digit_factor(e, t), sum[i]);
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < NG; ++i)
+#pragma unroll
+            for (int v = 0; v < 4; ++v) {                      // the digits' sums
+                const float x = xor_reduce<2, 1>(sum[i][v], AddOp());
+                if (t == 0) red[parity][w][i][4 * g + v][c] = x;
+            }
+        __syncthreads();
+        for (int e = threadIdx.x; e < NG * 64; e += kQ4Waves * 64) {
+            const int n = e & 15, cc = (e >> 4) & 3, i = e >> 6, row = a.row0 + kQ4Rows * i + cc;
+            float s = 0.f, up = 0.f;
+#pragma unroll
+            for (int ww = 0; ww < kQ4Waves; ++ww) { s += red[parity][ww][i][n][cc]; up += red[parity][ww][i][(n + 8) & 15][cc]; }
+            finish(a, row < a.rows, row, tile, n, s, up, inv_s[row < a.rows ? row : 0]);
+        }
+        // no second barrier: the next tile writes the other half of `red`
+    }
+}
+
+size_t q4_workspace_bytes(int rows, int N, int K) { (void)rows; (void)N; (void)K; return 0; }
+
+hipError_t launch_q4_gemm(const Q4GemmArgs &a, int epilogue, hipStream_t stream) {
+    if (a.rows < 1 || a.rows > kMaxRows || !q4_group_ok(a.group)) return hipErrorInvalidValue;
+    Q4Kernel k{};
+    k.W = (const uint4 *)a.W;
+    k.S = (const uint16_t *)((const char *)a.W + q4_scales_offset(a.N, a.K));
+    k.N = a.N; k.K = a.K; k.KB = (a.K + kQ4Block - 1) / kQ4Block; k.tiles = (a.N + 15) / 16;
+    k.X = a.X; k.x_kind = a.x_kind; k.ldx = a.ldx; k.KS = (a.K + 31) / 32; k.rows = a.rows;
+    k.Y = a.Y; k.ldy = a.ldy;
+    k.ssq_in = a.ssq_in; k.ssq_in_parts = a.ssq_in_parts; k.inv_d = 1.0f / (float)a.K; k.eps = a.eps;
+    k.gain_next = a.gain_next; k.Xnext = (uint16_t *)a.Xnext; k.ssq_out = a.ssq_out;
+    k.Xout = (uint16_t *)a.Xout; k.KS_out = (a.K_out + 31) / 32; k.epilogue = epilogue;
+    return with_group(a.group, [&](auto g) {
+        for (int r0 = 0; r0 < a.rows; r0 += 4 * kQ4Rows) {
+            k.row0 = r0;
+            const int ng = (std::min(a.rows - r0, 4 * kQ4Rows) + kQ4Rows - 1) / kQ4Rows;
+            const dim3 grid(std::min(k.tiles, 1024)), block(kQ4Waves * 64);
+            if (ng == 1) hipLaunchKernelGGL((q4_gemm_kernel<1, g()>), grid, block, 0, stream, k);
+            else if (ng == 2) hipLaunchKernelGGL((q4_gemm_kernel<2, g()>), grid, block, 0, stream, k);
+            else hipLaunchKernelGGL((q4_gemm_kernel<4, g()>), grid, block, 0, stream, k);
+        }
+    });
+}
+
+}  // namespace spd

@@ -20,13 +20,16 @@ _lib = ctypes.CDLL(LIB_PATH)
 SPD_OK = 0
 SPD_ERR_INVALID_ARG, SPD_ERR_SHAPE, SPD_ERR_CAPACITY, SPD_ERR_HIP = -1, -2, -3, -4
 SPD_TARGET_IS_PROBS, SPD_DRAFT_IS_PROBS = 1, 2
-SPD_MAX_ROWS, SPD_MAX_M = 64, 8
+SPD_ROWS_ARE_PROBS = SPD_W_IS_BF16 = SPD_X_IS_BF16 = 1
+SPD_MAX_ROWS, SPD_MAX_M, SPD_MAX_TOP = 64, 8, 32
 
 EXPORTS = ["spd_last_error", "spd_model_bytes", "spd_model_create", "spd_model_destroy", "spd_kv_set_len",
            "spd_kv_get_len", "spd_prefill", "spd_prefill_tokens", "spd_verify_forward", "spd_draft_step",
            "spd_accept_workspace_bytes", "spd_speculative_accept", "spd_trace_enable", "spd_trace_read",
            "spd_model_set_tuning", "spd_kv_lens_to_device", "spd_kv_lens_from_device", "spd_draft_step_strided",
-           "spd_block_finish", "spd_device_status", "spd_speculative_accept_static", "spd_kv_export", "spd_probe_read_chain"]
+           "spd_block_finish", "spd_device_status", "spd_speculative_accept_static", "spd_kv_export", "spd_probe_read_chain",
+           "spd_model_bytes_q4", "spd_model_create_q4", "spd_q4_bytes", "spd_q4_quantize", "spd_q4_dequantize", "spd_q4_pack",
+           "spd_q4_matmul_workspace_bytes", "spd_q4_matmul", "spd_logprobs_workspace_bytes", "spd_token_logprobs"]
 TRACE_KINDS = ["qkv", "o", "gate_up", "down", "lm_head", "attention", "embed"]
 PROJECTIONS = ["qkv", "o", "gate_up", "down", "lm_head"]
 
@@ -61,6 +64,19 @@ class spd_weights(ctypes.Structure):
                 ("mlp_norm", _PP), ("w_gate", _PP), ("w_up", _PP), ("w_down", _PP)]
 
 
+class spd_q4_matrix(ctypes.Structure):
+    _fields_ = [("q", ctypes.c_void_p), ("scales", ctypes.c_void_p)]
+
+
+_QP = ctypes.POINTER(spd_q4_matrix)
+
+
+class spd_weights_q4(ctypes.Structure):
+    _fields_ = [("group", ctypes.c_int32), ("embed", ctypes.c_void_p), ("lm_head", spd_q4_matrix), ("final_norm", ctypes.c_void_p),
+                ("attn_norm", _PP), ("wq", _QP), ("wk", _QP), ("wv", _QP), ("wo", _QP),
+                ("mlp_norm", _PP), ("w_gate", _QP), ("w_up", _QP), ("w_down", _QP)]
+
+
 _vp, _i32, _f32, _u32, _sz = ctypes.c_void_p, ctypes.c_int32, ctypes.c_float, ctypes.c_uint32, ctypes.c_size_t
 _szp = ctypes.POINTER(ctypes.c_size_t)
 _lib.spd_last_error.restype = ctypes.c_char_p
@@ -88,6 +104,17 @@ _lib.spd_kv_lens_from_device.argtypes = [_vp, _vp]
 _lib.spd_device_status.argtypes = [_vp, _vp]
 _lib.spd_draft_step_strided.argtypes = [_vp, _vp, _i32, _i32, _i32, _f32, _vp, _i32, _vp, _sz, _vp, _i32, _vp]
 _lib.spd_block_finish.argtypes = [_vp, _vp, _vp, _vp, _vp, _vp, _i32, _i32, _f32, _vp, _vp, _vp, _vp, _i32, _vp, _vp, _sz, _vp]
+_lib.spd_model_bytes_q4.argtypes = [ctypes.POINTER(spd_model_config), _i32, _szp, _szp, _szp]
+_lib.spd_model_create_q4.argtypes = [ctypes.POINTER(spd_model_config), ctypes.POINTER(spd_weights_q4), _vp, _sz, _vp, _sz,
+                                     _vp, _sz, _vp, ctypes.POINTER(_vp)]
+_lib.spd_q4_bytes.argtypes = [_i32, _i32, _i32, _szp]
+_lib.spd_q4_quantize.argtypes = [_vp, _sz, _u32, _i32, _i32, _i32, _vp, _vp, _vp]
+_lib.spd_q4_dequantize.argtypes = [_vp, _vp, _i32, _i32, _i32, _vp, _sz, _u32, _vp]
+_lib.spd_q4_pack.argtypes = [_vp, _vp, _i32, _i32, _i32, _vp, _sz, _vp]
+_lib.spd_q4_matmul_workspace_bytes.argtypes = [_i32, _i32, _i32, _szp]
+_lib.spd_q4_matmul.argtypes = [_vp, _i32, _i32, _i32, _vp, _sz, _u32, _i32, _vp, _sz, _vp, _sz, _vp]
+_lib.spd_logprobs_workspace_bytes.argtypes = [_i32, _i32, _i32, _szp]
+_lib.spd_token_logprobs.argtypes = [_vp, _sz, _vp, _i32, _i32, _f32, _u32, _vp, _vp, _vp, _i32, _vp, _vp, _vp, _sz, _vp]
 for _name in EXPORTS:
     if _name != "spd_last_error":
         getattr(_lib, _name).restype = _i32
@@ -127,6 +154,24 @@ def _raw(t, dtype):
     return t.data_ptr()
 
 
+def _matrix(t, *dtypes):
+    """Data pointer and row stride of a device matrix whose rows are contiguous (a view into a wider buffer is fine)."""
+    assert t.is_cuda and t.dim() == 2 and t.dtype in dtypes, f"expected a device matrix of {dtypes}, got {tuple(t.shape)} {t.dtype}"
+    assert t.device.index == _current_device(), "tensors have to be on the current device"
+    assert t.shape[1] <= 1 or t.stride(1) == 1, "contiguous rows only"
+    stride = t.stride(0) if t.shape[0] > 1 else t.shape[1]
+    assert stride >= t.shape[1], "rows overlap"
+    return t.data_ptr(), stride
+
+
+def _own(t, dtype, *shape):
+    """Data pointer of a contiguous tensor on the current device, of this type and shape."""
+    if t is None:
+        return None
+    assert t.device.index == _current_device() and tuple(t.shape) == shape, f"expected {shape} on the current device, got {tuple(t.shape)} on {t.device}"
+    return _ptr(t, dtype)
+
+
 def make_config(shape, max_seqs, max_positions):
     """spd_model_config from a synth.ModelShape-like object."""
     return spd_model_config(shape.n_layers, shape.d_model, shape.n_heads, shape.head_dim, shape.d_ffn,
@@ -140,13 +185,33 @@ def spd_model_bytes(cfg):
     return p.value, k.value, w.value
 
 
+def spd_model_bytes_q4(cfg, group):
+    p, k, w = ctypes.c_size_t(), ctypes.c_size_t(), ctypes.c_size_t()
+    _check(_lib.spd_model_bytes_q4(ctypes.byref(cfg), group, ctypes.byref(p), ctypes.byref(k), ctypes.byref(w)))
+    return p.value, k.value, w.value
+
+
+def quantize_weights(weights, group=128):
+    """Weights as produced by synth.make_weights with every matrix but the embedding table as a pair (q, scales) of
+    spd_q4_quantize: what Model takes for a model in 4 bits.  With tied embeddings the LM head is the quantised table."""
+    def q4(w):
+        q = torch.empty((w.shape[0], (w.shape[1] + 1) // 2), dtype=torch.uint8, device=w.device)
+        scales = torch.empty((w.shape[0], (w.shape[1] + group - 1) // group), dtype=torch.bfloat16, device=w.device)
+        spd_q4_quantize(w, group, q, scales)
+        return q, scales
+    head = weights.get("lm_head")
+    return {"group": group, "embed": weights["embed"], "lm_head": q4(weights["embed"] if head is None else head), "final_norm": weights["final_norm"],
+            "layers": [{k: v if k.endswith("norm") else q4(v) for k, v in lw.items()} for lw in weights["layers"]]}
+
+
 class Model:
     """Owns the three device buffers (torch allocations) and the spd_model handle."""
 
     def __init__(self, cfg, weights, device="cuda"):
-        """weights: dict as produced by synth.make_weights, tensors on `device`."""
+        """weights: dict as produced by synth.make_weights, or by quantize_weights for a model in 4 bits, tensors on `device`."""
         self.cfg = cfg
-        pb, kb, wb = spd_model_bytes(cfg)
+        group = weights.get("group")
+        pb, kb, wb = spd_model_bytes_q4(cfg, group) if group else spd_model_bytes(cfg)
         self.packed = torch.empty(pb, dtype=torch.uint8, device=device)
         self.kv = torch.zeros(kb, dtype=torch.uint8, device=device)
         self.workspace = torch.empty(wb, dtype=torch.uint8, device=device)
@@ -160,11 +225,27 @@ class Model:
             return a
 
         bf, f32 = torch.bfloat16, torch.float32
+        handle = ctypes.c_void_p()
+        if group:
+            d, hd, F, V = cfg.d_model, cfg.n_heads * cfg.head_dim, cfg.d_ffn, cfg.vocab
+            shapes = {"wq": (hd, d), "wk": (hd, d), "wv": (hd, d), "wo": (d, hd), "w_gate": (F, d), "w_up": (F, d), "w_down": (d, F)}
+
+            def matrix(pair, n, k):
+                return spd_q4_matrix(_own(pair[0], torch.uint8, n, (k + 1) // 2), _own(pair[1], bf, n, (k + group - 1) // group))
+            mats = {key: (spd_q4_matrix * L)(*[matrix(lw[key], *shapes[key]) for lw in weights["layers"]]) for key in shapes}
+            norms = [arr("attn_norm", f32), arr("mlp_norm", f32)]
+            w = spd_weights_q4(group, _ptr(weights["embed"], bf), matrix(weights["lm_head"], V, d), _ptr(weights["final_norm"], f32),
+                               ctypes.cast(norms[0], _PP), *[ctypes.cast(mats[k], _QP) for k in ("wq", "wk", "wv", "wo")],
+                               ctypes.cast(norms[1], _PP), *[ctypes.cast(mats[k], _QP) for k in ("w_gate", "w_up", "w_down")])
+            _check(_lib.spd_model_create_q4(ctypes.byref(cfg), ctypes.byref(w), _ptr(self.packed), pb, _ptr(self.kv), kb,
+                                            _ptr(self.workspace), wb, _stream(), ctypes.byref(handle)))
+            self.handle = handle
+            torch.cuda.current_stream().synchronize()     # re-tiling done: the caller may drop `weights`
+            return
         keep = [arr("attn_norm", f32), arr("wq", bf), arr("wk", bf), arr("wv", bf), arr("wo", bf),
                 arr("mlp_norm", f32), arr("w_gate", bf), arr("w_up", bf), arr("w_down", bf)]
         w = spd_weights(_ptr(weights["embed"], bf), _ptr(weights.get("lm_head"), bf), _ptr(weights["final_norm"], f32),
                         *[ctypes.cast(a, _PP) for a in keep])
-        handle = ctypes.c_void_p()
         _check(_lib.spd_model_create(ctypes.byref(cfg), ctypes.byref(w), _ptr(self.packed), pb, _ptr(self.kv), kb,
                                      _ptr(self.workspace), wb, _stream(), ctypes.byref(handle)))
         self.handle = handle
@@ -304,6 +385,74 @@ def spd_speculative_accept_static(target, draft, draft_tokens, u, temperature, f
                                               _ptr(draft_tokens, torch.int32), _ptr(u, torch.float32), n_seqs, gamma, vocab,
                                               float(temperature), int(flags), _ptr(n_accepted_out, torch.int32),
                                               _ptr(next_token_out, torch.int32), _ptr(accept_prob_out, torch.float32), _stream()))
+
+
+def spd_logprobs_workspace_bytes(n_rows, vocab, n_top):
+    b = ctypes.c_size_t()
+    _check(_lib.spd_logprobs_workspace_bytes(n_rows, vocab, n_top, ctypes.byref(b)))
+    return b.value
+
+
+def spd_token_logprobs(rows, tokens, temperature, flags, logprob_out=None, entropy_out=None, rank_out=None, top_tokens_out=None,
+                       top_logprobs_out=None, workspace=None):
+    """rows [n, vocab] (a view into a wider buffer is fine); the number of alternatives is that of top_tokens_out's columns."""
+    n, vocab = rows.shape
+    ptr, stride = _matrix(rows, torch.float32)
+    n_top = 0 if top_tokens_out is None else top_tokens_out.shape[1]
+    if workspace is None:
+        workspace = torch.empty(spd_logprobs_workspace_bytes(n, vocab, n_top), dtype=torch.uint8, device=rows.device)
+    _check(_lib.spd_token_logprobs(ptr, stride, _own(tokens, torch.int32, n), n, vocab, float(temperature), int(flags),
+                                   _own(logprob_out, torch.float32, n), _own(entropy_out, torch.float32, n), _own(rank_out, torch.int32, n),
+                                   n_top, _own(top_tokens_out, torch.int32, n, n_top), _own(top_logprobs_out, torch.float32, n, n_top),
+                                   _own(workspace, torch.uint8, workspace.numel()), workspace.numel(), _stream()))
+
+
+def spd_q4_bytes(n, k, group):
+    b = ctypes.c_size_t()
+    _check(_lib.spd_q4_bytes(n, k, group, ctypes.byref(b)))
+    return b.value
+
+
+def spd_q4_quantize(w, group, q_out, scales_out):
+    n, k = w.shape
+    ptr, stride = _matrix(w, torch.float32, torch.bfloat16)
+    _check(_lib.spd_q4_quantize(ptr, stride, SPD_W_IS_BF16 if w.dtype == torch.bfloat16 else 0, n, k, group, _own(q_out, torch.uint8, n, (k + 1) // 2),
+                                _own(scales_out, torch.bfloat16, n, (k + group - 1) // group), _stream()))
+
+
+def spd_q4_dequantize(q, scales, group, w_out):
+    n, k = w_out.shape
+    ptr, stride = _matrix(w_out, torch.float32, torch.bfloat16)
+    _check(_lib.spd_q4_dequantize(_own(q, torch.uint8, n, (k + 1) // 2), _own(scales, torch.bfloat16, n, (k + group - 1) // group), n, k, group, ptr,
+                                  stride, SPD_W_IS_BF16 if w_out.dtype == torch.bfloat16 else 0, _stream()))
+
+
+class Q4Matrix:
+    """A matrix [n, k] in 4 bits, laid out for spd_q4_matmul (owns the packed buffer; q and scales may be dropped)."""
+
+    def __init__(self, q, scales, k, group):
+        self.n, self.k, self.group = q.shape[0], int(k), int(group)
+        self.packed = torch.empty(spd_q4_bytes(self.n, self.k, self.group), dtype=torch.uint8, device=q.device)
+        _check(_lib.spd_q4_pack(_own(q, torch.uint8, self.n, (self.k + 1) // 2), _own(scales, torch.bfloat16, self.n, (self.k + self.group - 1) // self.group),
+                                self.n, self.k, self.group, _ptr(self.packed), self.packed.numel(), _stream()))
+
+
+def spd_q4_matmul_workspace_bytes(rows, n, k):
+    b = ctypes.c_size_t()
+    _check(_lib.spd_q4_matmul_workspace_bytes(rows, n, k, ctypes.byref(b)))
+    return b.value
+
+
+def spd_q4_matmul(matrix, x, y, workspace=None):
+    """y [rows, matrix.n] float32 = x [rows, matrix.k] (float32 or bfloat16) times the matrix; both may be views into wider buffers."""
+    rows = x.shape[0]
+    assert x.shape[1] == matrix.k and tuple(y.shape) == (rows, matrix.n)
+    xp, xs = _matrix(x, torch.float32, torch.bfloat16)
+    yp, ys = _matrix(y, torch.float32)
+    if workspace is None:
+        workspace = torch.empty(spd_q4_matmul_workspace_bytes(rows, matrix.n, matrix.k), dtype=torch.uint8, device=x.device)
+    _check(_lib.spd_q4_matmul(_ptr(matrix.packed), matrix.n, matrix.k, matrix.group, xp, xs, SPD_X_IS_BF16 if x.dtype == torch.bfloat16 else 0, rows,
+                              yp, ys, _own(workspace, torch.uint8, workspace.numel()), workspace.numel(), _stream()))
 
 
 def spd_probe_read_chain(buffer, stage_bytes, reps=20):
