@@ -54,6 +54,7 @@ extern "C" {
 #define SPD_MAX_M             8    /* new tokens per sequence per forward call    */
 
 #define SPD_MAX_TOP          32    /* alternatives per row of spd_token_logprobs      */
+#define SPD_MAX_LOGPROB_VOCAB (1 << 24)  /* entries per row of spd_token_logprobs       */
 
 /* flags of spd_speculative_accept */
 #define SPD_TARGET_IS_PROBS  1u    /* target rows are probabilities, not logits   */
@@ -297,7 +298,7 @@ int32_t spd_speculative_accept_static(const float *target, const float *draft, c
  * Entries at -infinity (probability 0) weigh nothing and are no alternatives: places they leave hold token -1 and -infinity.  A
  * row of nothing else: log probability -infinity, entropy 0.  A token outside 0..vocab-1: -infinity, rank vocab.  A row with a NaN or
  * +infinity (probabilities: a negative or infinite one or a NaN) has no distribution: NaN, rank and alternatives -1.
- * Errors: SPD_ERR_INVALID_ARG, SPD_ERR_CAPACITY (workspace too small). */
+ * Errors: SPD_ERR_INVALID_ARG, SPD_ERR_SHAPE (vocab > SPD_MAX_LOGPROB_VOCAB), SPD_ERR_CAPACITY (workspace too small). */
 int32_t spd_logprobs_workspace_bytes(int32_t n_rows, int32_t vocab, int32_t n_top, size_t *h_bytes);
 int32_t spd_token_logprobs(const float *rows, size_t row_stride, const int32_t *tokens, int32_t n_rows, int32_t vocab,
                            float temperature, uint32_t flags, float *logprob_out, float *entropy_out, int32_t *rank_out,
@@ -305,7 +306,7 @@ int32_t spd_token_logprobs(const float *rows, size_t row_stride, const int32_t *
                            void *workspace, size_t workspace_bytes, void *stream);
 
 /* ---- weights in 4 bits (format: spd_q4_matrix) -----------------------------------------------------
- * spd_q4_quantize: a = the largest magnitude of a group, scale = a / 7 rounded to bfloat16, q = w / scale rounded to the nearest
+ * spd_q4_quantize: a = the largest magnitude of a group, scale = a * (float32)(1 / 7) rounded to bfloat16, q = w / scale (float32) rounded to the nearest
  * integer (even on ties), limited to -8..7; 0 where the scale is 0.  A group with a value that is not finite: scale NaN, q 0.
  * w: float32, or bfloat16 with SPD_W_IS_BF16, [N, K] with w_stride elements between rows.
  * spd_q4_dequantize: the values that q and scales stand for (rounded once if bfloat16).

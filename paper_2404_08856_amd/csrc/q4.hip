@@ -68,7 +68,7 @@ __global__ __launch_bounds__(256) void q4_quantize_kernel(const T *__restrict__ 
     if (G >= 64) m = __builtin_elementwise_maximum(m, lane_xor<4>(m));
     if (G >= 128) m = __builtin_elementwise_maximum(m, lane_xor<8>(m));
     const bool finite = m < INFINITY;
-    const uint16_t s16 = finite ? f32_to_bf16_bits(m / 7.0f) : (uint16_t)0x7fc0;
+    const uint16_t s16 = finite ? f32_to_bf16_bits(m * (1.0f / 7.0f)) : (uint16_t)0x7fc0;
     const float s = bf16_bits_to_f32(s16);
     uint32_t bytes = 0;
 #pragma unroll

@@ -26,7 +26,7 @@ def quantize_ref(w, G):
         part = w[:, G * i:G * (i + 1)].astype(np.float32)
         a = np.max(np.abs(part), axis=1)
         fine = np.isfinite(a)
-        s = to_bf16(np.where(fine, a, np.float32(0)) / np.float32(7))
+        s = to_bf16(np.where(fine, a, np.float32(0)) * (np.float32(1) / np.float32(7)))
         quot = np.divide(part, s[:, None], out=np.zeros_like(part), where=(fine & (s != 0))[:, None])
         q[:, G * i:G * (i + 1)] = np.clip(np.rint(quot), -8, 7)
         scales[:, i] = np.where(fine, s, np.float32(np.nan))
