@@ -330,14 +330,15 @@ __device__ __forceinline__ void block_digits(const float (&v)[8], int exponent, 
 __device__ __forceinline__ uint32_t upper_nibbles(uint32_t w) { return w & 0xf0f0f0f0u; }
 __device__ __forceinline__ uint32_t lower_nibbles(uint32_t w) { return (w << 4) & 0xf0f0f0f0u; }
 
-// sum += a block of a tile (w: its words, sc: scales of the lane's 4 rows) times a row group's digits
-template <int G>
+// sum += a block of a tile (w: its words, sc: scales of the lane's 4 rows) times a row group's digits.  FACTOR: f is their
+// block's factor; otherwise the digits of a whole row have one, and the sum takes it in the end.
+template <int G, bool FACTOR>
 __device__ __forceinline__ void block_product(const uint4 &w, const float (&sc)[kQ4Block / G][4], const uint32_t (&B)[8], float f, f32x4_t &sum) {
     const uint32_t words[4] = {w.x, w.y, w.z, w.w};
     const i32x4_t none = {0, 0, 0, 0};
     auto add = [&](const i32x4_t &acc, int gi) __attribute__((always_inline)) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) sum[i] = __builtin_fmaf((float)acc[i], sc[gi][i] * f, sum[i]);
+        for (int i = 0; i < 4; ++i) sum[i] = __builtin_fmaf((float)acc[i], FACTOR ? sc[gi][i] * f : sc[gi][i], sum[i]);
     };
     if constexpr (G == 32) {
 #pragma unroll
@@ -360,15 +361,23 @@ __device__ __forceinline__ void block_product(const uint4 &w, const float (&sc)[
 }
 
 template <int G>
-__device__ __forceinline__ void load_scales(const uint16_t *S, size_t block, int g, float (&sc)[kQ4Block / G][4]) {
-    constexpr int per = kQ4Block / G;
-    const uint2 *p = reinterpret_cast<const uint2 *>(S + (block * 4 + g) * (4 * per));
+struct Q4Words {                                               // a lane's part of a block: 32 weights of one row, the scales of 4
+    uint4 w;
+    uint2 s[kQ4Block / G];
+    __device__ __forceinline__ void load(const Q4Kernel &a, size_t block, int lane) {
+        constexpr int per = kQ4Block / G;
+        typedef __attribute__((ext_vector_type(4))) unsigned int u32x4_t;
+        const u32x4_t v = __builtin_nontemporal_load(reinterpret_cast<const u32x4_t *>(a.W) + block * 64 + lane);    // read once
+        w = uint4{v.x, v.y, v.z, v.w};
+        const uint2 *p = reinterpret_cast<const uint2 *>(a.S + (block * 4 + (lane >> 4)) * (4 * per));
 #pragma unroll
-    for (int gi = 0; gi < per; ++gi) {
-        const uint2 v = p[gi];
-        sc[gi][0] = bf16_lo(v.x); sc[gi][1] = bf16_hi(v.x); sc[gi][2] = bf16_lo(v.y); sc[gi][3] = bf16_hi(v.y);
+        for (int i = 0; i < per; ++i) s[i] = p[i];
     }
-}
+    __device__ __forceinline__ void scales(float (&sc)[kQ4Block / G][4]) const {
+#pragma unroll
+        for (int i = 0; i < kQ4Block / G; ++i) { sc[i][0] = bf16_lo(s[i].x); sc[i][1] = bf16_hi(s[i].x); sc[i][2] = bf16_lo(s[i].y); sc[i][3] = bf16_hi(s[i].y); }
+    }
+};
 
 // The value (gate, up: of the two halves of a tile) of row `row`, column n of tile t into place; the 16 columns of a row sit in 16 neighbouring lanes
 __device__ __forceinline__ void finish(const Q4Kernel &a, bool active, int row, int t, int n, float sum, float up, float inv) {
@@ -399,17 +408,12 @@ __device__ __forceinline__ void finish(const Q4Kernel &a, bool active, int row, 
     }
 }
 
-// A workgroup takes tiles of 16 outputs; its 8 waves take the blocks of a tile's row in turn and meet in LDS.
-constexpr int kQ4Waves = 8;
-template <int NG, int G>
-__global__ __launch_bounds__(kQ4Waves * 64) void q4_gemm_kernel(Q4Kernel a) {
-    const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int g = lane >> 4, t = lane & 3, c = (lane & 15) >> 2;
-    __shared__ float red[2][kQ4Waves][NG][16][kQ4Rows];
-    __shared__ float inv_s[kMaxRows];
-    const int last = min(a.rows, a.row0 + NG * kQ4Rows);
+// 1 / rms of rows row0 .. last - 1 into inv_s (1 without a norm); the caller synchronises
+template <int WAVES>
+__device__ __forceinline__ void row_scales(const Q4Kernel &a, int last, float *inv_s) {
+    const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
     if (a.ssq_in) {
-        for (int r = a.row0 + w; r < last; r += kQ4Waves) {
+        for (int r = a.row0 + w; r < last; r += WAVES) {
             float sum = 0.f;
             for (int p = lane; p < a.ssq_in_parts; p += 64) sum += a.ssq_in[(size_t)r * (a.K / 16) + p];
             sum = wave_sum(sum);
@@ -418,46 +422,262 @@ __global__ __launch_bounds__(kQ4Waves * 64) void q4_gemm_kernel(Q4Kernel a) {
     } else if (threadIdx.x < kMaxRows) {
         inv_s[threadIdx.x] = 1.0f;
     }
+}
+
+// ---- few rows (1 .. 8): the waves of a workgroup share a tile's blocks ------------------------------------
+// A workgroup takes tiles of 16 outputs, wave w blocks w, w + WAVES, ... of each, and the waves meet in LDS.  Every workgroup makes
+// the digits for itself, while its first weights are on their way.  NB > 0: the wave's digits (NB blocks) stay in
+// registers for all of the workgroup's tiles, and a block's words are replaced by the next tile's as soon as they
+// are used; NB = 0: any K, digits made anew for every tile.
+template <int WAVES, int NG, int G, int NB>
+__global__ __launch_bounds__(WAVES * 64) void q4_few_kernel(Q4Kernel a) {
+    const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int g = lane >> 4, t = lane & 3, c = (lane & 15) >> 2;
+    __shared__ float red[2][WAVES][NG][16][kQ4Rows];
+    __shared__ float inv_s[kMaxRows];
+    constexpr int RES = NB > 0 ? NB : 1;
+    Q4Words<G> words[RES];
+    uint32_t B[NG][RES][8];
+    float f[NG][RES];
+    int tile = blockIdx.x;
+    auto digits = [&](int b, int i) __attribute__((always_inline)) {
+#pragma unroll
+        for (int rg = 0; rg < NG; ++rg) {
+            float v[8];
+            load_x8(a, a.row0 + kQ4Rows * rg + c, b < a.KB ? kQ4Block * b + 32 * t + 8 * g : a.K, v);      // (beyond the matrix: zeros)
+            const int e = block_exponent(v);
+            block_digits(v, e, B[rg][i]);
+            f[rg][i] = digit_factor(e, t);
+        }
+    };
+    if (NB > 0) {
+#pragma unroll
+        for (int i = 0; i < NB; ++i) words[i].load(a, (size_t)tile * a.KB + min(w + i * WAVES, a.KB - 1), lane);
+#pragma unroll
+        for (int i = 0; i < NB; ++i) digits(w + i * WAVES, i);
+    }
+    row_scales<WAVES>(a, min(a.rows, a.row0 + NG * kQ4Rows), inv_s);
     int parity = 0;
-    for (int tile = blockIdx.x; tile < a.tiles; tile += gridDim.x, parity ^= 1) {
+    for (; tile < a.tiles; tile += gridDim.x, parity ^= 1) {
         f32x4_t sum[NG];
 #pragma unroll
-        for (int i = 0; i < NG; ++i) sum[i] = f32x4_t{0.f, 0.f, 0.f, 0.f};
-        for (int b = w; b < a.KB; b += kQ4Waves) {
-            const size_t block = (size_t)tile * a.KB + b;
-            const uint4 words = a.W[block * 64 + lane];
+        for (int rg = 0; rg < NG; ++rg) sum[rg] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+        auto multiply = [&](int i) __attribute__((always_inline)) {
             float sc[kQ4Block / G][4];
-            load_scales<G>(a.S, block, g, sc);
+            words[i].scales(sc);
 #pragma unroll
-            for (int i = 0; i < NG; ++i) {
-                float v[8];
-                uint32_t B[8];
-                load_x8(a, a.row0 + kQ4Rows * i + c, kQ4Block * b + 32 * t + 8 * g, v);
-                const int e = block_exponent(v);
-                block_digits(v, e, B);
-                block_product<G>(words, sc, B, digit_factor(e, t), sum[i]);
+            for (int rg = 0; rg < NG; ++rg) block_product<G, true>(words[i].w, sc, B[rg][i], f[rg][i], sum[rg]);
+        };
+        if (NB > 0) {
+            const int next = tile + (int)gridDim.x < a.tiles ? tile + (int)gridDim.x : tile;      // (a harmless second read in the end)
+#pragma unroll
+            for (int i = 0; i < NB; ++i) {
+                multiply(i);
+                words[i].load(a, (size_t)next * a.KB + min(w + i * WAVES, a.KB - 1), lane);
+                __builtin_amdgcn_sched_barrier(0);            // keep "use, replace" in program order
+            }
+        } else {
+            for (int b = w; b < a.KB; b += WAVES) {
+                words[0].load(a, (size_t)tile * a.KB + b, lane);
+                digits(b, 0);
+                multiply(0);
             }
         }
 #pragma unroll
-        for (int i = 0; i < NG; ++i)
+        for (int rg = 0; rg < NG; ++rg)
 #pragma unroll
             for (int v = 0; v < 4; ++v) {                      // the digits' sums
-                const float x = xor_reduce<2, 1>(sum[i][v], AddOp());
-                if (t == 0) red[parity][w][i][4 * g + v][c] = x;
+                const float x = xor_reduce<2, 1>(sum[rg][v], AddOp());
+                if (t == 0) red[parity][w][rg][4 * g + v][c] = x;
             }
         __syncthreads();
-        for (int e = threadIdx.x; e < NG * 64; e += kQ4Waves * 64) {
-            const int n = e & 15, cc = (e >> 4) & 3, i = e >> 6, row = a.row0 + kQ4Rows * i + cc;
+        for (int e = threadIdx.x; e < NG * 64; e += WAVES * 64) {
+            const int n = e & 15, cc = (e >> 4) & 3, rg = e >> 6, row = a.row0 + kQ4Rows * rg + cc;
             float s = 0.f, up = 0.f;
 #pragma unroll
-            for (int ww = 0; ww < kQ4Waves; ++ww) { s += red[parity][ww][i][n][cc]; up += red[parity][ww][i][(n + 8) & 15][cc]; }
+            for (int ww = 0; ww < WAVES; ++ww) s += red[parity][ww][rg][n][cc];
+            if (a.epilogue == EPI_SWIGLU)
+#pragma unroll
+                for (int ww = 0; ww < WAVES; ++ww) up += red[parity][ww][rg][(n + 8) & 15][cc];
             finish(a, row < a.rows, row, tile, n, s, up, inv_s[row < a.rows ? row : 0]);
         }
         // no second barrier: the next tile writes the other half of `red`
     }
 }
 
-size_t q4_workspace_bytes(int rows, int N, int K) { (void)rows; (void)N; (void)K; return 0; }
+// ---- many rows (9 .. 64) -------------------------------------------------------------------------------
+// The digits are made once, by a kernel of their own, with one exponent per row.  Layout: [row group][block][step][lane] of 16
+// bytes, then the factor of each of a row group's 16 columns.
+constexpr int kQ4DigitThreads = 1024;
+__global__ __launch_bounds__(kQ4DigitThreads) void q4_digits_kernel(Q4Kernel a, uint4 *digits, float *factors) {
+    constexpr int WAVES = kQ4DigitThreads / 64;
+    const int rg = blockIdx.x, lane = threadIdx.x & 63, w = threadIdx.x >> 6, g = lane >> 4, t = lane & 3, c = (lane & 15) >> 2;
+    __shared__ float top[WAVES][kQ4Rows];
+    float m = 0.f, v[8];
+    for (int b = w; b < a.KB; b += WAVES) {
+        load_x8(a, kQ4Rows * rg + c, kQ4Block * b + 32 * t + 8 * g, v);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) m = __builtin_elementwise_maximum(m, fabsf(v[e]));
+    }
+    m = __builtin_elementwise_maximum(m, lane_xor<1>(m));
+    m = __builtin_elementwise_maximum(m, lane_xor<2>(m));
+    m = __builtin_elementwise_maximum(m, lane_xor<16>(m));
+    m = __builtin_elementwise_maximum(m, lane_xor<32>(m));
+    if (g == 0 && t == 0) top[w][c] = m;
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < WAVES; ++i) m = __builtin_elementwise_maximum(m, top[i][c]);
+    const int exponent = max((int)(__float_as_uint(m) >> 23 & 255u), 36);
+    if (w == 0 && g == 0) factors[16 * rg + lane] = digit_factor(exponent, t);
+    for (int b = w; b < a.KB; b += WAVES) {
+        uint32_t B[8];
+        load_x8(a, kQ4Rows * rg + c, kQ4Block * b + 32 * t + 8 * g, v);
+        block_digits(v, exponent, B);
+        uint4 *dst = digits + ((size_t)rg * a.KB + b) * 128 + lane;
+        dst[0] = uint4{B[0], B[1], B[2], B[3]};
+        dst[64] = uint4{B[4], B[5], B[6], B[7]};
+    }
+}
+
+// 8 waves: 4 pairs of tiles x 2 halves of the workgroup's blocks.  The digits of a block go through LDS, where the 4 waves of a half
+// read them; a wave uses what it reads for both of its tiles.  To fill the chip where a matrix has few tiles the blocks
+// are cut into `slices` across workgroups, whose sums q4_join_kernel adds.
+constexpr int kQ4ManyTiles = 8;
+template <int NG, int G>
+__global__ __launch_bounds__(512) void q4_many_kernel(Q4Kernel a, const uint4 *digits, const float *factors, float *partials, int slices, int ng) {
+    const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), half = w >> 2, wt = w & 3;
+    const int g = lane >> 4, t = lane & 3, c = (lane & 15) >> 2;
+    const int group = blockIdx.x / slices, slice = blockIdx.x - group * slices;
+    const int b0 = (int)((long)a.KB * slice / slices), b1 = (int)((long)a.KB * (slice + 1) / slices), mid = (b0 + b1) / 2;
+    const int first = half ? mid : b0, last = half ? b1 : mid, steps = b1 - mid;        // the second half is the longer one
+    extern __shared__ uint4 lds[];                             // [2 buffers][2 halves][NG][2][64]
+    const int t0 = group * kQ4ManyTiles + 2 * wt;
+    f32x4_t sum[2][NG];
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+#pragma unroll
+        for (int rg = 0; rg < NG; ++rg) sum[i][rg] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+    const int me = threadIdx.x & 255;                          // of the half's 256 threads
+    constexpr int PER = NG / 2;                                // 16-byte pieces of a block's digits per thread (NG is even)
+    uint4 stage[PER];
+    Q4Words<G> words[2];
+    auto fetch = [&](int b) __attribute__((always_inline)) {
+        b = min(b, a.KB - 1);
+#pragma unroll
+        for (int i = 0; i < PER; ++i) {
+            const int piece = i * 256 + me, rg = min(piece >> 7, ng - 1);
+            stage[i] = digits[((size_t)rg * a.KB + b) * 128 + (piece & 127)];
+        }
+    };
+    auto store = [&](int buffer) __attribute__((always_inline)) {
+#pragma unroll
+        for (int i = 0; i < PER; ++i) lds[(buffer * 2 + half) * NG * 128 + i * 256 + me] = stage[i];
+    };
+    auto weights = [&](int b) __attribute__((always_inline)) {
+#pragma unroll
+        for (int i = 0; i < 2; ++i) words[i].load(a, (size_t)min(t0 + i, a.tiles - 1) * a.KB + min(b, a.KB - 1), lane);
+    };
+    fetch(first);
+    weights(first);
+    for (int s = 0; s < steps; ++s) {
+        store(s & 1);
+        if (s + 1 < steps) fetch(first + s + 1);
+        __syncthreads();
+        Q4Words<G> now[2] = {words[0], words[1]};
+        if (s + 1 < steps) weights(first + s + 1);
+        if (first + s < last) {
+            float sc[2][kQ4Block / G][4];
+            now[0].scales(sc[0]);
+            now[1].scales(sc[1]);
+            const uint4 *src = lds + ((s & 1) * 2 + half) * NG * 128;
+#pragma unroll
+            for (int rg = 0; rg < NG; ++rg) {
+                const uint4 lo = src[rg * 128 + lane], hi = src[rg * 128 + 64 + lane];
+                const uint32_t B[8] = {lo.x, lo.y, lo.z, lo.w, hi.x, hi.y, hi.z, hi.w};
+                block_product<G, false>(now[0].w, sc[0], B, 1.f, sum[0][rg]);
+                block_product<G, false>(now[1].w, sc[1], B, 1.f, sum[1][rg]);
+            }
+        }
+    }
+    __syncthreads();                                           // the digits have been read
+    float *red = reinterpret_cast<float *>(lds);               // [half][4 pairs][2][NG][16 rows of the tile][4]
+    __shared__ float inv_s[kMaxRows];
+    row_scales<8>(a, a.rows, inv_s);
+#pragma unroll
+    for (int rg = 0; rg < NG; ++rg) {
+        const float f = factors[16 * min(rg, ng - 1) + (lane & 15)];
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+#pragma unroll
+            for (int v = 0; v < 4; ++v) {
+                const float x = xor_reduce<2, 1>(sum[i][rg][v] * f, AddOp());
+                if (t == 0) red[((((half * 4 + wt) * 2 + i) * NG + rg) * 16 + 4 * g + v) * 4 + c] = x;
+            }
+    }
+    __syncthreads();
+    constexpr int HALF = 8 * NG * 64;
+    for (int e = threadIdx.x; e < HALF; e += 512) {
+        const int n = e & 15, cc = (e >> 4) & 3, rg = (e >> 6) % NG, ti = (e >> 6) / NG, row = kQ4Rows * rg + cc, tile = group * kQ4ManyTiles + ti;
+        const int at = ((ti * NG + rg) * 16 + n) * 4 + cc, at_up = ((ti * NG + rg) * 16 + ((n + 8) & 15)) * 4 + cc;
+        const float s = red[at] + red[HALF + at], up = red[at_up] + red[HALF + at_up];
+        if (slices > 1) {
+            if (row < a.rows && tile < a.tiles) partials[((size_t)slice * a.rows + row) * (a.tiles * 16) + tile * 16 + n] = s;
+        } else {
+            finish(a, row < a.rows && tile < a.tiles, row, tile, n, s, up, inv_s[row < a.rows ? row : 0]);
+        }
+    }
+}
+
+// The sums of the slices, in order, into place: 16 rows of a tile per workgroup
+__global__ __launch_bounds__(256) void q4_join_kernel(Q4Kernel a, const float *partials, int slices) {
+    const int tile = blockIdx.x, n = threadIdx.x & 15, row = blockIdx.y * 16 + (threadIdx.x >> 4);
+    __shared__ float inv_s[kMaxRows];
+    a.row0 = blockIdx.y * 16;
+    row_scales<4>(a, min(a.rows, a.row0 + 16), inv_s);
+    __syncthreads();
+    const bool active = row < a.rows;
+    float s = 0.f, up = 0.f;
+    const size_t ld = (size_t)a.tiles * 16;
+    for (int i = 0; active && i < slices; ++i) {
+        const float *p = partials + ((size_t)i * a.rows + row) * ld + tile * 16;
+        s += p[n];
+        if (a.epilogue == EPI_SWIGLU) up += p[(n + 8) & 15];
+    }
+    finish(a, active, row, tile, n, s, up, inv_s[active ? row : 0]);
+}
+
+constexpr int kQ4FewRows = 8, kQ4MaxSlices = 8;
+static int many_slices(int N, int K) {                        // about one workgroup per CU, at least 4 blocks each
+    const int groups = ((N + 15) / 16 + kQ4ManyTiles - 1) / kQ4ManyTiles, KB = (K + kQ4Block - 1) / kQ4Block;
+    return std::max(1, std::min({256 / groups, kQ4MaxSlices, KB / 4}));
+}
+static size_t digit_bytes(int rows, int K) { return (size_t)((rows + 3) / 4) * ((K + kQ4Block - 1) / kQ4Block) * 2048; }
+
+size_t q4_workspace_bytes(int rows, int N, int K) {
+    if (rows <= kQ4FewRows) return 0;
+    const int slices = many_slices(N, K);
+    return digit_bytes(rows, K) + 1024 + (slices > 1 ? (size_t)slices * rows * ((N + 15) / 16 * 16) * 4 : 0);
+}
+
+template <int NG, int G>
+static hipError_t launch_many(const Q4Kernel &k, const uint4 *digits, const float *factors, float *partials, int slices, int ng, hipStream_t stream) {
+    constexpr size_t lds = (size_t)NG * 8192;
+    static const hipError_t ready = hipFuncSetAttribute((const void *)q4_many_kernel<NG, G>, hipFuncAttributeMaxDynamicSharedMemorySize, lds);
+    if (ready != hipSuccess) return ready;
+    const int groups = (k.tiles + kQ4ManyTiles - 1) / kQ4ManyTiles;
+    hipLaunchKernelGGL((q4_many_kernel<NG, G>), dim3(groups * slices), dim3(512), lds, stream, k, digits, factors, partials, slices, ng);
+    return hipGetLastError();
+}
+
+template <int NG, int G>
+static void launch_few(const Q4Kernel &k, hipStream_t stream) {
+    // Blocks of digits that a wave keeps: 4 where 8 waves cover K with them.  A workgroup that has one tile only gains nothing by keeping any.
+    const dim3 grid(std::min(k.tiles, 256));
+    if (k.KB <= 8) hipLaunchKernelGGL((q4_few_kernel<8, NG, G, 1>), dim3(std::min(k.tiles, 1024)), dim3(512), 0, stream, k);
+    else if (k.KB <= 16) hipLaunchKernelGGL((q4_few_kernel<8, NG, G, 2>), dim3(std::min(k.tiles, 512)), dim3(512), 0, stream, k);
+    else if (k.KB <= 32) hipLaunchKernelGGL((q4_few_kernel<8, NG, G, 4>), grid, dim3(512), 0, stream, k);
+    else hipLaunchKernelGGL((q4_few_kernel<16, NG, G, 0>), grid, dim3(1024), 0, stream, k);
+}
 
 hipError_t launch_q4_gemm(const Q4GemmArgs &a, int epilogue, hipStream_t stream) {
     if (a.rows < 1 || a.rows > kMaxRows || !q4_group_ok(a.group)) return hipErrorInvalidValue;
@@ -470,16 +690,23 @@ hipError_t launch_q4_gemm(const Q4GemmArgs &a, int epilogue, hipStream_t stream)
     k.ssq_in = a.ssq_in; k.ssq_in_parts = a.ssq_in_parts; k.inv_d = 1.0f / (float)a.K; k.eps = a.eps;
     k.gain_next = a.gain_next; k.Xnext = (uint16_t *)a.Xnext; k.ssq_out = a.ssq_out;
     k.Xout = (uint16_t *)a.Xout; k.KS_out = (a.K_out + 31) / 32; k.epilogue = epilogue;
-    return with_group(a.group, [&](auto g) {
-        for (int r0 = 0; r0 < a.rows; r0 += 4 * kQ4Rows) {
-            k.row0 = r0;
-            const int ng = (std::min(a.rows - r0, 4 * kQ4Rows) + kQ4Rows - 1) / kQ4Rows;
-            const dim3 grid(std::min(k.tiles, 1024)), block(kQ4Waves * 64);
-            if (ng == 1) hipLaunchKernelGGL((q4_gemm_kernel<1, g()>), grid, block, 0, stream, k);
-            else if (ng == 2) hipLaunchKernelGGL((q4_gemm_kernel<2, g()>), grid, block, 0, stream, k);
-            else hipLaunchKernelGGL((q4_gemm_kernel<4, g()>), grid, block, 0, stream, k);
+    hipError_t rc = hipSuccess;
+    const hipError_t launched = with_group(a.group, [&](auto g) {
+        if (a.rows <= kQ4Rows) launch_few<1, g()>(k, stream);
+        else if (a.rows <= kQ4FewRows) launch_few<2, g()>(k, stream);
+        else {
+            const int ng = (a.rows + kQ4Rows - 1) / kQ4Rows, slices = many_slices(a.N, a.K);
+            uint4 *digits = (uint4 *)a.workspace;
+            float *factors = (float *)((char *)a.workspace + digit_bytes(a.rows, a.K)), *partials = factors + 256;
+            hipLaunchKernelGGL(q4_digits_kernel, dim3(ng), dim3(kQ4DigitThreads), 0, stream, k, digits, factors);
+            if (ng <= 4) rc = launch_many<4, g()>(k, digits, factors, partials, slices, ng, stream);
+            else if (ng <= 6) rc = launch_many<6, g()>(k, digits, factors, partials, slices, ng, stream);
+            else if (ng <= 10) rc = launch_many<10, g()>(k, digits, factors, partials, slices, ng, stream);
+            else rc = launch_many<16, g()>(k, digits, factors, partials, slices, ng, stream);
+            if (rc == hipSuccess && slices > 1) hipLaunchKernelGGL(q4_join_kernel, dim3(k.tiles, (a.rows + 15) / 16), dim3(256), 0, stream, k, partials, slices);
         }
     });
+    return rc != hipSuccess ? rc : launched;
 }
 
 }  // namespace spd
