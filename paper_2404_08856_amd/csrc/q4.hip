@@ -507,17 +507,27 @@ __global__ __launch_bounds__(WAVES * 64) void q4_few_kernel(Q4Kernel a) {
 
 // ---- many rows (9 .. 64) -------------------------------------------------------------------------------
 // The digits are made once, by a kernel of their own, with one exponent per row.  Layout: [row group][block][step][lane] of 16
-// bytes, then the factor of each of a row group's 16 columns.
+// bytes, then the factor of each of a row group's 16 columns.  A workgroup per row group; up to kKeep blocks per wave stay in registers between the
+// search for the largest magnitude and the digits.
 constexpr int kQ4DigitThreads = 1024;
+template <int KEEP>
 __global__ __launch_bounds__(kQ4DigitThreads) void q4_digits_kernel(Q4Kernel a, uint4 *digits, float *factors) {
-    constexpr int WAVES = kQ4DigitThreads / 64;
+    constexpr int WAVES = kQ4DigitThreads / 64, HELD = KEEP > 0 ? KEEP : 1;
     const int rg = blockIdx.x, lane = threadIdx.x & 63, w = threadIdx.x >> 6, g = lane >> 4, t = lane & 3, c = (lane & 15) >> 2;
     __shared__ float top[WAVES][kQ4Rows];
-    float m = 0.f, v[8];
-    for (int b = w; b < a.KB; b += WAVES) {
-        load_x8(a, kQ4Rows * rg + c, kQ4Block * b + 32 * t + 8 * g, v);
+    float m = 0.f, v[HELD][8];
+    auto load = [&](int b, float (&x)[8]) __attribute__((always_inline)) { load_x8(a, kQ4Rows * rg + c, b < a.KB ? kQ4Block * b + 32 * t + 8 * g : a.K, x); };
+    auto look = [&](const float (&x)[8]) __attribute__((always_inline)) {
 #pragma unroll
-        for (int e = 0; e < 8; ++e) m = __builtin_elementwise_maximum(m, fabsf(v[e]));
+        for (int e = 0; e < 8; ++e) m = __builtin_elementwise_maximum(m, fabsf(x[e]));
+    };
+    if (KEEP > 0) {
+#pragma unroll
+        for (int i = 0; i < KEEP; ++i) load(w + i * WAVES, v[i]);
+#pragma unroll
+        for (int i = 0; i < KEEP; ++i) look(v[i]);
+    } else {
+        for (int b = w; b < a.KB; b += WAVES) { load(b, v[0]); look(v[0]); }
     }
     m = __builtin_elementwise_maximum(m, lane_xor<1>(m));
     m = __builtin_elementwise_maximum(m, lane_xor<2>(m));
@@ -529,99 +539,131 @@ __global__ __launch_bounds__(kQ4DigitThreads) void q4_digits_kernel(Q4Kernel a, 
     for (int i = 0; i < WAVES; ++i) m = __builtin_elementwise_maximum(m, top[i][c]);
     const int exponent = max((int)(__float_as_uint(m) >> 23 & 255u), 36);
     if (w == 0 && g == 0) factors[16 * rg + lane] = digit_factor(exponent, t);
-    for (int b = w; b < a.KB; b += WAVES) {
+    auto make = [&](int b, const float (&x)[8]) __attribute__((always_inline)) {
         uint32_t B[8];
-        load_x8(a, kQ4Rows * rg + c, kQ4Block * b + 32 * t + 8 * g, v);
-        block_digits(v, exponent, B);
+        block_digits(x, exponent, B);
+        if (b >= a.KB) return;
         uint4 *dst = digits + ((size_t)rg * a.KB + b) * 128 + lane;
         dst[0] = uint4{B[0], B[1], B[2], B[3]};
         dst[64] = uint4{B[4], B[5], B[6], B[7]};
+    };
+    if (KEEP > 0) {
+#pragma unroll
+        for (int i = 0; i < KEEP; ++i) make(w + i * WAVES, v[i]);
+    } else {
+        for (int b = w; b < a.KB; b += WAVES) { load(b, v[0]); make(b, v[0]); }
     }
 }
 
-// 8 waves: 4 pairs of tiles x 2 halves of the workgroup's blocks.  The digits of a block go through LDS, where the 4 waves of a half
-// read them; a wave uses what it reads for both of its tiles.  To fill the chip where a matrix has few tiles the blocks
-// are cut into `slices` across workgroups, whose sums q4_join_kernel adds.
-constexpr int kQ4ManyTiles = 8;
-template <int NG, int G>
-__global__ __launch_bounds__(512) void q4_many_kernel(Q4Kernel a, const uint4 *digits, const float *factors, float *partials, int slices, int ng) {
+// 8 multiplying waves, 4 pairs of tiles x 2 halves of the row groups, and 2 loader waves that bring the digits of a block after the
+// other into LDS (LDS-direct loads, NBUF - 1 blocks ahead), where a multiplying wave uses what it reads for both of its tiles.  The
+// weights come through registers, RD blocks ahead.  To fill the chip where a matrix has few tiles the blocks are cut
+// into `slices` across workgroups, whose sums q4_join_kernel adds.  Workgroups begin at different blocks of their slice, so
+// that those of an XCD do not all ask for the same digits at once.
+constexpr int kQ4ManyTiles = 8, kQ4Loaders = 2;
+constexpr int many_ring(int G) { return G == 32 ? 2 : 4; }
+constexpr int many_buffers(int NH) { return NH <= 4 ? 6 : NH <= 6 ? 5 : 4; }
+template <int NH, int G>
+__global__ __launch_bounds__((8 + kQ4Loaders) * 64) void q4_many_kernel(Q4Kernel a, const uint4 *digits, const float *factors, float *partials, int slices, int ng) {
+    constexpr int NG = 2 * NH, RD = many_ring(G), NBUF = many_buffers(NH), PB = 2 * NG / kQ4Loaders;      // pieces of 1 KiB per loader wave and block
+    static_assert((NBUF - 1) * PB <= 63, "outstanding loads of a loader wave");
     const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), half = w >> 2, wt = w & 3;
     const int g = lane >> 4, t = lane & 3, c = (lane & 15) >> 2;
     const int group = blockIdx.x / slices, slice = blockIdx.x - group * slices;
-    const int b0 = (int)((long)a.KB * slice / slices), b1 = (int)((long)a.KB * (slice + 1) / slices), mid = (b0 + b1) / 2;
-    const int first = half ? mid : b0, last = half ? b1 : mid, steps = b1 - mid;        // the second half is the longer one
-    extern __shared__ uint4 lds[];                             // [2 buffers][2 halves][NG][2][64]
-    const int t0 = group * kQ4ManyTiles + 2 * wt;
-    f32x4_t sum[2][NG];
-#pragma unroll
-    for (int i = 0; i < 2; ++i)
-#pragma unroll
-        for (int rg = 0; rg < NG; ++rg) sum[i][rg] = f32x4_t{0.f, 0.f, 0.f, 0.f};
-    const int me = threadIdx.x & 255;                          // of the half's 256 threads
-    constexpr int PER = NG / 2;                                // 16-byte pieces of a block's digits per thread (NG is even)
-    uint4 stage[PER];
-    Q4Words<G> words[2];
-    auto fetch = [&](int b) __attribute__((always_inline)) {
-        b = min(b, a.KB - 1);
-#pragma unroll
-        for (int i = 0; i < PER; ++i) {
-            const int piece = i * 256 + me, rg = min(piece >> 7, ng - 1);
-            stage[i] = digits[((size_t)rg * a.KB + b) * 128 + (piece & 127)];
-        }
+    const int b0 = (int)((long)a.KB * slice / slices), len = (int)((long)a.KB * (slice + 1) / slices) - b0;
+    const int rounds = (len + RD - 1) / RD * RD;               // steps beyond the slice load what is never used
+    const int rot = (int)(((long)(blockIdx.x >> 3) * len) / ((gridDim.x + 7) >> 3));
+    auto block_at = [&](int s) __attribute__((always_inline)) {
+        const int p = s + rot;
+        return b0 + (p < len ? p : p - len < len ? p - len : 0);
     };
-    auto store = [&](int buffer) __attribute__((always_inline)) {
-#pragma unroll
-        for (int i = 0; i < PER; ++i) lds[(buffer * 2 + half) * NG * 128 + i * 256 + me] = stage[i];
-    };
-    auto weights = [&](int b) __attribute__((always_inline)) {
-#pragma unroll
-        for (int i = 0; i < 2; ++i) words[i].load(a, (size_t)min(t0 + i, a.tiles - 1) * a.KB + min(b, a.KB - 1), lane);
-    };
-    fetch(first);
-    weights(first);
-    for (int s = 0; s < steps; ++s) {
-        store(s & 1);
-        if (s + 1 < steps) fetch(first + s + 1);
-        __syncthreads();
-        Q4Words<G> now[2] = {words[0], words[1]};
-        if (s + 1 < steps) weights(first + s + 1);
-        if (first + s < last) {
-            float sc[2][kQ4Block / G][4];
-            now[0].scales(sc[0]);
-            now[1].scales(sc[1]);
-            const uint4 *src = lds + ((s & 1) * 2 + half) * NG * 128;
-#pragma unroll
-            for (int rg = 0; rg < NG; ++rg) {
-                const uint4 lo = src[rg * 128 + lane], hi = src[rg * 128 + 64 + lane];
-                const uint32_t B[8] = {lo.x, lo.y, lo.z, lo.w, hi.x, hi.y, hi.z, hi.w};
-                block_product<G, false>(now[0].w, sc[0], B, 1.f, sum[0][rg]);
-                block_product<G, false>(now[1].w, sc[1], B, 1.f, sum[1][rg]);
-            }
-        }
-    }
-    __syncthreads();                                           // the digits have been read
-    float *red = reinterpret_cast<float *>(lds);               // [half][4 pairs][2][NG][16 rows of the tile][4]
+    extern __shared__ uint4 lds[];                             // [NBUF][NG][2][64]
     __shared__ float inv_s[kMaxRows];
-    row_scales<8>(a, a.rows, inv_s);
+    f32x4_t sum[2][NH];
+    const int t0 = group * kQ4ManyTiles + 2 * wt;
+    if (w >= 8) {
+        const int first = w - 8;
+        auto issue = [&](int s) __attribute__((always_inline)) {
+            const uint4 *src = digits + (size_t)block_at(s) * 128 + lane;
+            uint4 *dst = lds + (s % NBUF) * NG * 128;
 #pragma unroll
-    for (int rg = 0; rg < NG; ++rg) {
-        const float f = factors[16 * min(rg, ng - 1) + (lane & 15)];
+            for (int r = 0; r < PB; ++r) {
+                const int piece = first + r * kQ4Loaders, rg = piece >> 1;       // wave-uniform
+                __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void *)(src + (size_t)min(rg, ng - 1) * a.KB * 128 + (piece & 1) * 64),
+                                                 (__attribute__((address_space(3))) void *)(dst + piece * 64), 16, 0, 0);
+            }
+        };
+#pragma unroll
+        for (int s = 0; s < NBUF - 1; ++s) issue(s);
+        asm volatile("s_waitcnt vmcnt(%0)" ::"n"((NBUF - 2) * PB) : "memory");   // block 0 has landed (loads complete in order)
+        __builtin_amdgcn_s_barrier();
+        for (int s = 0; s < rounds; ++s) {
+            issue(s + NBUF - 1);                               // into the buffer that the products left one step ago
+            asm volatile("s_waitcnt vmcnt(%0)" ::"n"((NBUF - 2) * PB) : "memory");   // block s + 1 has landed
+            __builtin_amdgcn_s_barrier();
+        }
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    } else {
 #pragma unroll
         for (int i = 0; i < 2; ++i)
 #pragma unroll
-            for (int v = 0; v < 4; ++v) {
-                const float x = xor_reduce<2, 1>(sum[i][rg][v] * f, AddOp());
-                if (t == 0) red[((((half * 4 + wt) * 2 + i) * NG + rg) * 16 + 4 * g + v) * 4 + c] = x;
+            for (int rg = 0; rg < NH; ++rg) sum[i][rg] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+        Q4Words<G> ring[RD][2];
+        auto weights = [&](int slot, int s) __attribute__((always_inline)) {
+            const int b = block_at(s);
+#pragma unroll
+            for (int i = 0; i < 2; ++i) ring[slot][i].load(a, (size_t)min(t0 + i, a.tiles - 1) * a.KB + b, lane);     // (beyond the matrix: a valid tile, dropped)
+        };
+#pragma unroll
+        for (int s = 0; s < RD; ++s) weights(s, s);
+        __syncthreads();
+        int buffer = 0;
+        for (int s0 = 0; s0 < rounds; s0 += RD) {
+#pragma unroll
+            for (int h = 0; h < RD; ++h) {
+                if (s0 + h < len) {
+                    float sc[2][kQ4Block / G][4];
+                    ring[h][0].scales(sc[0]);
+                    ring[h][1].scales(sc[1]);
+                    const uint4 *src = lds + (buffer * NG + half * NH) * 128 + lane;
+#pragma unroll
+                    for (int rg = 0; rg < NH; ++rg) {
+                        const uint4 lo = src[rg * 128], hi = src[rg * 128 + 64];
+                        const uint32_t B[8] = {lo.x, lo.y, lo.z, lo.w, hi.x, hi.y, hi.z, hi.w};
+                        block_product<G, false>(ring[h][0].w, sc[0], B, 1.f, sum[0][rg]);
+                        block_product<G, false>(ring[h][1].w, sc[1], B, 1.f, sum[1][rg]);
+                    }
+                }
+                weights(h, s0 + h + RD);
+                __builtin_amdgcn_sched_barrier(0);             // keep "multiply, refill the freed slots" in program order
+                buffer = buffer + 1 == NBUF ? 0 : buffer + 1;
+                __syncthreads();
             }
+        }
     }
+    __syncthreads();                                           // the loaders' surplus blocks have landed: the buffers are free
+    float *red = reinterpret_cast<float *>(lds);               // [tile of the group][NG][16 rows of the tile][4]
+    if (w < 8) {
+#pragma unroll
+        for (int rg = 0; rg < NH; ++rg) {
+            const int all = half * NH + rg;
+            const float f = factors[16 * min(all, ng - 1) + (lane & 15)];
+#pragma unroll
+            for (int i = 0; i < 2; ++i)
+#pragma unroll
+                for (int v = 0; v < 4; ++v) {
+                    const float x = xor_reduce<2, 1>(sum[i][rg][v] * f, AddOp());
+                    if (t == 0) red[(((2 * wt + i) * NG + all) * 16 + 4 * g + v) * 4 + c] = x;
+                }
+        }
+    }
+    row_scales<8 + kQ4Loaders>(a, a.rows, inv_s);
     __syncthreads();
-    constexpr int HALF = 8 * NG * 64;
-    for (int e = threadIdx.x; e < HALF; e += 512) {
+    for (int e = threadIdx.x; e < kQ4ManyTiles * NG * 64; e += (8 + kQ4Loaders) * 64) {
         const int n = e & 15, cc = (e >> 4) & 3, rg = (e >> 6) % NG, ti = (e >> 6) / NG, row = kQ4Rows * rg + cc, tile = group * kQ4ManyTiles + ti;
-        const int at = ((ti * NG + rg) * 16 + n) * 4 + cc, at_up = ((ti * NG + rg) * 16 + ((n + 8) & 15)) * 4 + cc;
-        const float s = red[at] + red[HALF + at], up = red[at_up] + red[HALF + at_up];
+        const float s = red[((ti * NG + rg) * 16 + n) * 4 + cc], up = red[((ti * NG + rg) * 16 + ((n + 8) & 15)) * 4 + cc];
         if (slices > 1) {
-            if (row < a.rows && tile < a.tiles) partials[((size_t)slice * a.rows + row) * (a.tiles * 16) + tile * 16 + n] = s;
+            if (row < a.rows && tile < a.tiles) partials[((size_t)slice * a.rows + row) * ((size_t)a.tiles * 16) + tile * 16 + n] = s;
         } else {
             finish(a, row < a.rows && tile < a.tiles, row, tile, n, s, up, inv_s[row < a.rows ? row : 0]);
         }
@@ -647,9 +689,16 @@ __global__ __launch_bounds__(256) void q4_join_kernel(Q4Kernel a, const float *p
 }
 
 constexpr int kQ4FewRows = 8, kQ4MaxSlices = 8;
-static int many_slices(int N, int K) {                        // about one workgroup per CU, at least 4 blocks each
+// Slices of K: what makes rounds of workgroups x blocks of one the least, with about 4 blocks' time for a workgroup's start and end
+static int many_slices(int N, int K) {
     const int groups = ((N + 15) / 16 + kQ4ManyTiles - 1) / kQ4ManyTiles, KB = (K + kQ4Block - 1) / kQ4Block;
-    return std::max(1, std::min({256 / groups, kQ4MaxSlices, KB / 4}));
+    int best = 1;
+    long least = 0;
+    for (int s = 1; s <= std::min(kQ4MaxSlices, std::max(1, KB / 4)); ++s) {
+        const long cost = (long)((groups * s + 255) / 256) * ((KB + s - 1) / s + 4);
+        if (s == 1 || cost < least) { best = s; least = cost; }
+    }
+    return best;
 }
 static size_t digit_bytes(int rows, int K) { return (size_t)((rows + 3) / 4) * ((K + kQ4Block - 1) / kQ4Block) * 2048; }
 
@@ -659,13 +708,13 @@ size_t q4_workspace_bytes(int rows, int N, int K) {
     return digit_bytes(rows, K) + 1024 + (slices > 1 ? (size_t)slices * rows * ((N + 15) / 16 * 16) * 4 : 0);
 }
 
-template <int NG, int G>
+template <int NH, int G>
 static hipError_t launch_many(const Q4Kernel &k, const uint4 *digits, const float *factors, float *partials, int slices, int ng, hipStream_t stream) {
-    constexpr size_t lds = (size_t)NG * 8192;
-    static const hipError_t ready = hipFuncSetAttribute((const void *)q4_many_kernel<NG, G>, hipFuncAttributeMaxDynamicSharedMemorySize, lds);
+    constexpr size_t lds = (size_t)many_buffers(NH) * NH * 4096;
+    const hipError_t ready = hipFuncSetAttribute((const void *)q4_many_kernel<NH, G>, hipFuncAttributeMaxDynamicSharedMemorySize, lds);
     if (ready != hipSuccess) return ready;
     const int groups = (k.tiles + kQ4ManyTiles - 1) / kQ4ManyTiles;
-    hipLaunchKernelGGL((q4_many_kernel<NG, G>), dim3(groups * slices), dim3(512), lds, stream, k, digits, factors, partials, slices, ng);
+    hipLaunchKernelGGL((q4_many_kernel<NH, G>), dim3(groups * slices), dim3((8 + kQ4Loaders) * 64), lds, stream, k, digits, factors, partials, slices, ng);
     return hipGetLastError();
 }
 
@@ -698,11 +747,15 @@ hipError_t launch_q4_gemm(const Q4GemmArgs &a, int epilogue, hipStream_t stream)
             const int ng = (a.rows + kQ4Rows - 1) / kQ4Rows, slices = many_slices(a.N, a.K);
             uint4 *digits = (uint4 *)a.workspace;
             float *factors = (float *)((char *)a.workspace + digit_bytes(a.rows, a.K)), *partials = factors + 256;
-            hipLaunchKernelGGL(q4_digits_kernel, dim3(ng), dim3(kQ4DigitThreads), 0, stream, k, digits, factors);
-            if (ng <= 4) rc = launch_many<4, g()>(k, digits, factors, partials, slices, ng, stream);
-            else if (ng <= 6) rc = launch_many<6, g()>(k, digits, factors, partials, slices, ng, stream);
-            else if (ng <= 10) rc = launch_many<10, g()>(k, digits, factors, partials, slices, ng, stream);
-            else rc = launch_many<16, g()>(k, digits, factors, partials, slices, ng, stream);
+            if (k.KB <= 32) hipLaunchKernelGGL(q4_digits_kernel<2>, dim3(ng), dim3(kQ4DigitThreads), 0, stream, k, digits, factors);
+            else if (k.KB <= 96) hipLaunchKernelGGL(q4_digits_kernel<6>, dim3(ng), dim3(kQ4DigitThreads), 0, stream, k, digits, factors);
+            else hipLaunchKernelGGL(q4_digits_kernel<0>, dim3(ng), dim3(kQ4DigitThreads), 0, stream, k, digits, factors);
+            if (ng <= 4) rc = launch_many<2, g()>(k, digits, factors, partials, slices, ng, stream);
+            else if (ng <= 6) rc = launch_many<3, g()>(k, digits, factors, partials, slices, ng, stream);
+            else if (ng <= 8) rc = launch_many<4, g()>(k, digits, factors, partials, slices, ng, stream);
+            else if (ng <= 10) rc = launch_many<5, g()>(k, digits, factors, partials, slices, ng, stream);
+            else if (ng <= 12) rc = launch_many<6, g()>(k, digits, factors, partials, slices, ng, stream);
+            else rc = launch_many<8, g()>(k, digits, factors, partials, slices, ng, stream);
             if (rc == hipSuccess && slices > 1) hipLaunchKernelGGL(q4_join_kernel, dim3(k.tiles, (a.rows + 15) / 16), dim3(256), 0, stream, k, partials, slices);
         }
     });
