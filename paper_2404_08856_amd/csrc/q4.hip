@@ -6,10 +6,11 @@
 // The product is made of integers.  The values of an activation row in a block of 128 columns share the exponent E of their
 // largest magnitude: x = v * 2^(E - 30) with a 31-bit integer v (what is cut off is below 2^-30 of the largest one, where
 // float32 itself keeps 2^-24 of each), and v is four signed base-256 digits.  Four rows x four digits are the 16
-// columns of v_mfma_i32_16x16x64_i8; a nibble in the upper half of a byte is 16 q as an 8-bit integer, so the weights need
-// one mask (and every other one a shift) per 4 of them and no zero point.  A group's sum is exact in 32 bits (at most
-// 128 * 128 * 128 = 2^21) and in the float32 it is turned into; then one fused multiply-add with scale * 2^(E - 34 + 8 digit),
-// which is exact too, adds it to the float32 sum of the row.  So a product rounds once per group, in float32.
+// rows of v_mfma_i32_16x16x64_i8; a nibble in the upper half of a byte is 16 q as an 8-bit integer, so the weights need
+// one mask (and every other one a shift) per 4 of them and no zero point.  The sums of a group are exact in 32 bits (at most
+// 128 * 128 * 128 = 2^21 a digit), those of two neighbouring digits together as well (2^30).  A lane ends with the four digits' sums of one
+// activation row and one output: two shift-and-adds, two conversions and a fused multiply-add make their float32 value (rounded three times), another
+// one with scale * 2^(E - 34) adds it to the output's float32 sum.
 // A row with a value that is not finite gives NaN; a block whose largest magnitude is below 2^-90 keeps less than 31 bits.
 #include <algorithm>
 
@@ -157,7 +158,7 @@ hipError_t launch_q4_dequantize(const void *q, const void *scales, int N, int K,
 // Tiles of 16 rows, blocks of 128 columns: block (t, b) at index t * KB + b is 1 KiB, lane l = r + 16 g holds row 16 t + r in its
 // 16 bytes: word j < 4 has columns 128 b + 32 j + 8 g + e (e < 4) in the upper halves of its bytes and + 4 + e in the lower
 // ones.  Two masks make of words 2 s, 2 s + 1 the operand of matrix-core step s (64 columns, in an order that the activations follow).
-// Behind the blocks the scales, [t][b][g][128 / G][4] for rows 16 t + 4 g + i: what the lane that ends with these rows' sums reads at once.
+// Behind the blocks the scales, [t][b][16 rows][128 / G].
 // Rows and columns beyond the matrix are zero.
 size_t q4_scales_offset(int N, int K) { return ((size_t)((N + 15) / 16) * ((K + kQ4Block - 1) / kQ4Block) * 1024 + 255) / 256 * 256; }
 size_t q4_packed_bytes(int N, int K, int G) {
@@ -207,10 +208,10 @@ __global__ __launch_bounds__(256) void q4_pack_kernel(Q4PackArgs a) {
     }
     a.blocks[id * 64 + lane] = uint4{w[0], w[1], w[2], w[3]};
     const int per = kQ4Block / a.G, groups = (a.K + a.G - 1) / a.G;      // scales of the block: 16 rows x per
-    for (int i = lane; i < 16 * per; i += 64) {                          // [g][per][4]
-        const int gg = i / (4 * per), gi = (i / 4) % per, group = b * per + gi;
+    for (int i = lane; i < 16 * per; i += 64) {                          // [row][per]
+        const int group = b * per + i % per;
         uint16_t v = 0;
-        if (group < groups && source_row(a, 16 * t + 4 * gg + (i & 3), which, row)) v = a.s[which][(size_t)row * groups + group];
+        if (group < groups && source_row(a, 16 * t + i / per, which, row)) v = a.s[which][(size_t)row * groups + group];
         a.scales[id * (16 * per) + i] = v;
     }
 }
@@ -288,9 +289,9 @@ __device__ __forceinline__ int block_exponent(const float (&v)[8]) {
     m = __builtin_elementwise_maximum(m, lane_xor<32>(m));
     return max((int)(__float_as_uint(m) >> 23 & 255u), 36);
 }
-// what a digit-t sum of 16 q * digit is worth
-__device__ __forceinline__ float digit_factor(int exponent, int t) {
-    return exponent == 255 ? __uint_as_float(0x7fc00000u) : __uint_as_float((unsigned)(exponent - 33 + 8 * t) << 23);
+// what a sum of 16 q * v is worth
+__device__ __forceinline__ float digit_factor(int exponent) {
+    return exponent == 255 ? __uint_as_float(0x7fc00000u) : __uint_as_float((unsigned)(exponent - 33) << 23);
 }
 __device__ __forceinline__ void block_digits(const float (&v)[8], int exponent, uint32_t (&B)[8]) {
     const float up = __uint_as_float((unsigned)(283 - exponent) << 23);       // 2^(30 - E): |v| stays below 2^30
@@ -327,57 +328,52 @@ __device__ __forceinline__ void block_digits(const float (&v)[8], int exponent, 
     for (int j = 0; j < 4; ++j) { B[2 * j] = a[j][0]; B[2 * j + 1] = a[j][1]; }
 }
 
-__device__ __forceinline__ uint32_t upper_nibbles(uint32_t w) { return w & 0xf0f0f0f0u; }
-__device__ __forceinline__ uint32_t lower_nibbles(uint32_t w) { return (w << 4) & 0xf0f0f0f0u; }
-
-// sum += a block of a tile (w: its words, sc: scales of the lane's 4 rows) times a row group's digits.  FACTOR: f is their
-// block's factor; otherwise the digits of a whole row have one, and the sum takes it in the end.
-template <int G, bool FACTOR>
-__device__ __forceinline__ void block_product(const uint4 &w, const float (&sc)[kQ4Block / G][4], const uint32_t (&B)[8], float f, f32x4_t &sum) {
-    const uint32_t words[4] = {w.x, w.y, w.z, w.w};
-    const i32x4_t none = {0, 0, 0, 0};
-    auto add = [&](const i32x4_t &acc, int gi) __attribute__((always_inline)) {
-#pragma unroll
-        for (int i = 0; i < 4; ++i) sum[i] = __builtin_fmaf((float)acc[i], FACTOR ? sc[gi][i] * f : sc[gi][i], sum[i]);
-    };
-    if constexpr (G == 32) {
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            const long A = (long)((unsigned long)lower_nibbles(words[j]) << 32 | upper_nibbles(words[j]));
-            const long b = (long)((unsigned long)B[2 * j + 1] << 32 | B[2 * j]);
-            add(__builtin_amdgcn_mfma_i32_16x16x32_i8(A, b, none, 0, 0, 0), j);
-        }
-    } else {
-        i32x4_t acc = none;
-#pragma unroll
-        for (int s = 0; s < 2; ++s) {
-            const i32x4_t A = {(int)upper_nibbles(words[2 * s]), (int)lower_nibbles(words[2 * s]), (int)upper_nibbles(words[2 * s + 1]), (int)lower_nibbles(words[2 * s + 1])};
-            const i32x4_t b = {(int)B[4 * s], (int)B[4 * s + 1], (int)B[4 * s + 2], (int)B[4 * s + 3]};
-            acc = __builtin_amdgcn_mfma_i32_16x16x64_i8(A, b, G == 64 ? none : acc, 0, 0, 0);
-            if (G == 64) add(acc, s);
-        }
-        if (G == 128) add(acc, 0);
-    }
+// the sums of 16 q * v from those of its digits
+__device__ __forceinline__ float join_digits(const i32x4_t &d) {
+    return __builtin_fmaf((float)((d[3] << 8) + d[2]), 65536.0f, (float)((d[1] << 8) + d[0]));
 }
 
 template <int G>
-struct Q4Words {                                               // a lane's part of a block: 32 weights of one row, the scales of 4
+struct Q4Words {                                               // a lane's part of a block: 32 weights of a row and the row's scales
+    static constexpr int per = kQ4Block / G;
     uint4 w;
-    uint2 s[kQ4Block / G];
+    uint32_t s[(per + 1) / 2];
+    template <bool ONCE>                                       // read by nobody else
     __device__ __forceinline__ void load(const Q4Kernel &a, size_t block, int lane) {
-        constexpr int per = kQ4Block / G;
         typedef __attribute__((ext_vector_type(4))) unsigned int u32x4_t;
-        const u32x4_t v = __builtin_nontemporal_load(reinterpret_cast<const u32x4_t *>(a.W) + block * 64 + lane);    // read once
+        const u32x4_t *src = reinterpret_cast<const u32x4_t *>(a.W) + block * 64 + lane;
+        const u32x4_t v = ONCE ? __builtin_nontemporal_load(src) : *src;
         w = uint4{v.x, v.y, v.z, v.w};
-        const uint2 *p = reinterpret_cast<const uint2 *>(a.S + (block * 4 + (lane >> 4)) * (4 * per));
-#pragma unroll
-        for (int i = 0; i < per; ++i) s[i] = p[i];
+        const uint16_t *p = a.S + (block * 16 + (lane & 15)) * per;
+        if constexpr (G == 128) s[0] = *p;
+        else if constexpr (G == 64) s[0] = *reinterpret_cast<const uint32_t *>(p);
+        else { const uint2 q = *reinterpret_cast<const uint2 *>(p); s[0] = q.x; s[1] = q.y; }
     }
-    __device__ __forceinline__ void scales(float (&sc)[kQ4Block / G][4]) const {
-#pragma unroll
-        for (int i = 0; i < kQ4Block / G; ++i) { sc[i][0] = bf16_lo(s[i].x); sc[i][1] = bf16_hi(s[i].x); sc[i][2] = bf16_lo(s[i].y); sc[i][3] = bf16_hi(s[i].y); }
+    __device__ __forceinline__ float scale(int i) const { return i & 1 ? bf16_hi(s[i / 2]) : bf16_lo(s[i / 2]); }
+    // operand of step s
+    __device__ __forceinline__ i32x4_t operand(int i) const {
+        const uint32_t a = i ? w.z : w.x, b = i ? w.w : w.y;
+        return i32x4_t{(int)(a & 0xf0f0f0f0u), (int)((a << 4) & 0xf0f0f0f0u), (int)(b & 0xf0f0f0f0u), (int)((b << 4) & 0xf0f0f0f0u)};
     }
 };
+
+// The digits' sums of each group of a block: digits x, weights w, two steps of 64 columns
+template <int G>
+__device__ __forceinline__ void group_sums(const i32x4_t (&x)[2], const i32x4_t (&w)[2], i32x4_t (&o)[kQ4Block / G]) {
+    const i32x4_t none = {0, 0, 0, 0};
+    auto half = [](const i32x4_t &v, int h) { return (long)((unsigned long)(unsigned)v[2 * h + 1] << 32 | (unsigned)v[2 * h]); };
+#pragma unroll
+    for (int s = 0; s < 2; ++s) {
+        if constexpr (G == 32) {
+            o[2 * s] = __builtin_amdgcn_mfma_i32_16x16x32_i8(half(x[s], 0), half(w[s], 0), none, 0, 0, 0);
+            o[2 * s + 1] = __builtin_amdgcn_mfma_i32_16x16x32_i8(half(x[s], 1), half(w[s], 1), none, 0, 0, 0);
+        } else if constexpr (G == 64) {
+            o[s] = __builtin_amdgcn_mfma_i32_16x16x64_i8(x[s], w[s], none, 0, 0, 0);
+        } else {
+            o[0] = __builtin_amdgcn_mfma_i32_16x16x64_i8(x[s], w[s], s ? o[0] : none, 0, 0, 0);
+        }
+    }
+}
 
 // The value (gate, up: of the two halves of a tile) of row `row`, column n of tile t into place; the 16 columns of a row sit in 16 neighbouring lanes
 __device__ __forceinline__ void finish(const Q4Kernel &a, bool active, int row, int t, int n, float sum, float up, float inv) {
@@ -433,12 +429,12 @@ template <int WAVES, int NG, int G, int NB>
 __global__ __launch_bounds__(WAVES * 64) void q4_few_kernel(Q4Kernel a) {
     const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int g = lane >> 4, t = lane & 3, c = (lane & 15) >> 2;
-    __shared__ float red[2][WAVES][NG][16][kQ4Rows];
+    __shared__ float red[2][WAVES][NG][64];                    // [..][activation row][16 outputs]
     __shared__ float inv_s[kMaxRows];
-    constexpr int RES = NB > 0 ? NB : 1;
+    constexpr int RES = NB > 0 ? NB : 1, per = kQ4Block / G;
     Q4Words<G> words[RES];
-    uint32_t B[NG][RES][8];
-    float f[NG][RES];
+    i32x4_t B[NG][RES][2];
+    float f[NG][RES];                                          // of the row whose sums the lane gets
     int tile = blockIdx.x;
     auto digits = [&](int b, int i) __attribute__((always_inline)) {
 #pragma unroll
@@ -446,59 +442,61 @@ __global__ __launch_bounds__(WAVES * 64) void q4_few_kernel(Q4Kernel a) {
             float v[8];
             load_x8(a, a.row0 + kQ4Rows * rg + c, b < a.KB ? kQ4Block * b + 32 * t + 8 * g : a.K, v);      // (beyond the matrix: zeros)
             const int e = block_exponent(v);
-            block_digits(v, e, B[rg][i]);
-            f[rg][i] = digit_factor(e, t);
+            uint32_t d[8];
+            block_digits(v, e, d);
+            B[rg][i][0] = i32x4_t{(int)d[0], (int)d[1], (int)d[2], (int)d[3]};
+            B[rg][i][1] = i32x4_t{(int)d[4], (int)d[5], (int)d[6], (int)d[7]};
+            f[rg][i] = digit_factor(__shfl(e, 4 * g, 64));
         }
     };
     if (NB > 0) {
 #pragma unroll
-        for (int i = 0; i < NB; ++i) words[i].load(a, (size_t)tile * a.KB + min(w + i * WAVES, a.KB - 1), lane);
+        for (int i = 0; i < NB; ++i) words[i].template load<true>(a, (size_t)tile * a.KB + min(w + i * WAVES, a.KB - 1), lane);
 #pragma unroll
         for (int i = 0; i < NB; ++i) digits(w + i * WAVES, i);
     }
     row_scales<WAVES>(a, min(a.rows, a.row0 + NG * kQ4Rows), inv_s);
     int parity = 0;
     for (; tile < a.tiles; tile += gridDim.x, parity ^= 1) {
-        f32x4_t sum[NG];
+        float sum[NG];
 #pragma unroll
-        for (int rg = 0; rg < NG; ++rg) sum[rg] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+        for (int rg = 0; rg < NG; ++rg) sum[rg] = 0.f;
         auto multiply = [&](int i) __attribute__((always_inline)) {
-            float sc[kQ4Block / G][4];
-            words[i].scales(sc);
+            const i32x4_t x[2] = {words[i].operand(0), words[i].operand(1)};
 #pragma unroll
-            for (int rg = 0; rg < NG; ++rg) block_product<G, true>(words[i].w, sc, B[rg][i], f[rg][i], sum[rg]);
+            for (int rg = 0; rg < NG; ++rg) {
+                i32x4_t o[per];
+                group_sums<G>(B[rg][i], x, o);
+#pragma unroll
+                for (int p = 0; p < per; ++p) sum[rg] = __builtin_fmaf(join_digits(o[p]), words[i].scale(p) * f[rg][i], sum[rg]);
+            }
         };
         if (NB > 0) {
             const int next = tile + (int)gridDim.x < a.tiles ? tile + (int)gridDim.x : tile;      // (a harmless second read in the end)
 #pragma unroll
             for (int i = 0; i < NB; ++i) {
                 multiply(i);
-                words[i].load(a, (size_t)next * a.KB + min(w + i * WAVES, a.KB - 1), lane);
+                words[i].template load<true>(a, (size_t)next * a.KB + min(w + i * WAVES, a.KB - 1), lane);
                 __builtin_amdgcn_sched_barrier(0);            // keep "use, replace" in program order
             }
         } else {
             for (int b = w; b < a.KB; b += WAVES) {
-                words[0].load(a, (size_t)tile * a.KB + b, lane);
+                words[0].template load<true>(a, (size_t)tile * a.KB + b, lane);
                 digits(b, 0);
                 multiply(0);
             }
         }
 #pragma unroll
-        for (int rg = 0; rg < NG; ++rg)
-#pragma unroll
-            for (int v = 0; v < 4; ++v) {                      // the digits' sums
-                const float x = xor_reduce<2, 1>(sum[rg][v], AddOp());
-                if (t == 0) red[parity][w][rg][4 * g + v][c] = x;
-            }
+        for (int rg = 0; rg < NG; ++rg) red[parity][w][rg][lane] = sum[rg];
         __syncthreads();
         for (int e = threadIdx.x; e < NG * 64; e += WAVES * 64) {
-            const int n = e & 15, cc = (e >> 4) & 3, rg = e >> 6, row = a.row0 + kQ4Rows * rg + cc;
+            const int n = e & 15, i = e & 63, rg = e >> 6, row = a.row0 + kQ4Rows * rg + (i >> 4);
             float s = 0.f, up = 0.f;
 #pragma unroll
-            for (int ww = 0; ww < WAVES; ++ww) s += red[parity][ww][rg][n][cc];
+            for (int ww = 0; ww < WAVES; ++ww) s += red[parity][ww][rg][i];
             if (a.epilogue == EPI_SWIGLU)
 #pragma unroll
-                for (int ww = 0; ww < WAVES; ++ww) up += red[parity][ww][rg][(n + 8) & 15][cc];
+                for (int ww = 0; ww < WAVES; ++ww) up += red[parity][ww][rg][i ^ 8];
             finish(a, row < a.rows, row, tile, n, s, up, inv_s[row < a.rows ? row : 0]);
         }
         // no second barrier: the next tile writes the other half of `red`
@@ -507,7 +505,7 @@ __global__ __launch_bounds__(WAVES * 64) void q4_few_kernel(Q4Kernel a) {
 
 // ---- many rows (9 .. 64) -------------------------------------------------------------------------------
 // The digits are made once, by a kernel of their own, with one exponent per row.  Layout: [row group][block][step][lane] of 16
-// bytes, then the factor of each of a row group's 16 columns.  A workgroup per row group; up to kKeep blocks per wave stay in registers between the
+// bytes, then the factor of each row.  A workgroup per row group; up to kKeep blocks per wave stay in registers between the
 // search for the largest magnitude and the digits.
 constexpr int kQ4DigitThreads = 1024;
 template <int KEEP>
@@ -538,7 +536,7 @@ __global__ __launch_bounds__(kQ4DigitThreads) void q4_digits_kernel(Q4Kernel a, 
 #pragma unroll
     for (int i = 0; i < WAVES; ++i) m = __builtin_elementwise_maximum(m, top[i][c]);
     const int exponent = max((int)(__float_as_uint(m) >> 23 & 255u), 36);
-    if (w == 0 && g == 0) factors[16 * rg + lane] = digit_factor(exponent, t);
+    if (w == 0 && g == 0 && t == 0) factors[kQ4Rows * rg + c] = digit_factor(exponent);
     auto make = [&](int b, const float (&x)[8]) __attribute__((always_inline)) {
         uint32_t B[8];
         block_digits(x, exponent, B);
@@ -555,51 +553,86 @@ __global__ __launch_bounds__(kQ4DigitThreads) void q4_digits_kernel(Q4Kernel a, 
     }
 }
 
-// 8 multiplying waves, 4 pairs of tiles x 2 halves of the row groups, and 2 loader waves that bring the digits of a block after the
-// other into LDS (LDS-direct loads, NBUF - 1 blocks ahead), where a multiplying wave uses what it reads for both of its tiles.  The
-// weights come through registers, RD blocks ahead.  To fill the chip where a matrix has few tiles the blocks are cut
-// into `slices` across workgroups, whose sums q4_join_kernel adds.  Workgroups begin at different blocks of their slice, so
+// sum[i][rg] += a block of tile i of a pair times the digits of NG row groups at src (LDS).  Written out in the order in which it should be
+// issued: digits are asked for two row groups ahead, and while the matrix core has a row group the sums of the one before are added.
+template <int NG, int G>
+__device__ __forceinline__ void pair_products(const Q4Words<G> (&words)[2], const uint4 *src, float (&sum)[2][NG]) {
+    constexpr int per = kQ4Block / G, AHEAD = 2;
+    uint4 B[AHEAD + 1][2];
+    auto ask = [&](int rg) __attribute__((always_inline)) { B[rg % (AHEAD + 1)][0] = src[rg * 128]; B[rg % (AHEAD + 1)][1] = src[rg * 128 + 64]; };
+#pragma unroll
+    for (int rg = 0; rg < (AHEAD < NG ? AHEAD : NG); ++rg) ask(rg);
+    i32x4_t x[2][2], acc[2][2][per];
+    float sc[2][per];
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        x[i][0] = words[i].operand(0); x[i][1] = words[i].operand(1);
+#pragma unroll
+        for (int p = 0; p < per; ++p) sc[i][p] = words[i].scale(p);
+    }
+#pragma unroll
+    for (int rg = 0; rg < NG + 1; ++rg) {
+        if (rg + AHEAD < NG) ask(rg + AHEAD);
+        if (rg < NG) {
+            const i32x4_t d[2] = {__builtin_bit_cast(i32x4_t, B[rg % (AHEAD + 1)][0]), __builtin_bit_cast(i32x4_t, B[rg % (AHEAD + 1)][1])};
+#pragma unroll
+            for (int i = 0; i < 2; ++i) group_sums<G>(d, x[i], acc[rg & 1][i]);
+        }
+        if (rg > 0) {
+#pragma unroll
+            for (int i = 0; i < 2; ++i)
+#pragma unroll
+                for (int p = 0; p < per; ++p) sum[i][rg - 1] = __builtin_fmaf(join_digits(acc[(rg - 1) & 1][i][p]), sc[i][p], sum[i][rg - 1]);
+        }
+        __builtin_amdgcn_sched_barrier(0);
+    }
+}
+
+// 8 multiplying waves, 4 pairs of tiles x even and odd blocks, and 2 loader waves that bring the digits of two blocks after
+// the other into LDS (LDS-direct loads, NBUF - 1 steps ahead), where a multiplying wave uses what it reads for both of its tiles.  The
+// weights come through registers, RD steps ahead.  To fill the chip where a matrix has few tiles the blocks are cut
+// into `slices` across workgroups, whose sums q4_join_kernel adds.  Workgroups begin at different steps of their slice, so
 // that those of an XCD do not all ask for the same digits at once.
 constexpr int kQ4ManyTiles = 8, kQ4Loaders = 2;
-constexpr int many_ring(int G) { return G == 32 ? 2 : 4; }
-constexpr int many_buffers(int NH) { return NH <= 4 ? 6 : NH <= 6 ? 5 : 4; }
-template <int NH, int G>
-__global__ __launch_bounds__((8 + kQ4Loaders) * 64) void q4_many_kernel(Q4Kernel a, const uint4 *digits, const float *factors, float *partials, int slices, int ng) {
-    constexpr int NG = 2 * NH, RD = many_ring(G), NBUF = many_buffers(NH), PB = 2 * NG / kQ4Loaders;      // pieces of 1 KiB per loader wave and block
+constexpr int many_buffers(int NG) { return NG <= 8 ? 4 : NG <= 12 ? 3 : 2; }
+template <int NG, int G>
+__global__ __launch_bounds__((8 + kQ4Loaders) * 64) __attribute__((amdgpu_waves_per_eu(2, 3))) void q4_many_kernel(Q4Kernel a, const uint4 *digits, const float *factors, float *partials, int slices, int ng) {
+    constexpr int RD = G == 32 && NG >= 12 ? 2 : 4, NBUF = many_buffers(NG), PB = 4 * NG / kQ4Loaders;      // pieces of 1 KiB per loader wave and step
     static_assert((NBUF - 1) * PB <= 63, "outstanding loads of a loader wave");
-    const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), half = w >> 2, wt = w & 3;
-    const int g = lane >> 4, t = lane & 3, c = (lane & 15) >> 2;
+    const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), odd = w >> 2, wt = w & 3;
     const int group = blockIdx.x / slices, slice = blockIdx.x - group * slices;
     const int b0 = (int)((long)a.KB * slice / slices), len = (int)((long)a.KB * (slice + 1) / slices) - b0;
-    const int rounds = (len + RD - 1) / RD * RD;               // steps beyond the slice load what is never used
-    const int rot = (int)(((long)(blockIdx.x >> 3) * len) / ((gridDim.x + 7) >> 3));
-    auto block_at = [&](int s) __attribute__((always_inline)) {
+    const int steps = (len + 1) / 2, rounds = (steps + RD - 1) / RD * RD;         // steps beyond the slice load what is never used
+    const int rot = (int)(((long)(blockIdx.x >> 3) * steps) / ((gridDim.x + 7) >> 3));
+    // position (in blocks of the slice) of step s's even or odd block; at or beyond len: there is none
+    auto position = [&](int s, int o) __attribute__((always_inline)) {
         const int p = s + rot;
-        return b0 + (p < len ? p : p - len < len ? p - len : 0);
+        return 2 * (p < steps ? p : p - steps < steps ? p - steps : 0) + o;
     };
-    extern __shared__ uint4 lds[];                             // [NBUF][NG][2][64]
+    extern __shared__ uint4 lds[];                             // [NBUF][even, odd][NG][2][64]
     __shared__ float inv_s[kMaxRows];
-    f32x4_t sum[2][NH];
+    float sum[2][NG];
     const int t0 = group * kQ4ManyTiles + 2 * wt;
     if (w >= 8) {
         const int first = w - 8;
         auto issue = [&](int s) __attribute__((always_inline)) {
-            const uint4 *src = digits + (size_t)block_at(s) * 128 + lane;
-            uint4 *dst = lds + (s % NBUF) * NG * 128;
+            const uint4 *src = digits + lane;
+            uint4 *dst = lds + (s % NBUF) * NG * 256;
+            const size_t at[2] = {(size_t)(b0 + min(position(s, 0), len - 1)) * 128, (size_t)(b0 + min(position(s, 1), len - 1)) * 128};
 #pragma unroll
             for (int r = 0; r < PB; ++r) {
-                const int piece = first + r * kQ4Loaders, rg = piece >> 1;       // wave-uniform
-                __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void *)(src + (size_t)min(rg, ng - 1) * a.KB * 128 + (piece & 1) * 64),
+                const int piece = first + r * kQ4Loaders, o = piece / (2 * NG), rg = (piece >> 1) % NG;       // wave-uniform
+                __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void *)(src + at[o] + (size_t)min(rg, ng - 1) * a.KB * 128 + (piece & 1) * 64),
                                                  (__attribute__((address_space(3))) void *)(dst + piece * 64), 16, 0, 0);
             }
         };
 #pragma unroll
         for (int s = 0; s < NBUF - 1; ++s) issue(s);
-        asm volatile("s_waitcnt vmcnt(%0)" ::"n"((NBUF - 2) * PB) : "memory");   // block 0 has landed (loads complete in order)
+        asm volatile("s_waitcnt vmcnt(%0)" ::"n"((NBUF - 2) * PB) : "memory");   // step 0 has landed (loads complete in order)
         __builtin_amdgcn_s_barrier();
         for (int s = 0; s < rounds; ++s) {
             issue(s + NBUF - 1);                               // into the buffer that the products left one step ago
-            asm volatile("s_waitcnt vmcnt(%0)" ::"n"((NBUF - 2) * PB) : "memory");   // block s + 1 has landed
+            asm volatile("s_waitcnt vmcnt(%0)" ::"n"((NBUF - 2) * PB) : "memory");   // step s + 1 has landed
             __builtin_amdgcn_s_barrier();
         }
         asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
@@ -607,12 +640,12 @@ __global__ __launch_bounds__((8 + kQ4Loaders) * 64) void q4_many_kernel(Q4Kernel
 #pragma unroll
         for (int i = 0; i < 2; ++i)
 #pragma unroll
-            for (int rg = 0; rg < NH; ++rg) sum[i][rg] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+            for (int rg = 0; rg < NG; ++rg) sum[i][rg] = 0.f;
         Q4Words<G> ring[RD][2];
         auto weights = [&](int slot, int s) __attribute__((always_inline)) {
-            const int b = block_at(s);
+            const int b = b0 + min(position(s, odd), len - 1);
 #pragma unroll
-            for (int i = 0; i < 2; ++i) ring[slot][i].load(a, (size_t)min(t0 + i, a.tiles - 1) * a.KB + b, lane);     // (beyond the matrix: a valid tile, dropped)
+            for (int i = 0; i < 2; ++i) ring[slot][i].template load<true>(a, (size_t)min(t0 + i, a.tiles - 1) * a.KB + b, lane);     // (beyond the matrix: a valid tile, dropped)
         };
 #pragma unroll
         for (int s = 0; s < RD; ++s) weights(s, s);
@@ -621,19 +654,7 @@ __global__ __launch_bounds__((8 + kQ4Loaders) * 64) void q4_many_kernel(Q4Kernel
         for (int s0 = 0; s0 < rounds; s0 += RD) {
 #pragma unroll
             for (int h = 0; h < RD; ++h) {
-                if (s0 + h < len) {
-                    float sc[2][kQ4Block / G][4];
-                    ring[h][0].scales(sc[0]);
-                    ring[h][1].scales(sc[1]);
-                    const uint4 *src = lds + (buffer * NG + half * NH) * 128 + lane;
-#pragma unroll
-                    for (int rg = 0; rg < NH; ++rg) {
-                        const uint4 lo = src[rg * 128], hi = src[rg * 128 + 64];
-                        const uint32_t B[8] = {lo.x, lo.y, lo.z, lo.w, hi.x, hi.y, hi.z, hi.w};
-                        block_product<G, false>(ring[h][0].w, sc[0], B, 1.f, sum[0][rg]);
-                        block_product<G, false>(ring[h][1].w, sc[1], B, 1.f, sum[1][rg]);
-                    }
-                }
+                if (s0 + h < steps && position(s0 + h, odd) < len) pair_products<NG, G>(ring[h], lds + (buffer * 2 + odd) * NG * 128 + lane, sum);
                 weights(h, s0 + h + RD);
                 __builtin_amdgcn_sched_barrier(0);             // keep "multiply, refill the freed slots" in program order
                 buffer = buffer + 1 == NBUF ? 0 : buffer + 1;
@@ -641,31 +662,25 @@ __global__ __launch_bounds__((8 + kQ4Loaders) * 64) void q4_many_kernel(Q4Kernel
             }
         }
     }
-    __syncthreads();                                           // the loaders' surplus blocks have landed: the buffers are free
-    float *red = reinterpret_cast<float *>(lds);               // [tile of the group][NG][16 rows of the tile][4]
+    __syncthreads();                                           // the loaders' surplus steps have landed: the buffers are free
+    float *red = reinterpret_cast<float *>(lds);               // [even, odd][tile of the group][NG][activation row][16 outputs]
+    constexpr int HALF = kQ4ManyTiles * NG * 64;
     if (w < 8) {
 #pragma unroll
-        for (int rg = 0; rg < NH; ++rg) {
-            const int all = half * NH + rg;
-            const float f = factors[16 * min(all, ng - 1) + (lane & 15)];
+        for (int i = 0; i < 2; ++i)
 #pragma unroll
-            for (int i = 0; i < 2; ++i)
-#pragma unroll
-                for (int v = 0; v < 4; ++v) {
-                    const float x = xor_reduce<2, 1>(sum[i][rg][v] * f, AddOp());
-                    if (t == 0) red[(((2 * wt + i) * NG + all) * 16 + 4 * g + v) * 4 + c] = x;
-                }
-        }
+            for (int rg = 0; rg < NG; ++rg) red[odd * HALF + ((2 * wt + i) * NG + rg) * 64 + lane] = sum[i][rg];
     }
     row_scales<8 + kQ4Loaders>(a, a.rows, inv_s);
     __syncthreads();
-    for (int e = threadIdx.x; e < kQ4ManyTiles * NG * 64; e += (8 + kQ4Loaders) * 64) {
-        const int n = e & 15, cc = (e >> 4) & 3, rg = (e >> 6) % NG, ti = (e >> 6) / NG, row = kQ4Rows * rg + cc, tile = group * kQ4ManyTiles + ti;
-        const float s = red[((ti * NG + rg) * 16 + n) * 4 + cc], up = red[((ti * NG + rg) * 16 + ((n + 8) & 15)) * 4 + cc];
+    for (int e = threadIdx.x; e < HALF; e += (8 + kQ4Loaders) * 64) {
+        const int n = e & 15, rg = (e >> 6) % NG, row = kQ4Rows * rg + ((e >> 4) & 3), tile = group * kQ4ManyTiles + (e >> 6) / NG;
+        const bool active = row < a.rows && tile < a.tiles;
+        const float f = factors[active ? row : 0], s = (red[e] + red[HALF + e]) * f, up = (red[e ^ 8] + red[HALF + (e ^ 8)]) * f;
         if (slices > 1) {
-            if (row < a.rows && tile < a.tiles) partials[((size_t)slice * a.rows + row) * ((size_t)a.tiles * 16) + tile * 16 + n] = s;
+            if (active) partials[((size_t)slice * a.rows + row) * ((size_t)a.tiles * 16) + tile * 16 + n] = s;
         } else {
-            finish(a, row < a.rows && tile < a.tiles, row, tile, n, s, up, inv_s[row < a.rows ? row : 0]);
+            finish(a, active, row, tile, n, s, up, inv_s[active ? row : 0]);
         }
     }
 }
@@ -708,13 +723,13 @@ size_t q4_workspace_bytes(int rows, int N, int K) {
     return digit_bytes(rows, K) + 1024 + (slices > 1 ? (size_t)slices * rows * ((N + 15) / 16 * 16) * 4 : 0);
 }
 
-template <int NH, int G>
+template <int NG, int G>
 static hipError_t launch_many(const Q4Kernel &k, const uint4 *digits, const float *factors, float *partials, int slices, int ng, hipStream_t stream) {
-    constexpr size_t lds = (size_t)many_buffers(NH) * NH * 4096;
-    const hipError_t ready = hipFuncSetAttribute((const void *)q4_many_kernel<NH, G>, hipFuncAttributeMaxDynamicSharedMemorySize, lds);
+    constexpr size_t lds = (size_t)many_buffers(NG) * NG * 4096;
+    const hipError_t ready = hipFuncSetAttribute((const void *)q4_many_kernel<NG, G>, hipFuncAttributeMaxDynamicSharedMemorySize, lds);
     if (ready != hipSuccess) return ready;
     const int groups = (k.tiles + kQ4ManyTiles - 1) / kQ4ManyTiles;
-    hipLaunchKernelGGL((q4_many_kernel<NH, G>), dim3(groups * slices), dim3((8 + kQ4Loaders) * 64), lds, stream, k, digits, factors, partials, slices, ng);
+    hipLaunchKernelGGL((q4_many_kernel<NG, G>), dim3(groups * slices), dim3((8 + kQ4Loaders) * 64), lds, stream, k, digits, factors, partials, slices, ng);
     return hipGetLastError();
 }
 
@@ -750,12 +765,12 @@ hipError_t launch_q4_gemm(const Q4GemmArgs &a, int epilogue, hipStream_t stream)
             if (k.KB <= 32) hipLaunchKernelGGL(q4_digits_kernel<2>, dim3(ng), dim3(kQ4DigitThreads), 0, stream, k, digits, factors);
             else if (k.KB <= 96) hipLaunchKernelGGL(q4_digits_kernel<6>, dim3(ng), dim3(kQ4DigitThreads), 0, stream, k, digits, factors);
             else hipLaunchKernelGGL(q4_digits_kernel<0>, dim3(ng), dim3(kQ4DigitThreads), 0, stream, k, digits, factors);
-            if (ng <= 4) rc = launch_many<2, g()>(k, digits, factors, partials, slices, ng, stream);
-            else if (ng <= 6) rc = launch_many<3, g()>(k, digits, factors, partials, slices, ng, stream);
-            else if (ng <= 8) rc = launch_many<4, g()>(k, digits, factors, partials, slices, ng, stream);
-            else if (ng <= 10) rc = launch_many<5, g()>(k, digits, factors, partials, slices, ng, stream);
-            else if (ng <= 12) rc = launch_many<6, g()>(k, digits, factors, partials, slices, ng, stream);
-            else rc = launch_many<8, g()>(k, digits, factors, partials, slices, ng, stream);
+            if (ng <= 4) rc = launch_many<4, g()>(k, digits, factors, partials, slices, ng, stream);
+            else if (ng <= 6) rc = launch_many<6, g()>(k, digits, factors, partials, slices, ng, stream);
+            else if (ng <= 8) rc = launch_many<8, g()>(k, digits, factors, partials, slices, ng, stream);
+            else if (ng <= 10) rc = launch_many<10, g()>(k, digits, factors, partials, slices, ng, stream);
+            else if (ng <= 12) rc = launch_many<12, g()>(k, digits, factors, partials, slices, ng, stream);
+            else rc = launch_many<16, g()>(k, digits, factors, partials, slices, ng, stream);
             if (rc == hipSuccess && slices > 1) hipLaunchKernelGGL(q4_join_kernel, dim3(k.tiles, (a.rows + 15) / 16), dim3(256), 0, stream, k, partials, slices);
         }
     });
