@@ -588,12 +588,12 @@ __device__ __forceinline__ void pair_products(const Q4Words<G> (&words)[2], cons
     }
 }
 
-// 8 multiplying waves, 4 pairs of tiles x even and odd blocks, and 2 loader waves that bring the digits of two blocks after
+// 8 multiplying waves, 4 pairs of tiles x even and odd blocks, and 4 loader waves that bring the digits of two blocks after
 // the other into LDS (LDS-direct loads, NBUF - 1 steps ahead), where a multiplying wave uses what it reads for both of its tiles.  The
 // weights come through registers, RD steps ahead.  To fill the chip where a matrix has few tiles the blocks are cut
 // into `slices` across workgroups, whose sums q4_join_kernel adds.  Workgroups begin at different steps of their slice, so
 // that those of an XCD do not all ask for the same digits at once.
-constexpr int kQ4ManyTiles = 8, kQ4Loaders = 2;
+constexpr int kQ4ManyTiles = 8, kQ4Loaders = 4;
 constexpr int many_buffers(int NG) { return NG <= 8 ? 4 : NG <= 12 ? 3 : 2; }
 template <int NG, int G>
 __global__ __launch_bounds__((8 + kQ4Loaders) * 64) __attribute__((amdgpu_waves_per_eu(2, 3))) void q4_many_kernel(Q4Kernel a, const uint4 *digits, const float *factors, float *partials, int slices, int ng) {
@@ -614,17 +614,22 @@ __global__ __launch_bounds__((8 + kQ4Loaders) * 64) __attribute__((amdgpu_waves_
     float sum[2][NG];
     const int t0 = group * kQ4ManyTiles + 2 * wt;
     if (w >= 8) {
-        const int first = w - 8;
-        auto issue = [&](int s) __attribute__((always_inline)) {
-            const uint4 *src = digits + lane;
-            uint4 *dst = lds + (s % NBUF) * NG * 256;
-            const size_t at[2] = {(size_t)(b0 + min(position(s, 0), len - 1)) * 128, (size_t)(b0 + min(position(s, 1), len - 1)) * 128};
+        const int first = w - 8, o = first >> 1;               // two loaders for the even blocks, two for the odd ones
+        unsigned offset[PB];                                   // bytes from the block's first row group: a handful of scalar instructions per load
 #pragma unroll
-            for (int r = 0; r < PB; ++r) {
-                const int piece = first + r * kQ4Loaders, o = piece / (2 * NG), rg = (piece >> 1) % NG;       // wave-uniform
-                __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void *)(src + at[o] + (size_t)min(rg, ng - 1) * a.KB * 128 + (piece & 1) * 64),
-                                                 (__attribute__((address_space(3))) void *)(dst + piece * 64), 16, 0, 0);
-            }
+        for (int r = 0; r < PB; ++r) {
+            const int piece = (first & 1) + 2 * r;             // of the block's 2 NG
+            offset[r] = (unsigned)(min(piece >> 1, ng - 1) * a.KB * 128 + (piece & 1) * 64) * 16u;
+        }
+        int buffer = 0;
+        auto issue = [&](int s) __attribute__((always_inline)) {
+            const char *src = reinterpret_cast<const char *>(digits) + (size_t)(b0 + min(position(s, o), len - 1)) * 2048;
+            uint4 *dst = lds + (buffer * 2 + o) * NG * 128 + (first & 1) * 64;
+#pragma unroll
+            for (int r = 0; r < PB; ++r)
+                __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void *)(src + offset[r] + 16u * lane),
+                                                 (__attribute__((address_space(3))) void *)(dst + r * 128), 16, 0, 0);
+            buffer = buffer + 1 == NBUF ? 0 : buffer + 1;
         };
 #pragma unroll
         for (int s = 0; s < NBUF - 1; ++s) issue(s);
