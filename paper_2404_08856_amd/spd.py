@@ -154,22 +154,29 @@ def _raw(t, dtype):
     return t.data_ptr()
 
 
-def _matrix(t, *dtypes):
-    """Data pointer and row stride of a device matrix whose rows are contiguous (a view into a wider buffer is fine)."""
-    assert t.is_cuda and t.dim() == 2 and t.dtype in dtypes, f"expected a device matrix of {dtypes}, got {tuple(t.shape)} {t.dtype}"
-    assert t.device.index == _current_device(), "tensors have to be on the current device"
-    assert t.shape[1] <= 1 or t.stride(1) == 1, "contiguous rows only"
-    stride = t.stride(0) if t.shape[0] > 1 else t.shape[1]
-    assert stride >= t.shape[1], "rows overlap"
-    return t.data_ptr(), stride
+# The calls below take 5 us of device time at the least; what is checked here is read from each tensor once.
+def _matrix(t, device, dtypes):
+    """Data pointer and row stride of a matrix on the current device whose rows are contiguous (a view into a wider buffer is fine)."""
+    (n, k), (stride, step) = t.shape, t.stride()
+    assert t.get_device() == device and t.dtype in dtypes, f"expected {dtypes} on device {device}, got {t.dtype} on {t.device}"
+    assert (step == 1 or k <= 1) and (stride >= k or n <= 1), f"contiguous rows that do not overlap only, got strides {t.stride()}"
+    return t.data_ptr(), stride if n > 1 else k
 
 
-def _own(t, dtype, *shape):
-    """Data pointer of a contiguous tensor on the current device, of this type and shape."""
+def _own(t, device, dtype, shape):
+    """Data pointer of a contiguous tensor on the current device, of this type and shape (a tuple)."""
     if t is None:
         return None
-    assert t.device.index == _current_device() and tuple(t.shape) == shape, f"expected {shape} on the current device, got {tuple(t.shape)} on {t.device}"
-    return _ptr(t, dtype)
+    assert t.dtype == dtype and t.shape == shape and t.get_device() == device and t.is_contiguous(), \
+        f"expected contiguous {dtype} {shape} on device {device}, got {t.dtype} {tuple(t.shape)} on {t.device}"
+    return t.data_ptr()
+
+
+def _scratch(workspace, device):
+    """Data pointer and bytes of a workspace: contiguous uint8 on the current device."""
+    n = workspace.numel()
+    assert workspace.dtype == torch.uint8 and workspace.get_device() == device and workspace.is_contiguous(), "a workspace is uint8 on the current device"
+    return workspace.data_ptr(), n
 
 
 def make_config(shape, max_seqs, max_positions):
@@ -227,11 +234,11 @@ class Model:
         bf, f32 = torch.bfloat16, torch.float32
         handle = ctypes.c_void_p()
         if group:
-            d, hd, F, V = cfg.d_model, cfg.n_heads * cfg.head_dim, cfg.d_ffn, cfg.vocab
+            d, hd, F, V, here = cfg.d_model, cfg.n_heads * cfg.head_dim, cfg.d_ffn, cfg.vocab, _current_device()
             shapes = {"wq": (hd, d), "wk": (hd, d), "wv": (hd, d), "wo": (d, hd), "w_gate": (F, d), "w_up": (F, d), "w_down": (d, F)}
 
             def matrix(pair, n, k):
-                return spd_q4_matrix(_own(pair[0], torch.uint8, n, (k + 1) // 2), _own(pair[1], bf, n, (k + group - 1) // group))
+                return spd_q4_matrix(_own(pair[0], here, torch.uint8, (n, (k + 1) // 2)), _own(pair[1], here, bf, (n, (k + group - 1) // group)))
             mats = {key: (spd_q4_matrix * L)(*[matrix(lw[key], *shapes[key]) for lw in weights["layers"]]) for key in shapes}
             norms = [arr("attn_norm", f32), arr("mlp_norm", f32)]
             w = spd_weights_q4(group, _ptr(weights["embed"], bf), matrix(weights["lm_head"], V, d), _ptr(weights["final_norm"], f32),
@@ -387,6 +394,9 @@ def spd_speculative_accept_static(target, draft, draft_tokens, u, temperature, f
                                               _ptr(next_token_out, torch.int32), _ptr(accept_prob_out, torch.float32), _stream()))
 
 
+_F32, _F32_BF16 = (torch.float32,), (torch.float32, torch.bfloat16)
+
+
 def spd_logprobs_workspace_bytes(n_rows, vocab, n_top):
     b = ctypes.c_size_t()
     _check(_lib.spd_logprobs_workspace_bytes(n_rows, vocab, n_top, ctypes.byref(b)))
@@ -397,14 +407,15 @@ def spd_token_logprobs(rows, tokens, temperature, flags, logprob_out=None, entro
                        top_logprobs_out=None, workspace=None):
     """rows [n, vocab] (a view into a wider buffer is fine); the number of alternatives is that of top_tokens_out's columns."""
     n, vocab = rows.shape
-    ptr, stride = _matrix(rows, torch.float32)
+    here = _current_device()
+    ptr, stride = _matrix(rows, here, _F32)
     n_top = 0 if top_tokens_out is None else top_tokens_out.shape[1]
     if workspace is None:
         workspace = torch.empty(spd_logprobs_workspace_bytes(n, vocab, n_top), dtype=torch.uint8, device=rows.device)
-    _check(_lib.spd_token_logprobs(ptr, stride, _own(tokens, torch.int32, n), n, vocab, float(temperature), int(flags),
-                                   _own(logprob_out, torch.float32, n), _own(entropy_out, torch.float32, n), _own(rank_out, torch.int32, n),
-                                   n_top, _own(top_tokens_out, torch.int32, n, n_top), _own(top_logprobs_out, torch.float32, n, n_top),
-                                   _own(workspace, torch.uint8, workspace.numel()), workspace.numel(), _stream()))
+    one, top, f32, i32 = (n,), (n, n_top), torch.float32, torch.int32
+    _check(_lib.spd_token_logprobs(ptr, stride, _own(tokens, here, i32, one), n, vocab, temperature, flags, _own(logprob_out, here, f32, one),
+                                   _own(entropy_out, here, f32, one), _own(rank_out, here, i32, one), n_top, _own(top_tokens_out, here, i32, top),
+                                   _own(top_logprobs_out, here, f32, top), *_scratch(workspace, here), _raw_stream(here)))
 
 
 def spd_q4_bytes(n, k, group):
@@ -415,16 +426,18 @@ def spd_q4_bytes(n, k, group):
 
 def spd_q4_quantize(w, group, q_out, scales_out):
     n, k = w.shape
-    ptr, stride = _matrix(w, torch.float32, torch.bfloat16)
-    _check(_lib.spd_q4_quantize(ptr, stride, SPD_W_IS_BF16 if w.dtype == torch.bfloat16 else 0, n, k, group, _own(q_out, torch.uint8, n, (k + 1) // 2),
-                                _own(scales_out, torch.bfloat16, n, (k + group - 1) // group), _stream()))
+    here = _current_device()
+    ptr, stride = _matrix(w, here, _F32_BF16)
+    _check(_lib.spd_q4_quantize(ptr, stride, SPD_W_IS_BF16 if w.dtype == torch.bfloat16 else 0, n, k, group, _own(q_out, here, torch.uint8, (n, (k + 1) // 2)),
+                                _own(scales_out, here, torch.bfloat16, (n, (k + group - 1) // group)), _raw_stream(here)))
 
 
 def spd_q4_dequantize(q, scales, group, w_out):
     n, k = w_out.shape
-    ptr, stride = _matrix(w_out, torch.float32, torch.bfloat16)
-    _check(_lib.spd_q4_dequantize(_own(q, torch.uint8, n, (k + 1) // 2), _own(scales, torch.bfloat16, n, (k + group - 1) // group), n, k, group, ptr,
-                                  stride, SPD_W_IS_BF16 if w_out.dtype == torch.bfloat16 else 0, _stream()))
+    here = _current_device()
+    ptr, stride = _matrix(w_out, here, _F32_BF16)
+    _check(_lib.spd_q4_dequantize(_own(q, here, torch.uint8, (n, (k + 1) // 2)), _own(scales, here, torch.bfloat16, (n, (k + group - 1) // group)), n, k, group,
+                                  ptr, stride, SPD_W_IS_BF16 if w_out.dtype == torch.bfloat16 else 0, _raw_stream(here)))
 
 
 class Q4Matrix:
@@ -433,8 +446,9 @@ class Q4Matrix:
     def __init__(self, q, scales, k, group):
         self.n, self.k, self.group = q.shape[0], int(k), int(group)
         self.packed = torch.empty(spd_q4_bytes(self.n, self.k, self.group), dtype=torch.uint8, device=q.device)
-        _check(_lib.spd_q4_pack(_own(q, torch.uint8, self.n, (self.k + 1) // 2), _own(scales, torch.bfloat16, self.n, (self.k + self.group - 1) // self.group),
-                                self.n, self.k, self.group, _ptr(self.packed), self.packed.numel(), _stream()))
+        here = _current_device()
+        _check(_lib.spd_q4_pack(_own(q, here, torch.uint8, (self.n, (self.k + 1) // 2)), _own(scales, here, torch.bfloat16, (self.n, (self.k + self.group - 1) // self.group)),
+                                self.n, self.k, self.group, *_scratch(self.packed, here), _raw_stream(here)))
 
 
 def spd_q4_matmul_workspace_bytes(rows, n, k):
@@ -445,14 +459,15 @@ def spd_q4_matmul_workspace_bytes(rows, n, k):
 
 def spd_q4_matmul(matrix, x, y, workspace=None):
     """y [rows, matrix.n] float32 = x [rows, matrix.k] (float32 or bfloat16) times the matrix; both may be views into wider buffers."""
-    rows = x.shape[0]
-    assert x.shape[1] == matrix.k and tuple(y.shape) == (rows, matrix.n)
-    xp, xs = _matrix(x, torch.float32, torch.bfloat16)
-    yp, ys = _matrix(y, torch.float32)
+    rows, k = x.shape
+    assert k == matrix.k and y.shape == (rows, matrix.n), f"expected [rows, {matrix.k}] and [rows, {matrix.n}], got {tuple(x.shape)} and {tuple(y.shape)}"
+    here = _current_device()
     if workspace is None:
-        workspace = torch.empty(spd_q4_matmul_workspace_bytes(rows, matrix.n, matrix.k), dtype=torch.uint8, device=x.device)
-    _check(_lib.spd_q4_matmul(_ptr(matrix.packed), matrix.n, matrix.k, matrix.group, xp, xs, SPD_X_IS_BF16 if x.dtype == torch.bfloat16 else 0, rows,
-                              yp, ys, _own(workspace, torch.uint8, workspace.numel()), workspace.numel(), _stream()))
+        workspace = torch.empty(spd_q4_matmul_workspace_bytes(rows, matrix.n, k), dtype=torch.uint8, device=x.device)
+    packed = matrix.packed
+    assert packed.get_device() == here, "the matrix is on another device than the current one"
+    _check(_lib.spd_q4_matmul(packed.data_ptr(), matrix.n, k, matrix.group, *_matrix(x, here, _F32_BF16), SPD_X_IS_BF16 if x.dtype == torch.bfloat16 else 0, rows,
+                              *_matrix(y, here, _F32), *_scratch(workspace, here), _raw_stream(here)))
 
 
 def spd_probe_read_chain(buffer, stage_bytes, reps=20):
