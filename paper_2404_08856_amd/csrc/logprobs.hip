@@ -62,6 +62,21 @@ __device__ __forceinline__ float exponent2(float v, float mx, float scale2) {   
 // Partial results of a slice in the workspace
 struct LpRecord { LpPart p; unsigned pad[3]; };
 
+// The wave's 64 values in descending order over the lanes (bitonic: 21 exchanges)
+template <int SIZE, int N>
+__device__ __forceinline__ float sort_step(float v, int lane) {
+    const float o = lane_xor<N>(v);
+    v = ((lane & N) != 0) == ((lane & SIZE) != 0) ? fmaxf(v, o) : fminf(v, o);
+    if constexpr (N > 1) v = sort_step<SIZE, N / 2>(v, lane);
+    return v;
+}
+template <int SIZE = 2>
+__device__ __forceinline__ float sort_descending(float v, int lane) {
+    v = sort_step<SIZE, SIZE / 2>(v, lane);
+    if constexpr (SIZE < 64) v = sort_descending<SIZE * 2>(v, lane);
+    return v;
+}
+
 // One workgroup per row, or per slice of one of at most THREADS * NV quads; the entries stay in registers.
 //
 // Alternatives: the n-th largest of 64 bucket maxima (a bucket is what the lanes of one number hold) is a bound that at least n
@@ -116,12 +131,8 @@ __global__ __launch_bounds__(THREADS, 8) void logprobs_kernel(LogprobArgs a, int
         for (int i = 1; i < WAVES; ++i) p.mn = MinimumOp()(p.mn, s_min[i]);
     }
     if (w == 0 && a.n_top > 0) {                              // the n-th largest bucket (one of NaN: any bound will do)
-        int above = 0;
-        for (int i = 0; i < 64; ++i) {
-            const float o = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(bucket), i));
-            above += o > bucket || (o == bucket && i < lane);
-        }
-        if (above == a.n_top - 1) s_bound = bucket;
+        const float sorted = sort_descending(bucket, lane);
+        if (lane == a.n_top - 1) s_bound = sorted;
     }
     float sum = 0.f, dot = 0.f;
     if (p.mx > lowest) {

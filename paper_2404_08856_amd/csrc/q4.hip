@@ -4,8 +4,8 @@
 //   W[n][k] = scale[n][k / G] * q[n][k],   q in -8 .. 7,   scale bfloat16,   G = 32, 64 or 128
 //
 // The product is made of integers.  The values of an activation row in a block of 128 columns share the exponent E of their
-// largest magnitude: x = v * 2^(E - 30) with a 31-bit integer v (what is cut off is below 2^-30 of the largest one, where
-// float32 itself keeps 2^-24 of each), and v is four signed base-256 digits.  Four rows x four digits are the 16
+// largest magnitude: x = v * 2^(E - 30) with a 31-bit integer v (what is cut off is below 2^-30 of the largest one or 2^-24 of x itself, float32's own
+// rounding), and v is four signed base-256 digits.  Four rows x four digits are the 16
 // rows of v_mfma_i32_16x16x64_i8; a nibble in the upper half of a byte is 16 q as an 8-bit integer, so the weights need
 // one mask (and every other one a shift) per 4 of them and no zero point.  The sums of a group are exact in 32 bits (at most
 // 128 * 128 * 128 = 2^21 a digit), those of two neighbouring digits together as well (2^30).  A lane ends with the four digits' sums of one
@@ -252,13 +252,14 @@ struct Q4Kernel {
 };
 
 // Values k0 .. k0 + 7 (k0 % 8 == 0) of an activation row, zeros beyond the matrix
+template <int KIND>
 __device__ __forceinline__ void load_x8(const Q4Kernel &a, int row, int k0, float (&v)[8]) {
     if (row >= a.rows || k0 >= a.K) {
 #pragma unroll
         for (int e = 0; e < 8; ++e) v[e] = 0.f;
-    } else if (a.x_kind == Q4_X_F32) {
+    } else if constexpr (KIND == Q4_X_F32) {
         load8((const float *)a.X + (size_t)row * a.ldx, k0, a.K, v);
-    } else if (a.x_kind == Q4_X_BF16) {
+    } else if constexpr (KIND == Q4_X_BF16) {
         load8((const uint16_t *)a.X + (size_t)row * a.ldx, k0, a.K, v);
     } else {                                                   // the sum of the terms is the float32 value they were made of
         const uint16_t *X = (const uint16_t *)a.X;
@@ -272,6 +273,13 @@ __device__ __forceinline__ void load_x8(const Q4Kernel &a, int row, int k0, floa
             v[2 * e + 1] = bf16_hi(p0[e]) + (bf16_hi(p1[e]) + bf16_hi(p2[e]));
         }
     }
+}
+// f(KIND) for the call's kind of activations: the branch stands around all loads of a unit, not around each
+template <class F>
+__device__ __forceinline__ void with_kind(const Q4Kernel &a, F f) {
+    if (a.x_kind == Q4_X_F32) f(std::integral_constant<int, Q4_X_F32>());
+    else if (a.x_kind == Q4_X_BF16) f(std::integral_constant<int, Q4_X_BF16>());
+    else f(std::integral_constant<int, Q4_X_PACKED>());
 }
 
 __device__ __forceinline__ uint32_t byte_perm(uint32_t hi, uint32_t lo, uint32_t sel) { return __builtin_amdgcn_perm(hi, lo, sel); }
@@ -295,17 +303,18 @@ __device__ __forceinline__ float digit_factor(int exponent) {
 }
 __device__ __forceinline__ void block_digits(const float (&v)[8], int exponent, uint32_t (&B)[8]) {
     const float up = __uint_as_float((unsigned)(283 - exponent) << 23);       // 2^(30 - E): |v| stays below 2^30
+    // The bytes of v + 0x808080, the lower three less 128 each, are the digits.  The sum is made in float32 (0x808080 has its 8 leading bits only).
     uint32_t z[8];
 #pragma unroll
-    for (int e = 0; e < 8; ++e) z[e] = ((uint32_t)(int)(v[e] * up) + 0x00808080u) ^ 0x00808080u;   // its bytes are the digits
+    for (int e = 0; e < 8; ++e) z[e] = (uint32_t)(int)__builtin_fmaf(v[e], up, 8421504.0f);
     uint32_t a[4][2];
 #pragma unroll
     for (int h = 0; h < 2; ++h) {                              // bytes of 4 columns by digit
         const uint32_t p0 = byte_perm(z[4 * h + 1], z[4 * h], 0x05010400u), p1 = byte_perm(z[4 * h + 1], z[4 * h], 0x07030602u);
         const uint32_t q0 = byte_perm(z[4 * h + 3], z[4 * h + 2], 0x05010400u), q1 = byte_perm(z[4 * h + 3], z[4 * h + 2], 0x07030602u);
-        a[0][h] = byte_perm(q0, p0, 0x05040100u);
-        a[1][h] = byte_perm(q0, p0, 0x07060302u);
-        a[2][h] = byte_perm(q1, p1, 0x05040100u);
+        a[0][h] = byte_perm(q0, p0, 0x05040100u) ^ 0x80808080u;
+        a[1][h] = byte_perm(q0, p0, 0x07060302u) ^ 0x80808080u;
+        a[2][h] = byte_perm(q1, p1, 0x05040100u) ^ 0x80808080u;
         a[3][h] = byte_perm(q1, p1, 0x07060302u);
     }
     const bool odd = threadIdx.x & 1, upper = threadIdx.x & 2;
@@ -421,71 +430,96 @@ __device__ __forceinline__ void row_scales(const Q4Kernel &a, int last, float *i
 }
 
 // ---- few rows (1 .. 8): the waves of a workgroup share a tile's blocks ------------------------------------
-// A workgroup takes tiles of 16 outputs, wave w blocks w, w + WAVES, ... of each, and the waves meet in LDS.  Every workgroup makes
-// the digits for itself, while its first weights are on their way.  NB > 0: the wave's digits (NB blocks) stay in
+// A workgroup takes tiles of 16 outputs; its waves take the blocks of a tile's row in units of NB and meet in LDS.  Every workgroup makes
+// the digits for itself, while its first weights are on their way.  KEEP: one unit per wave covers K; its digits stay in
 // registers for all of the workgroup's tiles, and a block's words are replaced by the next tile's as soon as they
-// are used; NB = 0: any K, digits made anew for every tile.
-template <int WAVES, int NG, int G, int NB>
+// are used.  Otherwise any K, and the digits of a unit are made anew for every tile.
+// Rows: FULL groups of up to 4 and (SINGLE) one row more.  A row group's digits take as long to make for one row as for four, so the single
+// row's are made for NB blocks at once, in the places of the group's other rows: the matrix core then multiplies a block's weights by the digits
+// of all NB blocks, and of the sums only the lanes of the right block's place are added.
+template <int WAVES, int FULL, bool SINGLE, int G, int NB, bool KEEP>
 __global__ __launch_bounds__(WAVES * 64) void q4_few_kernel(Q4Kernel a) {
+    constexpr int NG = FULL + SINGLE, per = kQ4Block / G, GROUPS = FULL > 0 ? FULL : 1;
+    static_assert(NB <= kQ4Rows, "places of the single row's blocks");
     const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int g = lane >> 4, t = lane & 3, c = (lane & 15) >> 2;
     __shared__ float red[2][WAVES][NG][64];                    // [..][activation row][16 outputs]
     __shared__ float inv_s[kMaxRows];
-    constexpr int RES = NB > 0 ? NB : 1, per = kQ4Block / G;
-    Q4Words<G> words[RES];
-    i32x4_t B[NG][RES][2];
-    float f[NG][RES];                                          // of the row whose sums the lane gets
-    int tile = blockIdx.x;
-    auto digits = [&](int b, int i) __attribute__((always_inline)) {
+    Q4Words<G> words[NB];
+    i32x4_t B[GROUPS][NB][2], B1[2];
+    float f[GROUPS][NB], f1[NB];                               // of the row whose sums the lane gets
+    auto load_words = [&](int tile, int b, Q4Words<G> &o) __attribute__((always_inline)) { o.template load<true>(a, (size_t)tile * a.KB + min(b, a.KB - 1), lane); };
+    auto convert = [&](const float (&v)[8], i32x4_t (&o)[2]) __attribute__((always_inline)) {
+        const int e = block_exponent(v);
+        uint32_t d[8];
+        block_digits(v, e, d);
+        o[0] = i32x4_t{(int)d[0], (int)d[1], (int)d[2], (int)d[3]};
+        o[1] = i32x4_t{(int)d[4], (int)d[5], (int)d[6], (int)d[7]};
+        return digit_factor(__shfl(e, 4 * g, 64));
+    };
+    // digits of blocks b0 .. b0 + NB - 1 (beyond the matrix: zeros)
+    auto digits = [&](int b0) __attribute__((always_inline)) {
+        float v[GROUPS][NB][8], v1[8];
+        auto first = [&](int b) __attribute__((always_inline)) { return b < a.KB ? kQ4Block * b + 32 * t + 8 * g : a.K; };
+        with_kind(a, [&](auto kind) __attribute__((always_inline)) {
 #pragma unroll
-        for (int rg = 0; rg < NG; ++rg) {
-            float v[8];
-            load_x8(a, a.row0 + kQ4Rows * rg + c, b < a.KB ? kQ4Block * b + 32 * t + 8 * g : a.K, v);      // (beyond the matrix: zeros)
-            const int e = block_exponent(v);
-            uint32_t d[8];
-            block_digits(v, e, d);
-            B[rg][i][0] = i32x4_t{(int)d[0], (int)d[1], (int)d[2], (int)d[3]};
-            B[rg][i][1] = i32x4_t{(int)d[4], (int)d[5], (int)d[6], (int)d[7]};
-            f[rg][i] = digit_factor(__shfl(e, 4 * g, 64));
+            for (int i = 0; i < NB; ++i)
+#pragma unroll
+                for (int rg = 0; rg < FULL; ++rg) load_x8<kind()>(a, a.row0 + kQ4Rows * rg + c, first(b0 + i), v[rg][i]);
+            if (SINGLE) load_x8<kind()>(a, a.row0 + kQ4Rows * FULL, c < NB ? first(b0 + c) : a.K, v1);
+        });
+#pragma unroll
+        for (int i = 0; i < NB; ++i)
+#pragma unroll
+            for (int rg = 0; rg < FULL; ++rg) f[rg][i] = convert(v[rg][i], B[rg][i]);
+        if (SINGLE) {
+            const float own = convert(v1, B1);
+#pragma unroll
+            for (int i = 0; i < NB; ++i) f1[i] = g == i ? own : 0.f;
         }
     };
-    if (NB > 0) {
+    float sum[NG];
+    auto multiply = [&](int i) __attribute__((always_inline)) {
+        const i32x4_t x[2] = {words[i].operand(0), words[i].operand(1)};
 #pragma unroll
-        for (int i = 0; i < NB; ++i) words[i].template load<true>(a, (size_t)tile * a.KB + min(w + i * WAVES, a.KB - 1), lane);
+        for (int rg = 0; rg < NG; ++rg) {
+            const bool single = rg == FULL;
+            const float factor = single ? f1[i] : f[single ? 0 : rg][i];
+            i32x4_t o[per];
+            group_sums<G>(single ? B1 : B[single ? 0 : rg][i], x, o);
 #pragma unroll
-        for (int i = 0; i < NB; ++i) digits(w + i * WAVES, i);
+            for (int p = 0; p < per; ++p) sum[rg] = __builtin_fmaf(join_digits(o[p]), words[i].scale(p) * factor, sum[rg]);
+        }
+    };
+    int tile = blockIdx.x;
+    if (KEEP) {
+#pragma unroll
+        for (int i = 0; i < NB; ++i) load_words(tile, w * NB + i, words[i]);
+        digits(w * NB);
     }
     row_scales<WAVES>(a, min(a.rows, a.row0 + NG * kQ4Rows), inv_s);
     int parity = 0;
     for (; tile < a.tiles; tile += gridDim.x, parity ^= 1) {
-        float sum[NG];
 #pragma unroll
         for (int rg = 0; rg < NG; ++rg) sum[rg] = 0.f;
-        auto multiply = [&](int i) __attribute__((always_inline)) {
-            const i32x4_t x[2] = {words[i].operand(0), words[i].operand(1)};
-#pragma unroll
-            for (int rg = 0; rg < NG; ++rg) {
-                i32x4_t o[per];
-                group_sums<G>(B[rg][i], x, o);
-#pragma unroll
-                for (int p = 0; p < per; ++p) sum[rg] = __builtin_fmaf(join_digits(o[p]), words[i].scale(p) * f[rg][i], sum[rg]);
-            }
-        };
-        if (NB > 0) {
+        if (KEEP) {
             const int next = tile + (int)gridDim.x < a.tiles ? tile + (int)gridDim.x : tile;      // (a harmless second read in the end)
 #pragma unroll
             for (int i = 0; i < NB; ++i) {
                 multiply(i);
-                words[i].template load<true>(a, (size_t)next * a.KB + min(w + i * WAVES, a.KB - 1), lane);
+                load_words(next, w * NB + i, words[i]);
                 __builtin_amdgcn_sched_barrier(0);            // keep "use, replace" in program order
             }
         } else {
-            for (int b = w; b < a.KB; b += WAVES) {
-                words[0].template load<true>(a, (size_t)tile * a.KB + b, lane);
-                digits(b, 0);
-                multiply(0);
+            for (int b0 = w * NB; b0 < a.KB; b0 += WAVES * NB) {
+#pragma unroll
+                for (int i = 0; i < NB; ++i) load_words(tile, b0 + i, words[i]);
+                digits(b0);
+#pragma unroll
+                for (int i = 0; i < NB; ++i) multiply(i);
             }
         }
+        if (SINGLE) sum[FULL] = xor_reduce<32, 16>(sum[FULL], AddOp());       // (its row is the first place's; the others hold no row)
 #pragma unroll
         for (int rg = 0; rg < NG; ++rg) red[parity][w][rg][lane] = sum[rg];
         __syncthreads();
@@ -514,18 +548,22 @@ __global__ __launch_bounds__(kQ4DigitThreads) void q4_digits_kernel(Q4Kernel a, 
     const int rg = blockIdx.x, lane = threadIdx.x & 63, w = threadIdx.x >> 6, g = lane >> 4, t = lane & 3, c = (lane & 15) >> 2;
     __shared__ float top[WAVES][kQ4Rows];
     float m = 0.f, v[HELD][8];
-    auto load = [&](int b, float (&x)[8]) __attribute__((always_inline)) { load_x8(a, kQ4Rows * rg + c, b < a.KB ? kQ4Block * b + 32 * t + 8 * g : a.K, x); };
+    auto load = [&](auto kind, int b, float (&x)[8]) __attribute__((always_inline)) { load_x8<kind()>(a, kQ4Rows * rg + c, b < a.KB ? kQ4Block * b + 32 * t + 8 * g : a.K, x); };
     auto look = [&](const float (&x)[8]) __attribute__((always_inline)) {
 #pragma unroll
         for (int e = 0; e < 8; ++e) m = __builtin_elementwise_maximum(m, fabsf(x[e]));
     };
+    with_kind(a, [&](auto kind) __attribute__((always_inline)) {
+        if (KEEP > 0) {
+#pragma unroll
+            for (int i = 0; i < KEEP; ++i) load(kind, w + i * WAVES, v[i]);
+        } else {
+            for (int b = w; b < a.KB; b += WAVES) { load(kind, b, v[0]); look(v[0]); }
+        }
+    });
     if (KEEP > 0) {
 #pragma unroll
-        for (int i = 0; i < KEEP; ++i) load(w + i * WAVES, v[i]);
-#pragma unroll
         for (int i = 0; i < KEEP; ++i) look(v[i]);
-    } else {
-        for (int b = w; b < a.KB; b += WAVES) { load(b, v[0]); look(v[0]); }
     }
     m = __builtin_elementwise_maximum(m, lane_xor<1>(m));
     m = __builtin_elementwise_maximum(m, lane_xor<2>(m));
@@ -549,7 +587,9 @@ __global__ __launch_bounds__(kQ4DigitThreads) void q4_digits_kernel(Q4Kernel a, 
 #pragma unroll
         for (int i = 0; i < KEEP; ++i) make(w + i * WAVES, v[i]);
     } else {
-        for (int b = w; b < a.KB; b += WAVES) { load(b, v[0]); make(b, v[0]); }
+        with_kind(a, [&](auto kind) __attribute__((always_inline)) {
+            for (int b = w; b < a.KB; b += WAVES) { load(kind, b, v[0]); make(b, v[0]); }
+        });
     }
 }
 
@@ -738,14 +778,15 @@ static hipError_t launch_many(const Q4Kernel &k, const uint4 *digits, const floa
     return hipGetLastError();
 }
 
-template <int NG, int G>
+template <int FULL, bool SINGLE, int G>
 static void launch_few(const Q4Kernel &k, hipStream_t stream) {
-    // Blocks of digits that a wave keeps: 4 where 8 waves cover K with them.  A workgroup that has one tile only gains nothing by keeping any.
-    const dim3 grid(std::min(k.tiles, 256));
-    if (k.KB <= 8) hipLaunchKernelGGL((q4_few_kernel<8, NG, G, 1>), dim3(std::min(k.tiles, 1024)), dim3(512), 0, stream, k);
-    else if (k.KB <= 16) hipLaunchKernelGGL((q4_few_kernel<8, NG, G, 2>), dim3(std::min(k.tiles, 512)), dim3(512), 0, stream, k);
-    else if (k.KB <= 32) hipLaunchKernelGGL((q4_few_kernel<8, NG, G, 4>), grid, dim3(512), 0, stream, k);
-    else hipLaunchKernelGGL((q4_few_kernel<16, NG, G, 0>), grid, dim3(1024), 0, stream, k);
+    const int KB = k.KB;
+    if (KB <= 8) hipLaunchKernelGGL((q4_few_kernel<8, FULL, SINGLE, G, 1, true>), dim3(std::min(k.tiles, 1024)), dim3(512), 0, stream, k);
+    else if (KB <= 16) hipLaunchKernelGGL((q4_few_kernel<8, FULL, SINGLE, G, 2, true>), dim3(std::min(k.tiles, 512)), dim3(512), 0, stream, k);
+    else if (KB <= 32) hipLaunchKernelGGL((q4_few_kernel<16, FULL, SINGLE, G, 2, true>), dim3(std::min(k.tiles, 256)), dim3(1024), 0, stream, k);
+    else if constexpr (FULL == 2) hipLaunchKernelGGL((q4_few_kernel<16, FULL, SINGLE, G, 2, false>), dim3(std::min(k.tiles, 256)), dim3(1024), 0, stream, k);   // (registers)
+    else if (KB <= 64) hipLaunchKernelGGL((q4_few_kernel<16, FULL, SINGLE, G, 4, true>), dim3(std::min(k.tiles, 256)), dim3(1024), 0, stream, k);
+    else hipLaunchKernelGGL((q4_few_kernel<16, FULL, SINGLE, G, 4, false>), dim3(std::min(k.tiles, 256)), dim3(1024), 0, stream, k);
 }
 
 hipError_t launch_q4_gemm(const Q4GemmArgs &a, int epilogue, hipStream_t stream) {
@@ -761,8 +802,10 @@ hipError_t launch_q4_gemm(const Q4GemmArgs &a, int epilogue, hipStream_t stream)
     k.Xout = (uint16_t *)a.Xout; k.KS_out = (a.K_out + 31) / 32; k.epilogue = epilogue;
     hipError_t rc = hipSuccess;
     const hipError_t launched = with_group(a.group, [&](auto g) {
-        if (a.rows <= kQ4Rows) launch_few<1, g()>(k, stream);
-        else if (a.rows <= kQ4FewRows) launch_few<2, g()>(k, stream);
+        if (a.rows == 1) launch_few<0, true, g()>(k, stream);
+        else if (a.rows <= kQ4Rows) launch_few<1, false, g()>(k, stream);
+        else if (a.rows == kQ4Rows + 1) launch_few<1, true, g()>(k, stream);
+        else if (a.rows <= kQ4FewRows) launch_few<2, false, g()>(k, stream);
         else {
             const int ng = (a.rows + kQ4Rows - 1) / kQ4Rows, slices = many_slices(a.N, a.K);
             uint4 *digits = (uint4 *)a.workspace;
