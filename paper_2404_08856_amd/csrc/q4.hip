@@ -429,7 +429,7 @@ __device__ __forceinline__ void row_scales(const Q4Kernel &a, int last, float *i
     }
 }
 
-// ---- few rows (1 .. 8): the waves of a workgroup share a tile's blocks ------------------------------------
+// ---- few rows (1 .. 16): the waves of a workgroup share a tile's blocks ------------------------------------
 // A workgroup takes tiles of 16 outputs; its waves take the blocks of a tile's row in units of NB and meet in LDS.  Every workgroup makes
 // the digits for itself, while its first weights are on their way.  KEEP: one unit per wave covers K; its digits stay in
 // registers for all of the workgroup's tiles, and a block's words are replaced by the next tile's as soon as they
@@ -459,19 +459,23 @@ __global__ __launch_bounds__(WAVES * 64) void q4_few_kernel(Q4Kernel a) {
     };
     // digits of blocks b0 .. b0 + NB - 1 (beyond the matrix: zeros)
     auto digits = [&](int b0) __attribute__((always_inline)) {
-        float v[GROUPS][NB][8], v1[8];
         auto first = [&](int b) __attribute__((always_inline)) { return b < a.KB ? kQ4Block * b + 32 * t + 8 * g : a.K; };
-        with_kind(a, [&](auto kind) __attribute__((always_inline)) {
+        float v1[8];
+#pragma unroll
+        for (int r0 = 0; r0 < (FULL > 0 ? FULL : 1); r0 += 2) {    // two groups at a time: what their loads take of registers
+            float v[2][NB][8];
+            with_kind(a, [&](auto kind) __attribute__((always_inline)) {
+#pragma unroll
+                for (int i = 0; i < NB; ++i)
+#pragma unroll
+                    for (int rg = r0; rg < FULL && rg < r0 + 2; ++rg) load_x8<kind()>(a, a.row0 + kQ4Rows * rg + c, first(b0 + i), v[rg - r0][i]);
+                if (SINGLE && r0 == 0) load_x8<kind()>(a, a.row0 + kQ4Rows * FULL, c < NB ? first(b0 + c) : a.K, v1);
+            });
 #pragma unroll
             for (int i = 0; i < NB; ++i)
 #pragma unroll
-                for (int rg = 0; rg < FULL; ++rg) load_x8<kind()>(a, a.row0 + kQ4Rows * rg + c, first(b0 + i), v[rg][i]);
-            if (SINGLE) load_x8<kind()>(a, a.row0 + kQ4Rows * FULL, c < NB ? first(b0 + c) : a.K, v1);
-        });
-#pragma unroll
-        for (int i = 0; i < NB; ++i)
-#pragma unroll
-            for (int rg = 0; rg < FULL; ++rg) f[rg][i] = convert(v[rg][i], B[rg][i]);
+                for (int rg = r0; rg < FULL && rg < r0 + 2; ++rg) f[rg][i] = convert(v[rg - r0][i], B[rg][i]);
+        }
         if (SINGLE) {
             const float own = convert(v1, B1);
 #pragma unroll
@@ -537,7 +541,7 @@ __global__ __launch_bounds__(WAVES * 64) void q4_few_kernel(Q4Kernel a) {
     }
 }
 
-// ---- many rows (9 .. 64) -------------------------------------------------------------------------------
+// ---- many rows -------------------------------------------------------------------------------
 // The digits are made once, by a kernel of their own, with one exponent per row.  Layout: [row group][block][step][lane] of 16
 // bytes, then the factor of each row.  A workgroup per row group; up to kKeep blocks per wave stay in registers between the
 // search for the largest magnitude and the digits.
@@ -748,7 +752,10 @@ __global__ __launch_bounds__(256) void q4_join_kernel(Q4Kernel a, const float *p
     finish(a, active, row, tile, n, s, up, inv_s[active ? row : 0]);
 }
 
-constexpr int kQ4FewRows = 8, kQ4MaxSlices = 8;
+// Up to how many rows the kernel of few rows goes: as many row groups as a workgroup's registers keep the digits of.  Few / many at G = 128:
+// 16 rows, 768 x 768 6.1 / 9.4 us; 12 rows, 4096 x 4096 12.2 / 16.1, 32000 x 4096 20.9 / 22.5; 12 rows, 4096 x 11008, digits anew, 26 / 24.9.
+static int few_rows(int K) { return K <= 16 * kQ4Block ? 16 : K <= 32 * kQ4Block ? 12 : 8; }
+constexpr int kQ4MaxSlices = 8;
 // Slices of K: what makes rounds of workgroups x blocks of one the least, with about 4 blocks' time for a workgroup's start and end
 static int many_slices(int N, int K) {
     const int groups = ((N + 15) / 16 + kQ4ManyTiles - 1) / kQ4ManyTiles, KB = (K + kQ4Block - 1) / kQ4Block;
@@ -763,7 +770,7 @@ static int many_slices(int N, int K) {
 static size_t digit_bytes(int rows, int K) { return (size_t)((rows + 3) / 4) * ((K + kQ4Block - 1) / kQ4Block) * 2048; }
 
 size_t q4_workspace_bytes(int rows, int N, int K) {
-    if (rows <= kQ4FewRows) return 0;
+    if (rows <= few_rows(K)) return 0;
     const int slices = many_slices(N, K);
     return digit_bytes(rows, K) + 1024 + (slices > 1 ? (size_t)slices * rows * ((N + 15) / 16 * 16) * 4 : 0);
 }
@@ -781,7 +788,10 @@ static hipError_t launch_many(const Q4Kernel &k, const uint4 *digits, const floa
 template <int FULL, bool SINGLE, int G>
 static void launch_few(const Q4Kernel &k, hipStream_t stream) {
     const int KB = k.KB;
-    if (KB <= 8) hipLaunchKernelGGL((q4_few_kernel<8, FULL, SINGLE, G, 1, true>), dim3(std::min(k.tiles, 1024)), dim3(512), 0, stream, k);
+    if constexpr (FULL > 2) {                                  // (K of at most 32 blocks, 16 for four groups: see few_rows)
+        if (FULL == 4 || KB <= 16) hipLaunchKernelGGL((q4_few_kernel<8, FULL, SINGLE, G, 2, true>), dim3(std::min(k.tiles, 256)), dim3(512), 0, stream, k);
+        else if constexpr (FULL == 3) hipLaunchKernelGGL((q4_few_kernel<8, FULL, SINGLE, G, 4, true>), dim3(std::min(k.tiles, 256)), dim3(512), 0, stream, k);
+    } else if (KB <= 8) hipLaunchKernelGGL((q4_few_kernel<8, FULL, SINGLE, G, 1, true>), dim3(std::min(k.tiles, 1024)), dim3(512), 0, stream, k);
     else if (KB <= 16) hipLaunchKernelGGL((q4_few_kernel<8, FULL, SINGLE, G, 2, true>), dim3(std::min(k.tiles, 512)), dim3(512), 0, stream, k);
     else if (KB <= 32) hipLaunchKernelGGL((q4_few_kernel<16, FULL, SINGLE, G, 2, true>), dim3(std::min(k.tiles, 256)), dim3(1024), 0, stream, k);
     else if constexpr (FULL == 2) hipLaunchKernelGGL((q4_few_kernel<16, FULL, SINGLE, G, 2, false>), dim3(std::min(k.tiles, 256)), dim3(1024), 0, stream, k);   // (registers)
@@ -805,7 +815,9 @@ hipError_t launch_q4_gemm(const Q4GemmArgs &a, int epilogue, hipStream_t stream)
         if (a.rows == 1) launch_few<0, true, g()>(k, stream);
         else if (a.rows <= kQ4Rows) launch_few<1, false, g()>(k, stream);
         else if (a.rows == kQ4Rows + 1) launch_few<1, true, g()>(k, stream);
-        else if (a.rows <= kQ4FewRows) launch_few<2, false, g()>(k, stream);
+        else if (a.rows <= 2 * kQ4Rows) launch_few<2, false, g()>(k, stream);
+        else if (a.rows <= few_rows(a.K) && a.rows <= 3 * kQ4Rows) launch_few<3, false, g()>(k, stream);
+        else if (a.rows <= few_rows(a.K)) launch_few<4, false, g()>(k, stream);
         else {
             const int ng = (a.rows + kQ4Rows - 1) / kQ4Rows, slices = many_slices(a.N, a.K);
             uint4 *digits = (uint4 *)a.workspace;

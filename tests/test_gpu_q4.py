@@ -103,14 +103,20 @@ SHAPES = [(1, 16, 32, 32), (1, 1, 1, 32), (2, 17, 127, 64), (3, 40, 128, 128), (
           (31, 80, 1152, 64), (40, 528, 515, 32), (64, 65, 3001, 128), (64, 1040, 768, 64), (1, 4112, 1280, 128), (5, 4100, 130, 64)]
 
 
-@pytest.mark.parametrize("rows,N,K,G", SHAPES)
+# every way that a few rows' digits are held: blocks of K that waves keep (1, 2, 4 each), any K; one row, up to 4, 5, up to 8, up to 12, up to 16
+LONG = [(rows, N, K, G) for rows in (1, 3, 5, 7, 11, 14) for N, K, G in ((48, 900, 128), (48, 2000, 64), (4128, 1150, 32), (33, 4100, 128), (64, 5555, 32), (17, 8200, 64), (31, 11008, 128), (16, 17000, 64))]
+
+
+@pytest.mark.parametrize("rows,N,K,G", SHAPES + LONG)
 @pytest.mark.parametrize("bf16", [False, True])
 def test_product_of_integers_is_exact(rows, N, K, G, bf16):
-    """Integers up to 60 and scales that are powers of two up to 2: every sum is a multiple of 1/4 below 2^22 (60 * 8 * 2 * 4096 < 2^22), so float32 has it exactly in any order."""
+    """Integers up to 60 (15 where K is over 4096) and scales that are powers of two up to 2: every sum is a multiple of 1/4 below 2^22
+    (60 * 8 * 2 * 4096 and 15 * 8 * 2 * 17000 are), so float32 has it exactly in any order."""
     spd = spd_mod()
     rng = np.random.default_rng(rows + 7 * N + 31 * K + G)
-    x = rng.integers(-60, 61, (rows, K)).astype(np.float64)
-    x[:, rng.integers(0, K)] = 60
+    top = 60 if K <= 4096 else 15
+    x = rng.integers(-top, top + 1, (rows, K)).astype(np.float64)
+    x[:, rng.integers(0, K)] = top
     if rows > 2:
         x[1] = 0
     q = rng.integers(-8, 8, (N, K))
@@ -124,7 +130,7 @@ def test_product_of_integers_is_exact(rows, N, K, G, bf16):
         assert torch.isnan(y._base[:, N:]).all()
 
 
-@pytest.mark.parametrize("rows,N,K,G", SHAPES)
+@pytest.mark.parametrize("rows,N,K,G", SHAPES + LONG[::5])
 @pytest.mark.parametrize("kind", ["normal", "one-sided", "outliers", "tiny", "huge"])
 def test_product_within_its_roundings(rows, N, K, G, kind):
     """Against 64 bits.  A row's digits leave out at most 2^-29 of its largest magnitude per entry; their magnitudes add up to at
