@@ -141,8 +141,8 @@ int32_t spd_model_create(const spd_model_config *h_cfg, const spd_weights *h_wei
 /* The same for a model whose matrices stay in 4 bits (spd_weights_q4): 3.8 times fewer bytes per step at groups of 128.  All
  * calls on such a model are those of any other; its products are as exact as the bf16 model's (float32 activations and sums),
  * so it differs from a bf16 model of the dequantised weights by float32 rounding only.  A row of activations with a
- * value that is not finite gives NaN.  Prompts run in passes of 64 rows; of spd_tuning only the attention's fields and
- * wait_spin_limit have an effect.  Errors as spd_model_create, SPD_ERR_SHAPE for another group. */
+ * value that is not finite gives NaN.  Of spd_tuning only the attention's fields, batch_kernel (prompts in passes of 64 or 40 rows) and
+ * wait_spin_limit have an effect.  The workspace also holds one matrix at 16 bits, for prompts.  Errors as spd_model_create, SPD_ERR_SHAPE for another group. */
 int32_t spd_model_bytes_q4(const spd_model_config *h_cfg, int32_t group, size_t *h_packed_bytes,
                            size_t *h_kv_bytes, size_t *h_workspace_bytes);
 int32_t spd_model_create_q4(const spd_model_config *h_cfg, const spd_weights_q4 *h_weights,

@@ -177,7 +177,9 @@ constexpr int kPrefillRows = 2048;   // rows per pass at most
 // batched path / these kernels, empty cache and 500 cached positions): four 7B layers, 32 rows 677 / 683 and 801 / 749,
 // 40 rows 712 / 699 and 864 / 763; the 12-layer draft, 24 rows 769 / 791 and 948 / 920, 32 rows 867 / 796 and 1110 / 924;
 // the 4-layer draft, 24 rows 294 / 307 and 382 / 368, 32 rows 330 / 309 and 450 / 370.
-inline int prefill_min_rows(int d_model) { return d_model >= 2048 ? 33 : 25; }
+// Matrices in 4 bits (unpacked for these kernels first): four 7B layers, 48 rows 772 / 835, 64 rows 924 / 842; the 12-layer draft, 24 rows 871 / 870,
+// 25 rows 996 / 851; the 4-layer draft, 25 rows 381 / 322.
+inline int prefill_min_rows(int d_model, bool q4) { return d_model >= 2048 ? (q4 ? 56 : 33) : 25; }
 int prefill_row_parts(int d);        // parts of the sums of squares that the input rows' kernel leaves per row
 hipError_t launch_prefill_rows(const void *embed_bf16, const int32_t *tokens, const float *embeds, int rows, int d, int vocab,
                                const float *gain, float *h, void *X, float *ssq, int ssq_ld, hipStream_t stream);
@@ -196,10 +198,12 @@ struct PrefillGemmArgs {
     void *Xout;               // SWIGLU: activations of N / 2 columns
     float *partials;          // scratch for the sums of K slices (prefill_partial_bytes)
     unsigned *arrive;         // kPrefillMaxSplit counters, zero between launches
+    const float *wscale;      // factors of the weights' rows, [N / 16][ceil(K / 32)][16], alike in every group_steps K-steps (1, 2 or 4); NULL: 1
+    int group_steps;
 };
 constexpr int kPrefillMaxSlices = 8, kPrefillMaxSplit = 1024;    // K slices per tile; workgroups of a sliced launch
 size_t prefill_partial_bytes(int N, int max_rows);
-int prefill_ssq_parts(int n_tiles, int rows);
+int prefill_ssq_parts(int n_tiles, int rows, bool scaled);
 hipError_t launch_prefill_gemm(const PrefillGemmArgs &a, int epilogue, hipStream_t stream);
 struct PrefillAttnArgs {
     const float *qkv;         // [rows, 3 * H * dh] before RoPE
@@ -261,6 +265,8 @@ hipError_t launch_q4_quantize(const void *W, bool bf16, size_t ldw, int N, int K
 hipError_t launch_q4_dequantize(const void *q, const void *scales, int N, int K, int G, void *W, bool bf16, size_t ldw, hipStream_t stream);
 // sources and modes as in launch_pack_weight
 hipError_t launch_q4_pack(const void *const (&q)[3], const void *const (&scales)[3], int mode, int N, int K, int G, void *packed, hipStream_t stream);
+// Tiles tile0 .. tile0 + n_tiles - 1 of a packed matrix as the prompt kernels read it: its integers in bf16 blocks (as of launch_pack_weight), and PrefillGemmArgs::wscale
+hipError_t launch_q4_unpack(const void *packed, int N, int K, int G, int tile0, int n_tiles, void *blocks, float *wscale, hipStream_t stream);
 enum Q4Activations { Q4_X_F32 = 0, Q4_X_BF16 = 1, Q4_X_PACKED = 2 };
 struct Q4GemmArgs {
     const void *W;            // packed

@@ -53,6 +53,7 @@ struct Layout {                    // byte offsets inside the three buffers
     // workspace
     size_t h, qkv, xn, xo, xf, rope, logits, ssq_a, ssq_b, d_lens, d_error, qa_count, qa_abort, part, arrive, zero, chain;
     size_t ph, pqkv, pxn, pxo, pxf, pssq_a, pssq_b, ppart;      // prefill passes of up to prefill_rows rows
+    size_t pw, pwscale;             // matrices in 4 bits: one of them as the prompt kernels read it
     int prefill_rows, pssq_ld;      // pssq: [part][pssq_ld] of the rows
     size_t ws_total;
 };
@@ -139,6 +140,12 @@ void make_layout(const spd_model_config &c, int q4_group, Layout &L) {
     L.pssq_a = take(pr * pssq_parts * 4);
     L.pssq_b = take(pr * pssq_parts * 4);
     L.ppart = take(std::max({prefill_partial_bytes(3 * HD, L.prefill_rows), prefill_partial_bytes(d, L.prefill_rows), prefill_partial_bytes(2 * F, L.prefill_rows)}));
+    L.pw = L.pwscale = 0;
+    if (q4_group) {
+        const size_t most = std::max({packed_matrix_bytes(3 * HD, d), packed_matrix_bytes(d, HD), packed_matrix_bytes(2 * F, d), packed_matrix_bytes(d, F)});
+        L.pw = take(most);
+        L.pwscale = take(most / 16);                       // a float for 16 rows and a K-step, where the block takes 1 KiB
+    }
     L.ws_total = off;
 }
 
@@ -636,7 +643,7 @@ int32_t run_layers(spd_model *m, int first, AttnArgs &at, int seq0, int n_seqs, 
             qa.abort_flag = (int *)(m->ws + L.qa_abort);
             PROF_KERNEL(PK_QKV, launch_qkv_attention(qa, st));
         } else {
-            g.W = m->packed + L.wqkv[l]; g.X = xn; g.N = at.row_cached ? HD : 3 * HD; g.K = d; g.rows = rows; g.Y = qkv; g.ldy = 3 * HD;
+            g.W = m->packed + L.wqkv[l]; g.X = xn; g.N = at.row_cached && !m->q4_group ? HD : 3 * HD; g.K = d; g.rows = rows; g.Y = qkv; g.ldy = 3 * HD;
             g.ssq_in = ssq_b; g.ssq_in_parts = l == first ? 1 : d_tiles; g.eps = c.rms_eps;
             PROF_GEMM(PK_QKV, g, EPI_STORE, m->t_qkv);
             WeightPrefetch pf{};
@@ -741,35 +748,44 @@ int32_t prefill_pass(spd_model *m, int32_t seq, const float *embeds, const int32
         at.d_len = (const int32_t *)(m->ws + L.d_lens) + seq;
         at.d_error = (int32_t *)(m->ws + L.d_error);
     }
-    const int parts = prefill_ssq_parts(d / 16, M);
+    const int parts = prefill_ssq_parts(d / 16, M, m->q4_group != 0);
+    // g.W: features first .. first + g.N - 1 of the packed matrix (N x g.K) at `off`
+    auto weights = [&](PrefillGemmArgs &g, size_t off, int N, int first) -> hipError_t {
+        if (!m->q4_group) { g.W = m->packed + off + packed_matrix_bytes(first, g.K); return hipSuccess; }
+        g.W = m->ws + L.pw; g.wscale = (const float *)(m->ws + L.pwscale); g.group_steps = m->q4_group / kStepK;
+        return launch_q4_unpack(m->packed + off, N, g.K, m->q4_group, first / kTileN, g.N / kTileN, m->ws + L.pw, (float *)(m->ws + L.pwscale), st);
+    };
+    auto project = [&](PrefillGemmArgs &g, size_t off, int N, int first, Epilogue epi) -> hipError_t {
+        const hipError_t rc = weights(g, off, N, first);
+        return rc != hipSuccess ? rc : launch_prefill_gemm(g, epi, st);
+    };
     for (int l = 0; l < c.n_layers; ++l) {
         const bool last = l + 1 == c.n_layers;
         char *kv_l = m->kv + (size_t)l * L.kv_layer_stride;
         at.k_cache = kv_l + (size_t)seq * c.n_heads * c.max_positions * c.head_dim * 2;
         at.v_cache = kv_l + align_up(L.kv_k_bytes, 256) + (size_t)seq * c.n_heads * c.head_dim * L.v_stride * 2;
         const int q0 = last ? HD : 0;                     // the last layer's queries are not needed: features HD .. 3 HD - 1
-        const char *wqkv = m->packed + L.wqkv[l] + packed_matrix_bytes(q0, d);
         PrefillGemmArgs common{};
         common.rows = M; common.ssq_ld = L.pssq_ld; common.eps = c.rms_eps;
         common.partials = (float *)(m->ws + L.ppart); common.arrive = (unsigned *)(m->ws + L.arrive);
         PrefillGemmArgs g = common;
-        g.W = wqkv; g.X = xn; g.N = 3 * HD - q0; g.K = d; g.Y = qkv + q0; g.ldy = 3 * HD;
+        g.X = xn; g.N = 3 * HD - q0; g.K = d; g.Y = qkv + q0; g.ldy = 3 * HD;
         g.ssq_in = ssq_b; g.ssq_parts = l == 0 ? prefill_row_parts(d) : parts;
-        PROF_TRY(PK_QKV, launch_prefill_gemm(g, EPI_STORE, st));
+        PROF_TRY(PK_QKV, project(g, L.wqkv[l], 3 * HD, q0, EPI_STORE));
         PROF_TRY(PK_ATTENTION, launch_prefill_attention(at, !last, st));
         if (last) break;
         g = common;
-        g.W = m->packed + L.wo[l]; g.X = xo; g.N = d; g.K = HD; g.Y = h; g.ldy = d;
+        g.X = xo; g.N = d; g.K = HD; g.Y = h; g.ldy = d;
         g.gain_next = gain_of(L.mlp_norm[l]); g.Xnext = xn; g.ssq_out = ssq_a;
-        PROF_TRY(PK_O, launch_prefill_gemm(g, EPI_RESIDUAL, st));
+        PROF_TRY(PK_O, project(g, L.wo[l], d, 0, EPI_RESIDUAL));
         g = common;
-        g.W = m->packed + L.wgu[l]; g.X = xn; g.N = 2 * F; g.K = d; g.Xout = xf;
+        g.X = xn; g.N = 2 * F; g.K = d; g.Xout = xf;
         g.ssq_in = ssq_a; g.ssq_parts = parts;
-        PROF_TRY(PK_GATE_UP, launch_prefill_gemm(g, EPI_SWIGLU, st));
+        PROF_TRY(PK_GATE_UP, project(g, L.wgu[l], 2 * F, 0, EPI_SWIGLU));
         g = common;
-        g.W = m->packed + L.wdown[l]; g.X = xf; g.N = d; g.K = F; g.Y = h; g.ldy = d;
+        g.X = xf; g.N = d; g.K = F; g.Y = h; g.ldy = d;
         g.gain_next = gain_of(L.attn_norm[l + 1]); g.Xnext = xn; g.ssq_out = ssq_b;
-        PROF_TRY(PK_DOWN, launch_prefill_gemm(g, EPI_RESIDUAL, st));
+        PROF_TRY(PK_DOWN, project(g, L.wdown[l], d, 0, EPI_RESIDUAL));
     }
     int32_t *d_len = (int32_t *)(m->ws + L.d_lens) + seq;
     if (m->dev_lens) HIP_TRY(launch_lens_add(d_len, 1, M, st));
@@ -799,9 +815,9 @@ int32_t prefill_common(spd_model *m, int32_t seq, const float *embeds, const int
         return fail(SPD_ERR_CAPACITY, "KV cache overflow in prefill: %d + %d > %d", m->lens[seq], n_rows, m->cfg.max_positions);
     float *scratch = (float *)(m->ws + m->L.logits);
     if (m->dev_lens) m->lens_least[seq] = std::min(m->lens_least[seq] + n_rows, m->cfg.max_positions);
-    // passes through the prefill kernels, unless a kernel family was asked for (batch_kernel = 1 or 2); they read matrices in bf16
-    if (!m->q4_group && !m->t_qkv.no_batch && !m->t_qkv.force_batch) {
-        const int min_rows = prefill_min_rows(m->cfg.d_model);
+    // passes through the prefill kernels, unless a kernel family was asked for (batch_kernel = 1 or 2)
+    if (!m->t_qkv.no_batch && !m->t_qkv.force_batch) {
+        const int min_rows = prefill_min_rows(m->cfg.d_model, m->q4_group != 0);
         while (n_rows >= min_rows) {
             const int M = std::min(n_rows, m->L.prefill_rows);
             const int32_t rc = prefill_pass(m, seq, embeds, tokens, M, M == n_rows ? last_logits : nullptr, st);

@@ -134,6 +134,8 @@ struct PrefillGemmKernelArgs {
     bool fold;                // sums of 16 K-steps between the partial and the running sum (small shape)
     float *partials;          // J > 1: [tile][slice][TN * TR * 256] sums
     unsigned *arrive;         // J > 1: one counter per tile, zero between launches
+    const float *wscale;      // SCALED: [n_tiles][KS][16] factors of the weights' rows in each K-step, alike in every group_steps of them
+    int group_steps;          // a power of two
 };
 
 // J > 1: the K range is cut into J slices, one workgroup each.
@@ -151,13 +153,18 @@ constexpr int kPgBuf = 3;     // LDS stages: one whose fragments are read, two o
 // Accumulation: partial sums over 4 or 8 K-steps are added to a running sum, so no long chain rounds at the size of
 // the result.  The second and third terms (2^-8 and 2^-16 of the first) have an accumulator of their own where the
 // registers allow it (NW * NX <= 8); otherwise they go into the short partial sum ahead of the first term.
-template <int WN, int WR, int NW, int NX, int EPI>
+// SCALED (matrices held in 4 bits): the weights are the integers, exact in bf16, and the partial sums of a group of columns are
+// added with the factors of the weights' rows.  A wave brings those of its tiles in with each stage, one load more.
+template <int WN, int WR, int NW, int NX, int EPI, bool SCALED>
 __global__ __launch_bounds__(WN *WR * 64, 2) void prefill_gemm_kernel(PrefillGemmKernelArgs a) {
     constexpr int WAVES = WN * WR, TN = WN * NW, TR = WR * NX, BLK = TN + kTerms * TR, PB = BLK / WAVES;
     static_assert(BLK % WAVES == 0, "equal loads per wave: the waits count them");
+    constexpr int PL = PB + SCALED;                       // loads per wave and stage
     constexpr bool OWN_REST = NW * NX <= 8;
+    static_assert(!SCALED || (OWN_REST && NW <= 16), "factors of a wave's tiles in one load");
     static_assert(NW % 2 == 0, "the SwiGLU epilogue takes tiles in pairs");
     __shared__ uint4 S[kPgBuf][BLK][64];
+    __shared__ float4 F[SCALED ? kPgBuf : 1][SCALED ? WAVES : 1][64];      // [..][4 tile + features / 4]
     const int lane = threadIdx.x & 63;
     const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     // Workgroup -> tile.  Workgroups go round robin over the 8 XCDs; each XCD takes a contiguous run of an order that
@@ -193,13 +200,16 @@ __global__ __launch_bounds__(WN *WR * 64, 2) void prefill_gemm_kernel(PrefillGem
         }
     }
     const unsigned lds0 = lds_addr(&S[0][0][0]);
+    const unsigned f0 = lds_addr(&F[0][SCALED ? w : 0][0]);
+    const unsigned factors = SCALED ? ((unsigned)min(t0 + (w % WN) * NW + (lane >> 2) % NW, a.n_tiles - 1) * (unsigned)a.KS * 4u + (lane & 3)) * 16u : 0u;
     auto issue_one = [&](int s, int buf, int i) __attribute__((always_inline)) {
         const int ss = s < KS ? s : KS - 1;               // past the end: a harmless re-read
-        lds_dma16(src[i] + (size_t)ss * step[i], 16u * lane, lds0 + (unsigned)((buf * BLK + w + i * WAVES) * 1024));
+        if (SCALED && i == PB) lds_dma16(a.wscale + (size_t)(k0 + ss) * 16, factors, f0 + (unsigned)(buf * WAVES * 1024));
+        else lds_dma16(src[i] + (size_t)ss * step[i], 16u * lane, lds0 + (unsigned)((buf * BLK + w + i * WAVES) * 1024));
     };
     auto issue = [&](int s, int buf) __attribute__((always_inline)) {
 #pragma unroll
-        for (int i = 0; i < PB; ++i) issue_one(s, buf, i);
+        for (int i = 0; i < PL; ++i) issue_one(s, buf, i);
     };
     issue(0, 0);
     issue(1, 1);
@@ -256,8 +266,26 @@ __global__ __launch_bounds__(WN *WR * 64, 2) void prefill_gemm_kernel(PrefillGem
 #pragma unroll
             for (int j = 0; j < NX; ++j) mid[i][j] = f32x4_t{0.f, 0.f, 0.f, 0.f};
     }
-    auto fold_partial = [&] __attribute__((always_inline)) {
-        if (--left == 0) {
+    // SCALED: whether a group of columns, or the slice, ends with step s; the factors of that step
+    auto group_ends = [&](int s) __attribute__((always_inline)) { return SCALED && (((k0 + s + 1) & (a.group_steps - 1)) == 0 || s + 1 >= KS); };
+    float4 factor[SCALED ? NW : 1];
+    auto read_factors = [&](int buf) __attribute__((always_inline)) {
+#pragma unroll
+        for (int i = 0; i < (SCALED ? NW : 0); ++i) factor[i] = F[buf][w][4 * i + (lane >> 4)];
+    };
+    auto fold_partial = [&](int s) __attribute__((always_inline)) {
+        if constexpr (SCALED) {
+            if (!group_ends(s)) return;
+#pragma unroll
+            for (int i = 0; i < NW; ++i)
+#pragma unroll
+                for (int j = 0; j < NX; ++j) {
+                    const float f[4] = {factor[i].x, factor[i].y, factor[i].z, factor[i].w};
+#pragma unroll
+                    for (int v = 0; v < 4; ++v) sum[i][j][v] = __builtin_fmaf(part[i][j][v] + rest[i][j][v], f[v], sum[i][j][v]);
+                    part[i][j] = rest[i][j] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+                }
+        } else if (--left == 0) {
             left = chunk;
 #pragma unroll
             for (int i = 0; i < NW; ++i)
@@ -283,7 +311,7 @@ __global__ __launch_bounds__(WN *WR * 64, 2) void prefill_gemm_kernel(PrefillGem
     };
     // One K-step: its fragments are in wf and x, the next one's are read from buffer `next` (into wf and xn), stage `later` goes into `buf`
     auto multiply = [&](uint4 (&x)[kTerms][NX], uint4 (&xn)[kTerms][NX], int next, int later, int buf) __attribute__((always_inline)) {
-        constexpr int XR = (kTerms * NX + NW - 1) / NW, LR = (PB + NW - 1) / NW;     // reads and loads per weight fragment
+        constexpr int XR = (kTerms * NX + NW - 1) / NW, LR = (PL + NW - 1) / NW;     // reads and loads per weight fragment
 #pragma unroll
         for (int i = 0; i < NW; ++i) {
 #pragma unroll
@@ -297,15 +325,16 @@ __global__ __launch_bounds__(WN *WR * 64, 2) void prefill_gemm_kernel(PrefillGem
                 }
             wf[i] = S[next][wn * NW + i][lane];
 #pragma unroll
-            for (int q = i * LR; q < (i + 1) * LR && q < PB; ++q) issue_one(later, buf, q);
+            for (int q = i * LR; q < (i + 1) * LR && q < PL; ++q) issue_one(later, buf, q);
             __builtin_amdgcn_sched_barrier(0);
         }
-        fold_partial();
+        fold_partial(later - kPgBuf);
+        if (SCALED && group_ends(later - kPgBuf + 1)) read_factors(next);        // (before the step after it brings its own)
     };
     // the older of the two stages on their way has landed for everyone, and nobody reads the one before it any more (lgkmcnt: not
     // a read of it is still under way when a wave passes the barrier, wherever the compiler put the products)
     auto arrive = [&] __attribute__((always_inline)) {
-        asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"((kPgBuf - 2) * PB) : "memory");
+        asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"((kPgBuf - 2) * PL) : "memory");
         __builtin_amdgcn_s_barrier();
         asm volatile("" ::: "memory");
     };
@@ -320,6 +349,7 @@ __global__ __launch_bounds__(WN *WR * 64, 2) void prefill_gemm_kernel(PrefillGem
     for (int q = 0; q < kTerms * NX; ++q) read_x(xa, q, 0);
 #pragma unroll
     for (int i = 0; i < NW; ++i) wf[i] = S[0][wn * NW + i][lane];
+    if (SCALED && group_ends(0)) read_factors(0);
     int s = 0;
     for (; s + 1 < KS; s += 2) {
         arrive();
@@ -467,15 +497,15 @@ __global__ __launch_bounds__(WN *WR * 64, 2) void prefill_gemm_kernel(PrefillGem
     }
 }
 
-template <int WN, int WR, int NW, int NX>
+template <int WN, int WR, int NW, int NX, bool SCALED>
 static hipError_t launch_pg(PrefillGemmKernelArgs &k, int epilogue, hipStream_t stream) {
     k.n_blk = (k.n_tiles + WN * NW - 1) / (WN * NW);
     k.r_blk = (k.n_rt + WR * NX - 1) / (WR * NX);
     const dim3 grid(k.n_blk * k.r_blk * k.J), block(WN * WR * 64);
     switch (epilogue) {
-        case EPI_STORE: hipLaunchKernelGGL((prefill_gemm_kernel<WN, WR, NW, NX, EPI_STORE>), grid, block, 0, stream, k); break;
-        case EPI_RESIDUAL: hipLaunchKernelGGL((prefill_gemm_kernel<WN, WR, NW, NX, EPI_RESIDUAL>), grid, block, 0, stream, k); break;
-        case EPI_SWIGLU: hipLaunchKernelGGL((prefill_gemm_kernel<WN, WR, NW, NX, EPI_SWIGLU>), grid, block, 0, stream, k); break;
+        case EPI_STORE: hipLaunchKernelGGL((prefill_gemm_kernel<WN, WR, NW, NX, EPI_STORE, SCALED>), grid, block, 0, stream, k); break;
+        case EPI_RESIDUAL: hipLaunchKernelGGL((prefill_gemm_kernel<WN, WR, NW, NX, EPI_RESIDUAL, SCALED>), grid, block, 0, stream, k); break;
+        case EPI_SWIGLU: hipLaunchKernelGGL((prefill_gemm_kernel<WN, WR, NW, NX, EPI_SWIGLU, SCALED>), grid, block, 0, stream, k); break;
         default: return hipErrorInvalidValue;
     }
     return hipGetLastError();
@@ -512,7 +542,7 @@ size_t prefill_partial_bytes(int N, int max_rows) {
     const long tiles = (long)((N / 16 + 7) / 8) * ((max_rows + 63) / 64);
     return (size_t)std::min((long)kPrefillMaxSplit, tiles * kPrefillMaxSlices) * 32 * 1024;
 }
-int prefill_ssq_parts(int n_tiles, int rows) { return prefill_large(n_tiles, rows) ? (n_tiles + 7) / 8 : (n_tiles + 3) / 4; }
+int prefill_ssq_parts(int n_tiles, int rows, bool scaled) { return !scaled && prefill_large(n_tiles, rows) ? (n_tiles + 7) / 8 : (n_tiles + 3) / 4; }
 
 hipError_t launch_prefill_gemm(const PrefillGemmArgs &a, int epilogue, hipStream_t stream) {
     if (a.N % 16 != 0 || a.rows < 1 || a.rows > kPrefillRows) return hipErrorInvalidValue;
@@ -529,14 +559,16 @@ hipError_t launch_prefill_gemm(const PrefillGemmArgs &a, int epilogue, hipStream
     k.J = 1;
     k.fold = false;
     k.partials = a.partials; k.arrive = a.arrive;
-    if (prefill_large(k.n_tiles, a.rows)) return launch_pg<2, 4, 8, 2>(k, epilogue, stream);
+    k.wscale = a.wscale; k.group_steps = a.group_steps;
+    // (scaled weights take the small shape always: their factors' registers are the ones that it has for sums of four partial sums)
+    if (!a.wscale && prefill_large(k.n_tiles, a.rows)) return launch_pg<2, 4, 8, 2, false>(k, epilogue, stream);
     const int tiles = ((k.n_tiles + 7) / 8) * ((a.rows + 63) / 64);
     k.J = prefill_slices(tiles, k.KS);
     // Slices that fill the chip's 512 places are as short as they can be.  Where the estimate leaves places empty, fewer and longer ones were
     // faster, and their running sums would be longer chains of additions: 7B QKV at 100 rows, two slices of 64 steps instead of five of 26,
     // 10 % more flipped roundings of K and V, and as many with sums in between (0.3 % of a short prompt's time).
     k.fold = k.J > 1 && tiles * k.J <= 384;
-    return launch_pg<2, 2, 4, 2>(k, epilogue, stream);
+    return a.wscale ? launch_pg<2, 2, 4, 2, true>(k, epilogue, stream) : launch_pg<2, 2, 4, 2, false>(k, epilogue, stream);
 }
 
 // ---------------------------------------------------------------------------------

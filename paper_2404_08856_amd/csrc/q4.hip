@@ -228,6 +228,40 @@ hipError_t launch_q4_pack(const void *const (&q)[3], const void *const (&scales)
     return hipGetLastError();
 }
 
+// For prompts: a wave per block of 128 columns writes its four blocks of 32 in bf16 and their rows' factors.
+template <int G>
+__global__ __launch_bounds__(256) void q4_unpack_kernel(const uint4 *__restrict__ W, const uint16_t *__restrict__ S, int KB, int KS, int tile0, size_t blocks,
+                                                        uint4 *__restrict__ out, float *__restrict__ wscale) {
+    const size_t id = (size_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+    if (id >= blocks) return;
+    const int lane = threadIdx.x & 63, t = (int)(id / KB), b = (int)(id - (size_t)t * KB);
+    const size_t src = (size_t)tile0 * KB + id;
+    const uint4 w = W[src * 64 + lane];
+    const uint32_t words[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        if (4 * b + j >= KS) break;
+        uint32_t p[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {                          // columns 2 e, 2 e + 1 of the lane's 8
+            auto value = [&](int k) { return (float)((int)(words[j] << (24 - 8 * (k & 3) + (k < 4 ? 0 : 4))) >> 28); };
+            p[e] = f32_to_bf16_bits(value(2 * e)) | (uint32_t)f32_to_bf16_bits(value(2 * e + 1)) << 16;
+        }
+        out[((size_t)t * KS + 4 * b + j) * 64 + lane] = uint4{p[0], p[1], p[2], p[3]};
+    }
+    const int j = lane >> 4, row = lane & 15;
+    if (4 * b + j < KS) wscale[((size_t)t * KS + 4 * b + j) * 16 + row] = bf16_bits_to_f32(S[(src * 16 + row) * (kQ4Block / G) + 32 * j / G]);
+}
+
+hipError_t launch_q4_unpack(const void *packed, int N, int K, int G, int tile0, int n_tiles, void *blocks, float *wscale, hipStream_t stream) {
+    const int KB = (K + kQ4Block - 1) / kQ4Block;
+    const size_t n = (size_t)n_tiles * KB;
+    return with_group(G, [&](auto g) {
+        hipLaunchKernelGGL(q4_unpack_kernel<g()>, dim3((unsigned)((n + 3) / 4)), dim3(256), 0, stream, (const uint4 *)packed,
+                           (const uint16_t *)((const char *)packed + q4_scales_offset(N, K)), KB, (K + 31) / 32, tile0, n, (uint4 *)blocks, wscale);
+    });
+}
+
 // ---------------------------------------------------------------------------------
 // the product
 // ---------------------------------------------------------------------------------

@@ -41,7 +41,7 @@ TINY = synth.SHAPES["tiny_target"]
 @pytest.mark.parametrize("shape,group,n_seqs,M,prompt", [
     (TINY, 32, 1, 1, 3), (TINY, 64, 1, 5, 70), (TINY, 128, 2, 4, 33), (TINY, 32, 3, 5, 10), (TINY, 64, 8, 8, 20), (TINY, 128, 5, 2, 1),
     (synth.SHAPES["tiny_draft"], 128, 1, 2, 9), (synth.ModelShape(2, 768, 12, 64, 2048, 1024, tied_embeddings=True), 64, 1, 5, 65),
-    (synth.ModelShape(1, 4096, 32, 128, 11008, 512), 128, 1, 5, 40), (synth.ModelShape(1, 4096, 32, 128, 11008, 512), 64, 2, 8, 5)])
+    (synth.ModelShape(2, 4096, 32, 128, 11008, 512), 128, 1, 5, 60), (TINY, 32, 1, 3, 120), (TINY, 64, 2, 3, 25), (synth.ModelShape(2, 256, 2, 128, 680, 512), 32, 1, 2, 100), (synth.ModelShape(1, 4096, 32, 128, 11008, 512), 64, 2, 8, 5)])
 def test_prompt_and_verify_against_the_oracle(shape, group, n_seqs, M, prompt):
     model, wn = q4_model(shape, 11 + M, group, n_seqs, 128)
     cfg = oracle_cfg(shape)
