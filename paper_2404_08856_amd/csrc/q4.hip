@@ -320,16 +320,19 @@ __device__ __forceinline__ uint32_t byte_perm(uint32_t hi, uint32_t lo, uint32_t
 
 // Digits of a block of 128 columns for a row group.  Lane l = (4 c + t) + 16 g brings columns 32 t + 8 g .. + 7 of row c
 // and leaves with digit t (t = 3: the leading one) of columns 32 j + 8 g .. + 7, j < 4, of the row: B[2 j], B[2 j + 1].
-// exponent: of the largest magnitude among what the lane's row has in the block (biased, at least 36, 255: not finite).
-__device__ __forceinline__ int block_exponent(const float (&v)[8]) {
-    float m = 0.f;
-#pragma unroll
-    for (int e = 0; e < 8; ++e) m = __builtin_elementwise_maximum(m, fabsf(v[e]));        // NaN stays
+// exponent: of the largest magnitude among what the lane's row has there (biased, at least 36, 255: not finite).
+__device__ __forceinline__ int shared_exponent(float m) {      // m: the lane's largest magnitude, or NaN
     m = __builtin_elementwise_maximum(m, lane_xor<1>(m));
     m = __builtin_elementwise_maximum(m, lane_xor<2>(m));
     m = __builtin_elementwise_maximum(m, lane_xor<16>(m));
     m = __builtin_elementwise_maximum(m, lane_xor<32>(m));
     return max((int)(__float_as_uint(m) >> 23 & 255u), 36);
+}
+__device__ __forceinline__ int block_exponent(const float (&v)[8]) {
+    float m = 0.f;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) m = __builtin_elementwise_maximum(m, fabsf(v[e]));        // NaN stays
+    return shared_exponent(m);
 }
 // what a sum of 16 q * v is worth
 __device__ __forceinline__ float digit_factor(int exponent) {
@@ -452,10 +455,14 @@ template <int WAVES>
 __device__ __forceinline__ void row_scales(const Q4Kernel &a, int last, float *inv_s) {
     const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
     if (a.ssq_in) {
+        const int parts = a.ssq_in_parts;
         for (int r = a.row0 + w; r < last; r += WAVES) {
-            float sum = 0.f;
-            for (int p = lane; p < a.ssq_in_parts; p += 64) sum += a.ssq_in[(size_t)r * (a.K / 16) + p];
-            sum = wave_sum(sum);
+            const float *part = a.ssq_in + (size_t)r * (a.K / 16);
+            float v[4], sum = 0.f;                             // 256 parts (K = 4096) in one look
+#pragma unroll
+            for (int i = 0; i < 4; ++i) v[i] = lane + 64 * i < parts ? part[lane + 64 * i] : 0.f;
+            for (int p = lane + 256; p < parts; p += 64) sum += part[p];
+            sum = wave_sum(((v[0] + v[1]) + (v[2] + v[3])) + sum);
             if (lane == 0) inv_s[r] = 1.0f / sqrtf(sum * a.inv_d + a.eps);
         }
     } else if (threadIdx.x < kMaxRows) {
@@ -576,57 +583,53 @@ __global__ __launch_bounds__(WAVES * 64) void q4_few_kernel(Q4Kernel a) {
 }
 
 // ---- many rows -------------------------------------------------------------------------------
-// The digits are made once, by a kernel of their own, with one exponent per row.  Layout: [row group][block][step][lane] of 16
-// bytes, then the factor of each row.  A workgroup per row group; up to kKeep blocks per wave stay in registers between the
-// search for the largest magnitude and the digits.
-constexpr int kQ4DigitThreads = 1024;
-template <int KEEP>
-__global__ __launch_bounds__(kQ4DigitThreads) void q4_digits_kernel(Q4Kernel a, uint4 *digits, float *factors) {
-    constexpr int WAVES = kQ4DigitThreads / 64, HELD = KEEP > 0 ? KEEP : 1;
-    const int rg = blockIdx.x, lane = threadIdx.x & 63, w = threadIdx.x >> 6, g = lane >> 4, t = lane & 3, c = (lane & 15) >> 2;
-    __shared__ float top[WAVES][kQ4Rows];
-    float m = 0.f, v[HELD][8];
-    auto load = [&](auto kind, int b, float (&x)[8]) __attribute__((always_inline)) { load_x8<kind()>(a, kQ4Rows * rg + c, b < a.KB ? kQ4Block * b + 32 * t + 8 * g : a.K, x); };
+// The digits are made once, by a kernel of their own: a wave per row group and chunk of 4 blocks (more where K is over 16384, so that there are
+// at most 32), whose values of a row share an exponent.  Layout: [row group][block][step][lane] of 16 bytes, then the factors [row group][chunk][row].
+constexpr int kQ4Chunks = 32;
+static int chunk_shift(int KB) {
+    int s = 2;
+    while ((KB + (1 << s) - 1) >> s > kQ4Chunks) ++s;
+    return s;
+}
+template <bool KEEP>                                           // the chunk's values stay in registers between the search for the largest magnitude and the digits
+__global__ __launch_bounds__(64) void q4_digits_kernel(Q4Kernel a, uint4 *digits, float *factors, int shift) {
+    const int chunks = (a.KB + (1 << shift) - 1) >> shift, rg = blockIdx.x / chunks, chunk = blockIdx.x - rg * chunks;
+    const int lane = threadIdx.x, g = lane >> 4, t = lane & 3, c = (lane & 15) >> 2;
+    const int b0 = chunk << shift, n = min(1 << shift, a.KB - b0);
+    float m = 0.f, v[KEEP ? 4 : 1][8];
+    auto load = [&](auto kind, int i, float (&x)[8]) __attribute__((always_inline)) { load_x8<kind()>(a, kQ4Rows * rg + c, i < n ? kQ4Block * (b0 + i) + 32 * t + 8 * g : a.K, x); };
     auto look = [&](const float (&x)[8]) __attribute__((always_inline)) {
 #pragma unroll
         for (int e = 0; e < 8; ++e) m = __builtin_elementwise_maximum(m, fabsf(x[e]));
     };
     with_kind(a, [&](auto kind) __attribute__((always_inline)) {
-        if (KEEP > 0) {
+        if (KEEP) {
 #pragma unroll
-            for (int i = 0; i < KEEP; ++i) load(kind, w + i * WAVES, v[i]);
+            for (int i = 0; i < 4; ++i) load(kind, i, v[KEEP ? i : 0]);
         } else {
-            for (int b = w; b < a.KB; b += WAVES) { load(kind, b, v[0]); look(v[0]); }
+            for (int i = 0; i < n; ++i) { load(kind, i, v[0]); look(v[0]); }
         }
     });
-    if (KEEP > 0) {
+    if (KEEP) {
 #pragma unroll
-        for (int i = 0; i < KEEP; ++i) look(v[i]);
+        for (int i = 0; i < 4; ++i) look(v[KEEP ? i : 0]);
     }
-    m = __builtin_elementwise_maximum(m, lane_xor<1>(m));
-    m = __builtin_elementwise_maximum(m, lane_xor<2>(m));
-    m = __builtin_elementwise_maximum(m, lane_xor<16>(m));
-    m = __builtin_elementwise_maximum(m, lane_xor<32>(m));
-    if (g == 0 && t == 0) top[w][c] = m;
-    __syncthreads();
-#pragma unroll
-    for (int i = 0; i < WAVES; ++i) m = __builtin_elementwise_maximum(m, top[i][c]);
-    const int exponent = max((int)(__float_as_uint(m) >> 23 & 255u), 36);
-    if (w == 0 && g == 0 && t == 0) factors[kQ4Rows * rg + c] = digit_factor(exponent);
-    auto make = [&](int b, const float (&x)[8]) __attribute__((always_inline)) {
+    const int exponent = shared_exponent(m);
+    if (g == 0 && t == 0) factors[(rg * chunks + chunk) * kQ4Rows + c] = digit_factor(exponent);
+    auto make = [&](int i, const float (&x)[8]) __attribute__((always_inline)) {
         uint32_t B[8];
         block_digits(x, exponent, B);
-        if (b >= a.KB) return;
-        uint4 *dst = digits + ((size_t)rg * a.KB + b) * 128 + lane;
+        if (i >= n) return;
+        uint4 *dst = digits + ((size_t)rg * a.KB + b0 + i) * 128 + lane;
         dst[0] = uint4{B[0], B[1], B[2], B[3]};
         dst[64] = uint4{B[4], B[5], B[6], B[7]};
     };
-    if (KEEP > 0) {
+    if (KEEP) {
 #pragma unroll
-        for (int i = 0; i < KEEP; ++i) make(w + i * WAVES, v[i]);
+        for (int i = 0; i < 4; ++i) make(i, v[KEEP ? i : 0]);
     } else {
         with_kind(a, [&](auto kind) __attribute__((always_inline)) {
-            for (int b = w; b < a.KB; b += WAVES) { load(kind, b, v[0]); make(b, v[0]); }
+            for (int i = 0; i < n; ++i) { load(kind, i, v[0]); make(i, v[0]); }
         });
     }
 }
@@ -671,11 +674,12 @@ __device__ __forceinline__ void pair_products(const Q4Words<G> (&words)[2], cons
 // weights come through registers, RD steps ahead.  To fill the chip where a matrix has few tiles the blocks are cut
 // into `slices` across workgroups, whose sums q4_join_kernel adds.  Workgroups begin at different steps of their slice, so
 // that those of an XCD do not all ask for the same digits at once.
-constexpr int kQ4ManyTiles = 8, kQ4Loaders = 4;
+constexpr int kQ4ManyTiles = 8, kQ4Loaders = 4, kQ4MaxSlices = 8;
+constexpr int many_ring(int NG, int G) { return G == 32 && NG >= 8 ? 2 : G == 64 && NG == 16 ? 3 : 4; }     // what registers allow
 constexpr int many_buffers(int NG) { return NG <= 8 ? 4 : NG <= 12 ? 3 : 2; }
 template <int NG, int G>
-__global__ __launch_bounds__((8 + kQ4Loaders) * 64) __attribute__((amdgpu_waves_per_eu(2, 3))) void q4_many_kernel(Q4Kernel a, const uint4 *digits, const float *factors, float *partials, int slices, int ng) {
-    constexpr int RD = G == 32 && NG >= 12 ? 2 : 4, NBUF = many_buffers(NG), PB = 4 * NG / kQ4Loaders;      // pieces of 1 KiB per loader wave and step
+__global__ __launch_bounds__((8 + kQ4Loaders) * 64) __attribute__((amdgpu_waves_per_eu(2, 3))) void q4_many_kernel(Q4Kernel a, const uint4 *digits, const float *factors, float *partials, int slices, int ng, int shift) {
+    constexpr int RD = many_ring(NG, G), NBUF = many_buffers(NG), PB = 4 * NG / kQ4Loaders;      // pieces of 1 KiB per loader wave and step
     static_assert((NBUF - 1) * PB <= 63, "outstanding loads of a loader wave");
     const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), odd = w >> 2, wt = w & 3;
     const int group = blockIdx.x / slices, slice = blockIdx.x - group * slices;
@@ -689,7 +693,13 @@ __global__ __launch_bounds__((8 + kQ4Loaders) * 64) __attribute__((amdgpu_waves_
     };
     extern __shared__ uint4 lds[];                             // [NBUF][even, odd][NG][2][64]
     __shared__ float inv_s[kMaxRows];
-    float sum[2][NG];
+    __shared__ float F[kQ4Chunks][kMaxRows];                   // factors of the digits
+    const int chunks = (a.KB + (1 << shift) - 1) >> shift;
+    for (int e = threadIdx.x; e < chunks * ng * kQ4Rows; e += (8 + kQ4Loaders) * 64) {
+        const int rg = e / (chunks * kQ4Rows), in = e - rg * chunks * kQ4Rows;
+        F[in / kQ4Rows][rg * kQ4Rows + (in & 3)] = factors[e];
+    }
+    float sum[2][NG], total[2][NG];                            // of a chunk, of all
     const int t0 = group * kQ4ManyTiles + 2 * wt;
     if (w >= 8) {
         const int first = w - 8, o = first >> 1;               // two loaders for the even blocks, two for the odd ones
@@ -723,7 +733,7 @@ __global__ __launch_bounds__((8 + kQ4Loaders) * 64) __attribute__((amdgpu_waves_
 #pragma unroll
         for (int i = 0; i < 2; ++i)
 #pragma unroll
-            for (int rg = 0; rg < NG; ++rg) sum[i][rg] = 0.f;
+            for (int rg = 0; rg < NG; ++rg) sum[i][rg] = total[i][rg] = 0.f;
         Q4Words<G> ring[RD][2];
         auto weights = [&](int slot, int s) __attribute__((always_inline)) {
             const int b = b0 + min(position(s, odd), len - 1);
@@ -733,17 +743,34 @@ __global__ __launch_bounds__((8 + kQ4Loaders) * 64) __attribute__((amdgpu_waves_
 #pragma unroll
         for (int s = 0; s < RD; ++s) weights(s, s);
         __syncthreads();
-        int buffer = 0;
+        int buffer = 0, chunk = (b0 + min(position(0, odd), len - 1)) >> shift;
+        auto chunk_done = [&] __attribute__((always_inline)) {
+            const float *f = &F[chunk][lane >> 4];
+#pragma unroll
+            for (int rg = 0; rg < NG; ++rg) {
+                const float factor = f[rg * kQ4Rows];          // (row groups that there are not: never used)
+#pragma unroll
+                for (int i = 0; i < 2; ++i) { total[i][rg] = __builtin_fmaf(sum[i][rg], factor, total[i][rg]); sum[i][rg] = 0.f; }
+            }
+        };
         for (int s0 = 0; s0 < rounds; s0 += RD) {
 #pragma unroll
             for (int h = 0; h < RD; ++h) {
-                if (s0 + h < steps && position(s0 + h, odd) < len) pair_products<NG, G>(ring[h], lds + (buffer * 2 + odd) * NG * 128 + lane, sum);
+                const int p = position(s0 + h, odd);
+                if (s0 + h < steps && p < len) {
+                    if ((b0 + p) >> shift != chunk) {
+                        chunk_done();
+                        chunk = (b0 + p) >> shift;
+                    }
+                    pair_products<NG, G>(ring[h], lds + (buffer * 2 + odd) * NG * 128 + lane, sum);
+                }
                 weights(h, s0 + h + RD);
                 __builtin_amdgcn_sched_barrier(0);             // keep "multiply, refill the freed slots" in program order
                 buffer = buffer + 1 == NBUF ? 0 : buffer + 1;
                 __syncthreads();
             }
         }
+        chunk_done();
     }
     __syncthreads();                                           // the loaders' surplus steps have landed: the buffers are free
     float *red = reinterpret_cast<float *>(lds);               // [even, odd][tile of the group][NG][activation row][16 outputs]
@@ -752,14 +779,14 @@ __global__ __launch_bounds__((8 + kQ4Loaders) * 64) __attribute__((amdgpu_waves_
 #pragma unroll
         for (int i = 0; i < 2; ++i)
 #pragma unroll
-            for (int rg = 0; rg < NG; ++rg) red[odd * HALF + ((2 * wt + i) * NG + rg) * 64 + lane] = sum[i][rg];
+            for (int rg = 0; rg < NG; ++rg) red[odd * HALF + ((2 * wt + i) * NG + rg) * 64 + lane] = total[i][rg];
     }
     row_scales<8 + kQ4Loaders>(a, a.rows, inv_s);
     __syncthreads();
     for (int e = threadIdx.x; e < HALF; e += (8 + kQ4Loaders) * 64) {
         const int n = e & 15, rg = (e >> 6) % NG, row = kQ4Rows * rg + ((e >> 4) & 3), tile = group * kQ4ManyTiles + (e >> 6) / NG;
         const bool active = row < a.rows && tile < a.tiles;
-        const float f = factors[active ? row : 0], s = (red[e] + red[HALF + e]) * f, up = (red[e ^ 8] + red[HALF + (e ^ 8)]) * f;
+        const float s = red[e] + red[HALF + e], up = red[e ^ 8] + red[HALF + (e ^ 8)];
         if (slices > 1) {
             if (active) partials[((size_t)slice * a.rows + row) * ((size_t)a.tiles * 16) + tile * 16 + n] = s;
         } else {
@@ -772,24 +799,23 @@ __global__ __launch_bounds__((8 + kQ4Loaders) * 64) __attribute__((amdgpu_waves_
 __global__ __launch_bounds__(256) void q4_join_kernel(Q4Kernel a, const float *partials, int slices) {
     const int tile = blockIdx.x, n = threadIdx.x & 15, row = blockIdx.y * 16 + (threadIdx.x >> 4);
     __shared__ float inv_s[kMaxRows];
+    const bool active = row < a.rows;
+    const size_t ld = (size_t)a.tiles * 16;
+    float part[kQ4MaxSlices];                                  // all on their way together
+#pragma unroll
+    for (int i = 0; i < kQ4MaxSlices; ++i) part[i] = active && i < slices ? partials[((size_t)i * a.rows + row) * ld + tile * 16 + n] : 0.f;
     a.row0 = blockIdx.y * 16;
     row_scales<4>(a, min(a.rows, a.row0 + 16), inv_s);
     __syncthreads();
-    const bool active = row < a.rows;
-    float s = 0.f, up = 0.f;
-    const size_t ld = (size_t)a.tiles * 16;
-    for (int i = 0; active && i < slices; ++i) {
-        const float *p = partials + ((size_t)i * a.rows + row) * ld + tile * 16;
-        s += p[n];
-        if (a.epilogue == EPI_SWIGLU) up += p[(n + 8) & 15];
-    }
-    finish(a, active, row, tile, n, s, up, inv_s[active ? row : 0]);
+    float s = 0.f;
+#pragma unroll
+    for (int i = 0; i < kQ4MaxSlices; ++i) s += part[i];
+    finish(a, active, row, tile, n, s, lane_xor<8>(s), inv_s[active ? row : 0]);
 }
 
 // Up to how many rows the kernel of few rows goes: as many row groups as a workgroup's registers keep the digits of.  Few / many at G = 128:
 // 16 rows, 768 x 768 6.1 / 9.4 us; 12 rows, 4096 x 4096 12.2 / 16.1, 32000 x 4096 20.9 / 22.5; 12 rows, 4096 x 11008, digits anew, 26 / 24.9.
 static int few_rows(int K) { return K <= 16 * kQ4Block ? 16 : K <= 32 * kQ4Block ? 12 : 8; }
-constexpr int kQ4MaxSlices = 8;
 // Slices of K: what makes rounds of workgroups x blocks of one the least, with about 4 blocks' time for a workgroup's start and end
 static int many_slices(int N, int K) {
     const int groups = ((N + 15) / 16 + kQ4ManyTiles - 1) / kQ4ManyTiles, KB = (K + kQ4Block - 1) / kQ4Block;
@@ -806,16 +832,16 @@ static size_t digit_bytes(int rows, int K) { return (size_t)((rows + 3) / 4) * (
 size_t q4_workspace_bytes(int rows, int N, int K) {
     if (rows <= few_rows(K)) return 0;
     const int slices = many_slices(N, K);
-    return digit_bytes(rows, K) + 1024 + (slices > 1 ? (size_t)slices * rows * ((N + 15) / 16 * 16) * 4 : 0);
+    return digit_bytes(rows, K) + kQ4Chunks * kMaxRows * 4 + (slices > 1 ? (size_t)slices * rows * ((N + 15) / 16 * 16) * 4 : 0);
 }
 
 template <int NG, int G>
-static hipError_t launch_many(const Q4Kernel &k, const uint4 *digits, const float *factors, float *partials, int slices, int ng, hipStream_t stream) {
+static hipError_t launch_many(const Q4Kernel &k, const uint4 *digits, const float *factors, float *partials, int slices, int ng, int shift, hipStream_t stream) {
     constexpr size_t lds = (size_t)many_buffers(NG) * NG * 4096;
     const hipError_t ready = hipFuncSetAttribute((const void *)q4_many_kernel<NG, G>, hipFuncAttributeMaxDynamicSharedMemorySize, lds);
     if (ready != hipSuccess) return ready;
     const int groups = (k.tiles + kQ4ManyTiles - 1) / kQ4ManyTiles;
-    hipLaunchKernelGGL((q4_many_kernel<NG, G>), dim3(groups * slices), dim3((8 + kQ4Loaders) * 64), lds, stream, k, digits, factors, partials, slices, ng);
+    hipLaunchKernelGGL((q4_many_kernel<NG, G>), dim3(groups * slices), dim3((8 + kQ4Loaders) * 64), lds, stream, k, digits, factors, partials, slices, ng, shift);
     return hipGetLastError();
 }
 
@@ -855,16 +881,16 @@ hipError_t launch_q4_gemm(const Q4GemmArgs &a, int epilogue, hipStream_t stream)
         else {
             const int ng = (a.rows + kQ4Rows - 1) / kQ4Rows, slices = many_slices(a.N, a.K);
             uint4 *digits = (uint4 *)a.workspace;
-            float *factors = (float *)((char *)a.workspace + digit_bytes(a.rows, a.K)), *partials = factors + 256;
-            if (k.KB <= 32) hipLaunchKernelGGL(q4_digits_kernel<2>, dim3(ng), dim3(kQ4DigitThreads), 0, stream, k, digits, factors);
-            else if (k.KB <= 96) hipLaunchKernelGGL(q4_digits_kernel<6>, dim3(ng), dim3(kQ4DigitThreads), 0, stream, k, digits, factors);
-            else hipLaunchKernelGGL(q4_digits_kernel<0>, dim3(ng), dim3(kQ4DigitThreads), 0, stream, k, digits, factors);
-            if (ng <= 4) rc = launch_many<4, g()>(k, digits, factors, partials, slices, ng, stream);
-            else if (ng <= 6) rc = launch_many<6, g()>(k, digits, factors, partials, slices, ng, stream);
-            else if (ng <= 8) rc = launch_many<8, g()>(k, digits, factors, partials, slices, ng, stream);
-            else if (ng <= 10) rc = launch_many<10, g()>(k, digits, factors, partials, slices, ng, stream);
-            else if (ng <= 12) rc = launch_many<12, g()>(k, digits, factors, partials, slices, ng, stream);
-            else rc = launch_many<16, g()>(k, digits, factors, partials, slices, ng, stream);
+            float *factors = (float *)((char *)a.workspace + digit_bytes(a.rows, a.K)), *partials = factors + kQ4Chunks * kMaxRows;
+            const int shift = chunk_shift(k.KB), chunks = (k.KB + (1 << shift) - 1) >> shift;
+            if (shift == 2) hipLaunchKernelGGL(q4_digits_kernel<true>, dim3(ng * chunks), dim3(64), 0, stream, k, digits, factors, shift);
+            else hipLaunchKernelGGL(q4_digits_kernel<false>, dim3(ng * chunks), dim3(64), 0, stream, k, digits, factors, shift);
+            if (ng <= 4) rc = launch_many<4, g()>(k, digits, factors, partials, slices, ng, shift, stream);
+            else if (ng <= 6) rc = launch_many<6, g()>(k, digits, factors, partials, slices, ng, shift, stream);
+            else if (ng <= 8) rc = launch_many<8, g()>(k, digits, factors, partials, slices, ng, shift, stream);
+            else if (ng <= 10) rc = launch_many<10, g()>(k, digits, factors, partials, slices, ng, shift, stream);
+            else if (ng <= 12) rc = launch_many<12, g()>(k, digits, factors, partials, slices, ng, shift, stream);
+            else rc = launch_many<16, g()>(k, digits, factors, partials, slices, ng, shift, stream);
             if (rc == hipSuccess && slices > 1) hipLaunchKernelGGL(q4_join_kernel, dim3(k.tiles, (a.rows + 15) / 16), dim3(256), 0, stream, k, partials, slices);
         }
     });
