@@ -675,7 +675,7 @@ __device__ __forceinline__ void pair_products(const Q4Words<G> (&words)[2], cons
 // into `slices` across workgroups, whose sums q4_join_kernel adds.  Workgroups begin at different steps of their slice, so
 // that those of an XCD do not all ask for the same digits at once.
 constexpr int kQ4ManyTiles = 8, kQ4Loaders = 4, kQ4MaxSlices = 8;
-constexpr int many_ring(int NG, int G) { return G == 32 && NG >= 8 ? 2 : G == 64 && NG == 16 ? 3 : 4; }     // what registers allow
+constexpr int many_ring(int NG, int G) { return G == 32 && NG >= 8 ? 2 : NG == 16 ? 3 : 4; }     // what registers allow
 constexpr int many_buffers(int NG) { return NG <= 8 ? 4 : NG <= 12 ? 3 : 2; }
 template <int NG, int G>
 __global__ __launch_bounds__((8 + kQ4Loaders) * 64) __attribute__((amdgpu_waves_per_eu(2, 3))) void q4_many_kernel(Q4Kernel a, const uint4 *digits, const float *factors, float *partials, int slices, int ng, int shift) {
