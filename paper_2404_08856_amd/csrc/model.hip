@@ -270,11 +270,11 @@ enum ProfKind { PK_QKV = 0, PK_O, PK_GATE_UP, PK_DOWN, PK_LM_HEAD, PK_ATTENTION,
 hipError_t project_q4(const spd_model *m, const GemmArgs &g, Epilogue epi, hipStream_t st) {
     Q4GemmArgs a{};
     a.W = g.W; a.N = g.N; a.K = g.K; a.group = m->q4_group; a.rows = g.rows;
-    a.X = g.X; a.x_kind = Q4_X_PACKED;
+    a.X = g.X; a.x_kind = g.x_rows ? Q4_X_F32 : Q4_X_PACKED; a.ldx = g.K;
     a.Y = g.Y; a.ldy = g.ldy;
     a.ssq_in = g.ssq_in; a.ssq_in_parts = g.ssq_in_parts; a.eps = g.eps;
-    a.gain_next = g.gain_next; a.Xnext = g.Xnext; a.ssq_out = g.ssq_out;
-    a.Xout = g.Xout; a.K_out = g.K_out;
+    a.gain_next = g.gain_next; a.Xnext = (float *)g.Xnext; a.ssq_out = g.ssq_out;
+    a.Xout = (float *)g.Xout; a.K_out = g.K_out;
     a.workspace = m->ws + m->L.part;
     return launch_q4_gemm(a, epi, st);
 }
@@ -566,7 +566,7 @@ int32_t run_lm_head(spd_model *m, int rows, float *logits_out, hipStream_t st) {
     GemmArgs g{};
     g.batch_partials = (float *)(m->ws + L.part); g.batch_arrive = (unsigned *)(m->ws + L.arrive); g.batch_zero = m->ws + L.zero;
     g.W = m->packed + L.lm_head; g.X = m->ws + L.xn; g.N = c.vocab; g.K = c.d_model; g.rows = rows; g.Y = logits_out; g.ldy = c.vocab;
-    g.ssq_in = (float *)(m->ws + L.ssq_b); g.ssq_in_parts = c.d_model / 16; g.eps = c.rms_eps;
+    g.ssq_in = (float *)(m->ws + L.ssq_b); g.ssq_in_parts = c.d_model / 16; g.eps = c.rms_eps; g.x_rows = true;
     PROF_GEMM(PK_LM_HEAD, g, EPI_STORE, m->t_lm);
     return SPD_OK;
 }
@@ -644,7 +644,7 @@ int32_t run_layers(spd_model *m, int first, AttnArgs &at, int seq0, int n_seqs, 
             PROF_KERNEL(PK_QKV, launch_qkv_attention(qa, st));
         } else {
             g.W = m->packed + L.wqkv[l]; g.X = xn; g.N = at.row_cached && !m->q4_group ? HD : 3 * HD; g.K = d; g.rows = rows; g.Y = qkv; g.ldy = 3 * HD;
-            g.ssq_in = ssq_b; g.ssq_in_parts = l == first ? 1 : d_tiles; g.eps = c.rms_eps;
+            g.ssq_in = ssq_b; g.ssq_in_parts = l == first ? 1 : d_tiles; g.eps = c.rms_eps; g.x_rows = l != first;
             PROF_GEMM(PK_QKV, g, EPI_STORE, m->t_qkv);
             WeightPrefetch pf{};
             if (prefetch) {
@@ -667,12 +667,12 @@ int32_t run_layers(spd_model *m, int first, AttnArgs &at, int seq0, int n_seqs, 
         g = GemmArgs{};
         g.batch_partials = (float *)(m->ws + L.part); g.batch_arrive = (unsigned *)(m->ws + L.arrive); g.batch_zero = m->ws + L.zero; g.fold = kv_cached;
         g.W = m->packed + L.wgu[l]; g.X = xn; g.N = 2 * F; g.K = d; g.rows = rows; g.Xout = xf; g.K_out = F;
-        g.ssq_in = ssq_a; g.ssq_in_parts = d_tiles; g.eps = c.rms_eps;
+        g.ssq_in = ssq_a; g.ssq_in_parts = d_tiles; g.eps = c.rms_eps; g.x_rows = true;
         PROF_GEMM(PK_GATE_UP, g, EPI_SWIGLU, m->t_gu);
         g = GemmArgs{};
         g.batch_partials = (float *)(m->ws + L.part); g.batch_arrive = (unsigned *)(m->ws + L.arrive); g.batch_zero = m->ws + L.zero; g.fold = kv_cached;
         g.W = m->packed + L.wdown[l]; g.X = xf; g.N = d; g.K = F; g.rows = rows; g.Y = h; g.ldy = d;
-        g.gain_next = gain_of(l + 1 < c.n_layers ? L.attn_norm[l + 1] : L.final_norm); g.Xnext = xn; g.ssq_out = ssq_b;
+        g.gain_next = gain_of(l + 1 < c.n_layers ? L.attn_norm[l + 1] : L.final_norm); g.Xnext = xn; g.ssq_out = ssq_b; g.x_rows = true;
         PROF_GEMM(PK_DOWN, g, EPI_RESIDUAL, m->t_down);
     }
     return logits_out ? run_lm_head(m, rows, logits_out, st) : SPD_OK;

@@ -279,10 +279,10 @@ struct Q4Kernel {
     int ssq_in_parts;
     float inv_d, eps;
     const float *gain_next;
-    uint16_t *Xnext;
+    float *Xnext;
     float *ssq_out;
-    uint16_t *Xout;
-    int KS_out, epilogue;
+    float *Xout;
+    int K_out, epilogue;
 };
 
 // Values k0 .. k0 + 7 (k0 % 8 == 0) of an activation row, zeros beyond the matrix
@@ -427,10 +427,7 @@ __device__ __forceinline__ void finish(const Q4Kernel &a, bool active, int row, 
     if (a.epilogue == EPI_SWIGLU) {
         if (!active || n >= 8) return;
         const float gate = sum * inv;
-        uint16_t t3[kTerms];
-        split3(gate / (1.0f + expf(-gate)) * (up * inv), t3);
-#pragma unroll
-        for (int q = 0; q < kTerms; ++q) a.Xout[xpack_index(row, t * 8 + n, a.KS_out, q)] = t3[q];
+        a.Xout[(size_t)row * a.K_out + t * 8 + n] = gate / (1.0f + expf(-gate)) * (up * inv);
     } else if (a.epilogue == EPI_STORE) {
         if (active && col < a.N) a.Y[(size_t)row * a.ldy + col] = sum * inv;
     } else {
@@ -438,12 +435,7 @@ __device__ __forceinline__ void finish(const Q4Kernel &a, bool active, int row, 
         if (active) {
             hnew = a.Y[(size_t)row * a.ldy + col] + sum;
             a.Y[(size_t)row * a.ldy + col] = hnew;
-            if (a.gain_next) {
-                uint16_t t3[kTerms];
-                split3(hnew * a.gain_next[col], t3);
-#pragma unroll
-                for (int q = 0; q < kTerms; ++q) a.Xnext[xpack_index(row, col, a.tiles / 2, q)] = t3[q];
-            }
+            if (a.gain_next) a.Xnext[(size_t)row * a.N + col] = hnew * a.gain_next[col];
         }
         const float sq = row_sum(hnew * hnew);
         if (a.ssq_out && n == 0 && active) a.ssq_out[(size_t)row * a.tiles + t] = sq;
@@ -868,8 +860,8 @@ hipError_t launch_q4_gemm(const Q4GemmArgs &a, int epilogue, hipStream_t stream)
     k.X = a.X; k.x_kind = a.x_kind; k.ldx = a.ldx; k.KS = (a.K + 31) / 32; k.rows = a.rows;
     k.Y = a.Y; k.ldy = a.ldy;
     k.ssq_in = a.ssq_in; k.ssq_in_parts = a.ssq_in_parts; k.inv_d = 1.0f / (float)a.K; k.eps = a.eps;
-    k.gain_next = a.gain_next; k.Xnext = (uint16_t *)a.Xnext; k.ssq_out = a.ssq_out;
-    k.Xout = (uint16_t *)a.Xout; k.KS_out = (a.K_out + 31) / 32; k.epilogue = epilogue;
+    k.gain_next = a.gain_next; k.Xnext = a.Xnext; k.ssq_out = a.ssq_out;
+    k.Xout = a.Xout; k.K_out = a.K_out; k.epilogue = epilogue;
     hipError_t rc = hipSuccess;
     const hipError_t launched = with_group(a.group, [&](auto g) {
         if (a.rows == 1) launch_few<0, true, g()>(k, stream);
