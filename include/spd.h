@@ -55,6 +55,8 @@ extern "C" {
 
 #define SPD_MAX_TOP          32    /* alternatives per row of spd_token_logprobs      */
 #define SPD_MAX_LOGPROB_VOCAB (1 << 24)  /* entries per row of spd_token_logprobs       */
+#define SPD_MAX_LOGPROB_ROWS  (1 << 22)  /* its rows, times vocab / 32768 rounded up    */
+#define SPD_Q4_MAX_K          (1 << 24)  /* in_features of a matrix in 4 bits; out_features times in_features / 512 rounded up: 2^26 at most */
 
 /* flags of spd_speculative_accept */
 #define SPD_TARGET_IS_PROBS  1u    /* target rows are probabilities, not logits   */
@@ -298,7 +300,7 @@ int32_t spd_speculative_accept_static(const float *target, const float *draft, c
  * Entries at -infinity (probability 0) weigh nothing and are no alternatives: places they leave hold token -1 and -infinity.  A
  * row of nothing else: log probability -infinity, entropy 0.  A token outside 0..vocab-1: -infinity, rank vocab.  A row with a NaN or
  * +infinity (probabilities: a negative or infinite one or a NaN) has no distribution: NaN, rank and alternatives -1.
- * Errors: SPD_ERR_INVALID_ARG, SPD_ERR_SHAPE (vocab > SPD_MAX_LOGPROB_VOCAB), SPD_ERR_CAPACITY (workspace too small). */
+ * Errors: SPD_ERR_INVALID_ARG, SPD_ERR_SHAPE (vocab > SPD_MAX_LOGPROB_VOCAB, too many rows), SPD_ERR_CAPACITY (workspace too small). */
 int32_t spd_logprobs_workspace_bytes(int32_t n_rows, int32_t vocab, int32_t n_top, size_t *h_bytes);
 int32_t spd_token_logprobs(const float *rows, size_t row_stride, const int32_t *tokens, int32_t n_rows, int32_t vocab,
                            float temperature, uint32_t flags, float *logprob_out, float *entropy_out, int32_t *rank_out,
@@ -311,7 +313,7 @@ int32_t spd_token_logprobs(const float *rows, size_t row_stride, const int32_t *
  * w: float32, or bfloat16 with SPD_W_IS_BF16, [N, K] with w_stride elements between rows.
  * spd_q4_dequantize: the values that q and scales stand for (rounded once if bfloat16).
  * spd_q4_pack: re-tiles a matrix for the matrix cores into `packed` (spd_q4_bytes bytes, 256-byte aligned), which spd_q4_matmul reads.
- * Errors: SPD_ERR_INVALID_ARG, SPD_ERR_SHAPE (N or K < 1, another group), SPD_ERR_CAPACITY. */
+ * Errors: SPD_ERR_INVALID_ARG, SPD_ERR_SHAPE (N or K < 1, another group, too large), SPD_ERR_CAPACITY. */
 int32_t spd_q4_bytes(int32_t N, int32_t K, int32_t group, size_t *h_packed_bytes);
 int32_t spd_q4_quantize(const void *w, size_t w_stride, uint32_t flags, int32_t N, int32_t K, int32_t group,
                         void *q_out, void *scales_out, void *stream);

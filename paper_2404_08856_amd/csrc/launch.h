@@ -255,6 +255,7 @@ struct LogprobArgs {
     float *top_logprobs;
     void *workspace;                 // logprobs_workspace_bytes
 };
+int logprob_slices(int vocab);       // workgroups per row
 size_t logprobs_workspace_bytes(int n_rows, int vocab, int n_top);
 hipError_t launch_logprobs(const LogprobArgs &a, hipStream_t stream);
 

@@ -331,7 +331,7 @@ __global__ __launch_bounds__(kMergeThreads) void logprobs_merge_kernel(LogprobAr
 }
 
 constexpr int kSliceEntries = 32768;      // what a workgroup of 1024 holds in registers
-static int logprob_slices(int vocab) { return (int)(((long)vocab + kSliceEntries - 1) / kSliceEntries); }
+int logprob_slices(int vocab) { return (int)(((long)vocab + kSliceEntries - 1) / kSliceEntries); }
 
 size_t logprobs_workspace_bytes(int n_rows, int vocab, int n_top) {
     const size_t slices = logprob_slices(vocab);

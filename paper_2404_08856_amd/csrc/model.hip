@@ -1030,7 +1030,8 @@ namespace {
 int32_t check_q4(const char *what, int32_t N, int32_t K, int32_t group) {
     if (N < 1 || K < 1) return fail(SPD_ERR_SHAPE, "%s: N = %d and K = %d must be positive", what, N, K);
     if (!q4_group_ok(group)) return fail(SPD_ERR_SHAPE, "%s: group %d must be 32, 64 or 128", what, group);
-    if ((int64_t)((N + 15ll) / 16) * ((K + 127ll) / 128) > (int64_t)1 << 31) return fail(SPD_ERR_SHAPE, "%s: %d x %d is more than 2^42 weights", what, N, K);
+    // (a launch has fewer than 2^32 threads: a wave per 512 weights of a row; and the digits of a row group are reached by 32-bit offsets)
+    if (K > SPD_Q4_MAX_K || (int64_t)N * ((K + 511) / 512) > (int64_t)1 << 26) return fail(SPD_ERR_SHAPE, "%s: %d x %d is too large", what, N, K);
     return SPD_OK;
 }
 constexpr uint32_t kTypeFlags = SPD_W_IS_BF16;
@@ -1121,6 +1122,7 @@ int32_t spd_token_logprobs(const float *rows, size_t row_stride, const int32_t *
     if (n_rows < 1 || vocab < 1) return fail(SPD_ERR_INVALID_ARG, "n_rows, vocab >= 1 required");
     if (vocab > SPD_MAX_LOGPROB_VOCAB) return fail(SPD_ERR_SHAPE, "vocab %d exceeds %d", vocab, SPD_MAX_LOGPROB_VOCAB);
     if (n_top < 0 || n_top > SPD_MAX_TOP) return fail(SPD_ERR_INVALID_ARG, "n_top = %d must be in 0..%d", n_top, SPD_MAX_TOP);
+    if (n_rows > SPD_MAX_LOGPROB_ROWS / logprob_slices(vocab)) return fail(SPD_ERR_SHAPE, "n_rows = %d is too many for vocab = %d", n_rows, vocab);
     if (row_stride < (size_t)vocab) return fail(SPD_ERR_INVALID_ARG, "row_stride must cover a row");
     if (flags & ~SPD_ROWS_ARE_PROBS) return fail(SPD_ERR_INVALID_ARG, "unknown flag bits");
     const bool probs = flags & SPD_ROWS_ARE_PROBS;

@@ -37,13 +37,14 @@ def test_null_pointers(at):
     expect(bad, "spd_logprobs_workspace_bytes", i32(1), i32(16), i32(0), null)
 
 
-@pytest.mark.parametrize("N,K,group", [(0, 64, 32), (16, 0, 32), (-1, 64, 32), (16, 64, 16), (16, 64, 0), (16, 64, 256), (16, 64, -32)])
+@pytest.mark.parametrize("N,K,group", [(0, 64, 32), (16, 0, 32), (-1, 64, 32), (16, 64, 16), (16, 64, 0), (16, 64, 256), (16, 64, -32),
+                                       (1, 2**24 + 1, 32), (2**26 + 1, 64, 128), (2**25 + 1, 1024, 64), (2**31 - 1, 2**31 - 1, 32)])
 def test_shapes(N, K, group):
     spd, _ = lib()
     n = ctypes.c_size_t()
     bad = spd.SPD_ERR_SHAPE
     expect(bad, "spd_q4_bytes", i32(N), i32(K), i32(group), ctypes.byref(n))
-    expect(bad, "spd_q4_quantize", some, sz(64), u32(0), i32(N), i32(K), i32(group), some, some, null)
+    expect(bad, "spd_q4_quantize", some, sz(max(K, 64)), u32(0), i32(N), i32(K), i32(group), some, some, null)
     expect(bad, "spd_q4_dequantize", some, some, i32(N), i32(K), i32(group), some, sz(64), u32(0), null)
     expect(bad, "spd_q4_pack", some, some, i32(N), i32(K), i32(group), some, sz(1 << 30), null)
     expect(bad, "spd_q4_matmul", some, i32(N), i32(K), i32(group), some, sz(64), u32(0), i32(1), some, sz(16), some, sz(1 << 30), null)
@@ -102,6 +103,9 @@ def test_log_probability_arguments():
     for t in (0.0, -1.0, float("nan"), float("inf"), 1e-45):
         lp(bad, temperature=t)
     lp(bad, ws=odd)
+    lp(spd.SPD_ERR_SHAPE, vocab=2**24 + 1, stride=2**25)
+    lp(spd.SPD_ERR_SHAPE, n=2**22 + 1)
+    lp(spd.SPD_ERR_SHAPE, n=2**21 + 1, vocab=32769, stride=32769)
     n = ctypes.c_size_t()
     for rows, vocab, top in ((0, 10, 1), (1, 0, 1), (1, 10, -1), (1, 10, 33)):
         expect(bad, "spd_logprobs_workspace_bytes", i32(rows), i32(vocab), i32(top), ctypes.byref(n))
