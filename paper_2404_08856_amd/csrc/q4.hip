@@ -676,7 +676,7 @@ __global__ __launch_bounds__((8 + kQ4Loaders) * 64) __attribute__((amdgpu_waves_
     const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), odd = w >> 2, wt = w & 3;
     const int group = blockIdx.x / slices, slice = blockIdx.x - group * slices;
     const int b0 = (int)((long)a.KB * slice / slices), len = (int)((long)a.KB * (slice + 1) / slices) - b0;
-    const int steps = (len + 1) / 2, rounds = (steps + RD - 1) / RD * RD;         // steps beyond the slice load what is never used
+    const int steps = (len + 1) / 2;                           // (those beyond load what is never used)
     const int rot = (int)(((long)(blockIdx.x >> 3) * steps) / ((gridDim.x + 7) >> 3));
     // position (in blocks of the slice) of step s's even or odd block; at or beyond len: there is none
     auto position = [&](int s, int o) __attribute__((always_inline)) {
@@ -715,7 +715,7 @@ __global__ __launch_bounds__((8 + kQ4Loaders) * 64) __attribute__((amdgpu_waves_
         for (int s = 0; s < NBUF - 1; ++s) issue(s);
         asm volatile("s_waitcnt vmcnt(%0)" ::"n"((NBUF - 2) * PB) : "memory");   // step 0 has landed (loads complete in order)
         __builtin_amdgcn_s_barrier();
-        for (int s = 0; s < rounds; ++s) {
+        for (int s = 0; s < steps; ++s) {
             issue(s + NBUF - 1);                               // into the buffer that the products left one step ago
             asm volatile("s_waitcnt vmcnt(%0)" ::"n"((NBUF - 2) * PB) : "memory");   // step s + 1 has landed
             __builtin_amdgcn_s_barrier();
@@ -745,11 +745,12 @@ __global__ __launch_bounds__((8 + kQ4Loaders) * 64) __attribute__((amdgpu_waves_
                 for (int i = 0; i < 2; ++i) { total[i][rg] = __builtin_fmaf(sum[i][rg], factor, total[i][rg]); sum[i][rg] = 0.f; }
             }
         };
-        for (int s0 = 0; s0 < rounds; s0 += RD) {
+        for (int s0 = 0; s0 < steps; s0 += RD) {
 #pragma unroll
             for (int h = 0; h < RD; ++h) {
+                if (s0 + h >= steps) break;
                 const int p = position(s0 + h, odd);
-                if (s0 + h < steps && p < len) {
+                if (p < len) {
                     if ((b0 + p) >> shift != chunk) {
                         chunk_done();
                         chunk = (b0 + p) >> shift;
