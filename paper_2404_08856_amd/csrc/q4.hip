@@ -664,8 +664,8 @@ __device__ __forceinline__ void pair_products(const Q4Words<G> (&words)[2], cons
 // 8 multiplying waves, 4 pairs of tiles x even and odd blocks, and 4 loader waves that bring the digits of two blocks after
 // the other into LDS (LDS-direct loads, NBUF - 1 steps ahead), where a multiplying wave uses what it reads for both of its tiles.  The
 // weights come through registers, RD steps ahead.  To fill the chip where a matrix has few tiles the blocks are cut
-// into `slices` across workgroups, whose sums q4_join_kernel adds.  Workgroups begin at different steps of their slice, so
-// that those of an XCD do not all ask for the same digits at once.
+// into `slices` across workgroups, whose sums q4_join_kernel adds.  (Workgroups that
+// begin at different steps of their slice, as the batched projections in bf16 do, are 1 to 2 % slower here, and weights loaded non-temporally 4 %.)
 constexpr int kQ4ManyTiles = 8, kQ4Loaders = 4, kQ4MaxSlices = 8;
 constexpr int many_ring(int NG, int G) { return G == 32 && NG >= 8 ? 2 : NG == 16 ? 3 : 4; }     // what registers allow
 constexpr int many_buffers(int NG) { return NG <= 8 ? 4 : NG <= 12 ? 3 : 2; }
@@ -677,12 +677,8 @@ __global__ __launch_bounds__((8 + kQ4Loaders) * 64) __attribute__((amdgpu_waves_
     const int group = blockIdx.x / slices, slice = blockIdx.x - group * slices;
     const int b0 = (int)((long)a.KB * slice / slices), len = (int)((long)a.KB * (slice + 1) / slices) - b0;
     const int steps = (len + 1) / 2;                           // (those beyond load what is never used)
-    const int rot = (int)(((long)(blockIdx.x >> 3) * steps) / ((gridDim.x + 7) >> 3));
     // position (in blocks of the slice) of step s's even or odd block; at or beyond len: there is none
-    auto position = [&](int s, int o) __attribute__((always_inline)) {
-        const int p = s + rot;
-        return 2 * (p < steps ? p : p - steps < steps ? p - steps : 0) + o;
-    };
+    auto position = [&](int s, int o) __attribute__((always_inline)) { return 2 * s + o; };
     extern __shared__ uint4 lds[];                             // [NBUF][even, odd][NG][2][64]
     __shared__ float inv_s[kMaxRows];
     __shared__ float F[kQ4Chunks][kMaxRows];                   // factors of the digits
@@ -730,7 +726,7 @@ __global__ __launch_bounds__((8 + kQ4Loaders) * 64) __attribute__((amdgpu_waves_
         auto weights = [&](int slot, int s) __attribute__((always_inline)) {
             const int b = b0 + min(position(s, odd), len - 1);
 #pragma unroll
-            for (int i = 0; i < 2; ++i) ring[slot][i].template load<true>(a, (size_t)min(t0 + i, a.tiles - 1) * a.KB + b, lane);     // (beyond the matrix: a valid tile, dropped)
+            for (int i = 0; i < 2; ++i) ring[slot][i].template load<false>(a, (size_t)min(t0 + i, a.tiles - 1) * a.KB + b, lane);     // (beyond the matrix: a valid tile, dropped)
         };
 #pragma unroll
         for (int s = 0; s < RD; ++s) weights(s, s);
