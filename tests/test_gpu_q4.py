@@ -216,3 +216,22 @@ def test_calls_on_two_streams_and_a_captured_call():
             spd.spd_q4_matmul(m, static, eager, ws)
             torch.cuda.synchronize()
             assert torch.equal(eager, y)
+
+
+@pytest.mark.parametrize("bf16", [False, True])
+def test_quantizer_next_to_ties(bf16):
+    """Quotients at and next to every half: n + 1/2 times the scale, exactly, one step of float32 below and above, for scales of all magnitudes."""
+    spd = spd_mod()
+    rng = np.random.default_rng(3)
+    rows = []
+    for e in list(range(-140, 120, 13)) + [-126, -127, -133]:
+        s = to_bf16([np.ldexp(1 + rng.integers(0, 128) / 128, e)])[0]
+        half = (np.arange(-7, 7) + 0.5).astype(np.float32) * s
+        w = np.concatenate([[7 * s], half, np.nextafter(half, np.float32(np.inf)), np.nextafter(half, np.float32(-np.inf)), np.zeros(64)])[:64]
+        rows.append(w.astype(np.float32))
+    w = np.stack(rows)
+    w = to_bf16(w) if bf16 else w
+    q, s = torch.empty((len(w), 32), dtype=torch.uint8, device="cuda"), torch.empty((len(w), 1), dtype=torch.bfloat16, device="cuda")
+    spd.spd_q4_quantize(torch.from_numpy(w).to(torch.bfloat16 if bf16 else torch.float32).cuda(), 64, q, s)
+    want_q, want_s = quantize_ref(w, 64)
+    assert np.array_equal(s.float().cpu().numpy(), want_s) and np.array_equal(q.cpu().numpy(), pack_nibbles(want_q))
