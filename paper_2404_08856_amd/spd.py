@@ -131,8 +131,8 @@ def _check(rc):
 
 # Pointers go to ctypes as plain integers, and the stream without a Python object around it: an accept call of one sequence was 12 us of this
 # and one launch, more than its kernel takes.
-_current_device = torch.cuda.current_device
-_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda device: torch.cuda.current_stream(device).cuda_stream)     # (no name that torch promises)
+_current_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device              # (no names that torch promises)
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda device: torch.cuda.current_stream(device).cuda_stream)
 
 
 def _stream():
@@ -154,13 +154,16 @@ def _raw(t, dtype):
     return t.data_ptr()
 
 
-# The calls below take 5 us of device time at the least; what is checked here is read from each tensor once.
-def _matrix(t, device, dtypes):
-    """Data pointer and row stride of a matrix on the current device whose rows are contiguous (a view into a wider buffer is fine)."""
-    (n, k), (stride, step) = t.shape, t.stride()
-    assert t.get_device() == device and t.dtype in dtypes, f"expected {dtypes} on device {device}, got {t.dtype} on {t.device}"
+# The smaller of the calls below take 3 to 8 us of device time: what is checked here is read from each tensor once.
+_F32, _BF16, _I32, _U8 = torch.float32, torch.bfloat16, torch.int32, torch.uint8
+
+
+def _matrix(t, device):
+    """Data pointer, row stride and whether bfloat16, of a float32 or bfloat16 matrix on the current device with contiguous rows (a view into a wider buffer is fine)."""
+    (n, k), (stride, step), dtype = t.shape, t.stride(), t.dtype
+    assert t.get_device() == device and (dtype == _F32 or dtype == _BF16), f"expected float32 or bfloat16 on device {device}, got {dtype} on {t.device}"
     assert (step == 1 or k <= 1) and (stride >= k or n <= 1), f"contiguous rows that do not overlap only, got strides {t.stride()}"
-    return t.data_ptr(), stride if n > 1 else k
+    return t.data_ptr(), stride if n > 1 else k, 1 if dtype == _BF16 else 0
 
 
 def _own(t, device, dtype, shape):
@@ -174,9 +177,8 @@ def _own(t, device, dtype, shape):
 
 def _scratch(workspace, device):
     """Data pointer and bytes of a workspace: contiguous uint8 on the current device."""
-    n = workspace.numel()
-    assert workspace.dtype == torch.uint8 and workspace.get_device() == device and workspace.is_contiguous(), "a workspace is uint8 on the current device"
-    return workspace.data_ptr(), n
+    assert workspace.dtype == _U8 and workspace.get_device() == device and workspace.is_contiguous(), "a workspace is uint8 on the current device"
+    return workspace.data_ptr(), workspace.numel()
 
 
 def make_config(shape, max_seqs, max_positions):
@@ -394,9 +396,6 @@ def spd_speculative_accept_static(target, draft, draft_tokens, u, temperature, f
                                               _ptr(next_token_out, torch.int32), _ptr(accept_prob_out, torch.float32), _stream()))
 
 
-_F32, _F32_BF16 = (torch.float32,), (torch.float32, torch.bfloat16)
-
-
 def spd_logprobs_workspace_bytes(n_rows, vocab, n_top):
     b = ctypes.c_size_t()
     _check(_lib.spd_logprobs_workspace_bytes(n_rows, vocab, n_top, ctypes.byref(b)))
@@ -408,14 +407,15 @@ def spd_token_logprobs(rows, tokens, temperature, flags, logprob_out=None, entro
     """rows [n, vocab] (a view into a wider buffer is fine); the number of alternatives is that of top_tokens_out's columns."""
     n, vocab = rows.shape
     here = _current_device()
-    ptr, stride = _matrix(rows, here, _F32)
+    ptr, stride, bf16 = _matrix(rows, here)
+    assert not bf16, "rows are float32"
     n_top = 0 if top_tokens_out is None else top_tokens_out.shape[1]
     if workspace is None:
         workspace = torch.empty(spd_logprobs_workspace_bytes(n, vocab, n_top), dtype=torch.uint8, device=rows.device)
-    one, top, f32, i32 = (n,), (n, n_top), torch.float32, torch.int32
-    _check(_lib.spd_token_logprobs(ptr, stride, _own(tokens, here, i32, one), n, vocab, temperature, flags, _own(logprob_out, here, f32, one),
-                                   _own(entropy_out, here, f32, one), _own(rank_out, here, i32, one), n_top, _own(top_tokens_out, here, i32, top),
-                                   _own(top_logprobs_out, here, f32, top), *_scratch(workspace, here), _raw_stream(here)))
+    one, top = (n,), (n, n_top)
+    _check(_lib.spd_token_logprobs(ptr, stride, _own(tokens, here, _I32, one), n, vocab, temperature, flags, _own(logprob_out, here, _F32, one),
+                                   _own(entropy_out, here, _F32, one), _own(rank_out, here, _I32, one), n_top, _own(top_tokens_out, here, _I32, top),
+                                   _own(top_logprobs_out, here, _F32, top), *_scratch(workspace, here), _raw_stream(here)))
 
 
 def spd_q4_bytes(n, k, group):
@@ -427,17 +427,17 @@ def spd_q4_bytes(n, k, group):
 def spd_q4_quantize(w, group, q_out, scales_out):
     n, k = w.shape
     here = _current_device()
-    ptr, stride = _matrix(w, here, _F32_BF16)
-    _check(_lib.spd_q4_quantize(ptr, stride, SPD_W_IS_BF16 if w.dtype == torch.bfloat16 else 0, n, k, group, _own(q_out, here, torch.uint8, (n, (k + 1) // 2)),
+    ptr, stride, bf16 = _matrix(w, here)
+    _check(_lib.spd_q4_quantize(ptr, stride, SPD_W_IS_BF16 * bf16, n, k, group, _own(q_out, here, torch.uint8, (n, (k + 1) // 2)),
                                 _own(scales_out, here, torch.bfloat16, (n, (k + group - 1) // group)), _raw_stream(here)))
 
 
 def spd_q4_dequantize(q, scales, group, w_out):
     n, k = w_out.shape
     here = _current_device()
-    ptr, stride = _matrix(w_out, here, _F32_BF16)
+    ptr, stride, bf16 = _matrix(w_out, here)
     _check(_lib.spd_q4_dequantize(_own(q, here, torch.uint8, (n, (k + 1) // 2)), _own(scales, here, torch.bfloat16, (n, (k + group - 1) // group)), n, k, group,
-                                  ptr, stride, SPD_W_IS_BF16 if w_out.dtype == torch.bfloat16 else 0, _raw_stream(here)))
+                                  ptr, stride, SPD_W_IS_BF16 * bf16, _raw_stream(here)))
 
 
 class Q4Matrix:
@@ -465,9 +465,11 @@ def spd_q4_matmul(matrix, x, y, workspace=None):
     if workspace is None:
         workspace = torch.empty(spd_q4_matmul_workspace_bytes(rows, matrix.n, k), dtype=torch.uint8, device=x.device)
     packed = matrix.packed
-    assert packed.get_device() == here, "the matrix is on another device than the current one"
-    _check(_lib.spd_q4_matmul(packed.data_ptr(), matrix.n, k, matrix.group, *_matrix(x, here, _F32_BF16), SPD_X_IS_BF16 if x.dtype == torch.bfloat16 else 0, rows,
-                              *_matrix(y, here, _F32), *_scratch(workspace, here), _raw_stream(here)))
+    xp, xs, bf16 = _matrix(x, here)
+    yp, ys, y_bf16 = _matrix(y, here)
+    wp, wn = _scratch(workspace, here)
+    assert packed.get_device() == here and not y_bf16, "the matrix is on the current device and y is float32"
+    _check(_lib.spd_q4_matmul(packed.data_ptr(), matrix.n, k, matrix.group, xp, xs, SPD_X_IS_BF16 * bf16, rows, yp, ys, wp, wn, _raw_stream(here)))
 
 
 def spd_probe_read_chain(buffer, stage_bytes, reps=20):
