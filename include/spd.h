@@ -55,8 +55,8 @@ extern "C" {
 
 #define SPD_MAX_TOP          32    /* alternatives per row of spd_token_logprobs      */
 #define SPD_MAX_LOGPROB_VOCAB (1 << 24)  /* entries per row of spd_token_logprobs       */
-#define SPD_MAX_LOGPROB_ROWS  (1 << 22)  /* its rows, times vocab / 32768 rounded up    */
-#define SPD_Q4_MAX_K          (1 << 24)  /* in_features of a matrix in 4 bits; out_features times in_features / 512 rounded up: 2^26 at most */
+#define SPD_MAX_LOGPROB_ROWS  ((1 << 22) - 1)  /* its rows, times vocab / 32768 rounded up    */
+#define SPD_Q4_MAX_K          (1 << 24)  /* in_features of a matrix in 4 bits; out_features times in_features / 512 rounded up: 2^26 - 4 at most */
 
 /* flags of spd_speculative_accept */
 #define SPD_TARGET_IS_PROBS  1u    /* target rows are probabilities, not logits   */

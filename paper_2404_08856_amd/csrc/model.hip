@@ -1031,7 +1031,7 @@ int32_t check_q4(const char *what, int32_t N, int32_t K, int32_t group) {
     if (N < 1 || K < 1) return fail(SPD_ERR_SHAPE, "%s: N = %d and K = %d must be positive", what, N, K);
     if (!q4_group_ok(group)) return fail(SPD_ERR_SHAPE, "%s: group %d must be 32, 64 or 128", what, group);
     // (a launch has fewer than 2^32 threads: a wave per 512 weights of a row; and the digits of a row group are reached by 32-bit offsets)
-    if (K > SPD_Q4_MAX_K || (int64_t)N * ((K + 511) / 512) > (int64_t)1 << 26) return fail(SPD_ERR_SHAPE, "%s: %d x %d is too large", what, N, K);
+    if (K > SPD_Q4_MAX_K || (int64_t)N * ((K + 511) / 512) > ((int64_t)1 << 26) - 4) return fail(SPD_ERR_SHAPE, "%s: %d x %d is too large", what, N, K);
     return SPD_OK;
 }
 constexpr uint32_t kTypeFlags = SPD_W_IS_BF16;

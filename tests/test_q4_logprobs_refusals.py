@@ -114,6 +114,42 @@ def test_log_probability_arguments():
         lp(spd.SPD_ERR_CAPACITY, n=1, vocab=1 << 20, stride=1 << 20, ws=null)
 
 
+@pytest.mark.parametrize("n,vocab", [(2**22, 5000), (2**22, 32768), (2**21, 32769)])
+def test_log_probabilities_of_as_many_rows_as_a_launch_has_no_threads_for(n, vocab):
+    spd, _ = lib()                                         # 2^22 workgroups of 1024: 2^32 threads
+    expect(spd.SPD_ERR_SHAPE, "spd_token_logprobs", some, sz(vocab), some, i32(n), i32(vocab), f32(1.0), u32(0), some, null, null, i32(0), null, null, some, sz(1 << 40), null)
+
+
+@pytest.mark.parametrize("N,K", [(2**26, 64), (2**26 - 3, 512), (2**11, 2**24)])
+def test_matrices_that_a_launch_has_no_threads_for(N, K):
+    spd, _ = lib()                                         # 2^24 workgroups of 256: 2^32 threads
+    n = ctypes.c_size_t()
+    expect(spd.SPD_ERR_SHAPE, "spd_q4_bytes", i32(N), i32(K), i32(128), ctypes.byref(n))
+    expect(spd.SPD_ERR_SHAPE, "spd_q4_quantize", some, sz(K), u32(0), i32(N), i32(K), i32(128), some, some, null)
+
+
+def test_what_the_binding_refuses():
+    torch = pytest.importorskip("torch")
+    spd, _ = lib()
+    host = -1                                              # the device number of a tensor in host memory
+    good = torch.zeros((4, 8))
+    assert spd._matrix(good, host) == (good.data_ptr(), 8, 0)
+    assert spd._matrix(good[:, 2:7].to(torch.bfloat16), host)[1:] == (5, 1)
+    assert spd._matrix(good[:, 2:7], host)[1] == 8 and spd._matrix(good[2:3, ::8], host)[1] == 1
+    for bad in (good.double(), good.t(), good[:, ::2], good[0:1].expand(4, 8)):
+        with pytest.raises(AssertionError):
+            spd._matrix(bad, host)
+    with pytest.raises(AssertionError):
+        spd._matrix(good, 0)
+    assert spd._own(None, host, torch.float32, (4, 8)) is None and spd._own(good, host, torch.float32, (4, 8)) == good.data_ptr()
+    for t, d, dtype, shape in ((good, 0, torch.float32, (4, 8)), (good, host, torch.int32, (4, 8)), (good, host, torch.float32, (8, 4)), (good[:, :4], host, torch.float32, (4, 4))):
+        with pytest.raises(AssertionError):
+            spd._own(t, d, dtype, shape)
+    for t, d in ((good, host), (good.to(torch.uint8), 0), (good.to(torch.uint8)[:, :4], host)):
+        with pytest.raises(AssertionError):
+            spd._scratch(t, d)
+
+
 def test_model_bytes_in_4_bits():
     from paper_2404_08856_amd import spd, synth
     s = synth.SHAPES["llama7b"]
