@@ -291,7 +291,7 @@ int32_t spd_speculative_accept_static(const float *target, const float *draft, c
  *   rows    float32 [n_rows, vocab], row_stride elements apart: logits, or probabilities
  *   tokens  int32 [n_rows]; NULL if neither logprob_out nor rank_out is wanted
  *   logprob_out       float32 [n_rows] or NULL: lp(x) = z_x - log(sum exp z) of z = logits / temperature, or log(row[x])
- *   entropy_out       float32 [n_rows] or NULL: -sum p lp, in nats
+ *   entropy_out       float32 [n_rows] or NULL: -sum p lp, in nats (given probabilities below 2^-126 count as 0 here)
  *   rank_out          int32 [n_rows] or NULL: entries before the token in descending order, equal ones by index (0: the first)
  *   top_tokens_out    int32, top_logprobs_out float32 [n_rows, n_top]: the first n_top entries in that order (0 <= n_top <= SPD_MAX_TOP)
  *   workspace         scratch of spd_logprobs_workspace_bytes bytes (which may be 0; then it may be NULL), 16-byte aligned; it may hold

@@ -142,7 +142,7 @@ __global__ __launch_bounds__(THREADS, 8) void logprobs_kernel(LogprobArgs a, int
             const float e4[4] = {v[i].x, v[i].y, v[i].z, v[i].w};
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
-                if (PROBS) dot += e4[j] > 0.f ? e4[j] * __log2f(e4[j]) : 0.f;
+                if (PROBS) dot += e4[j] >= 0x1p-126f ? e4[j] * __log2f(e4[j]) : 0.f;      // (of less the instruction takes no logarithm; they would add less than 2^-119)
                 else {
                     const float d = exponent2(e4[j], p.mx, scale2), e = __builtin_amdgcn_exp2f(d);
                     sum += e;

@@ -164,6 +164,17 @@ def test_probabilities_that_are_none():
     check(p, [1, 2, 3, 4], 1.0, True, 3)
 
 
+@pytest.mark.parametrize("V", [12, 32000, 40000])
+def test_probabilities_below_the_normal_range(V):
+    rng = np.random.default_rng(V)
+    p = np.full((3, V), 1.0 / V, dtype=np.float32)
+    p[0, 5], p[0, 7] = 1e-45, 1e-39
+    p[1] = np.exp2(-rng.integers(100, 148, V).astype(np.float64))
+    p[2] = 0
+    p[2, [1, 4]] = 1e-41, 1.0
+    check(p, [5, 3, 1], 1.0, True, 4)
+
+
 def test_optional_outputs_and_many_rows():
     spd = spd_mod()
     x, t = logits(300, 1111, 3)
