@@ -350,9 +350,10 @@ __device__ __forceinline__ int block_exponent(const float (&v)[8]) {
     for (int e = 0; e < 8; ++e) m = __builtin_elementwise_maximum(m, fabsf(v[e]));        // NaN stays
     return shared_exponent(m);
 }
-// what a sum of 16 q * v is worth
+// what a sum of 16 q * v is worth, times 2^UP
+template <int UP = 0>
 __device__ __forceinline__ float digit_factor(int exponent) {
-    return exponent == 255 ? __uint_as_float(0x7fc00000u) : __uint_as_float((unsigned)(exponent - 33) << 23);
+    return exponent == 255 ? __uint_as_float(0x7fc00000u) : __uint_as_float((unsigned)(exponent - 33 + UP) << 23);
 }
 __device__ __forceinline__ void block_digits(const float (&v)[8], int exponent, uint32_t (&B)[8]) {
     const float up = __uint_as_float((unsigned)(283 - exponent) << 23);       // 2^(30 - E): |v| stays below 2^30
@@ -593,7 +594,9 @@ __global__ __launch_bounds__(WAVES * 64) void q4_few_kernel(Q4Kernel a) {
 // ---- many rows -------------------------------------------------------------------------------
 // The digits are made once, by a kernel of their own: a wave per row group and chunk of 4 blocks (more where K is over 16384, so that there are
 // at most 32), whose values of a row share an exponent.  Layout: [row group][block][step][lane] of 16 bytes, then the factors [row group][chunk][row].
-constexpr int kQ4Chunks = 32;
+// (A sum of 16 q * v of a chunk times the scales is taken before the factors are: up to 2^45 times the largest scale, so
+// the scales go in as 2^-20 of themselves.)
+constexpr int kQ4Chunks = 32, kQ4ChunkUp = 20;
 static int chunk_shift(int KB) {
     int s = 2;
     while ((KB + (1 << s) - 1) >> s > kQ4Chunks) ++s;
@@ -623,7 +626,7 @@ __global__ __launch_bounds__(64) void q4_digits_kernel(Q4Kernel a, uint4 *digits
         for (int i = 0; i < 4; ++i) look(v[KEEP ? i : 0]);
     }
     const int exponent = shared_exponent(m);
-    if (g == 0 && t == 0) factors[(rg * chunks + chunk) * kQ4Rows + c] = digit_factor(exponent);
+    if (g == 0 && t == 0) factors[(rg * chunks + chunk) * kQ4Rows + c] = digit_factor<kQ4ChunkUp>(exponent);
     auto make = [&](int i, const float (&x)[8]) __attribute__((always_inline)) {
         uint32_t B[8];
         block_digits(x, exponent, B);
@@ -657,7 +660,7 @@ __device__ __forceinline__ void pair_products(const Q4Words<G> (&words)[2], cons
     for (int i = 0; i < 2; ++i) {
         x[i][0] = words[i].operand(0); x[i][1] = words[i].operand(1);
 #pragma unroll
-        for (int p = 0; p < per; ++p) sc[i][p] = words[i].scale(p);
+        for (int p = 0; p < per; ++p) sc[i][p] = words[i].scale(p) * (1.0f / (1 << kQ4ChunkUp));
     }
 #pragma unroll
     for (int rg = 0; rg < NG + 1; ++rg) {

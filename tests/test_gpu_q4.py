@@ -130,6 +130,20 @@ def test_product_of_integers_is_exact(rows, N, K, G, bf16):
         assert torch.isnan(y._base[:, N:]).all()
 
 
+@pytest.mark.parametrize("rows,N,K,G", [(1, 33, 1000, 32), (6, 40, 4500, 128), (20, 64, 3000, 64), (40, 528, 4096, 128), (64, 31, 17000, 32)])
+@pytest.mark.parametrize("power", [-88, 88])
+def test_scales_far_from_one(rows, N, K, G, power):
+    """As above times a power of two that every result bears (2^22 * 2^88; 2^-2 * 2^-88): as exact."""
+    spd = spd_mod()
+    rng = np.random.default_rng(rows + K)
+    x = rng.integers(-15, 16, (rows, K)).astype(np.float64)
+    q = rng.integers(-8, 8, (N, K))
+    scales = np.exp2(rng.integers(-2, 2, (N, (K + G - 1) // G)) + power).astype(np.float32)
+    y = torch.empty((rows, N), device="cuda")
+    spd.spd_q4_matmul(device_matrix(q, scales, G), torch.from_numpy(x.astype(np.float32)).cuda(), y)
+    assert np.array_equal(y.double().cpu().numpy(), x @ values(q, scales, G).T)
+
+
 @pytest.mark.parametrize("rows,N,K,G", SHAPES + LONG[::5])
 @pytest.mark.parametrize("kind", ["normal", "one-sided", "outliers", "tiny", "huge"])
 def test_product_within_its_roundings(rows, N, K, G, kind):
