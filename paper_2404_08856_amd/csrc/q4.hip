@@ -728,7 +728,7 @@ __global__ __launch_bounds__((8 + kQ4Loaders) * 64) __attribute__((amdgpu_waves_
         };
 #pragma unroll
         for (int s = 0; s < NBUF - 1; ++s) issue(s);
-        asm volatile("s_waitcnt vmcnt(%0)" ::"n"((NBUF - 2) * PB) : "memory");   // step 0 has landed (loads complete in order)
+        asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"((NBUF - 2) * PB) : "memory");   // step 0 has landed (loads complete in order), and what this wave wrote to F
         __builtin_amdgcn_s_barrier();
         for (int s = 0; s < steps; ++s) {
             issue(s + NBUF - 1);                               // into the buffer that the products left one step ago
