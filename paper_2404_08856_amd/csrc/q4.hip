@@ -646,15 +646,16 @@ __global__ __launch_bounds__(64) void q4_digits_kernel(Q4Kernel a, uint4 *digits
 }
 
 // sum[i][rg] += a block of tile i of a pair times the digits of NG row groups at src (LDS).  Written out in the order in which it should be
-// issued: digits are asked for two row groups ahead, and while the matrix core has a row group the sums of the one before are added.
+// issued: digits are asked for two row groups ahead, and while the matrix core has a row group the sums of the one before are added (LAG; not
+// where four sums a row group in two sets take too many registers: 64 rows x 32000 x 4096 at G = 32 102 us with spills, 73 without).
 template <int NG, int G>
 __device__ __forceinline__ void pair_products(const Q4Words<G> (&words)[2], const uint4 *src, float (&sum)[2][NG]) {
-    constexpr int per = kQ4Block / G, AHEAD = 2;
+    constexpr int per = kQ4Block / G, AHEAD = 2, LAG = G == 32 && NG >= 12 ? 0 : 1;
     uint4 B[AHEAD + 1][2];
     auto ask = [&](int rg) __attribute__((always_inline)) { B[rg % (AHEAD + 1)][0] = src[rg * 128]; B[rg % (AHEAD + 1)][1] = src[rg * 128 + 64]; };
 #pragma unroll
     for (int rg = 0; rg < (AHEAD < NG ? AHEAD : NG); ++rg) ask(rg);
-    i32x4_t x[2][2], acc[2][2][per];
+    i32x4_t x[2][2], acc[1 + LAG][2][per];
     float sc[2][per];
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
@@ -663,18 +664,19 @@ __device__ __forceinline__ void pair_products(const Q4Words<G> (&words)[2], cons
         for (int p = 0; p < per; ++p) sc[i][p] = words[i].scale(p) * (1.0f / (1 << kQ4ChunkUp));
     }
 #pragma unroll
-    for (int rg = 0; rg < NG + 1; ++rg) {
+    for (int rg = 0; rg < NG + LAG; ++rg) {
         if (rg + AHEAD < NG) ask(rg + AHEAD);
         if (rg < NG) {
             const i32x4_t d[2] = {__builtin_bit_cast(i32x4_t, B[rg % (AHEAD + 1)][0]), __builtin_bit_cast(i32x4_t, B[rg % (AHEAD + 1)][1])};
 #pragma unroll
-            for (int i = 0; i < 2; ++i) group_sums<G>(d, x[i], acc[rg & 1][i]);
+            for (int i = 0; i < 2; ++i) group_sums<G>(d, x[i], acc[rg & LAG][i]);
         }
-        if (rg > 0) {
+        if (rg >= LAG) {
+            const int done = rg - LAG;
 #pragma unroll
             for (int i = 0; i < 2; ++i)
 #pragma unroll
-                for (int p = 0; p < per; ++p) sum[i][rg - 1] = __builtin_fmaf(join_digits(acc[(rg - 1) & 1][i][p]), sc[i][p], sum[i][rg - 1]);
+                for (int p = 0; p < per; ++p) sum[i][done] = __builtin_fmaf(join_digits(acc[done & LAG][i][p]), sc[i][p], sum[i][done]);
         }
         __builtin_amdgcn_sched_barrier(0);
     }
