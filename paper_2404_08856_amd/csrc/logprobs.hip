@@ -348,13 +348,16 @@ static void launch_rows(const LogprobArgs &a, int slices, int slice_quads, hipSt
     else hipLaunchKernelGGL((logprobs_kernel<THREADS, NV, false, false>), grid, block, 0, stream, a, slices, slice_quads);
 }
 
+// Threads per row: the fewest that hold it in at most 8 quads each, and not fewer than are worth a row's own latency.  Alternatives
+// (us for 1, 320, 2048 rows): 1000 entries with 4 quads 4.4, 5.4, 8.8 instead of 3.9, 4.5, 7.0; 4096 in 1024 threads 4.3, 6.2, 18.6 instead of
+// 4.4, 5.5, 10.8; 8192 in 256 x 8 5.4, 6.8, 15.9 and in 1024 4.6, 6.8, 21.7 instead of 4.6, 6.3, 16.1; 16384 in 1024 5.4, 10.0, 32.6 instead of 5.4, 9.8, 27.6.
 hipError_t launch_logprobs(const LogprobArgs &a, hipStream_t stream) {
     const int slices = logprob_slices(a.vocab), n4 = (a.vocab - 1) / 4 + 1;
     const int per = (n4 + slices - 1) / slices;
     if (per <= 256) launch_rows<256, 1>(a, slices, per, stream);
     else if (per <= 1024) launch_rows<256, 4>(a, slices, per, stream);
-    else if (per <= 2048) launch_rows<1024, 2>(a, slices, per, stream);
-    else if (per <= 4096) launch_rows<1024, 4>(a, slices, per, stream);
+    else if (per <= 2048) launch_rows<512, 4>(a, slices, per, stream);
+    else if (per <= 4096) launch_rows<512, 8>(a, slices, per, stream);
     else launch_rows<1024, 8>(a, slices, per, stream);
     if (slices > 1) hipLaunchKernelGGL(logprobs_merge_kernel, dim3(a.n_rows), dim3(kMergeThreads), 0, stream, a, slices);
     return hipGetLastError();

@@ -490,6 +490,9 @@ __device__ __forceinline__ void row_scales(const Q4Kernel &a, int last, float *i
 template <int WAVES, int FULL, bool SINGLE, int G, int NB, bool KEEP>
 __global__ __launch_bounds__(WAVES * 64) void q4_few_kernel(Q4Kernel a) {
     constexpr int NG = FULL + SINGLE, per = kQ4Block / G, GROUPS = FULL > 0 ? FULL : 1;
+    // Whether the words behind the last tile's are left unread, or (a loop without that branch) the last tile's are read twice.  Branch / read twice:
+    // one row, 12288 x 8192 10.1 / 11.3 us; 5 rows, the same 14.7 / 15.4, 22016 x 4096 12.6 / 12.4; 12 rows, 22016 x 4096 18.4 / 17.8.  (5 rows at G = 32: 118 registers would go to memory.)
+    constexpr bool STOP = FULL == 0 || (FULL == 1 && NB == 4 && G == 128);
     static_assert(NB <= kQ4Rows, "places of the single row's blocks");
     const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int g = lane >> 4, t = lane & 3, c = (lane & 15) >> 2;
@@ -557,11 +560,12 @@ __global__ __launch_bounds__(WAVES * 64) void q4_few_kernel(Q4Kernel a) {
 #pragma unroll
         for (int rg = 0; rg < NG; ++rg) sum[rg] = 0.f;
         if (KEEP) {
-            const int next = tile + (int)gridDim.x < a.tiles ? tile + (int)gridDim.x : tile;      // (a harmless second read in the end)
+            const bool more = tile + (int)gridDim.x < a.tiles;
+            const int next = more ? tile + (int)gridDim.x : tile;
 #pragma unroll
             for (int i = 0; i < NB; ++i) {
                 multiply(i);
-                load_words(next, w * NB + i, words[i]);
+                if (!STOP || more) load_words(next, w * NB + i, words[i]);
                 __builtin_amdgcn_sched_barrier(0);            // keep "use, replace" in program order
             }
         } else {
@@ -855,17 +859,21 @@ static hipError_t launch_many(const Q4Kernel &k, const uint4 *digits, const floa
     return hipGetLastError();
 }
 
+// Workgroups: one per CU, two where they are small (K of at most 8 blocks), each with as many tiles as that leaves it, so that digits are made
+// once a CU (twice as many: 5 rows, 8192 x 2048 7.1 us, now 6.0; 16384 x 1024 7.3, now 6.3; one row, 16384 x 2048 5.9, now 6.1).  Blocks of K per wave: 1 up to 8 (4 rows, 768 x 768
+// 3.1 us, with two 3.3), 2 up to 32 (16 waves of 2 and 8 of 4, 12288 x 4096: one row 7.2 / 7.0, 4 rows 8.4 / 9.7, 5 rows 9.3 / 14.4), 4 beyond.  Digits that stay
+// pay where a workgroup has a second tile (5 rows, 12288 x 8192 15.3 us, made anew 26.0; 4096 x 8192, one tile each, 10.6 and 9.8).
 template <int FULL, bool SINGLE, int G>
 static void launch_few(const Q4Kernel &k, hipStream_t stream) {
     const int KB = k.KB;
     if constexpr (FULL > 2) {                                  // (K of at most 32 blocks, 16 for four groups: see few_rows)
         if (FULL == 4 || KB <= 16) hipLaunchKernelGGL((q4_few_kernel<8, FULL, SINGLE, G, 2, true>), dim3(std::min(k.tiles, 256)), dim3(512), 0, stream, k);
         else if constexpr (FULL == 3) hipLaunchKernelGGL((q4_few_kernel<8, FULL, SINGLE, G, 4, true>), dim3(std::min(k.tiles, 256)), dim3(512), 0, stream, k);
-    } else if (KB <= 8) hipLaunchKernelGGL((q4_few_kernel<8, FULL, SINGLE, G, 1, true>), dim3(std::min(k.tiles, 1024)), dim3(512), 0, stream, k);
-    else if (KB <= 16) hipLaunchKernelGGL((q4_few_kernel<8, FULL, SINGLE, G, 2, true>), dim3(std::min(k.tiles, 512)), dim3(512), 0, stream, k);
+    } else if (KB <= 8) hipLaunchKernelGGL((q4_few_kernel<8, FULL, SINGLE, G, 1, true>), dim3(std::min(k.tiles, 512)), dim3(512), 0, stream, k);
+    else if (KB <= 16) hipLaunchKernelGGL((q4_few_kernel<8, FULL, SINGLE, G, 2, true>), dim3(std::min(k.tiles, 256)), dim3(512), 0, stream, k);
     else if (KB <= 32) hipLaunchKernelGGL((q4_few_kernel<16, FULL, SINGLE, G, 2, true>), dim3(std::min(k.tiles, 256)), dim3(1024), 0, stream, k);
     else if constexpr (FULL == 2) hipLaunchKernelGGL((q4_few_kernel<16, FULL, SINGLE, G, 2, false>), dim3(std::min(k.tiles, 256)), dim3(1024), 0, stream, k);   // (registers)
-    else if (KB <= 64) hipLaunchKernelGGL((q4_few_kernel<16, FULL, SINGLE, G, 4, true>), dim3(std::min(k.tiles, 256)), dim3(1024), 0, stream, k);
+    else if (KB <= 64 && k.tiles > 256) hipLaunchKernelGGL((q4_few_kernel<16, FULL, SINGLE, G, 4, true>), dim3(std::min(k.tiles, 256)), dim3(1024), 0, stream, k);
     else hipLaunchKernelGGL((q4_few_kernel<16, FULL, SINGLE, G, 4, false>), dim3(std::min(k.tiles, 256)), dim3(1024), 0, stream, k);
 }
 
