@@ -827,9 +827,16 @@ __global__ __launch_bounds__(256) void q4_join_kernel(Q4Kernel a, const float *p
     finish(a, active, row, tile, n, s, lane_xor<8>(s), inv_s[active ? row : 0]);
 }
 
-// Up to how many rows the kernel of few rows goes: as many row groups as a workgroup's registers keep the digits of.  Few / many at G = 128:
-// 16 rows, 768 x 768 6.1 / 9.4 us; 12 rows, 4096 x 4096 12.2 / 16.1, 32000 x 4096 20.9 / 22.5; 12 rows, 4096 x 11008, digits anew, 26 / 24.9.
-static int few_rows(int K) { return K <= 16 * kQ4Block ? 16 : K <= 32 * kQ4Block ? 12 : 8; }
+// Up to how many rows the kernel of few rows goes: as many row groups as a workgroup's registers keep the digits of, or, made anew for each of a
+// workgroup's tiles, as many as pay.  Few / many at G = 128, us: 16 rows, 768 x 768 6.1 / 9.4; 12 rows, 4096 x 4096 12.2 / 16.1, 32000 x 4096 20.9 / 22.5;
+// one tile each: 8 rows, 4096 x 8192 13.3 / 14.5, 4096 x 11008 15.7 / 15.7, 4096 x 16384 21.4 / 16.8, 4 rows there 15.1 / 16.8;
+// more tiles: 8 rows, 12288 x 8192 33.9 / 23.9, 5 rows there 14.7 / 23.8; 4 rows, 8192 x 11008 19.9 / 19.0, 2 rows 17.0 / 18.8, 32000 x 11008 60.8 / 45.0 (one row 39.0 / 45).
+static int few_rows(int N, int K) {
+    const int KB = (K + kQ4Block - 1) / kQ4Block, rounds = ((N + 15) / 16 + 255) / 256;
+    if (KB <= 32) return KB <= 16 ? 16 : 12;
+    if (rounds == 1) return KB <= 96 ? 8 : 4;
+    return KB <= 64 ? 5 : rounds == 2 ? 3 : 1;
+}
 // Slices of K: what makes rounds of workgroups x blocks of one the least, with about 4 blocks' time for a workgroup's start and end
 static int many_slices(int N, int K) {
     const int groups = ((N + 15) / 16 + kQ4ManyTiles - 1) / kQ4ManyTiles, KB = (K + kQ4Block - 1) / kQ4Block;
@@ -844,7 +851,7 @@ static int many_slices(int N, int K) {
 static size_t digit_bytes(int rows, int K) { return (size_t)((rows + 3) / 4) * ((K + kQ4Block - 1) / kQ4Block) * 2048; }
 
 size_t q4_workspace_bytes(int rows, int N, int K) {
-    if (rows <= few_rows(K)) return 0;
+    if (rows <= few_rows(N, K)) return 0;
     const int slices = many_slices(N, K);
     return digit_bytes(rows, K) + kQ4Chunks * kMaxRows * 4 + (slices > 1 ? (size_t)slices * rows * ((N + 15) / 16 * 16) * 4 : 0);
 }
@@ -890,13 +897,9 @@ hipError_t launch_q4_gemm(const Q4GemmArgs &a, int epilogue, hipStream_t stream)
     k.Xout = a.Xout; k.K_out = a.K_out; k.epilogue = epilogue;
     hipError_t rc = hipSuccess;
     const hipError_t launched = with_group(a.group, [&](auto g) {
+        const int few = few_rows(a.N, a.K);
         if (a.rows == 1) launch_few<0, true, g()>(k, stream);
-        else if (a.rows <= kQ4Rows) launch_few<1, false, g()>(k, stream);
-        else if (a.rows == kQ4Rows + 1) launch_few<1, true, g()>(k, stream);
-        else if (a.rows <= 2 * kQ4Rows) launch_few<2, false, g()>(k, stream);
-        else if (a.rows <= few_rows(a.K) && a.rows <= 3 * kQ4Rows) launch_few<3, false, g()>(k, stream);
-        else if (a.rows <= few_rows(a.K)) launch_few<4, false, g()>(k, stream);
-        else {
+        else if (a.rows > few) {
             const int ng = (a.rows + kQ4Rows - 1) / kQ4Rows, slices = many_slices(a.N, a.K);
             uint4 *digits = (uint4 *)a.workspace;
             float *factors = (float *)((char *)a.workspace + digit_bytes(a.rows, a.K)), *partials = factors + kQ4Chunks * kMaxRows;
@@ -910,7 +913,11 @@ hipError_t launch_q4_gemm(const Q4GemmArgs &a, int epilogue, hipStream_t stream)
             else if (ng <= 12) rc = launch_many<12, g()>(k, digits, factors, partials, slices, ng, shift, stream);
             else rc = launch_many<16, g()>(k, digits, factors, partials, slices, ng, shift, stream);
             if (rc == hipSuccess && slices > 1) hipLaunchKernelGGL(q4_join_kernel, dim3(k.tiles, (a.rows + 15) / 16), dim3(256), 0, stream, k, partials, slices);
-        }
+        } else if (a.rows <= kQ4Rows) launch_few<1, false, g()>(k, stream);
+        else if (a.rows == kQ4Rows + 1) launch_few<1, true, g()>(k, stream);
+        else if (a.rows <= 2 * kQ4Rows) launch_few<2, false, g()>(k, stream);
+        else if (a.rows <= 3 * kQ4Rows) launch_few<3, false, g()>(k, stream);
+        else launch_few<4, false, g()>(k, stream);
     });
     return rc != hipSuccess ? rc : launched;
 }

@@ -107,7 +107,10 @@ SHAPES = [(1, 16, 32, 32), (1, 1, 1, 32), (2, 17, 127, 64), (3, 40, 128, 128), (
 LONG = [(rows, N, K, G) for rows in (1, 3, 5, 7, 11, 14) for N, K, G in ((48, 900, 128), (48, 2000, 64), (4128, 1150, 32), (33, 4100, 128), (64, 5555, 32), (17, 8200, 64), (31, 11008, 128), (16, 17000, 64))]
 
 
-@pytest.mark.parametrize("rows,N,K,G", SHAPES + LONG)
+WIDE = [(7, 4112, 4200, 64), (8, 4112, 4300, 128), (4, 4112, 8300, 128), (2, 8208, 8200, 32), (5, 300, 12400, 64)]     # few rows of matrices that are large both ways
+
+
+@pytest.mark.parametrize("rows,N,K,G", SHAPES + LONG + WIDE)
 @pytest.mark.parametrize("bf16", [False, True])
 def test_product_of_integers_is_exact(rows, N, K, G, bf16):
     """Integers up to 60 (15 where K is over 4096) and scales that are powers of two up to 2: every sum is a multiple of 1/4 below 2^22
