@@ -214,12 +214,12 @@ __global__ __launch_bounds__(256) void q4_pack_kernel(Q4PackArgs a) {
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
             const int k0 = kQ4Block * b + 32 * j + 8 * g;
-#pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                const int k = k0 + e;
-                const uint32_t v = k < a.K ? (src[k >> 1] >> (4 * (k & 1))) & 15u : 0u;
-                w[j] |= v << (8 * (e & 3) + (e < 4 ? 4 : 0));
-            }
+            uint32_t v = 0;                                    // 8 columns as they lie
+            if (k0 + 8 <= a.K) v = reinterpret_cast<const ByteQuad *>(src + k0 / 2)->v;
+            else
+                for (int k = k0; k < a.K; ++k) v |= (uint32_t)(src[k >> 1] >> (4 * (k & 1)) & 15) << (4 * (k - k0));
+            auto spread = [](uint32_t x) { x = (x | x << 8) & 0x00ff00ffu; return (x | x << 4) & 0x0f0f0f0fu; };     // nibble i of 4 to byte i
+            w[j] = spread(v & 0xffffu) << 4 | spread(v >> 16);
         }
     }
     a.blocks[id * 64 + lane] = uint4{w[0], w[1], w[2], w[3]};
