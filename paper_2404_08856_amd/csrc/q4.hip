@@ -3,7 +3,7 @@
 //
 //   W[n][k] = scale[n][k / G] * q[n][k],   q in -8 .. 7,   scale bfloat16,   G = 32, 64 or 128
 //
-// The product is made of integers.  The values of an activation row in a block of 128 columns share the exponent E of their
+// The product is made of integers.  The values of an activation row in a block of 128 columns (many rows: a chunk of blocks) share the exponent E of their
 // largest magnitude: x = v * 2^(E - 30) with a 31-bit integer v (what is cut off is below 2^-30 of the largest one or 2^-24 of x itself, float32's own
 // rounding), and v is four signed base-256 digits.  Four rows x four digits are the 16
 // rows of v_mfma_i32_16x16x64_i8; a nibble in the upper half of a byte is 16 q as an 8-bit integer, so the weights need
@@ -12,6 +12,8 @@
 // activation row and one output: two shift-and-adds, two conversions and a fused multiply-add make their float32 value (rounded three times), another
 // one with scale * 2^(E - 34) adds it to the output's float32 sum.
 // A row with a value that is not finite gives NaN; a block whose largest magnitude is below 2^-90 keeps less than 31 bits.
+// (One product in bfloat16 takes the matrix core as long as one here, and float32's accuracy takes three terms of each activation there,
+// four digits here; but there each weight has to be made from its nibble, here a mask does.)
 #include <algorithm>
 
 #include "launch.h"
@@ -58,9 +60,9 @@ __device__ __forceinline__ void load8(const uint16_t *row, size_t k0, int K, flo
     }
 }
 
-// A wave per 512 columns of a row, 8 per lane; a group is 4, 8 or 16 neighbouring lanes.  Bound by memory.  With its inverse behind it, 4096 x 4096 bf16
-// 26.5 us (118 MB), 11003 x 4099 float32 83.6 (408 MB: 4.9 TB/s); loads that are not non-temporal 28.4 and 86.1, a quotient per weight 1.3 more and 0.6, two
-// and four units per wave 29.2 / 87.4 and 33.4 / 90.2, non-temporal stores in the inverse 33.1 / 106.7.
+// A wave per 512 columns of a row, 8 per lane; a group is 4, 8 or 16 neighbouring lanes.  Bound by memory: 4096 x 4096 bf16 12.7 us (42 MB, 3.3 TB/s).  With its inverse
+// behind it 26.5 (118 MB) and 11003 x 4099 float32 83.6 (408 MB: 4.9 TB/s; on another card 74.7); loads that are not non-temporal 28.4 and 86.1, a quotient per
+// weight 1.3 more and 0.6, two and four units per wave 29.2 / 87.4 and 33.4 / 90.2, non-temporal stores in the inverse 33.1 / 106.7.
 template <class T, int G>
 __global__ __launch_bounds__(256) void q4_quantize_kernel(const T *__restrict__ W, size_t ldw, int N, int K, uint8_t *__restrict__ q, uint16_t *__restrict__ scales) {
     const int per_row = (K + 511) / 512, lane = threadIdx.x & 63;
@@ -101,7 +103,7 @@ __global__ __launch_bounds__(256) void q4_quantize_kernel(const T *__restrict__ 
         for (size_t e = 0; k0 / 2 + e < row_bytes; ++e) dst[e] = (uint8_t)(bytes >> (8 * e));
 }
 
-// 8 columns per thread
+// 8 columns per thread.  Bound by memory: 4096 x 4096 to bf16 10.6 us (42 MB, 4.0 TB/s), to float32 15.5 (76 MB, 4.9 TB/s)
 template <class T, int G>
 __global__ __launch_bounds__(256) void q4_dequantize_kernel(const uint8_t *__restrict__ q, const uint16_t *__restrict__ scales, int N, int K, T *__restrict__ W, size_t ldw) {
     const int per_row = (K + 511) / 512, lane = threadIdx.x & 63;
@@ -175,7 +177,7 @@ hipError_t launch_q4_dequantize(const void *q, const void *scales, int N, int K,
 // 16 bytes: word j < 4 has columns 128 b + 32 j + 8 g + e (e < 4) in the upper halves of its bytes and + 4 + e in the lower
 // ones.  Two masks make of words 2 s, 2 s + 1 the operand of matrix-core step s (64 columns, in an order that the activations follow).
 // Behind the blocks the scales, [t][b][16 rows][128 / G].
-// Rows and columns beyond the matrix are zero.
+// Rows and columns beyond the matrix are zero.  A wave writes a block; a lane reads 4 times 4 bytes of its row (4096 x 4096: 8.3 us, 17 MB; once a model).
 size_t q4_scales_offset(int N, int K) { return ((size_t)((N + 15) / 16) * ((K + kQ4Block - 1) / kQ4Block) * 1024 + 255) / 256 * 256; }
 size_t q4_packed_bytes(int N, int K, int G) {
     return (q4_scales_offset(N, K) + (size_t)((N + 15) / 16) * ((K + kQ4Block - 1) / kQ4Block) * (4096 / G) + 255) / 256 * 256;
@@ -244,7 +246,8 @@ hipError_t launch_q4_pack(const void *const (&q)[3], const void *const (&scales)
     return hipGetLastError();
 }
 
-// For prompts: a wave per block of 128 columns writes its four blocks of 32 in bf16 and their rows' factors.
+// For prompts: a wave per block of 128 columns writes its four blocks of 32 in bf16 and their rows' factors.  Bound by memory: 22016 x 4096 40.4 us (237 MB, 5.9 TB/s),
+// 8 % of the time of a 640-row prompt in all.  (The same in the prompt kernel would be made anew for every 64 rows.)
 template <int G>
 __global__ __launch_bounds__(256) void q4_unpack_kernel(const uint4 *__restrict__ W, const uint16_t *__restrict__ S, int KB, int KS, int tile0, size_t blocks,
                                                         uint4 *__restrict__ out, float *__restrict__ wscale) {
@@ -487,6 +490,8 @@ __device__ __forceinline__ void row_scales(const Q4Kernel &a, int last, float *i
 // Rows: FULL groups of up to 4 and (SINGLE) one row more.  A row group's digits take as long to make for one row as for four, so the single
 // row's are made for NB blocks at once, in the places of the group's other rows: the matrix core then multiplies a block's weights by the digits
 // of all NB blocks, and of the sums only the lanes of the right block's place are added.
+// Bound by the stream of weights, and where that is short by a workgroup's chain: first loads, digits, products, sums through LDS.  G = 128: 22016 x 4096 one
+// row 10.4 us (46.9 MB, 4.5 TB/s), 5 rows 12.1, 8 rows 13.5, 12 rows 18; 4096 x 4096 one row 4.9 (4.1 where the weights are in the caches); 768 x 768 3.0, of which an empty kernel is most.
 template <int WAVES, int FULL, bool SINGLE, int G, int NB, bool KEEP>
 __global__ __launch_bounds__(WAVES * 64) void q4_few_kernel(Q4Kernel a) {
     constexpr int NG = FULL + SINGLE, per = kQ4Block / G, GROUPS = FULL > 0 ? FULL : 1;
@@ -597,7 +602,8 @@ __global__ __launch_bounds__(WAVES * 64) void q4_few_kernel(Q4Kernel a) {
 
 // ---- many rows -------------------------------------------------------------------------------
 // The digits are made once, by a kernel of their own: a wave per row group and chunk of 4 blocks (more where K is over 16384, so that there are
-// at most 32), whose values of a row share an exponent.  Layout: [row group][block][step][lane] of 16 bytes, then the factors [row group][chunk][row].
+// at most 32), whose values of a row share an exponent.  40 x 4096 4.6 us, a kernel's start and one round trip (an exponent per block of 128, as the
+// kernel of few rows has, took a multiplication per sum more in the product).  Layout: [row group][block][step][lane] of 16 bytes, then the factors [row group][chunk][row].
 // (A sum of 16 q * v of a chunk times the scales is taken before the factors are: up to 2^45 times the largest scale, so
 // the scales go in as 2^-20 of themselves.)
 constexpr int kQ4Chunks = 32, kQ4ChunkUp = 20;
@@ -691,6 +697,8 @@ __device__ __forceinline__ void pair_products(const Q4Words<G> (&words)[2], cons
 // weights come through registers, RD steps ahead.  To fill the chip where a matrix has few tiles the blocks are cut
 // into `slices` across workgroups, whose sums q4_join_kernel adds.  (Workgroups that
 // begin at different steps of their slice, as the batched projections in bf16 do, are 1 to 2 % slower here, and weights loaded non-temporally 4 %.)
+// 40 rows x 32000 x 4096 at G = 128 29.6 us (72 MB, 2.4 TB/s), 64 rows x 11003 x 4099 at G = 64 27.  Bound by the products and the instructions that join their sums: four
+// products and twelve such instructions take a SIMD 42.7 ns in a loop of nothing else, where the products alone take 31.9 and the others 22.2.
 constexpr int kQ4ManyTiles = 8, kQ4Loaders = 4, kQ4MaxSlices = 8;
 constexpr int many_ring(int NG, int G) { return G == 32 && NG >= 8 ? 2 : NG == 16 ? 3 : 4; }     // what registers allow
 constexpr int many_buffers(int NG) { return NG <= 8 ? 4 : NG <= 12 ? 3 : 2; }
@@ -809,7 +817,8 @@ __global__ __launch_bounds__((8 + kQ4Loaders) * 64) __attribute__((amdgpu_waves_
     }
 }
 
-// The sums of the slices, in order, into place: 16 rows of a tile per workgroup
+// The sums of the slices, in order, into place: 16 rows of a tile per workgroup.  4.8 us for 40 x 4096 in 8 slices: a kernel's start, one round trip.  (The last workgroup
+// of a tile group to arrive reading the others' sums instead: 64 rows x 11003 x 4099 41 us became 44.)
 __global__ __launch_bounds__(256) void q4_join_kernel(Q4Kernel a, const float *partials, int slices) {
     const int tile = blockIdx.x, n = threadIdx.x & 15, row = blockIdx.y * 16 + (threadIdx.x >> 4);
     __shared__ float inv_s[kMaxRows];
@@ -837,7 +846,8 @@ static int few_rows(int N, int K) {
     if (rounds == 1) return KB <= 96 ? 8 : 4;
     return KB <= 64 ? 5 : rounds == 2 ? 3 : 1;
 }
-// Slices of K: what makes rounds of workgroups x blocks of one the least, with about 4 blocks' time for a workgroup's start and end
+// Slices of K: what makes rounds of workgroups x blocks of one the least, with about 4 blocks' time for a workgroup's start and end.  (Where neither one nor more
+// slices fill the chip evenly some of it idles: 22016 x 4096 is 172 workgroups, 29 us at 40 rows.)
 static int many_slices(int N, int K) {
     const int groups = ((N + 15) / 16 + kQ4ManyTiles - 1) / kQ4ManyTiles, KB = (K + kQ4Block - 1) / kQ4Block;
     int best = 1;
