@@ -9,8 +9,8 @@
 // rows of v_mfma_i32_16x16x64_i8; a nibble in the upper half of a byte is 16 q as an 8-bit integer, so the weights need
 // one mask (and every other one a shift) per 4 of them and no zero point.  The sums of a group are exact in 32 bits (at most
 // 128 * 128 * 128 = 2^21 a digit), those of two neighbouring digits together as well (2^30).  A lane ends with the four digits' sums of one
-// activation row and one output: two shift-and-adds, two conversions and a fused multiply-add make their float32 value (rounded three times), another
-// one with scale * 2^(E - 34) adds it to the output's float32 sum.
+// activation row and one output: two shift-and-adds, two conversions and a fused multiply-add make their float32 value (rounded three times), a product
+// with the scale and another fused multiply-add with 2^(E - 34) bring it into the output's float32 sum.
 // A row with a value that is not finite gives NaN; a block whose largest magnitude is below 2^-90 keeps less than 31 bits.
 // (One product in bfloat16 takes the matrix core as long as one here, and float32's accuracy takes three terms of each activation there,
 // four digits here; but there each weight has to be made from its nibble, here a mask does.)
@@ -353,10 +353,12 @@ __device__ __forceinline__ int block_exponent(const float (&v)[8]) {
     for (int e = 0; e < 8; ++e) m = __builtin_elementwise_maximum(m, fabsf(v[e]));        // NaN stays
     return shared_exponent(m);
 }
-// what a sum of 16 q * v is worth, times 2^UP
-template <int UP = 0>
+// What a sum of 16 q * v is worth, 2^(E - 34), is small where the activations are, and times a small scale below any float32 while the result is
+// not.  So the scales meet the sums first: up to 2^44 a block, 2^56 a chunk, times 2^-20 of the scale, which the factor bears instead.
+constexpr int kQ4ScaleShift = 20;
+constexpr float kQ4ScaleDown = 1.0f / (1 << kQ4ScaleShift);
 __device__ __forceinline__ float digit_factor(int exponent) {
-    return exponent == 255 ? __uint_as_float(0x7fc00000u) : __uint_as_float((unsigned)(exponent - 33 + UP) << 23);
+    return exponent == 255 ? __uint_as_float(0x7fc00000u) : __uint_as_float((unsigned)(exponent - 33 + kQ4ScaleShift) << 23);
 }
 __device__ __forceinline__ void block_digits(const float (&v)[8], int exponent, uint32_t (&B)[8]) {
     const float up = __uint_as_float((unsigned)(283 - exponent) << 23);       // 2^(30 - E): |v| stays below 2^30
@@ -543,14 +545,19 @@ __global__ __launch_bounds__(WAVES * 64) void q4_few_kernel(Q4Kernel a) {
     float sum[NG];
     auto multiply = [&](int i) __attribute__((always_inline)) {
         const i32x4_t x[2] = {words[i].operand(0), words[i].operand(1)};
+        float sc[per];
+#pragma unroll
+        for (int p = 0; p < per; ++p) sc[p] = words[i].scale(p) * kQ4ScaleDown;
 #pragma unroll
         for (int rg = 0; rg < NG; ++rg) {
             const bool single = rg == FULL;
             const float factor = single ? f1[i] : f[single ? 0 : rg][i];
             i32x4_t o[per];
             group_sums<G>(single ? B1 : B[single ? 0 : rg][i], x, o);
+            float block = join_digits(o[0]) * sc[0];
 #pragma unroll
-            for (int p = 0; p < per; ++p) sum[rg] = __builtin_fmaf(join_digits(o[p]), words[i].scale(p) * factor, sum[rg]);
+            for (int p = 1; p < per; ++p) block = __builtin_fmaf(join_digits(o[p]), sc[p], block);
+            sum[rg] = __builtin_fmaf(block, factor, sum[rg]);
         }
     };
     int tile = blockIdx.x;
@@ -604,9 +611,7 @@ __global__ __launch_bounds__(WAVES * 64) void q4_few_kernel(Q4Kernel a) {
 // The digits are made once, by a kernel of their own: a wave per row group and chunk of 4 blocks (more where K is over 16384, so that there are
 // at most 32), whose values of a row share an exponent.  40 x 4096 4.6 us, a kernel's start and one round trip (an exponent per block of 128, as the
 // kernel of few rows has, took a multiplication per sum more in the product).  Layout: [row group][block][step][lane] of 16 bytes, then the factors [row group][chunk][row].
-// (A sum of 16 q * v of a chunk times the scales is taken before the factors are: up to 2^45 times the largest scale, so
-// the scales go in as 2^-20 of themselves.)
-constexpr int kQ4Chunks = 32, kQ4ChunkUp = 20;
+constexpr int kQ4Chunks = 32;
 static int chunk_shift(int KB) {
     int s = 2;
     while ((KB + (1 << s) - 1) >> s > kQ4Chunks) ++s;
@@ -636,7 +641,7 @@ __global__ __launch_bounds__(64) void q4_digits_kernel(Q4Kernel a, uint4 *digits
         for (int i = 0; i < 4; ++i) look(v[KEEP ? i : 0]);
     }
     const int exponent = shared_exponent(m);
-    if (g == 0 && t == 0) factors[(rg * chunks + chunk) * kQ4Rows + c] = digit_factor<kQ4ChunkUp>(exponent);
+    if (g == 0 && t == 0) factors[(rg * chunks + chunk) * kQ4Rows + c] = digit_factor(exponent);
     auto make = [&](int i, const float (&x)[8]) __attribute__((always_inline)) {
         uint32_t B[8];
         block_digits(x, exponent, B);
@@ -671,7 +676,7 @@ __device__ __forceinline__ void pair_products(const Q4Words<G> (&words)[2], cons
     for (int i = 0; i < 2; ++i) {
         x[i][0] = words[i].operand(0); x[i][1] = words[i].operand(1);
 #pragma unroll
-        for (int p = 0; p < per; ++p) sc[i][p] = words[i].scale(p) * (1.0f / (1 << kQ4ChunkUp));
+        for (int p = 0; p < per; ++p) sc[i][p] = words[i].scale(p) * kQ4ScaleDown;
     }
 #pragma unroll
     for (int rg = 0; rg < NG + LAG; ++rg) {
