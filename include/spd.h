@@ -296,7 +296,7 @@ int32_t spd_speculative_accept_static(const float *target, const float *draft, c
  *   top_tokens_out    int32, top_logprobs_out float32 [n_rows, n_top]: the first n_top entries in that order (0 <= n_top <= SPD_MAX_TOP)
  *   workspace         scratch of spd_logprobs_workspace_bytes bytes (which may be 0; then it may be NULL), 16-byte aligned; it may hold
  *                     anything before the call and nothing in it has to survive it.  Calls that share one must not overlap.
- * temperature > 0 (temperature 0 leaves no log probabilities: ask for those at 1); ignored for probabilities.
+ * temperature >= 4.3e-39, finite (temperature 0 leaves no log probabilities: ask for those at 1); ignored for probabilities.
  * Entries at -infinity (probability 0) weigh nothing and are no alternatives: places they leave hold token -1 and -infinity.  A
  * row of nothing else: log probability -infinity, entropy 0.  A token outside 0..vocab-1: -infinity, rank vocab.  A row with a NaN or
  * +infinity (probabilities: a negative or infinite one or a NaN) has no distribution: NaN, rank and alternatives -1.

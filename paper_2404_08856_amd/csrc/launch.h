@@ -256,6 +256,7 @@ struct LogprobArgs {
     void *workspace;                 // logprobs_workspace_bytes
 };
 int logprob_slices(int vocab);       // workgroups per row
+bool logprob_temperature_ok(float temperature);
 size_t logprobs_workspace_bytes(int n_rows, int vocab, int n_top);
 hipError_t launch_logprobs(const LogprobArgs &a, hipStream_t stream);
 

@@ -333,6 +333,12 @@ __global__ __launch_bounds__(kMergeThreads) void logprobs_merge_kernel(LogprobAr
     }
 }
 
+// both factors that the kernels take of it are numbers: an infinite one makes NaN of the largest entry's 0
+bool logprob_temperature_ok(float temperature) {
+    const float inv = 1.0f / temperature;
+    return temperature > 0.f && inv > 0.f && inv * kLog2e < INFINITY;
+}
+
 constexpr int kSliceEntries = 32768;      // what a workgroup of 1024 holds in registers
 int logprob_slices(int vocab) { return (int)(((long)vocab + kSliceEntries - 1) / kSliceEntries); }
 

@@ -1126,7 +1126,7 @@ int32_t spd_token_logprobs(const float *rows, size_t row_stride, const int32_t *
     if (row_stride < (size_t)vocab) return fail(SPD_ERR_INVALID_ARG, "row_stride must cover a row");
     if (flags & ~SPD_ROWS_ARE_PROBS) return fail(SPD_ERR_INVALID_ARG, "unknown flag bits");
     const bool probs = flags & SPD_ROWS_ARE_PROBS;
-    if (!probs && !(temperature > 0.f && 1.0f / temperature < INFINITY && 1.0f / temperature > 0.f)) return fail(SPD_ERR_INVALID_ARG, "temperature must be positive and finite");
+    if (!probs && !logprob_temperature_ok(temperature)) return fail(SPD_ERR_INVALID_ARG, "temperature must be positive and finite, and at least 4.3e-39");
     if ((uintptr_t)workspace & 15) return fail(SPD_ERR_INVALID_ARG, "workspace must be 16-byte aligned");
     const size_t need = logprobs_workspace_bytes(n_rows, vocab, n_top);
     if (need && (!workspace || workspace_bytes < need)) return fail(SPD_ERR_CAPACITY, "workspace smaller than spd_logprobs_workspace_bytes reports");

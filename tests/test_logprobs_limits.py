@@ -1,0 +1,26 @@
+"""Temperatures and sizes at the limits of the log probabilities' calls (refusals: no GPU work)."""
+import ctypes
+
+import numpy as np
+import pytest
+
+from tests.test_q4_logprobs_refusals import expect, f32, i32, lib, null, some, sz, u32
+
+
+@pytest.mark.parametrize("temperature", [1e-45, 2.9e-39, 3.5e-39, 4.2e-39])
+def test_temperatures_whose_exponents_have_no_factor(temperature):
+    """2^((l - max) log2(e) / T): the factor is beyond float32 below T = 4.24e-39, also where 1 / T is not (2.94e-39)."""
+    spd, _ = lib()
+    expect(spd.SPD_ERR_INVALID_ARG, "spd_token_logprobs", some, sz(100), some, i32(2), i32(100), f32(temperature), u32(0), some, null, null, i32(0), null, null, null, sz(0), null)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("V", [50, 32000, 40000])
+@pytest.mark.parametrize("temperature", [4.3e-39, 1e-38, 1e38, 3.4e38])
+def test_temperatures_next_to_the_limits(V, temperature):
+    """Differences below 0.6: divided by T they stay finite."""
+    from tests.test_gpu_logprobs import check
+    rng = np.random.default_rng(V)
+    x = (0.6 * rng.random((3, V)) - 0.3).astype(np.float32)
+    x[1, [3, V - 1]] = 0.3                                     # two first ones
+    check(x, [1, V - 1, V // 2], temperature, False, 4)
