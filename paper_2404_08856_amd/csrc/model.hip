@@ -1107,9 +1107,25 @@ int32_t spd_q4_matmul(const void *packed, int32_t N, int32_t K, int32_t group, c
     return SPD_OK;
 }
 
+}  // extern "C"
+
 // ---- log probabilities -------------------------------------------------------------------------
+namespace {
+int32_t check_logprobs(int32_t n_rows, int32_t vocab, int32_t n_top) {
+    if (n_rows < 1 || vocab < 1) return fail(SPD_ERR_INVALID_ARG, "n_rows, vocab >= 1 required");
+    if (vocab > SPD_MAX_LOGPROB_VOCAB) return fail(SPD_ERR_SHAPE, "vocab %d exceeds %d", vocab, SPD_MAX_LOGPROB_VOCAB);
+    if (n_top < 0 || n_top > SPD_MAX_TOP) return fail(SPD_ERR_INVALID_ARG, "n_top = %d must be in 0..%d", n_top, SPD_MAX_TOP);
+    if (n_rows > SPD_MAX_LOGPROB_ROWS / logprob_slices(vocab)) return fail(SPD_ERR_SHAPE, "n_rows = %d is too many for vocab = %d", n_rows, vocab);
+    return SPD_OK;
+}
+}  // namespace
+
+extern "C" {
+
 int32_t spd_logprobs_workspace_bytes(int32_t n_rows, int32_t vocab, int32_t n_top, size_t *bytes) {
-    if (!bytes || n_rows < 1 || vocab < 1 || vocab > SPD_MAX_LOGPROB_VOCAB || n_top < 0 || n_top > SPD_MAX_TOP) return fail(SPD_ERR_INVALID_ARG, "bad argument to spd_logprobs_workspace_bytes");
+    if (!bytes) return fail(SPD_ERR_INVALID_ARG, "NULL argument to spd_logprobs_workspace_bytes");
+    const int32_t rc = check_logprobs(n_rows, vocab, n_top);
+    if (rc) return rc;
     *bytes = logprobs_workspace_bytes(n_rows, vocab, n_top);
     return SPD_OK;
 }
@@ -1119,10 +1135,8 @@ int32_t spd_token_logprobs(const float *rows, size_t row_stride, const int32_t *
                            void *workspace, size_t workspace_bytes, void *stream) {
     if (!rows || (!tokens && (logprob_out || rank_out)) || (n_top > 0 && (!top_tokens_out || !top_logprobs_out)))
         return fail(SPD_ERR_INVALID_ARG, "NULL argument to spd_token_logprobs");
-    if (n_rows < 1 || vocab < 1) return fail(SPD_ERR_INVALID_ARG, "n_rows, vocab >= 1 required");
-    if (vocab > SPD_MAX_LOGPROB_VOCAB) return fail(SPD_ERR_SHAPE, "vocab %d exceeds %d", vocab, SPD_MAX_LOGPROB_VOCAB);
-    if (n_top < 0 || n_top > SPD_MAX_TOP) return fail(SPD_ERR_INVALID_ARG, "n_top = %d must be in 0..%d", n_top, SPD_MAX_TOP);
-    if (n_rows > SPD_MAX_LOGPROB_ROWS / logprob_slices(vocab)) return fail(SPD_ERR_SHAPE, "n_rows = %d is too many for vocab = %d", n_rows, vocab);
+    const int32_t rc = check_logprobs(n_rows, vocab, n_top);
+    if (rc) return rc;
     if (row_stride < (size_t)vocab) return fail(SPD_ERR_INVALID_ARG, "row_stride must cover a row");
     if (flags & ~SPD_ROWS_ARE_PROBS) return fail(SPD_ERR_INVALID_ARG, "unknown flag bits");
     const bool probs = flags & SPD_ROWS_ARE_PROBS;

@@ -24,3 +24,12 @@ def test_temperatures_next_to_the_limits(V, temperature):
     x = (0.6 * rng.random((3, V)) - 0.3).astype(np.float32)
     x[1, [3, V - 1]] = 0.3                                     # two first ones
     check(x, [1, V - 1, V // 2], temperature, False, 4)
+
+
+def test_sizes_that_the_call_refuses_have_no_workspace_either():
+    spd, l = lib()
+    n = ctypes.c_size_t()
+    for rows, vocab in ((1, 2**24 + 1), (2**22, 5000), (2**21, 32769), (2**31 - 1, 2**24)):
+        expect(spd.SPD_ERR_SHAPE, "spd_logprobs_workspace_bytes", i32(rows), i32(vocab), i32(1), ctypes.byref(n))
+    for rows, vocab in ((2**22 - 1, 32768), (2**21 - 1, 32769), (1, 2**24)):
+        assert l.spd_logprobs_workspace_bytes(i32(rows), i32(vocab), i32(1), ctypes.byref(n)) == 0
