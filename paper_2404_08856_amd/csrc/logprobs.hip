@@ -40,7 +40,8 @@ struct LpFinish {
         empty = !(p.mx > lowest);
         log_sum = a.probs ? 0.f : logf(p.sum);
     }
-    __device__ __forceinline__ float lp(float v) const { return a.probs ? logf(v) : (v - p.mx) * a.inv_temp - log_sum; }
+    // (halves: the difference of two float32 may be beyond float32 where its T-th is not)
+    __device__ __forceinline__ float lp(float v) const { return a.probs ? logf(v) : 2.0f * __builtin_fmaf(0.5f * v - 0.5f * p.mx, a.inv_temp, -0.5f * log_sum); }
     __device__ __forceinline__ void write(size_t r, int token, float mine) const {
         const float nan = __uint_as_float(0x7fc00000u);
         const bool known = token >= 0 && token < a.vocab;

@@ -33,3 +33,15 @@ def test_sizes_that_the_call_refuses_have_no_workspace_either():
         expect(spd.SPD_ERR_SHAPE, "spd_logprobs_workspace_bytes", i32(rows), i32(vocab), i32(1), ctypes.byref(n))
     for rows, vocab in ((2**22 - 1, 32768), (2**21 - 1, 32769), (1, 2**24)):
         assert l.spd_logprobs_workspace_bytes(i32(rows), i32(vocab), i32(1), ctypes.byref(n)) == 0
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("V", [40, 32000, 40000])
+@pytest.mark.parametrize("temperature", [3.0, 200.0])
+def test_differences_beyond_float32_that_the_temperature_brings_back(V, temperature):
+    """Up to 6.8e38 below the largest entry: finite once divided by T."""
+    from tests.test_gpu_logprobs import check
+    x = np.zeros((2, V), dtype=np.float32)
+    x[:, 5], x[:, 7:30] = 3.0e38, np.finfo(np.float32).min
+    x[1, 6] = 3.0e38
+    check(x, [7, 9], temperature, False, 32)
