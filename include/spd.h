@@ -141,8 +141,10 @@ int32_t spd_model_create(const spd_model_config *h_cfg, const spd_weights *h_wei
                          spd_model **h_out);
 
 /* The same for a model whose matrices stay in 4 bits (spd_weights_q4): 3.8 times fewer bytes per step at groups of 128.  All
- * calls on such a model are those of any other; its products are as exact as the bf16 model's (float32 activations and sums),
- * so it differs from a bf16 model of the dequantised weights by float32 rounding only.  A row of activations with a
+ * calls on such a model are those of any other.  Its products have float32 activations and sums as the bf16 model's have, and in
+ * prompts of many rows their exactness.  In the other calls an activation counts as in spd_q4_matmul, to 2^-29 of the largest one of its
+ * row, where the bf16 model keeps 24 bits of each: the model differs from a bf16 model of the dequantised weights by float32 rounding, and,
+ * where some activations of a row are more than about 1000 times the rest, by up to 2^-29 of those in each of the rest.  A row of activations with a
  * value that is not finite gives NaN.  Of spd_tuning only the attention's fields, batch_kernel (prompts in passes of 64 or 40 rows) and
  * wait_spin_limit have an effect.  The workspace also holds one matrix at 16 bits, for prompts.  Errors as spd_model_create, SPD_ERR_SHAPE for another group. */
 int32_t spd_model_bytes_q4(const spd_model_config *h_cfg, int32_t group, size_t *h_packed_bytes,
@@ -298,7 +300,7 @@ int32_t spd_speculative_accept_static(const float *target, const float *draft, c
  *                     anything before the call and nothing in it has to survive it.  Calls that share one must not overlap.
  * temperature >= 4.3e-39, finite (temperature 0 leaves no log probabilities: ask for those at 1); ignored for probabilities.
  * Entries at -infinity (probability 0) weigh nothing and are no alternatives: places they leave hold token -1 and -infinity.  A
- * row of nothing else: log probability -infinity, entropy 0.  A token outside 0..vocab-1: -infinity, rank vocab.  A row with a NaN or
+ * row of nothing else: log probability -infinity, entropy 0.  Finite entries more than 3.4e38 below the largest weigh nothing either (but are alternatives).  A token outside 0..vocab-1: -infinity, rank vocab.  A row with a NaN or
  * +infinity (probabilities: a negative or infinite one or a NaN) has no distribution: NaN, rank and alternatives -1.
  * Errors: SPD_ERR_INVALID_ARG, SPD_ERR_SHAPE (vocab > SPD_MAX_LOGPROB_VOCAB, too many rows), SPD_ERR_CAPACITY (workspace too small). */
 int32_t spd_logprobs_workspace_bytes(int32_t n_rows, int32_t vocab, int32_t n_top, size_t *h_bytes);
@@ -323,8 +325,8 @@ int32_t spd_q4_pack(const void *q, const void *scales, int32_t N, int32_t K, int
                     void *packed, size_t packed_bytes, void *stream);
 
 /* y[r][n] = sum over k of x[r][k] W[n][k] for rows <= SPD_MAX_ROWS rows: x float32, or bfloat16 with SPD_X_IS_BF16, x_stride
- * elements between rows, y float32, y_stride between rows.  Exact products, float32 sums; x counts with 30 bits below the
- * largest magnitude of its row (float32 keeps 24 below each), and magnitudes below 2^-90 with fewer; scales of
+ * elements between rows, y float32, y_stride between rows.  Exact products, float32 sums; an entry of x counts to 2^-29 of the
+ * largest magnitude of its row, to 2^-23 of itself or to 2^-120, whichever is most; scales of
  * magnitudes between 2^-90 and 2^90, 0 and NaN (in whose rows of W y is NaN).  A row of x with a value that is not finite gives NaN.  y must not overlap x.
  * workspace: spd_q4_matmul_workspace_bytes bytes (which may be 0; then it may be NULL), 256-byte aligned; it may hold anything before the
  * call and nothing in it has to survive it.  Calls that share one must not overlap.

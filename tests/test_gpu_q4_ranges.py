@@ -47,3 +47,15 @@ def test_small_activations_and_scales_within_their_roundings(rows, N, K, G, px, 
     mass, weight = np.abs(x) @ np.abs(w).T, np.sum(np.abs(w), axis=1)[None]
     tol = (groups + 24) * (2.0 ** -24 * (mass + 2.0 ** -6 * top * weight) + 2.0 ** -150) + 2.0 ** -29 * top * weight
     assert np.all(np.abs(product(q, scales, G, x) - x @ w.T) <= tol)
+
+
+@pytest.mark.parametrize("rows,N,K,G", SIZES)
+def test_integers_beside_a_column_2_29_times_as_large_are_exact(rows, N, K, G):
+    """An entry counts to 2^-29 of the largest magnitude of its row: integers stay whole beside 2^29.  Its own weights are 0, so the sums are those
+    of integers up to 15 (below 2^22)."""
+    rng = np.random.default_rng(5 * rows + K)
+    x = rng.integers(-15, 16, (rows, K)).astype(np.float64)
+    q = rng.integers(-8, 8, (N, K))
+    x[:, 77::128], q[:, 77::128] = 2.0 ** 29, 0
+    scales = np.exp2(rng.integers(-2, 2, (N, (K + G - 1) // G))).astype(np.float32)
+    assert np.array_equal(product(q, scales, G, x), x @ values(q, scales, G).T)
