@@ -704,8 +704,10 @@ __device__ __forceinline__ void pair_products(const Q4Words<G> (&words)[2], cons
 // weights come through registers, RD steps ahead.  To fill the chip where a matrix has few tiles the blocks are cut
 // into `slices` across workgroups, whose sums q4_join_kernel adds.  (Workgroups that
 // begin at different steps of their slice, as the batched projections in bf16 do, are 1 to 2 % slower here, and weights loaded non-temporally 4 %.)
-// 40 rows x 32000 x 4096 at G = 128 29.6 us (72 MB, 2.4 TB/s), 64 rows x 11003 x 4099 at G = 64 27.  Bound by the products and the instructions that join their sums: four
-// products and twelve such instructions take a SIMD 42.7 ns in a loop of nothing else, where the products alone take 31.9 and the others 22.2.
+// 40 rows x 32000 x 4096 at G = 128 29.6 us (72 MB, 2.4 TB/s), 64 rows x 11003 x 4099 at G = 64 27.  By counters, of the cycles of a busy SIMD there: products 35 and 30 %, other
+// vector instructions 44 and 61 (5.1 and 8.2 a product, where the joining of the sums takes 3 and 6: the rest are the masks of the weights, scales, addresses), both at
+// once 14 and 11, neither 35 and 20: two multiplying waves a SIMD that wait at the same barriers.  LDS reads take a fifth of a CU's cycles, without conflicts.  (Four products
+// and twelve other instructions take a SIMD 42.7 ns in a loop of nothing else, where the products alone take 31.9 and the others 22.2.)
 constexpr int kQ4ManyTiles = 8, kQ4Loaders = 4, kQ4MaxSlices = 8;
 constexpr int many_ring(int NG, int G) { return G == 32 && NG >= 8 ? 2 : NG == 16 ? 3 : 4; }     // what registers allow
 constexpr int many_buffers(int NG) { return NG <= 8 ? 4 : NG <= 12 ? 3 : 2; }
@@ -717,8 +719,6 @@ __global__ __launch_bounds__((8 + kQ4Loaders) * 64) __attribute__((amdgpu_waves_
     const int group = blockIdx.x / slices, slice = blockIdx.x - group * slices;
     const int b0 = (int)((long)a.KB * slice / slices), len = (int)((long)a.KB * (slice + 1) / slices) - b0;
     const int steps = (len + 1) / 2;                           // (those beyond load what is never used)
-    // position (in blocks of the slice) of step s's even or odd block; at or beyond len: there is none
-    auto position = [&](int s, int o) __attribute__((always_inline)) { return 2 * s + o; };
     extern __shared__ uint4 lds[];                             // [NBUF][even, odd][NG][2][64]
     __shared__ float inv_s[kMaxRows];
     __shared__ float F[kQ4Chunks][kMaxRows];                   // factors of the digits
@@ -739,7 +739,7 @@ __global__ __launch_bounds__((8 + kQ4Loaders) * 64) __attribute__((amdgpu_waves_
         }
         int buffer = 0;
         auto issue = [&](int s) __attribute__((always_inline)) {
-            const char *src = reinterpret_cast<const char *>(digits) + (size_t)(b0 + min(position(s, o), len - 1)) * 2048;
+            const char *src = reinterpret_cast<const char *>(digits) + (size_t)(b0 + min(2 * s + o, len - 1)) * 2048;
             uint4 *dst = lds + (buffer * 2 + o) * NG * 128 + (first & 1) * 64;
 #pragma unroll
             for (int r = 0; r < PB; ++r)
@@ -764,14 +764,14 @@ __global__ __launch_bounds__((8 + kQ4Loaders) * 64) __attribute__((amdgpu_waves_
             for (int rg = 0; rg < NG; ++rg) sum[i][rg] = total[i][rg] = 0.f;
         Q4Words<G> ring[RD][2];
         auto weights = [&](int slot, int s) __attribute__((always_inline)) {
-            const int b = b0 + min(position(s, odd), len - 1);
+            const int b = b0 + min(2 * s + odd, len - 1);
 #pragma unroll
             for (int i = 0; i < 2; ++i) ring[slot][i].template load<false>(a, (size_t)min(t0 + i, a.tiles - 1) * a.KB + b, lane);     // (beyond the matrix: a valid tile, dropped)
         };
 #pragma unroll
         for (int s = 0; s < RD; ++s) weights(s, s);
         __syncthreads();
-        int buffer = 0, chunk = (b0 + min(position(0, odd), len - 1)) >> shift;
+        int buffer = 0, chunk = (b0 + min(odd, len - 1)) >> shift;
         auto chunk_done = [&] __attribute__((always_inline)) {
             const float *f = &F[chunk][lane >> 4];
 #pragma unroll
@@ -785,7 +785,7 @@ __global__ __launch_bounds__((8 + kQ4Loaders) * 64) __attribute__((amdgpu_waves_
 #pragma unroll
             for (int h = 0; h < RD; ++h) {
                 if (s0 + h >= steps) break;
-                const int p = position(s0 + h, odd);
+                const int p = 2 * (s0 + h) + odd;               // block of the slice
                 if (p < len) {
                     if ((b0 + p) >> shift != chunk) {
                         chunk_done();
