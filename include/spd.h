@@ -327,7 +327,7 @@ int32_t spd_q4_pack(const void *q, const void *scales, int32_t N, int32_t K, int
 /* y[r][n] = sum over k of x[r][k] W[n][k] for rows <= SPD_MAX_ROWS rows: x float32, or bfloat16 with SPD_X_IS_BF16, x_stride
  * elements between rows, y float32, y_stride between rows.  Exact products, float32 sums; an entry of x counts to 2^-29 of the
  * largest magnitude of its row, to 2^-23 of itself or to 2^-120, whichever is most; scales of
- * magnitudes between 2^-90 and 2^90, 0 and NaN (in whose rows of W y is NaN).  A row of x with a value that is not finite gives NaN.  y must not overlap x.
+ * magnitudes between 2^-100 and 2^100, 0 and NaN (in whose rows of W y is NaN).  A row of x with a value that is not finite gives NaN.  y must not overlap x.
  * workspace: spd_q4_matmul_workspace_bytes bytes (which may be 0; then it may be NULL), 256-byte aligned; it may hold anything before the
  * call and nothing in it has to survive it.  Calls that share one must not overlap.
  * Errors: SPD_ERR_INVALID_ARG, SPD_ERR_SHAPE, SPD_ERR_CAPACITY (workspace too small). */

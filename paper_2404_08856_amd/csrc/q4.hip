@@ -356,9 +356,10 @@ __device__ __forceinline__ int block_exponent(const float (&v)[8]) {
     return shared_exponent(m);
 }
 // What a sum of 16 q * v is worth, 2^(E - 34), is small where the activations are, and times a small scale below any float32 while the result is
-// not.  So the scales meet the sums first: up to 2^44 a block, 2^56 a chunk, times 2^-20 of the scale, which the factor bears instead.
-constexpr int kQ4ScaleShift = 20;
-constexpr float kQ4ScaleDown = 1.0f / (1 << kQ4ScaleShift);
+// not.  So the scales meet the sums first: up to 2^44 a block, 2^56 a chunk, times 2^-32 of the scale, which the factor bears instead: scales up to 2^100 stay in
+// range, and those down to 2^-100 keep their 8 bits.
+constexpr int kQ4ScaleShift = 32;
+constexpr float kQ4ScaleDown = 0x1p-32f;
 __device__ __forceinline__ float digit_factor(int exponent) {
     return exponent == 255 ? __uint_as_float(0x7fc00000u) : __uint_as_float((unsigned)(exponent - 33 + kQ4ScaleShift) << 23);
 }

@@ -59,3 +59,10 @@ def test_integers_beside_a_column_2_29_times_as_large_are_exact(rows, N, K, G):
     x[:, 77::128], q[:, 77::128] = 2.0 ** 29, 0
     scales = np.exp2(rng.integers(-2, 2, (N, (K + G - 1) // G))).astype(np.float32)
     assert np.array_equal(product(q, scales, G, x), x @ values(q, scales, G).T)
+
+
+@pytest.mark.parametrize("rows,N,K,G", SIZES)
+@pytest.mark.parametrize("px,ps", [(-26, -98), (20, -98), (-86, 99), (-30, 99), (2, 99)])
+def test_scales_up_to_2_100_and_down_to_2_minus_100(rows, N, K, G, px, ps):
+    """As the integers above: sums below 2^22 * 2^(px + ps), multiples of 2^(px + ps - 2) >= 2^-126."""
+    test_integers_times_powers_of_two_on_both_sides_are_exact(rows, N, K, G, px, ps)
