@@ -84,15 +84,15 @@ def draw(rng):
         rows = _log_int(rng, seqs, 8192 * 48 // max(48, heads + 2 * kv_heads))
         case["new_hi"] = max(1, rows // seqs)
         case["new_lo"] = rng.choice([1, case["new_hi"]])
-        case["len_hi"] = _log_int(rng, 1, 8000)
+        case["len_hi"] = _log_int(rng, 1, max(1, min(8000, 250000000 // (seqs * kv_heads * dim) - case["new_hi"])))
         case["len_lo"] = rng.choice([0, case["len_hi"]])
         return {**case, **turn}
     tree = rng.random() < 0.2
     case["new_hi"] = rng.choice([1, _log_int(rng, 2, 64)]) if tree or rng.random() < 0.7 else min(_log_int(rng, 64, 4096), max(64, 8192 // seqs))
     # the scores of padded sequences, and what the caches hold, stay below those of the largest listed cases
-    case["new_hi"] = min(case["new_hi"], math.isqrt(500000000 // (seqs * heads)))
+    case["new_hi"] = min(case["new_hi"], math.isqrt(250000000 // (seqs * heads)))
     case["new_lo"] = rng.choice([1, case["new_hi"]])
-    most = min(500000000 // (seqs * heads * case["new_hi"]), 250000000 // (seqs * kv_heads * dim), 131000)
+    most = min(250000000 // (seqs * heads * case["new_hi"]), 250000000 // (seqs * kv_heads * dim), 131000)
     case["len_hi"] = min(_log_int(rng, 1, 131000), max(0, most - case["new_hi"]))
     case["len_lo"] = rng.choice([0, case["len_hi"] // 10, case["len_hi"]])
     return {**case, "window": rng.choice([0, 0, 0, _log_int(rng, 1, 8000)]) if not tree else 0, "tree": tree}
