@@ -62,10 +62,17 @@ extern "C" {
 #define SPD_TARGET_IS_PROBS  1u    /* target rows are probabilities, not logits   */
 #define SPD_DRAFT_IS_PROBS   2u    /* draft rows are probabilities, not logits    */
 
-/* flags of spd_token_logprobs, spd_q4_quantize / spd_q4_dequantize, spd_q4_matmul */
+/* flags of spd_token_logprobs, spd_q4_quantize / spd_q4_dequantize, spd_q4_matmul, spd_rope_apply, spd_paged_append, spd_paged_attention */
 #define SPD_ROWS_ARE_PROBS   1u    /* rows are probabilities, not logits          */
 #define SPD_W_IS_BF16        1u    /* weights bfloat16, else float32              */
 #define SPD_X_IS_BF16        1u    /* activations bfloat16, else float32          */
+#define SPD_ROPE_INVERSE     2u    /* spd_rope_apply: by the negative angles      */
+
+#define SPD_MAX_HEAD_DIM     256   /* spd_rope_apply; the paged calls: head_dim 64 or 128 */
+#define SPD_MAX_PAGED_SEQS   4096  /* sequences per paged call                    */
+#define SPD_MAX_PAGED_ROWS   (1 << 20)  /* rows per paged call, and of spd_rope_apply  */
+#define SPD_MAX_PAGED_HEADS  1024  /* heads of a row                              */
+#define SPD_MAX_PAGED_POSITIONS (1 << 30)  /* positions a row of a page table reaches */
 
 typedef struct spd_model spd_model;
 
@@ -335,6 +342,107 @@ int32_t spd_q4_matmul_workspace_bytes(int32_t rows, int32_t N, int32_t K, size_t
 int32_t spd_q4_matmul(const void *packed, int32_t N, int32_t K, int32_t group, const void *x, size_t x_stride,
                       uint32_t flags, int32_t rows, float *y, size_t y_stride,
                       void *workspace, size_t workspace_bytes, void *stream);
+
+/* ---- rotary positions -------------------------------------------------------------------------------
+ * Pair i < rotary_dim / 2 of a head is turned by the angle position * f_i:  (a, b) -> m (a cos - b sin, a sin + b cos), its elements
+ * i and i + rotary_dim / 2, or (interleaved) 2 i and 2 i + 1; elements from rotary_dim on stay as they are.
+ *   f_i = theta^(-2 i / rotary_dim) / h_factors[i] (h_factors NULL: 1), then by `scaling`, with t_i = original_positions f_i / (2 pi), the
+ *   pair's turns over the context that the model was trained on:
+ *     SPD_ROPE_NONE      f_i
+ *     SPD_ROPE_LINEAR    f_i / factor
+ *     SPD_ROPE_RAMP      f_i (r + (1 - r) / factor),  r = (t_i - low) / (high - low) limited to 0..1
+ *     SPD_ROPE_LOG_RAMP  the same with r = (ln t_i - ln low) / (ln high - ln low)
+ *   m = magnitude (1 if the model states none).
+ * Positions are any int32, negative ones too: a frequency is held as a 64-bit fraction of a turn, so that the angle's place within its
+ * turn is exact to 2^-32 turns however far the position.
+ * spd_rope_table makes the frequencies' table (spd_rope_table_bytes bytes, 16-byte aligned) once; spd_rope names it in the calls. */
+#define SPD_ROPE_NONE     0
+#define SPD_ROPE_LINEAR   1
+#define SPD_ROPE_RAMP     2
+#define SPD_ROPE_LOG_RAMP 3
+typedef struct {
+    int32_t      rotary_dim;          /* even, 2..SPD_MAX_HEAD_DIM                  */
+    int32_t      scaling;
+    float        theta;               /* > 0                                        */
+    float        factor, low, high;   /* factor > 0; ramps: high > low (log: low > 0) */
+    float        original_positions;  /* ramps: > 0                                 */
+    float        magnitude;
+    const float *h_factors;           /* host, [rotary_dim / 2], > 0; or NULL       */
+} spd_rope_config;
+typedef struct {
+    const void *table;
+    int32_t     rotary_dim, interleaved;
+} spd_rope;
+
+/* Rows of heads: head h of row r starts row_stride r + head_stride h elements behind `data`, its elements are neighbours. */
+typedef struct {
+    void  *data;
+    size_t row_stride, head_stride;
+} spd_heads;
+
+/* out = x turned, head_dim elements of each of n_heads heads of n_rows rows; float32, or bfloat16 with SPD_X_IS_BF16 (rounded once).
+ * positions: int32 [n_rows].  out may be x itself (the same data and strides); otherwise the two must not overlap.
+ * SPD_ROPE_INVERSE turns by the negative angles: the gradient of x from that of out, or, with magnitude 1, the turn taken back.
+ * Errors: SPD_ERR_INVALID_ARG (NULL, strides, unknown flags, a config's values), SPD_ERR_SHAPE (rotary_dim odd or above head_dim,
+ * head_dim above SPD_MAX_HEAD_DIM, rows or heads out of range), SPD_ERR_CAPACITY (table too small). */
+int32_t spd_rope_table_bytes(int32_t rotary_dim, size_t *h_bytes);
+int32_t spd_rope_table(const spd_rope_config *h_cfg, void *table, size_t table_bytes, void *stream);
+int32_t spd_rope_apply(const spd_rope *h_rope, const spd_heads *h_x, const spd_heads *h_out, const int32_t *positions, int32_t n_rows,
+                       int32_t n_heads, int32_t head_dim, uint32_t flags, void *stream);
+
+/* ---- a paged cache of keys and values, and attention over it -------------------------------------------------------
+ * The cache of one layer: n_pages pages of page_size positions (16, 32, 64, 128 or 256) of n_kv_heads heads of head_dim elements (64 or
+ * 128), in granules of 16 bytes, G elements (bfloat16: 8; e4m3: 16), laid out as the matrix cores read them:
+ *   k  [n_pages][n_kv_heads][head_dim / G][page_size][G]       element d of slot p: granule d / G, row p
+ *   v  [n_pages][n_kv_heads][page_size / G][head_dim][G]       slot p of element d: granule p / G, row d
+ * e4m3 (OCP: largest 448, no infinities): an element stands for itself times the scale of its head, k_scale / v_scale
+ * float32 [n_kv_heads], positive, device memory.  A page may be anyone's: several sequences' rows of the table may name it. */
+typedef struct {
+    void        *k, *v;                        /* 16-byte aligned */
+    const float *k_scale, *v_scale;            /* e4m3; else NULL */
+    int32_t      n_pages, page_size, n_kv_heads, head_dim, e4m3;
+} spd_paged_cache;
+
+/* The new rows of a call: those of sequence s are row_start[s] .. row_start[s + 1] - 1 (row_start int32 [n_seqs + 1], ascending; NULL: n_rows / n_seqs
+ * rows each), and row i of them has position lens[s] + i, lens int32 [n_seqs] the positions cached before.  Position p lies in slot
+ * p % page_size of page page_table[s * table_stride + p / page_size], p < max_pages * page_size.  All device memory.
+ * Rows behind row_start[n_seqs] belong to nobody: nothing is written for them.  A position beyond the table, or whose entry is not in
+ * 0..n_pages-1, is no place: nothing is appended there and nobody sees it (entries of pages that were given up may be -1).
+ * A length below 0 counts as 0, one beyond the table as its end. */
+typedef struct {
+    int32_t        n_seqs, n_rows, max_pages;
+    size_t         table_stride;
+    const int32_t *page_table, *lens, *row_start;
+} spd_paged_batch;
+
+/* Appends the rows' keys and values (n_kv_heads heads of head_dim; rounded once to bfloat16, or x / scale to the nearest e4m3, ties to
+ * even, limited to +-448; NaN stays NaN).  h_rope not NULL: keys are turned first, by positions[r] (int32 [n_rows]) or, if that is NULL, by the rows' own.
+ * h_q not NULL: n_heads heads of queries are turned in the same launch into h_q_out (which may be h_q itself).
+ * Rows float32, or bfloat16 with SPD_X_IS_BF16.  Places that two rows share (a page that two sequences append to) hold either's.
+ * Errors: SPD_ERR_INVALID_ARG, SPD_ERR_SHAPE; nothing is launched then. */
+int32_t spd_paged_append(const spd_paged_cache *h_cache, const spd_paged_batch *h_batch, const spd_heads *h_k, const spd_heads *h_v,
+                         const spd_heads *h_q, const spd_heads *h_q_out, int32_t n_heads, const spd_rope *h_rope, const int32_t *positions,
+                         uint32_t flags, void *stream);
+
+/* Attention of the new rows, whose keys and values are in their places by then, over their sequences' positions:
+ *   out[r][h] = sum_p softmax_p(scale q[r][h] . k[p]) v[p]      head h reads key head h / (n_heads / n_kv_heads)
+ * A row at position x sees p <= x; with window > 0 only p > x - window; with `seen` (uint64 [n_rows]; window 0) the cached
+ * positions p < lens[s], and of the sequence's new rows those whose bit is set (bit j: row j; at most 64 rows of a sequence
+ * can be seen): a tree of drafted tokens, whose rows have the bits of the tokens that they continue, and their own.
+ * Positions that a row does not see weigh nothing, whatever they hold; so do scores of -infinity.  A row that sees nothing: out 0.
+ * A key that is not finite and seen may leave its head's row NaN, such a value its element not finite.
+ * lse_out: float32 [n_rows][n_heads] or NULL, log sum exp of the scores (-infinity for a row that sees nothing): with it, parts of
+ * a softmax over several caches can be joined.
+ * q, out: float32, or bfloat16 with SPD_X_IS_BF16.  Sums and statistics are float32.  Products of float32 rows are exact to float32's roundings; with
+ * bfloat16 rows the softmax's weights are rounded to bfloat16 before the product with v where a sequence has many rows.
+ * workspace: spd_paged_attention_workspace_bytes bytes, 256-byte aligned; it may hold anything before the call, and nothing in it has to survive
+ * it.  Calls that share one must not overlap; the results of calls that do are undefined, those of later calls are not, with one exception: a call captured
+ * in a graph that overlapped with another needs the workspace cleared before its next replay.
+ * Errors: SPD_ERR_INVALID_ARG, SPD_ERR_SHAPE, SPD_ERR_CAPACITY (workspace too small); nothing is launched then. */
+int32_t spd_paged_attention_workspace_bytes(const spd_paged_cache *h_cache, const spd_paged_batch *h_batch, int32_t n_heads, size_t *h_bytes);
+int32_t spd_paged_attention(const spd_paged_cache *h_cache, const spd_paged_batch *h_batch, const spd_heads *h_q, const spd_heads *h_out,
+                            int32_t n_heads, float scale, int32_t window, const uint64_t *seen, float *lse_out, uint32_t flags,
+                            void *workspace, size_t workspace_bytes, void *stream);
 
 /* ---- the block loop without the host (Section 2.1, one block = gamma draft steps, one
  * target call, accept / resample, commit) ---------------------------------------------

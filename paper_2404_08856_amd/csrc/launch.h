@@ -292,4 +292,53 @@ struct Q4GemmArgs {
 size_t q4_workspace_bytes(int rows, int N, int K);
 hipError_t launch_q4_gemm(const Q4GemmArgs &a, int epilogue, hipStream_t stream);
 
+// ---- rotary positions, paged cache (paged.hip), attention over it (paged_attention.hip) ----
+struct HeadsArgs { void *p; size_t row, head; };            // strides in elements
+struct RopeTableArgs { uint64_t turn[128]; float magnitude; int n; };   // frequencies in 2^-64 turns a position
+struct RopeRef { const void *table; int R; bool interleaved; };          // table: {float magnitude; 12 bytes; uint64_t turn[R / 2]}
+constexpr size_t kRopeHeader = 16;
+struct RopeArgs {
+    HeadsArgs x, out;
+    RopeRef rope;
+    const int32_t *positions;
+    int n_rows, n_heads, dim;
+    bool bf16, inverse;
+};
+struct PagedCacheArgs {
+    void *k, *v;
+    const float *k_scale, *v_scale;
+    int n_pages, page_bits, n_kv, dim;                       // page_size = 1 << page_bits
+    bool e4m3;
+};
+struct PagedBatchArgs {
+    int n_seqs, n_rows, max_pages, each, capacity;           // each: rows a sequence without row_start; capacity = max_pages * page_size
+    size_t table_stride;
+    const int32_t *page_table, *lens, *row_start;
+};
+struct PagedAppendArgs {
+    PagedCacheArgs c;
+    PagedBatchArgs b;
+    HeadsArgs k, v, q, q_out;                                // q.p NULL: none
+    int n_heads;
+    RopeRef rope;                                            // table NULL: none
+    const int32_t *positions;
+    bool bf16;
+};
+struct PagedAttentionArgs {
+    PagedCacheArgs c;
+    PagedBatchArgs b;
+    HeadsArgs q, out;
+    int n_heads, window;
+    float scale;
+    const uint64_t *seen;
+    float *lse;
+    bool bf16;
+    void *workspace;
+};
+hipError_t launch_rope_table(const RopeTableArgs &a, void *table, hipStream_t stream);
+hipError_t launch_rope(const RopeArgs &a, hipStream_t stream);
+hipError_t launch_paged_append(const PagedAppendArgs &a, hipStream_t stream);
+size_t paged_attention_workspace_bytes(const PagedCacheArgs &c, const PagedBatchArgs &b, int n_heads);
+hipError_t launch_paged_attention(const PagedAttentionArgs &a, hipStream_t stream);
+
 }  // namespace spd

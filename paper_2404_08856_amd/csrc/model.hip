@@ -1155,3 +1155,183 @@ int32_t spd_token_logprobs(const float *rows, size_t row_stride, const int32_t *
 }
 
 }  // extern "C"
+
+// ---- rotary positions, paged cache -------------------------------------------------------------
+namespace {
+int32_t check_rope(const spd_rope *r, int32_t dim) {
+    if (!r->table || (uintptr_t)r->table & 15) return fail(SPD_ERR_INVALID_ARG, "the table of rotary positions must be given, 16-byte aligned");
+    if (r->rotary_dim < 2 || r->rotary_dim % 2 || r->rotary_dim > dim) return fail(SPD_ERR_SHAPE, "rotary_dim = %d must be even, in 2..%d", r->rotary_dim, dim);
+    if (r->interleaved != 0 && r->interleaved != 1) return fail(SPD_ERR_INVALID_ARG, "interleaved must be 0 or 1");
+    return SPD_OK;
+}
+// `size`: bytes of an element
+int32_t check_heads(const char *what, const spd_heads *h, int32_t n_rows, int32_t n_heads, int32_t dim, size_t size) {
+    if (!h->data) return fail(SPD_ERR_INVALID_ARG, "NULL data of %s", what);
+    if ((uintptr_t)h->data % size) return fail(SPD_ERR_INVALID_ARG, "data of %s must be aligned to its elements", what);
+    const size_t most = (size_t)1 << 40;
+    if (h->row_stride > most || h->head_stride > most) return fail(SPD_ERR_INVALID_ARG, "strides of %s are too large", what);
+    // heads within rows, or rows within heads
+    const size_t in_row = (size_t)(n_heads - 1) * h->head_stride + dim, in_head = (size_t)(n_rows - 1) * h->row_stride + dim;
+    const bool apart = (n_heads == 1 || h->head_stride >= (size_t)dim) && (n_rows == 1 || h->row_stride >= (size_t)dim) &&
+                       (n_rows == 1 || n_heads == 1 || h->row_stride >= in_row || h->head_stride >= in_head);
+    return apart ? SPD_OK : fail(SPD_ERR_INVALID_ARG, "heads of %s overlap", what);
+}
+HeadsArgs heads_args(const spd_heads *h) { return {h->data, h->row_stride, h->head_stride}; }
+
+int32_t check_paged(const spd_paged_cache *c, const spd_paged_batch *b, PagedCacheArgs &ca, PagedBatchArgs &ba) {
+    if (!c || !b || !c->k || !c->v || !b->page_table || !b->lens) return fail(SPD_ERR_INVALID_ARG, "NULL argument to a paged call");
+    if (c->head_dim != 64 && c->head_dim != 128) return fail(SPD_ERR_SHAPE, "head_dim = %d must be 64 or 128", c->head_dim);
+    if (c->page_size < 16 || c->page_size > 256 || (c->page_size & (c->page_size - 1))) return fail(SPD_ERR_SHAPE, "page_size = %d must be 16, 32, 64, 128 or 256", c->page_size);
+    if (c->n_pages < 1) return fail(SPD_ERR_SHAPE, "n_pages >= 1 required");
+    if (c->n_kv_heads < 1 || c->n_kv_heads > SPD_MAX_PAGED_HEADS) return fail(SPD_ERR_SHAPE, "n_kv_heads = %d must be in 1..%d", c->n_kv_heads, SPD_MAX_PAGED_HEADS);
+    if (c->e4m3 != 0 && c->e4m3 != 1) return fail(SPD_ERR_INVALID_ARG, "e4m3 must be 0 or 1");
+    if (c->e4m3 ? !c->k_scale || !c->v_scale : c->k_scale || c->v_scale) return fail(SPD_ERR_INVALID_ARG, "scales go with e4m3, both of them");
+    if (((uintptr_t)c->k | (uintptr_t)c->v) & 15) return fail(SPD_ERR_INVALID_ARG, "pages must be 16-byte aligned");
+    if (b->n_seqs < 1 || b->n_seqs > SPD_MAX_PAGED_SEQS) return fail(SPD_ERR_SHAPE, "n_seqs = %d must be in 1..%d", b->n_seqs, SPD_MAX_PAGED_SEQS);
+    if (b->n_rows < 1 || b->n_rows > SPD_MAX_PAGED_ROWS) return fail(SPD_ERR_SHAPE, "n_rows = %d must be in 1..%d", b->n_rows, SPD_MAX_PAGED_ROWS);
+    if (b->max_pages < 1 || b->max_pages > SPD_MAX_PAGED_POSITIONS / c->page_size) return fail(SPD_ERR_SHAPE, "max_pages = %d must be in 1..%d", b->max_pages, SPD_MAX_PAGED_POSITIONS / c->page_size);
+    if (b->table_stride < (size_t)b->max_pages && b->n_seqs > 1) return fail(SPD_ERR_INVALID_ARG, "table_stride must cover a row of the page table");
+    if (b->table_stride > (size_t)1 << 40) return fail(SPD_ERR_INVALID_ARG, "table_stride is too large");
+    if (!b->row_start && b->n_rows % b->n_seqs) return fail(SPD_ERR_SHAPE, "without row_start n_rows = %d must be a multiple of n_seqs = %d", b->n_rows, b->n_seqs);
+    ca.k = c->k; ca.v = c->v; ca.k_scale = c->k_scale; ca.v_scale = c->v_scale;
+    ca.n_pages = c->n_pages; ca.page_bits = __builtin_ctz((unsigned)c->page_size); ca.n_kv = c->n_kv_heads; ca.dim = c->head_dim; ca.e4m3 = c->e4m3;
+    ba.n_seqs = b->n_seqs; ba.n_rows = b->n_rows; ba.max_pages = b->max_pages; ba.each = b->n_rows / b->n_seqs; ba.capacity = b->max_pages * c->page_size;
+    ba.table_stride = b->table_stride; ba.page_table = b->page_table; ba.lens = b->lens; ba.row_start = b->row_start;
+    return SPD_OK;
+}
+int32_t check_query_heads(int32_t n_heads, int32_t n_kv) {
+    if (n_heads < 1 || n_heads > SPD_MAX_PAGED_HEADS || n_heads % n_kv) return fail(SPD_ERR_SHAPE, "n_heads = %d must be a multiple of n_kv_heads = %d, at most %d", n_heads, n_kv, SPD_MAX_PAGED_HEADS);
+    return SPD_OK;
+}
+bool positive(float x) { return x > 0.0f && std::isfinite(x); }
+}  // namespace
+
+extern "C" {
+
+int32_t spd_rope_table_bytes(int32_t rotary_dim, size_t *bytes) {
+    if (!bytes) return fail(SPD_ERR_INVALID_ARG, "NULL argument to spd_rope_table_bytes");
+    if (rotary_dim < 2 || rotary_dim % 2 || rotary_dim > SPD_MAX_HEAD_DIM) return fail(SPD_ERR_SHAPE, "rotary_dim = %d must be even, in 2..%d", rotary_dim, SPD_MAX_HEAD_DIM);
+    *bytes = kRopeHeader + (size_t)rotary_dim / 2 * sizeof(uint64_t);
+    return SPD_OK;
+}
+
+int32_t spd_rope_table(const spd_rope_config *c, void *table, size_t table_bytes, void *stream) {
+    if (!c || !table) return fail(SPD_ERR_INVALID_ARG, "NULL argument to spd_rope_table");
+    size_t need;
+    const int32_t rc = spd_rope_table_bytes(c->rotary_dim, &need);
+    if (rc) return rc;
+    if ((uintptr_t)table & 15) return fail(SPD_ERR_INVALID_ARG, "table must be 16-byte aligned");
+    if (table_bytes < need) return fail(SPD_ERR_CAPACITY, "table smaller than spd_rope_table_bytes reports");
+    if (!positive(c->theta) || !std::isfinite(c->magnitude)) return fail(SPD_ERR_INVALID_ARG, "theta must be positive, theta and magnitude finite");
+    if (c->scaling < SPD_ROPE_NONE || c->scaling > SPD_ROPE_LOG_RAMP) return fail(SPD_ERR_INVALID_ARG, "scaling = %d is unknown", c->scaling);
+    const bool ramp = c->scaling == SPD_ROPE_RAMP || c->scaling == SPD_ROPE_LOG_RAMP;
+    if (c->scaling != SPD_ROPE_NONE && !positive(c->factor)) return fail(SPD_ERR_INVALID_ARG, "factor must be positive and finite");
+    if (ramp && (!positive(c->original_positions) || !std::isfinite(c->low) || !std::isfinite(c->high) || !(c->high > c->low) || (c->scaling == SPD_ROPE_LOG_RAMP && !(c->low > 0.0f))))
+        return fail(SPD_ERR_INVALID_ARG, "a ramp needs original_positions > 0 and low < high, finite (0 < low where it is one of logarithms)");
+    RopeTableArgs a;
+    a.n = c->rotary_dim / 2;
+    a.magnitude = c->magnitude;
+    const long double two_pi = 6.283185307179586476925286766559L;
+    for (int i = 0; i < a.n; ++i) {
+        if (c->h_factors && !positive(c->h_factors[i])) return fail(SPD_ERR_INVALID_ARG, "h_factors must be positive and finite");
+        long double f = powl(c->theta, -2.0L * i / c->rotary_dim) / (c->h_factors ? (long double)c->h_factors[i] : 1.0L);
+        if (c->scaling == SPD_ROPE_LINEAR) f /= c->factor;
+        if (ramp) {
+            const long double t = c->original_positions * f / two_pi;
+            const long double at = c->scaling == SPD_ROPE_RAMP ? (t - c->low) / ((long double)c->high - c->low) : (logl(t) - logl(c->low)) / (logl(c->high) - logl(c->low));
+            const long double r = std::min(1.0L, std::max(0.0L, at));
+            f *= r + (1.0L - r) / c->factor;
+        }
+        f /= two_pi;
+        f -= floorl(f);                                                     // whole turns are none
+        a.turn[i] = f > 0.0L ? (uint64_t)std::min(ldexpl(f, 64), ldexpl(1.0L, 64) - 1.0L) : 0;
+    }
+    HIP_TRY(launch_rope_table(a, table, (hipStream_t)stream));
+    return SPD_OK;
+}
+
+int32_t spd_rope_apply(const spd_rope *rope, const spd_heads *x, const spd_heads *out, const int32_t *positions, int32_t n_rows, int32_t n_heads,
+                       int32_t head_dim, uint32_t flags, void *stream) {
+    if (!rope || !x || !out || !positions) return fail(SPD_ERR_INVALID_ARG, "NULL argument to spd_rope_apply");
+    if (n_rows < 1 || n_rows > SPD_MAX_PAGED_ROWS || n_heads < 1 || n_heads > SPD_MAX_PAGED_HEADS || head_dim < 2 || head_dim > SPD_MAX_HEAD_DIM)
+        return fail(SPD_ERR_SHAPE, "n_rows in 1..%d, n_heads in 1..%d and head_dim in 2..%d required", SPD_MAX_PAGED_ROWS, SPD_MAX_PAGED_HEADS, SPD_MAX_HEAD_DIM);
+    if (flags & ~(SPD_X_IS_BF16 | SPD_ROPE_INVERSE)) return fail(SPD_ERR_INVALID_ARG, "unknown flag bits");
+    const size_t size = flags & SPD_X_IS_BF16 ? 2 : 4;
+    int32_t rc = check_rope(rope, head_dim);
+    if (!rc) rc = check_heads("x", x, n_rows, n_heads, head_dim, size);
+    if (!rc) rc = check_heads("out", out, n_rows, n_heads, head_dim, size);
+    if (rc) return rc;
+    if (x->data == out->data && (x->row_stride != out->row_stride || x->head_stride != out->head_stride)) return fail(SPD_ERR_INVALID_ARG, "out in the place of x has the strides of x");
+    RopeArgs a;
+    a.x = heads_args(x); a.out = heads_args(out); a.rope = {rope->table, rope->rotary_dim, rope->interleaved != 0};
+    a.positions = positions; a.n_rows = n_rows; a.n_heads = n_heads; a.dim = head_dim;
+    a.bf16 = flags & SPD_X_IS_BF16; a.inverse = flags & SPD_ROPE_INVERSE;
+    HIP_TRY(launch_rope(a, (hipStream_t)stream));
+    return SPD_OK;
+}
+
+int32_t spd_paged_append(const spd_paged_cache *cache, const spd_paged_batch *batch, const spd_heads *k, const spd_heads *v, const spd_heads *q, const spd_heads *q_out,
+                         int32_t n_heads, const spd_rope *rope, const int32_t *positions, uint32_t flags, void *stream) {
+    if (!k || !v || !q != !q_out) return fail(SPD_ERR_INVALID_ARG, "NULL argument to spd_paged_append (q and q_out go together)");
+    PagedAppendArgs a{};
+    int32_t rc = check_paged(cache, batch, a.c, a.b);
+    if (rc) return rc;
+    if (flags & ~SPD_X_IS_BF16) return fail(SPD_ERR_INVALID_ARG, "unknown flag bits");
+    if (!rope && (q || positions)) return fail(SPD_ERR_INVALID_ARG, "queries and positions go with rotary positions");
+    const size_t size = flags & SPD_X_IS_BF16 ? 2 : 4;
+    const int rows = batch->n_rows, dim = cache->head_dim;
+    rc = check_heads("k", k, rows, cache->n_kv_heads, dim, size);
+    if (!rc) rc = check_heads("v", v, rows, cache->n_kv_heads, dim, size);
+    if (!rc && rope) rc = check_rope(rope, dim);
+    if (!rc && q) {
+        if (n_heads < 1 || n_heads > SPD_MAX_PAGED_HEADS) return fail(SPD_ERR_SHAPE, "n_heads = %d must be in 1..%d", n_heads, SPD_MAX_PAGED_HEADS);
+        rc = check_heads("q", q, rows, n_heads, dim, size);
+        if (!rc) rc = check_heads("q_out", q_out, rows, n_heads, dim, size);
+        if (!rc && q->data == q_out->data && (q->row_stride != q_out->row_stride || q->head_stride != q_out->head_stride))
+            rc = fail(SPD_ERR_INVALID_ARG, "q_out in the place of q has the strides of q");
+    }
+    if (rc) return rc;
+    a.k = heads_args(k); a.v = heads_args(v);
+    if (q) { a.q = heads_args(q); a.q_out = heads_args(q_out); a.n_heads = n_heads; }
+    if (rope) a.rope = {rope->table, rope->rotary_dim, rope->interleaved != 0};
+    a.positions = positions; a.bf16 = flags & SPD_X_IS_BF16;
+    HIP_TRY(launch_paged_append(a, (hipStream_t)stream));
+    return SPD_OK;
+}
+
+int32_t spd_paged_attention_workspace_bytes(const spd_paged_cache *cache, const spd_paged_batch *batch, int32_t n_heads, size_t *bytes) {
+    if (!bytes) return fail(SPD_ERR_INVALID_ARG, "NULL argument to spd_paged_attention_workspace_bytes");
+    PagedCacheArgs c;
+    PagedBatchArgs b;
+    int32_t rc = check_paged(cache, batch, c, b);
+    if (!rc) rc = check_query_heads(n_heads, c.n_kv);
+    if (rc) return rc;
+    *bytes = paged_attention_workspace_bytes(c, b, n_heads);
+    return SPD_OK;
+}
+
+int32_t spd_paged_attention(const spd_paged_cache *cache, const spd_paged_batch *batch, const spd_heads *q, const spd_heads *out, int32_t n_heads, float scale,
+                            int32_t window, const uint64_t *seen, float *lse_out, uint32_t flags, void *workspace, size_t workspace_bytes, void *stream) {
+    if (!q || !out) return fail(SPD_ERR_INVALID_ARG, "NULL argument to spd_paged_attention");
+    PagedAttentionArgs a{};
+    int32_t rc = check_paged(cache, batch, a.c, a.b);
+    if (!rc) rc = check_query_heads(n_heads, a.c.n_kv);
+    if (rc) return rc;
+    if (flags & ~SPD_X_IS_BF16) return fail(SPD_ERR_INVALID_ARG, "unknown flag bits");
+    const size_t size = flags & SPD_X_IS_BF16 ? 2 : 4;
+    rc = check_heads("q", q, a.b.n_rows, n_heads, a.c.dim, size);
+    if (!rc) rc = check_heads("out", out, a.b.n_rows, n_heads, a.c.dim, size);
+    if (rc) return rc;
+    if (!std::isfinite(scale)) return fail(SPD_ERR_INVALID_ARG, "scale must be finite");
+    if (window < 0) return fail(SPD_ERR_INVALID_ARG, "window must not be negative");
+    if (window && seen) return fail(SPD_ERR_INVALID_ARG, "a window and a tree of rows do not go together");
+    const size_t need = paged_attention_workspace_bytes(a.c, a.b, n_heads);
+    if ((uintptr_t)workspace & 255) return fail(SPD_ERR_INVALID_ARG, "workspace must be 256-byte aligned");
+    if (need && (!workspace || workspace_bytes < need)) return fail(SPD_ERR_CAPACITY, "workspace smaller than spd_paged_attention_workspace_bytes reports");
+    a.q = heads_args(q); a.out = heads_args(out); a.n_heads = n_heads; a.window = window; a.scale = scale; a.seen = seen; a.lse = lse_out;
+    a.bf16 = flags & SPD_X_IS_BF16; a.workspace = workspace;
+    HIP_TRY(launch_paged_attention(a, (hipStream_t)stream));
+    return SPD_OK;
+}
+
+}  // extern "C"

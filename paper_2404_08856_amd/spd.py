@@ -21,7 +21,10 @@ SPD_OK = 0
 SPD_ERR_INVALID_ARG, SPD_ERR_SHAPE, SPD_ERR_CAPACITY, SPD_ERR_HIP = -1, -2, -3, -4
 SPD_TARGET_IS_PROBS, SPD_DRAFT_IS_PROBS = 1, 2
 SPD_ROWS_ARE_PROBS = SPD_W_IS_BF16 = SPD_X_IS_BF16 = 1
+SPD_ROPE_INVERSE = 2
+SPD_ROPE_NONE, SPD_ROPE_LINEAR, SPD_ROPE_RAMP, SPD_ROPE_LOG_RAMP = range(4)
 SPD_MAX_ROWS, SPD_MAX_M, SPD_MAX_TOP = 64, 8, 32
+SPD_MAX_HEAD_DIM, SPD_MAX_PAGED_SEQS, SPD_MAX_PAGED_ROWS, SPD_MAX_PAGED_HEADS, SPD_MAX_PAGED_POSITIONS = 256, 4096, 1 << 20, 1024, 1 << 30
 
 EXPORTS = ["spd_last_error", "spd_model_bytes", "spd_model_create", "spd_model_destroy", "spd_kv_set_len",
            "spd_kv_get_len", "spd_prefill", "spd_prefill_tokens", "spd_verify_forward", "spd_draft_step",
@@ -29,7 +32,8 @@ EXPORTS = ["spd_last_error", "spd_model_bytes", "spd_model_create", "spd_model_d
            "spd_model_set_tuning", "spd_kv_lens_to_device", "spd_kv_lens_from_device", "spd_draft_step_strided",
            "spd_block_finish", "spd_device_status", "spd_speculative_accept_static", "spd_kv_export", "spd_probe_read_chain",
            "spd_model_bytes_q4", "spd_model_create_q4", "spd_q4_bytes", "spd_q4_quantize", "spd_q4_dequantize", "spd_q4_pack",
-           "spd_q4_matmul_workspace_bytes", "spd_q4_matmul", "spd_logprobs_workspace_bytes", "spd_token_logprobs"]
+           "spd_q4_matmul_workspace_bytes", "spd_q4_matmul", "spd_logprobs_workspace_bytes", "spd_token_logprobs",
+           "spd_rope_table_bytes", "spd_rope_table", "spd_rope_apply", "spd_paged_append", "spd_paged_attention_workspace_bytes", "spd_paged_attention"]
 TRACE_KINDS = ["qkv", "o", "gate_up", "down", "lm_head", "attention", "embed"]
 PROJECTIONS = ["qkv", "o", "gate_up", "down", "lm_head"]
 
@@ -77,6 +81,29 @@ class spd_weights_q4(ctypes.Structure):
                 ("mlp_norm", _PP), ("w_gate", _QP), ("w_up", _QP), ("w_down", _QP)]
 
 
+class spd_rope_config(ctypes.Structure):
+    _fields_ = [("rotary_dim", ctypes.c_int32), ("scaling", ctypes.c_int32), ("theta", ctypes.c_float), ("factor", ctypes.c_float), ("low", ctypes.c_float),
+                ("high", ctypes.c_float), ("original_positions", ctypes.c_float), ("magnitude", ctypes.c_float), ("h_factors", ctypes.POINTER(ctypes.c_float))]
+
+
+class spd_rope(ctypes.Structure):
+    _fields_ = [("table", ctypes.c_void_p), ("rotary_dim", ctypes.c_int32), ("interleaved", ctypes.c_int32)]
+
+
+class spd_heads(ctypes.Structure):
+    _fields_ = [("data", ctypes.c_void_p), ("row_stride", ctypes.c_size_t), ("head_stride", ctypes.c_size_t)]
+
+
+class spd_paged_cache(ctypes.Structure):
+    _fields_ = [("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("k_scale", ctypes.c_void_p), ("v_scale", ctypes.c_void_p), ("n_pages", ctypes.c_int32),
+                ("page_size", ctypes.c_int32), ("n_kv_heads", ctypes.c_int32), ("head_dim", ctypes.c_int32), ("e4m3", ctypes.c_int32)]
+
+
+class spd_paged_batch(ctypes.Structure):
+    _fields_ = [("n_seqs", ctypes.c_int32), ("n_rows", ctypes.c_int32), ("max_pages", ctypes.c_int32), ("table_stride", ctypes.c_size_t),
+                ("page_table", ctypes.c_void_p), ("lens", ctypes.c_void_p), ("row_start", ctypes.c_void_p)]
+
+
 _vp, _i32, _f32, _u32, _sz = ctypes.c_void_p, ctypes.c_int32, ctypes.c_float, ctypes.c_uint32, ctypes.c_size_t
 _szp = ctypes.POINTER(ctypes.c_size_t)
 _lib.spd_last_error.restype = ctypes.c_char_p
@@ -115,6 +142,12 @@ _lib.spd_q4_matmul_workspace_bytes.argtypes = [_i32, _i32, _i32, _szp]
 _lib.spd_q4_matmul.argtypes = [_vp, _i32, _i32, _i32, _vp, _sz, _u32, _i32, _vp, _sz, _vp, _sz, _vp]
 _lib.spd_logprobs_workspace_bytes.argtypes = [_i32, _i32, _i32, _szp]
 _lib.spd_token_logprobs.argtypes = [_vp, _sz, _vp, _i32, _i32, _f32, _u32, _vp, _vp, _vp, _i32, _vp, _vp, _vp, _sz, _vp]
+_lib.spd_rope_table_bytes.argtypes = [_i32, _szp]
+_lib.spd_rope_table.argtypes = [_vp, _vp, _sz, _vp]                    # (structures by address: byref objects as they are)
+_lib.spd_rope_apply.argtypes = [_vp, _vp, _vp, _vp, _i32, _i32, _i32, _u32, _vp]
+_lib.spd_paged_append.argtypes = [_vp, _vp, _vp, _vp, _vp, _vp, _i32, _vp, _vp, _u32, _vp]
+_lib.spd_paged_attention_workspace_bytes.argtypes = [_vp, _vp, _i32, _szp]
+_lib.spd_paged_attention.argtypes = [_vp, _vp, _vp, _vp, _i32, _f32, _i32, _vp, _vp, _u32, _vp, _sz, _vp]
 for _name in EXPORTS:
     if _name != "spd_last_error":
         getattr(_lib, _name).restype = _i32
@@ -470,6 +503,132 @@ def spd_q4_matmul(matrix, x, y, workspace=None):
     wp, wn = _scratch(workspace, here)
     assert packed.get_device() == here and not y_bf16, "the matrix is on the current device and y is float32"
     _check(_lib.spd_q4_matmul(packed.data_ptr(), matrix.n, k, matrix.group, xp, xs, SPD_X_IS_BF16 * bf16, rows, yp, ys, wp, wn, _raw_stream(here)))
+
+
+# The handles below keep one ctypes structure each and its address as an integer: a paged call marshals plain numbers.
+_U64 = torch.int64
+
+
+def _heads(t, device, dtype, dim):
+    """spd_heads of a [rows, heads, dim] tensor on the current device whose heads' elements are neighbours (any strides between rows and heads)."""
+    shape, (row, head, step) = t.shape, t.stride()
+    assert t.dtype == dtype and t.get_device() == device and shape[2] == dim and (step == 1 or dim == 1), \
+        f"expected {dtype} [rows, heads, {dim}] on device {device} with contiguous heads, got {t.dtype} {tuple(shape)} with strides {t.stride()} on {t.device}"
+    return spd_heads(t.data_ptr(), row, head)
+
+
+def _row_type(t):
+    dtype = t.dtype
+    assert dtype == _F32 or dtype == _BF16, f"expected float32 or bfloat16, got {dtype}"
+    return dtype, SPD_X_IS_BF16 if dtype == _BF16 else 0
+
+
+class Rope:
+    """Rotary positions: the frequencies' table of spd_rope_table (owned) and how pairs lie in a head.  factors: one divisor per pair, or None."""
+
+    def __init__(self, rotary_dim, theta=10000.0, interleaved=False, scaling=SPD_ROPE_NONE, factor=1.0, low=1.0, high=2.0, original_positions=1.0,
+                 magnitude=1.0, factors=None, device="cuda"):
+        b = ctypes.c_size_t()
+        _check(_lib.spd_rope_table_bytes(rotary_dim, ctypes.byref(b)))
+        assert factors is None or len(factors) == rotary_dim // 2, f"expected {rotary_dim // 2} factors"
+        own = None if factors is None else (ctypes.c_float * len(factors))(*[float(f) for f in factors])
+        cfg = spd_rope_config(rotary_dim, scaling, theta, factor, low, high, original_positions, magnitude, own)
+        self.table = torch.empty(b.value, dtype=torch.uint8, device=device)
+        here = _current_device()
+        _check(_lib.spd_rope_table(ctypes.byref(cfg), *_scratch(self.table, here), _raw_stream(here)))
+        self.rotary_dim, self.interleaved = int(rotary_dim), bool(interleaved)
+        self._struct = spd_rope(self.table.data_ptr(), self.rotary_dim, int(self.interleaved))
+        self._at = ctypes.addressof(self._struct)
+
+
+def spd_rope_apply(rope, x, positions, out, inverse=False):
+    """out [rows, heads, dim] (x itself will do) = x turned by positions [rows] int32."""
+    rows, heads, dim = x.shape
+    here = _current_device()
+    dtype, flags = _row_type(x)
+    assert out.shape == x.shape and rope.table.get_device() == here, f"expected an output of {tuple(x.shape)}, and the table on device {here}"
+    a, b = _heads(x, here, dtype, dim), _heads(out, here, dtype, dim)
+    _check(_lib.spd_rope_apply(rope._at, ctypes.byref(a), ctypes.byref(b), _own(positions, here, _I32, (rows,)), rows, heads, dim,
+                               flags | (SPD_ROPE_INVERSE if inverse else 0), _raw_stream(here)))
+
+
+def paged_cache_shapes(n_pages, page_size, n_kv_heads, head_dim, e4m3=False):
+    """Shapes of the key and value tensors of a paged cache (bfloat16, or float8_e4m3fn)."""
+    G = 16 if e4m3 else 8
+    return (n_pages, n_kv_heads, head_dim // G, page_size, G), (n_pages, n_kv_heads, page_size // G, head_dim, G)
+
+
+class PagedCache:
+    """One layer's pages: k and v as paged_cache_shapes says, bfloat16, or float8_e4m3fn with a scale per head (kept, not copied)."""
+
+    def __init__(self, k, v, k_scale=None, v_scale=None):
+        e4m3 = k.dtype == torch.float8_e4m3fn
+        here = k.get_device()
+        n_pages, heads, granules, page_size, G = k.shape
+        dim = granules * G
+        assert k.dtype == (torch.float8_e4m3fn if e4m3 else _BF16), f"expected bfloat16 or float8_e4m3fn pages, got {k.dtype}"
+        shapes = paged_cache_shapes(n_pages, page_size, heads, dim, e4m3)
+        assert (k_scale is not None and v_scale is not None) == e4m3, "pages in e4m3 have scales, others none"
+        self.k, self.v, self.k_scale, self.v_scale, self.device = k, v, k_scale, v_scale, here
+        self.n_pages, self.page_size, self.n_kv_heads, self.head_dim, self.e4m3 = n_pages, page_size, heads, dim, e4m3
+        self._struct = spd_paged_cache(_own(k, here, k.dtype, shapes[0]), _own(v, here, k.dtype, shapes[1]), _own(k_scale, here, _F32, (heads,)),
+                                       _own(v_scale, here, _F32, (heads,)), n_pages, page_size, heads, dim, int(e4m3))
+        self._at = ctypes.addressof(self._struct)
+
+
+class PagedBatch:
+    """The new rows of a paged call: page_table [n_seqs, max_pages] and lens [n_seqs] int32, row_start [n_seqs + 1] int32 or None (n_rows / n_seqs rows each).
+    The tensors are kept, not copied: what they hold when a call runs counts."""
+
+    def __init__(self, page_table, lens, n_rows, row_start=None):
+        here = page_table.get_device()
+        n_seqs, max_pages = page_table.shape
+        stride, step = page_table.stride()
+        assert page_table.dtype == _I32 and (step == 1 or max_pages <= 1) and (stride >= max_pages or n_seqs <= 1), "a page table is int32 with contiguous rows"
+        self.page_table, self.lens, self.row_start, self.device = page_table, lens, row_start, here
+        self.n_seqs, self.n_rows, self.max_pages = n_seqs, int(n_rows), max_pages
+        self._struct = spd_paged_batch(n_seqs, self.n_rows, max_pages, stride if n_seqs > 1 else max_pages, page_table.data_ptr(),
+                                       _own(lens, here, _I32, (n_seqs,)), _own(row_start, here, _I32, (n_seqs + 1,)))
+        self._at = ctypes.addressof(self._struct)
+
+
+def _paged_here(cache, batch):
+    here = _current_device()
+    assert cache.device == here and batch.device == here, f"the cache (device {cache.device}) and the batch ({batch.device}) are on the current device {here}"
+    return here
+
+
+def spd_paged_append(cache, batch, k, v, rope=None, positions=None, q=None, q_out=None):
+    """k, v [n_rows, n_kv_heads, dim] into their places; with rope, k (and q [n_rows, heads, dim] into q_out) turned by positions, or by the rows' own."""
+    here = _paged_here(cache, batch)
+    rows, dim = batch.n_rows, cache.head_dim
+    dtype, flags = _row_type(k)
+    assert k.shape == v.shape == (rows, cache.n_kv_heads, dim), f"expected keys and values {(rows, cache.n_kv_heads, dim)}, got {tuple(k.shape)} and {tuple(v.shape)}"
+    assert (q is None) == (q_out is None) and (q is None or q.shape == q_out.shape and q.shape[0] == rows), "q and q_out go together, with a row each"
+    assert rope is None or rope.table.get_device() == here, "the table is on the current device"
+    heads = [_heads(t, here, dtype, dim) for t in (k, v) + (() if q is None else (q, q_out))]
+    at = [ctypes.addressof(h) for h in heads] + [None, None]
+    _check(_lib.spd_paged_append(cache._at, batch._at, *at[:4], 0 if q is None else q.shape[1], None if rope is None else rope._at,
+                                 _own(positions, here, _I32, (rows,)), flags, _raw_stream(here)))
+
+
+def spd_paged_attention_workspace_bytes(cache, batch, n_heads):
+    b = ctypes.c_size_t()
+    _check(_lib.spd_paged_attention_workspace_bytes(cache._at, batch._at, n_heads, ctypes.byref(b)))
+    return b.value
+
+
+def spd_paged_attention(cache, batch, q, out, scale=None, window=0, seen=None, lse_out=None, workspace=None):
+    """out [n_rows, heads, dim] = attention of q over the rows' sequences; scale None: 1 / sqrt(dim); seen int64 [n_rows], the bits of new rows that a row sees."""
+    here = _paged_here(cache, batch)
+    rows, heads, dim = q.shape
+    dtype, flags = _row_type(q)
+    assert rows == batch.n_rows and out.shape == q.shape, f"expected {batch.n_rows} rows and an output of {tuple(q.shape)}, got {tuple(out.shape)}"
+    if workspace is None:
+        workspace = torch.empty(spd_paged_attention_workspace_bytes(cache, batch, heads), dtype=torch.uint8, device=q.device)
+    a, b = _heads(q, here, dtype, cache.head_dim), _heads(out, here, dtype, cache.head_dim)
+    _check(_lib.spd_paged_attention(cache._at, batch._at, ctypes.byref(a), ctypes.byref(b), heads, dim ** -0.5 if scale is None else scale, window,
+                                    _own(seen, here, _U64, (rows,)), _own(lse_out, here, _F32, (rows, heads)), flags, *_scratch(workspace, here), _raw_stream(here)))
 
 
 def spd_probe_read_chain(buffer, stage_bytes, reps=20):
