@@ -7,7 +7,9 @@
 // float32 rows: q and p as three bf16 terms each, exact to float32's roundings.  e4m3 keys and values are bf16 values, their scales one factor
 // of a head's scores and of its output.  The rows of the score tiles are keys in such an order that a lane ends with the weights of a whole granule
 // of keys, the 16 bytes of V that it reads for the second product: no data moves between lanes, and every load is 16 bytes of one granule.
+#include <algorithm>
 #include <atomic>
+#include <type_traits>
 
 #include "paged_plan.h"
 
@@ -409,13 +411,400 @@ __global__ __launch_bounds__(256, RT == 1 ? 2 : 1) void paged_few_kernel(PagedAt
     }
 }
 
+// ---- many rows: the waves of a workgroup share tiles of 64 keys in LDS -----------------------------
+// Each wave has 16 RT rows of the tile.  Keys and values come straight into LDS (e4m3: through registers, widened on the way) one tile ahead, in
+// such an order that every operand of the matrix cores is 16 neighbouring granules: place 32 u + 16 n + r of a tile of keys holds key
+// 32 u + 8 (r / 4) + 4 n + r % 4, the row r of score tile n of unit u.
+#pragma clang diagnostic push
+#pragma clang diagnostic ignored "-Winline-asm"
+__device__ __forceinline__ unsigned lds_place(const void *p) { return (unsigned)(uintptr_t)(const __attribute__((address_space(3))) void *)p; }
+// 16 bytes a lane, from any address each, to 1 KiB from dst on
+__device__ __forceinline__ void to_lds(const void *src, unsigned dst) {
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(__builtin_amdgcn_readfirstlane(dst)), "v"(src) : "memory", "m0");
+}
+#pragma clang diagnostic pop
+
+template <int NT, class C, int D, int RT>
+__global__ __launch_bounds__(256, 2) void paged_many_kernel(PagedAttentionArgs a, PagedPlan pl) {
+    constexpr int QT = 64 * RT, G = 16 / sizeof(C), KT = 64, KS = D / 32, DT = D / 16, PT = NT;
+    constexpr bool WIDEN = sizeof(C) == 1;
+    constexpr int LOADS = D / 8 * KT / 256;                          // granules of 16 bytes a thread brings of K, and of V (bf16)
+    __shared__ uint4 k_s[2][D / 8][KT], v_s[2][KT / 8][D];
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), r = lane & 15, g = lane >> 4;
+    const int P = 1 << a.c.page_bits, group = pl.group;
+    const size_t page_bytes = (size_t)a.c.n_kv * P * D * sizeof(C), head_bytes = (size_t)P * D * sizeof(C);
+    const bool q_wide = (uintptr_t)a.q.p % 16 == 0 && (a.q.row | a.q.head) % 8 == 0, out_wide = (uintptr_t)a.out.p % 16 == 0 && (a.out.row | a.out.head) % 4 == 0;
+    const PagedMap<QT> map(a, pl);
+    PagedRuns runs;
+    u64 mine;
+    const u64 all = map.total(mine);
+    if (all == 0) return;
+    runs.init(all, pl.least, gridDim.x);
+    if ((int)blockIdx.x >= runs.n) return;
+    const int eighth = runs.n / 8, w = (int)blockIdx.x < 8 * eighth ? (int)(blockIdx.x % 8 * eighth + blockIdx.x / 8) : (int)blockIdx.x;   // neighbours in the row of tiles on one XCD
+    u64 pos = runs.start(w), before;
+    const u64 end = runs.start(w + 1);
+    int s;
+    map.at(pos, mine, s, before);
+    PagedSeq<QT> seq;
+    seq.init(a, pl, s);
+    const int my_key = (lane & 32) + ((lane & 15) >> 2) * 8 + (lane & 16 ? 4 : 0) + (lane & 3);        // the key of this lane's place
+    while (pos < end) {
+        const u64 off = pos - before, head_cost = seq.before(seq.tiles);
+        if (off >= head_cost * a.c.n_kv) {
+            before += head_cost * a.c.n_kv;
+            do seq.init(a, pl, ++s); while (seq.tiles == 0 && s + 1 < a.b.n_seqs);
+            continue;
+        }
+        const int h = (int)(off / head_cost);
+        const u64 in_head = off - h * head_cost;
+        const int t = seq.tile_at(in_head);
+        const u64 cost = seq.cost(t), x0 = in_head - seq.before(t), x1 = min(cost, x0 + (end - pos));
+        const int packed = seq.n * group, valid = min(QT, packed - t * QT), len = seq.len;
+        const int i_first = t * QT / group, i_last = (t * QT + valid - 1) / group;
+        const int tile_end = a.seen ? min(len + min(seq.n, 64), a.b.capacity) : min(len + i_last + 1, a.b.capacity);
+        const int tile_lo = a.window ? max(0, len + i_first - a.window + 1) / KT * KT : 0;
+        const int steps = tile_end > tile_lo ? (tile_end - tile_lo + KT - 1) / KT : 0;
+        const int j0 = (int)((u64)steps * x0 / cost), j1 = (int)((u64)steps * x1 / cost);
+        // this wave's rows
+        const int row0 = wave * 16 * RT, rows = min(16 * RT, valid - row0);             // (0 or fewer: none)
+        const int wi_first = (t * QT + min(row0, valid - 1)) / group, wi_last = (t * QT + max(0, min(row0 + 16 * RT, valid) - 1)) / group;
+        const int all_hi = a.seen ? len : min(len + wi_first + 1, a.b.capacity), all_lo = a.window ? max(0, len + wi_last - a.window + 1) : 0;
+        const int any_hi = a.seen ? tile_end : min(len + wi_last + 1, a.b.capacity), any_lo = a.window ? max(0, len + wi_first - a.window + 1) : 0;
+        uint4 q[RT][KS][NT];
+        Sees sees[RT];
+#pragma unroll
+        for (int rt = 0; rt < RT; ++rt) {
+            const int pr = min(row0 + 16 * rt + r, valid - 1) + t * QT, i = pr / group, j = pr - i * group;
+            sees[rt].init(a, seq.first, len, i);
+            const size_t at = (size_t)(seq.first + i) * a.q.row + (size_t)(h * group + j) * a.q.head;
+#pragma unroll
+            for (int c = 0; c < KS; ++c) load_query<NT>(a, at + 32 * c + 8 * g, q_wide, q[rt][c]);
+            if (a.scale < 0.f) {
+#pragma unroll
+                for (int c = 0; c < KS; ++c)
+#pragma unroll
+                    for (int i2 = 0; i2 < NT; ++i2) {
+                        uint4 &x = q[rt][c][i2];
+                        x.x ^= 0x80008000u; x.y ^= 0x80008000u; x.z ^= 0x80008000u; x.w ^= 0x80008000u;
+                    }
+            }
+        }
+        const float factor = fabsf(a.scale) * kLog2e * (WIDEN ? a.c.k_scale[h] : 1.0f);
+        f32x4_t acc[RT][DT];
+        float m[RT], l[RT];
+#pragma unroll
+        for (int rt = 0; rt < RT; ++rt) {
+            m[rt] = -INFINITY;
+            l[rt] = 0.f;
+#pragma unroll
+            for (int d = 0; d < DT; ++d) acc[rt][d] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+        }
+        // pages of the step whose loads come next: of this lane's key, and of the granules of values that this wave (e4m3: thread) brings
+        constexpr int VG = WIDEN ? (D == 128 ? 2 : 1) : 2;
+        int k_page = -1, v_page[VG];
+        auto v_granule = [&](int i) { return WIDEN ? (tid + 256 * i) / D * 2 : wave * 2 + i; };        // of 8 keys
+        auto pages = [&](int j) {
+            const int key = tile_lo + j * KT;
+            k_page = paged_page(a.b, a.c, s, (key + my_key) >> a.c.page_bits);
+#pragma unroll
+            for (int i = 0; i < VG; ++i) v_page[i] = paged_page(a.b, a.c, s, (key + v_granule(i) * 8) >> a.c.page_bits);
+        };
+        uint4 kr[WIDEN ? LOADS / 2 : 1], vr[WIDEN ? LOADS / 2 : 1];
+        auto load = [&](int j, int buf) {
+            const int key = tile_lo + j * KT;
+            const char *kp = (const char *)a.c.k + (size_t)max(k_page, 0) * page_bytes + h * head_bytes + (size_t)((key + my_key) & (P - 1)) * 16;
+            if constexpr (WIDEN) {
+#pragma unroll
+                for (int i = 0; i < LOADS / 2; ++i) {
+                    kr[i] = *reinterpret_cast<const uint4 *>(kp + (size_t)(wave + 4 * i) * P * 16);
+                    const int d = (tid + 256 * i) % D, slot = (key + v_granule(i) * 8) & (P - 1);
+                    vr[i] = *reinterpret_cast<const uint4 *>((const char *)a.c.v + (size_t)max(v_page[i], 0) * page_bytes + h * head_bytes + (size_t)(slot / G * D + d) * 16);
+                }
+            } else {
+#pragma unroll
+                for (int i = 0; i < D / 32; ++i) to_lds(kp + (size_t)(wave * (D / 32) + i) * P * 16, lds_place(&k_s[buf][wave * (D / 32) + i][0]));
+#pragma unroll
+                for (int i = 0; i < 2; ++i) {
+                    const int slot = (key + v_granule(i) * 8) & (P - 1);
+                    const char *vp = (const char *)a.c.v + (size_t)max(v_page[i], 0) * page_bytes + h * head_bytes + (size_t)(slot / G * D + lane) * 16;
+#pragma unroll
+                    for (int x = 0; x < D / 64; ++x) to_lds(vp + x * 1024, lds_place(&v_s[buf][wave * 2 + i][64 * x]));
+                }
+            }
+        };
+        auto widen = [&](int buf) {
+            if constexpr (WIDEN) {
+#pragma unroll
+                for (int i = 0; i < LOADS / 2; ++i) {
+                    const int c = wave + 4 * i, d = (tid + 256 * i) % D, gv = v_granule(i);
+                    k_s[buf][2 * c][lane] = operand<C>(kr[i], 0);
+                    k_s[buf][2 * c + 1][lane] = operand<C>(kr[i], 1);
+                    v_s[buf][gv][d] = operand<C>(vr[i], 0);
+                    v_s[buf][gv + 1][d] = operand<C>(vr[i], 1);
+                }
+            }
+        };
+        bool there = true, there_next = true;                        // whether all keys of the step have a place
+        if (j0 < j1) {
+            pages(j0);
+            there_next = __all(k_page >= 0);
+            load(j0, 0);
+            widen(0);
+            if (j0 + 1 < j1) pages(j0 + 1);
+        }
+        for (int j = j0; j < j1; ++j) {
+            const int buf = (j - j0) & 1;
+            asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");      // this wave's part of the step is in LDS, and its reads of the other buffer are done
+            __syncthreads();
+            there = there_next;
+            const bool more = j + 1 < j1;
+            if (more) {
+                there_next = __all(k_page >= 0);
+                load(j + 1, buf ^ 1);
+                if (j + 2 < j1) pages(j + 2);
+            }
+            const int key0 = tile_lo + j * KT;
+            auto step = [&](auto whole_) {
+                constexpr bool WHOLE = decltype(whole_)::value;
+                f32x4_t sc[RT][4];
+#pragma unroll
+                for (int n = 0; n < 4; ++n) {
+                    uint4 kf[KS];
+#pragma unroll
+                    for (int c = 0; c < KS; ++c) kf[c] = k_s[buf][c * 4 + g][16 * n + r];
+#pragma unroll
+                    for (int rt = 0; rt < RT; ++rt) {
+                        sc[rt][n] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                        for (int i = NT - 1; i >= 0; --i)
+#pragma unroll
+                            for (int c = 0; c < KS; ++c) sc[rt][n] = mfma(kf[c], q[rt][c][i], sc[rt][n]);
+                    }
+                }
+                uint32_t seen_bits[RT][2], keep[2][4];
+                bool odd_values = false;
+                if constexpr (!WHOLE) {
+                    uint32_t bad = 0;
+#pragma unroll
+                    for (int u = 0; u < 2; ++u) {
+                        const int key = key0 + 32 * u + 8 * g;
+                        const bool here = paged_page(a.b, a.c, s, key >> a.c.page_bits) >= 0;
+#pragma unroll
+                        for (int rt = 0; rt < RT; ++rt) seen_bits[rt][u] = here ? sees[rt].keys(key, 8, len, tile_end) : 0;
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) {
+                            const int n = here ? min(max(tile_end - key - 2 * i, 0), 2) : 0;
+                            keep[u][i] = n == 2 ? 0xffffffffu : (1u << (16 * n)) - 1;
+                        }
+                        for (int d = 0; d < DT; ++d) {
+                            const uint4 v = v_s[buf][4 * u + g][16 * d + r];
+                            bad |= (((v.x & keep[u][0]) & 0x7f807f80u) + 0x00800080u) | (((v.y & keep[u][1]) & 0x7f807f80u) + 0x00800080u) |
+                                   (((v.z & keep[u][2]) & 0x7f807f80u) + 0x00800080u) | (((v.w & keep[u][3]) & 0x7f807f80u) + 0x00800080u);
+                        }
+                    }
+                    odd_values = __any((bad & 0x80008000u) != 0);
+                }
+                // weights: exponentials above the running maximum by up to 2^8 are let be, the sums are brought to a new maximum only beyond
+#pragma unroll
+                for (int rt = 0; rt < RT; ++rt) {
+                    float top = -INFINITY;
+                    if constexpr (WHOLE) {
+#pragma unroll
+                        for (int n = 0; n < 4; ++n)
+#pragma unroll
+                            for (int i = 0; i < 4; ++i) top = fmaxf(top, sc[rt][n][i]);
+                        top *= factor;
+                    } else {
+#pragma unroll
+                        for (int n = 0; n < 4; ++n)
+#pragma unroll
+                            for (int i = 0; i < 4; ++i) {
+                                const float z = seen_bits[rt][n / 2] >> (n % 2 * 4 + i) & 1 ? sc[rt][n][i] * factor : -INFINITY;
+                                sc[rt][n][i] = z;
+                                top = fmaxf(top, z);
+                            }
+                    }
+                    top = max_over_rows(top);
+                    if (__any(top > m[rt] + 8.0f)) {
+                        top = top > m[rt] + 8.0f ? top : m[rt];           // (a row's result does not depend on the others')
+                        const float shrink = __builtin_amdgcn_exp2f(m[rt] - (top > -INFINITY ? top : 0.f));
+                        m[rt] = top;
+                        l[rt] *= shrink;
+#pragma unroll
+                        for (int d = 0; d < DT; ++d)
+#pragma unroll
+                            for (int i = 0; i < 4; ++i) acc[rt][d][i] *= shrink;
+                    }
+                    const float use = m[rt] > -INFINITY ? m[rt] : 0.f;
+                    float sum = 0.f;
+#pragma unroll
+                    for (int n = 0; n < 4; ++n)
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) {
+                            sc[rt][n][i] = __builtin_amdgcn_exp2f(WHOLE ? __builtin_fmaf(sc[rt][n][i], factor, -use) : sc[rt][n][i] - use);
+                            sum += sc[rt][n][i];
+                        }
+                    l[rt] += sum;
+                }
+#pragma unroll
+                for (int u = 0; u < 2; ++u) {
+                    uint4 p[RT][PT];
+#pragma unroll
+                    for (int rt = 0; rt < RT; ++rt) {
+                        uint32_t words[PT][4];
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) {
+                            float x = sc[rt][2 * u + i / 2][i % 2 * 2], y = sc[rt][2 * u + i / 2][i % 2 * 2 + 1];
+#pragma unroll
+                            for (int k = 0; k < PT; ++k) {
+                                words[k][i] = two_bf16(x, y);
+                                if (k + 1 < PT) {
+                                    x -= bf16_lo(words[k][i]);
+                                    y -= bf16_hi(words[k][i]);
+                                }
+                            }
+                        }
+#pragma unroll
+                        for (int k = 0; k < PT; ++k) p[rt][k] = uint4{words[k][0], words[k][1], words[k][2], words[k][3]};
+                    }
+#pragma unroll
+                    for (int d = 0; d < DT; ++d) {
+                        uint4 v = v_s[buf][4 * u + g][16 * d + r];
+                        if constexpr (!WHOLE) { v.x &= keep[u][0]; v.y &= keep[u][1]; v.z &= keep[u][2]; v.w &= keep[u][3]; }
+                        if (WHOLE || !odd_values) {
+#pragma unroll
+                            for (int rt = 0; rt < RT; ++rt)
+#pragma unroll
+                                for (int k = PT - 1; k >= 0; --k) acc[rt][d] = mfma(v, p[rt][k], acc[rt][d]);
+                        } else {
+#pragma unroll
+                            for (int rt = 0; rt < RT; ++rt)
+#pragma unroll 1
+                                for (int x = 0; x < 16; ++x) {               // one row at a time, with zeros where it does not see
+                                    const uint32_t bits = __shfl(seen_bits[rt][u], 16 * g + x);
+                                    uint4 y = v;
+                                    y.x &= (bits & 1 ? 0xffffu : 0u) | (bits & 2 ? 0xffff0000u : 0u);
+                                    y.y &= (bits & 4 ? 0xffffu : 0u) | (bits & 8 ? 0xffff0000u : 0u);
+                                    y.z &= (bits & 16 ? 0xffffu : 0u) | (bits & 32 ? 0xffff0000u : 0u);
+                                    y.w &= (bits & 64 ? 0xffffu : 0u) | (bits & 128 ? 0xffff0000u : 0u);
+                                    f32x4_t one = acc[rt][d];
+#pragma unroll
+                                    for (int k = PT - 1; k >= 0; --k) one = mfma(y, p[rt][k], one);
+#pragma unroll
+                                    for (int i = 0; i < 4; ++i) acc[rt][d][i] = r == x ? one[i] : acc[rt][d][i];
+                                }
+                        }
+                    }
+                }
+            };
+            if (rows > 0 && key0 < any_hi && key0 + KT > any_lo) {
+                if (there && key0 >= all_lo && key0 + KT <= all_hi) step(std::integral_constant<bool, true>());
+                else step(std::integral_constant<bool, false>());
+            }
+            if (more) widen(buf ^ 1);
+        }
+        __syncthreads();                                              // the next tile's loads write what other waves may still read
+        // ---- results
+        const bool alone = x0 == 0 && x1 == cost;
+        const u64 item = pos - x0;
+        const int wa = alone ? w : runs.of(item), wb = alone ? w : runs.of(item + cost - 1);
+        constexpr int kSlot = QT * (D + 2);
+        float *slot = pl.slots + (size_t)(2 * w + (w == wa)) * kSlot;
+        const float v_scale = WIDEN ? a.c.v_scale[h] : 1.0f;
+        auto finish = [&](int rt) {
+            if (16 * rt + r >= rows) return;
+            const int pr = t * QT + row0 + 16 * rt + r, i = pr / group, j = pr - i * group;
+            const bool empty = m[rt] == -INFINITY && l[rt] == 0.f;
+            const float by = empty ? 0.f : v_scale / l[rt];
+            const size_t at = (size_t)(seq.first + i) * a.out.row + (size_t)(h * group + j) * a.out.head + 4 * g;
+#pragma unroll
+            for (int d = 0; d < DT; ++d) {
+                float o[4];
+#pragma unroll
+                for (int k = 0; k < 4; ++k) o[k] = empty ? 0.f : acc[rt][d][k] * by;
+                store_output<NT>(a, at + 16 * d, out_wide, o);
+            }
+            if (a.lse && g == 0) a.lse[(size_t)(seq.first + i) * a.n_heads + h * group + j] = empty ? -INFINITY : (m[rt] + __log2f(l[rt])) * kLn2;
+        };
+#pragma unroll
+        for (int rt = 0; rt < RT; ++rt) {
+            l[rt] = xor_reduce<32, 16>(l[rt], AddOp());
+            if (alone) {
+                finish(rt);
+            } else if (16 * rt + r < rows) {
+                const int row = row0 + 16 * rt + r;
+#pragma unroll
+                for (int d = 0; d < DT; ++d)
+#pragma unroll
+                    for (int k = 0; k < 4; k += 2) {
+                        const u64 two = (u64)__float_as_uint(acc[rt][d][k + 1]) << 32 | __float_as_uint(acc[rt][d][k]);
+                        __hip_atomic_store(reinterpret_cast<u64 *>(slot + row * D + 16 * d + 4 * g + k), two, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+                    }
+                if (g == 0) {
+                    agent_store(slot + QT * D + row, m[rt]);
+                    agent_store(slot + QT * D + QT + row, l[rt]);
+                }
+            }
+        }
+        if (!alone) {
+            asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+            __syncthreads();
+            if (tid == 0) {
+                __hip_atomic_store(pl.flags + 2 * w + (w == wa), pl.number, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+                asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+            }
+            __syncthreads();
+            bool all_there = true;
+            for (int k = wa + tid; k <= wb; k += 256)
+                all_there &= __hip_atomic_load(pl.flags + 2 * k + (k == wa), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == pl.number;
+            if (__syncthreads_and(all_there)) {
+#pragma unroll
+                for (int rt = 0; rt < RT; ++rt) {
+                    if (16 * rt + r >= rows) continue;
+                    const int row = row0 + 16 * rt + r;
+                    float top = -INFINITY, sum = 0.f;
+                    for (int k = wa; k <= wb; ++k) top = fmaxf(top, agent_load(pl.slots + (size_t)(2 * k + (k == wa)) * kSlot + QT * D + row));
+                    const float use = top > -INFINITY ? top : 0.f;
+#pragma unroll
+                    for (int d = 0; d < DT; ++d) acc[rt][d] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+                    for (int k = wa; k <= wb; ++k) {
+                        const float *part = pl.slots + (size_t)(2 * k + (k == wa)) * kSlot;
+                        const float f = __builtin_amdgcn_exp2f(agent_load(part + QT * D + row) - use);
+                        sum = __builtin_fmaf(agent_load(part + QT * D + QT + row), f, sum);
+                        u64 x[DT][2];
+#pragma unroll
+                        for (int d = 0; d < DT; ++d)
+#pragma unroll
+                            for (int e = 0; e < 2; ++e)
+                                x[d][e] = __hip_atomic_load(reinterpret_cast<const u64 *>(part + row * D + 16 * d + 4 * g + 2 * e), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+#pragma unroll
+                        for (int d = 0; d < DT; ++d)
+#pragma unroll
+                            for (int e = 0; e < 2; ++e) {
+                                acc[rt][d][2 * e] = __builtin_fmaf(__uint_as_float((unsigned)x[d][e]), f, acc[rt][d][2 * e]);
+                                acc[rt][d][2 * e + 1] = __builtin_fmaf(__uint_as_float((unsigned)(x[d][e] >> 32)), f, acc[rt][d][2 * e + 1]);
+                            }
+                    }
+                    m[rt] = top;
+                    l[rt] = sum;
+                    finish(rt);
+                }
+                for (int k = wa + tid; k <= wb; k += 256) __hip_atomic_store(pl.flags + 2 * k + (k == wa), 0ull, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+            }
+        }
+        pos += x1 - x0;
+    }
+}
+
 // ---- launches -----------------------------------------------------------------------
 
-constexpr int kFewGroups = 512;              // workgroups at most
+constexpr int kGroups = 512;                 // workgroups at most
+constexpr int kFewUpto = 64;                 // packed rows of a sequence that the kernel of few rows takes at most
 static size_t slot_floats(int QT, int dim) { return (size_t)QT * (dim + 2); }
 
 size_t paged_attention_workspace_bytes(const PagedCacheArgs &c, const PagedBatchArgs &, int) {
-    return 2 * kFewGroups * sizeof(u64) + 2 * kFewGroups * slot_floats(64, c.dim) * sizeof(float);
+    return 2 * kGroups * sizeof(u64) + 2 * kGroups * slot_floats(128, c.dim) * sizeof(float);
 }
 
 // A number that no workspace holds by chance, another one each call
@@ -433,17 +822,25 @@ hipError_t launch_paged_attention(const PagedAttentionArgs &a, hipStream_t strea
     pl.number = call_number();
     pl.group = a.n_heads / a.c.n_kv;
     pl.flags = (u64 *)a.workspace;
-    pl.slots = (float *)(pl.flags + 2 * kFewGroups);
-    pl.above = 0;
-    pl.upto = 0x7fffffff;
-    pl.least = 192;
-    const int packed = (a.b.n_rows + a.b.n_seqs - 1) / a.b.n_seqs * pl.group;
+    pl.slots = (float *)(pl.flags + 2 * kGroups);
+    // Rows of a sequence at most, as far as the host can tell: all, or, as long as no sequence is without any, all but one of each other.  What it
+    // says chooses kernels; a kernel that is alone takes every sequence.
+    const int most = a.b.row_start ? std::max(1, a.b.n_rows - a.b.n_seqs + 1) : a.b.each;
+    const bool few = most * pl.group <= kFewUpto, many = !few && (!a.b.row_start || a.b.n_seqs == 1);
+    const int mean = (a.b.n_rows + a.b.n_seqs - 1) / a.b.n_seqs * pl.group;
 #define SPD_FEW(NT, C, D, RT)  hipLaunchKernelGGL((paged_few_kernel<NT, C, D, RT>), dim3(RT == 1 ? 512 : 256), dim3(256), 0, stream, a, pl)
 #define SPD_FEW_RT(NT, C, D)                                                                                                 \
     do {                                                                                                                     \
-        if (packed <= 16) SPD_FEW(NT, C, D, 1);                                                                              \
-        else if (packed <= 32 || NT == 3) SPD_FEW(NT, C, D, 2);                                                              \
-        else SPD_FEW(NT, C, D, (NT == 3 ? 2 : 4));                                                                           \
+        if (!many) {                                                                                                         \
+            pl.above = 0; pl.upto = few ? 0x7fffffff : kFewUpto; pl.least = 192;                                             \
+            if (std::min(mean, kFewUpto) <= 16) SPD_FEW(NT, C, D, 1);                                                        \
+            else if (mean <= 32 || NT == 3) SPD_FEW(NT, C, D, 2);                                                            \
+            else SPD_FEW(NT, C, D, (NT == 3 ? 2 : 4));                                                                       \
+        }                                                                                                                    \
+        if (!few) {                                                                                                          \
+            pl.above = many ? 0 : kFewUpto; pl.upto = 0x7fffffff; pl.least = 512;                                            \
+            hipLaunchKernelGGL((paged_many_kernel<NT, C, D, 2>), dim3(kGroups), dim3(256), 0, stream, a, pl);                \
+        }                                                                                                                    \
     } while (0)
 #define SPD_FEW_D(NT, C) do { if (a.c.dim == 64) SPD_FEW_RT(NT, C, 64); else SPD_FEW_RT(NT, C, 128); } while (0)
     if (a.bf16 && a.c.e4m3) SPD_FEW_D(1, uint8_t);

@@ -12,6 +12,11 @@ namespace spd {
 
 typedef unsigned long long u64;
 
+// lane l's value, in scalar registers
+__device__ __forceinline__ u64 lane_value(u64 x, int l) {
+    return (u64)(unsigned)__builtin_amdgcn_readlane((int)(x >> 32), l) << 32 | (unsigned)__builtin_amdgcn_readlane((int)x, l);
+}
+
 struct PagedPlan {
     u64 number;              // of the call: what a flag of this call carries
     u64 least;               // cost of a workgroup at least
@@ -93,8 +98,8 @@ struct PagedMap {
     __device__ __forceinline__ u64 total(u64 &mine) const {      // mine: this lane's prefix over the first 64 sequences, itself included
         const int lane = threadIdx.x & 63;
         mine = scan(cost_of(lane), lane);
-        u64 sum = __shfl(mine, 63);
-        for (int s = 64; s < a.b.n_seqs; s += 64) sum += __shfl(scan(cost_of(s + lane), lane), 63);
+        u64 sum = lane_value(mine, 63);
+        for (int s = 64; s < a.b.n_seqs; s += 64) sum += lane_value(scan(cost_of(s + lane), lane), 63);
         return sum;
     }
     __device__ __forceinline__ void at(u64 x, u64 mine, int &s, u64 &before) const {
@@ -106,10 +111,10 @@ struct PagedMap {
             if (hit || s0 + 64 >= a.b.n_seqs) {
                 const int l = hit ? __builtin_ctzll(hit) : 63;   // (x is below the total: there is a hit)
                 s = s0 + l;
-                before = l ? __shfl(upto, l - 1) : base;
+                before = l ? lane_value(upto, l - 1) : base;
                 return;
             }
-            base = __shfl(upto, 63);
+            base = lane_value(upto, 63);
         }
     }
 };
