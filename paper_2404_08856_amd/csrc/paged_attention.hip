@@ -105,47 +105,47 @@ struct Sees {
 // ---- few rows: the waves of a workgroup share a tile's keys ----------------------------------------
 // A wave takes units of four granules of keys (32 in bf16, 64 in e4m3), one in four of the workgroup's run.  The registers of K and V are filled again for the
 // wave's next unit as soon as the product has read them.
-template <int NT, class C, int D, int RT>
-__global__ __launch_bounds__(256, RT == 1 ? 2 : 1) void paged_few_kernel(PagedAttentionArgs a, PagedPlan pl) {
+template <int NT, class C, int D, int RT, int NW>
+__global__ __launch_bounds__(NW * 64, NW / 4) void paged_few_kernel(PagedAttentionArgs a, PagedPlan pl) {
     constexpr int QT = 16 * RT, G = 16 / sizeof(C), UK = 4 * G, HALVES = G / 8, NK = 2 * HALVES;   // NK: score tiles of a unit
-    constexpr int KS = D / 32, KL = D / (4 * G), DT = D / 16, PT = NT == 1 ? 2 : 3;                 // K-steps, loads a key row, output tiles, terms of a weight
-    __shared__ float o_s[4][QT][D + 4], m_s[4][QT], l_s[4][QT];
+    constexpr int KS = D / 32, KL = D / (4 * G), DT = D / 16, PT = NT;                              // K-steps, loads a key row, output tiles, terms of a weight
+    __shared__ float o_s[NW][QT][D + 4], m_s[NW][QT], l_s[NW][QT];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), r = lane & 15, g = lane >> 4;
     const int P = 1 << a.c.page_bits, group = pl.group;
     const size_t page_bytes = (size_t)a.c.n_kv * P * D * sizeof(C), head_bytes = (size_t)P * D * sizeof(C);
     const bool q_wide = (uintptr_t)a.q.p % 16 == 0 && (a.q.row | a.q.head) % 8 == 0, out_wide = (uintptr_t)a.out.p % 16 == 0 && (a.out.row | a.out.head) % 4 == 0;
     const PagedMap<QT> map(a, pl);
     PagedRuns runs;
-    u64 mine;
-    const u64 all = map.total(mine);
+    unsigned mine;
+    const unsigned all = map.total(mine);
     if (all == 0) return;
     runs.init(all, pl.least, gridDim.x);
     const int w = blockIdx.x;
     if (w >= runs.n) return;
-    u64 pos = runs.start(w), before;
-    const u64 end = runs.start(w + 1);
+    unsigned pos = runs.start(w), before;
+    const unsigned end = runs.start(w + 1);
     int s;
     map.at(pos, mine, s, before);
     PagedSeq<QT> seq;
     seq.init(a, pl, s);
     while (pos < end) {
-        const u64 off = pos - before, head_cost = seq.before(seq.tiles);
+        const unsigned off = pos - before, head_cost = seq.whole;
         if (off >= head_cost * a.c.n_kv) {                          // the next sequence with rows for this kernel
             before += head_cost * a.c.n_kv;
             do seq.init(a, pl, ++s); while (seq.tiles == 0 && s + 1 < a.b.n_seqs);
             continue;
         }
         const int h = (int)(off / head_cost);
-        const u64 in_head = off - h * head_cost;
+        const unsigned in_head = off - h * head_cost;
         const int t = seq.tile_at(in_head);
-        const u64 cost = seq.cost(t), x0 = in_head - seq.before(t), x1 = min(cost, x0 + (end - pos));
+        const unsigned cost = seq.cost(t), x0 = in_head - seq.before(t), x1 = min(cost, x0 + (end - pos));
         // ---- the tile: packed rows t * QT .. , keys of all its rows
         const int packed = seq.n * group, valid = min(QT, packed - t * QT);
         const int i_first = t * QT / group, i_last = (t * QT + valid - 1) / group, len = seq.len;
         const int tile_end = a.seen ? min(len + min(seq.n, 64), a.b.capacity) : min(len + i_last + 1, a.b.capacity);
         const int tile_lo = a.window ? max(0, len + i_first - a.window + 1) / UK * UK : 0;
         const int units = tile_end > tile_lo ? (tile_end - tile_lo + UK - 1) / UK : 0;
-        const int u0 = (int)((u64)units * x0 / cost), u1 = (int)((u64)units * x1 / cost);
+        const int u0 = units_before(units, x0, cost), u1 = units_before(units, x1, cost);
         // a unit of keys all_lo .. all_hi - 1 is seen whole by every row
         const int all_hi = a.seen ? len : min(len + i_first + 1, a.b.capacity), all_lo = a.window ? max(0, len + i_last - a.window + 1) : 0;
         uint4 q[RT][KS][NT];
@@ -196,22 +196,25 @@ __global__ __launch_bounds__(256, RT == 1 ? 2 : 1) void paged_few_kernel(PagedAt
             load_v(u);
         }
         bool there = v_page >= 0;                                   // this lane's granule of the unit at hand
-        if (u + 4 < u1) pages(u + 4);
-        for (; u < u1; u += 4) {
-            const bool more = u + 4 < u1;
+        if (u + NW < u1) pages(u + NW);
+        for (; u < u1; u += NW) {
+            const bool more = u + NW < u1;
             const int key0 = tile_lo + u * UK, key = key0 + g * G;   // key: of this lane's weights
             f32x4_t sc[RT][NK];
 #pragma unroll
-            for (int rt = 0; rt < RT; ++rt)
+            for (int n = 0; n < NK; ++n) {
 #pragma unroll
-                for (int n = 0; n < NK; ++n) {
-                    sc[rt][n] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+                for (int rt = 0; rt < RT; ++rt) sc[rt][n] = f32x4_t{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-                    for (int i = NT - 1; i >= 0; --i)
+                for (int c = 0; c < KS; ++c) {
+                    const uint4 k = operand<C>(kf[n][c / HALVES], c % HALVES);
 #pragma unroll
-                        for (int c = 0; c < KS; ++c) sc[rt][n] = mfma(operand<C>(kf[n][c / HALVES], c % HALVES), q[rt][c][i], sc[rt][n]);
+                    for (int rt = 0; rt < RT; ++rt)
+#pragma unroll
+                        for (int i = NT - 1; i >= 0; --i) sc[rt][n] = mfma(k, q[rt][c][i], sc[rt][n]);
                 }
-            if (more) load_k(u + 4);
+            }
+            if (more) load_k(u + NW);
             const bool whole = key0 >= all_lo && key0 + UK <= all_hi && __all(there);
             uint32_t seen_bits[RT];                                  // bit e: key + e
             bool odd_values = false;
@@ -309,7 +312,9 @@ __global__ __launch_bounds__(256, RT == 1 ? 2 : 1) void paged_few_kernel(PagedAt
                             for (int i = 0; i < 4; ++i) keep[i] = (bits >> (8 * hv + 2 * i) & 1 ? 0xffffu : 0u) | (bits >> (8 * hv + 2 * i) & 2 ? 0xffff0000u : 0u);
 #pragma unroll
                             for (int d = 0; d < DT; ++d) {
-                                uint4 v = operand<C>(vf[d], hv);
+                                uint4 raw = vf[d];                   // (widened here each time: as many registers again otherwise)
+                                asm volatile("" : "+v"(raw.x), "+v"(raw.y), "+v"(raw.z), "+v"(raw.w));
+                                uint4 v = operand<C>(raw, hv);
                                 v.x &= keep[0]; v.y &= keep[1]; v.z &= keep[2]; v.w &= keep[3];
                                 f32x4_t one = acc[rt][d];            // (the other columns of the product are not theirs)
 #pragma unroll
@@ -321,8 +326,8 @@ __global__ __launch_bounds__(256, RT == 1 ? 2 : 1) void paged_few_kernel(PagedAt
                     }
             }
             there = v_page >= 0;
-            if (more) load_v(u + 4);
-            if (u + 8 < u1) pages(u + 8);
+            if (more) load_v(u + NW);
+            if (u + 2 * NW < u1) pages(u + 2 * NW);
         }
         // ---- the waves' parts
 #pragma unroll
@@ -334,7 +339,7 @@ __global__ __launch_bounds__(256, RT == 1 ? 2 : 1) void paged_few_kernel(PagedAt
         }
         __syncthreads();
         const bool alone = x0 == 0 && x1 == cost;
-        const u64 item = pos - x0;
+        const unsigned item = pos - x0;
         const int wa = alone ? w : runs.of(item), wb = alone ? w : runs.of(item + cost - 1);
         constexpr int kSlot = QT * (D + 2);
         float *slot = pl.slots + (size_t)(2 * w + (w == wa)) * kSlot;
@@ -348,14 +353,14 @@ __global__ __launch_bounds__(256, RT == 1 ? 2 : 1) void paged_few_kernel(PagedAt
             store_output<NT>(a, (size_t)(seq.first + i) * a.out.row + (size_t)(h * group + j) * a.out.head + d, out_wide, o);
             if (a.lse && d == 0) a.lse[(size_t)(seq.first + i) * a.n_heads + h * group + j] = empty ? -INFINITY : (top + __log2f(sum)) * kLn2;
         };
-        for (int idx = tid; idx < valid * (D / 4); idx += 256) {
+        for (int idx = tid; idx < valid * (D / 4); idx += NW * 64) {
             const int row = idx / (D / 4), d = idx % (D / 4) * 4;
             float top = m_s[0][row], sum = 0.f, o[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-            for (int k = 1; k < 4; ++k) top = fmaxf(top, m_s[k][row]);
+            for (int k = 1; k < NW; ++k) top = fmaxf(top, m_s[k][row]);
             const float use = top > -INFINITY ? top : 0.f;
 #pragma unroll
-            for (int k = 0; k < 4; ++k) {
+            for (int k = 0; k < NW; ++k) {
                 const float f = __builtin_amdgcn_exp2f(m_s[k][row] - use);
                 const float4 x = *reinterpret_cast<const float4 *>(&o_s[k][row][d]);
                 sum = __builtin_fmaf(l_s[k][row], f, sum);
@@ -368,7 +373,8 @@ __global__ __launch_bounds__(256, RT == 1 ? 2 : 1) void paged_few_kernel(PagedAt
                 finish(row, d, top, sum, o);
             } else {
 #pragma unroll
-                for (int k = 0; k < 4; ++k) agent_store(slot + row * D + d + k, o[k]);
+                for (int k = 0; k < 2; ++k)
+                    __hip_atomic_store(reinterpret_cast<u64 *>(slot + row * D + d) + k, (u64)__float_as_uint(o[2 * k + 1]) << 32 | __float_as_uint(o[2 * k]), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
                 if (d == 0) {
                     agent_store(slot + QT * D + row, top);
                     agent_store(slot + QT * D + QT + row, sum);
@@ -385,24 +391,39 @@ __global__ __launch_bounds__(256, RT == 1 ? 2 : 1) void paged_few_kernel(PagedAt
             }
             __syncthreads();
             bool all_there = true;
-            for (int k = wa + tid; k <= wb; k += 256)
+            for (int k = wa + tid; k <= wb; k += NW * 64)
                 all_there &= __hip_atomic_load(pl.flags + 2 * k + (k == wa), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == pl.number;
             if (__syncthreads_and(all_there)) {                     // (two may find so: they write the same)
-                for (int idx = tid; idx < valid * (D / 4); idx += 256) {
+                for (int idx = tid; idx < valid * (D / 4); idx += NW * 64) {
                     const int row = idx / (D / 4), d = idx % (D / 4) * 4;
                     float top = -INFINITY, sum = 0.f, o[4] = {0.f, 0.f, 0.f, 0.f};
-                    for (int k = wa; k <= wb; ++k) top = fmaxf(top, agent_load(pl.slots + (size_t)(2 * k + (k == wa)) * kSlot + QT * D + row));
-                    const float use = top > -INFINITY ? top : 0.f;
-                    for (int k = wa; k <= wb; ++k) {
-                        const float *part = pl.slots + (size_t)(2 * k + (k == wa)) * kSlot;
-                        const float f = __builtin_amdgcn_exp2f(agent_load(part + QT * D + row) - use);
-                        sum = __builtin_fmaf(agent_load(part + QT * D + QT + row), f, sum);
+                    constexpr int B = 4;                              // parts whose loads are on their way together
+                    for (int k0 = wa; k0 <= wb; k0 += B) {
+                        float pm[B], ps[B];
+                        u64 po[B][2];
 #pragma unroll
-                        for (int e = 0; e < 4; ++e) o[e] = __builtin_fmaf(agent_load(part + row * D + d + e), f, o[e]);
+                        for (int k = 0; k < B; ++k) {
+                            const int from = min(k0 + k, wb);
+                            const float *part = pl.slots + (size_t)(2 * from + (from == wa)) * kSlot;
+                            pm[k] = agent_load(part + QT * D + row);
+                            ps[k] = agent_load(part + QT * D + QT + row);
+#pragma unroll
+                            for (int e = 0; e < 2; ++e) po[k][e] = __hip_atomic_load(reinterpret_cast<const u64 *>(part + row * D + d) + e, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+                        }
+#pragma unroll
+                        for (int k = 0; k < B; ++k) {
+                            const float x = k0 + k <= wb ? pm[k] : -INFINITY, higher = fmaxf(top, x), use = higher > -INFINITY ? higher : 0.f;
+                            const float f = __builtin_amdgcn_exp2f(x - use), shrink = __builtin_amdgcn_exp2f(top - use);
+                            top = higher;
+                            if (k0 + k > wb) continue;
+                            sum = __builtin_fmaf(ps[k], f, sum * shrink);
+#pragma unroll
+                            for (int e = 0; e < 4; ++e) o[e] = __builtin_fmaf(__uint_as_float((unsigned)(po[k][e / 2] >> (e % 2 * 32))), f, o[e] * shrink);
+                        }
                     }
                     finish(row, d, top, sum, o);
                 }
-                for (int k = wa + tid; k <= wb; k += 256)            // for the next call that carries this number (a replay)
+                for (int k = wa + tid; k <= wb; k += NW * 64)            // for the next call that carries this number (a replay)
                     __hip_atomic_store(pl.flags + 2 * k + (k == wa), 0ull, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
             }
         }
@@ -436,36 +457,36 @@ __global__ __launch_bounds__(256, 2) void paged_many_kernel(PagedAttentionArgs a
     const bool q_wide = (uintptr_t)a.q.p % 16 == 0 && (a.q.row | a.q.head) % 8 == 0, out_wide = (uintptr_t)a.out.p % 16 == 0 && (a.out.row | a.out.head) % 4 == 0;
     const PagedMap<QT> map(a, pl);
     PagedRuns runs;
-    u64 mine;
-    const u64 all = map.total(mine);
+    unsigned mine;
+    const unsigned all = map.total(mine);
     if (all == 0) return;
     runs.init(all, pl.least, gridDim.x);
     if ((int)blockIdx.x >= runs.n) return;
     const int eighth = runs.n / 8, w = (int)blockIdx.x < 8 * eighth ? (int)(blockIdx.x % 8 * eighth + blockIdx.x / 8) : (int)blockIdx.x;   // neighbours in the row of tiles on one XCD
-    u64 pos = runs.start(w), before;
-    const u64 end = runs.start(w + 1);
+    unsigned pos = runs.start(w), before;
+    const unsigned end = runs.start(w + 1);
     int s;
     map.at(pos, mine, s, before);
     PagedSeq<QT> seq;
     seq.init(a, pl, s);
     const int my_key = (lane & 32) + ((lane & 15) >> 2) * 8 + (lane & 16 ? 4 : 0) + (lane & 3);        // the key of this lane's place
     while (pos < end) {
-        const u64 off = pos - before, head_cost = seq.before(seq.tiles);
+        const unsigned off = pos - before, head_cost = seq.whole;
         if (off >= head_cost * a.c.n_kv) {
             before += head_cost * a.c.n_kv;
             do seq.init(a, pl, ++s); while (seq.tiles == 0 && s + 1 < a.b.n_seqs);
             continue;
         }
         const int h = (int)(off / head_cost);
-        const u64 in_head = off - h * head_cost;
+        const unsigned in_head = off - h * head_cost;
         const int t = seq.tile_at(in_head);
-        const u64 cost = seq.cost(t), x0 = in_head - seq.before(t), x1 = min(cost, x0 + (end - pos));
+        const unsigned cost = seq.cost(t), x0 = in_head - seq.before(t), x1 = min(cost, x0 + (end - pos));
         const int packed = seq.n * group, valid = min(QT, packed - t * QT), len = seq.len;
         const int i_first = t * QT / group, i_last = (t * QT + valid - 1) / group;
         const int tile_end = a.seen ? min(len + min(seq.n, 64), a.b.capacity) : min(len + i_last + 1, a.b.capacity);
         const int tile_lo = a.window ? max(0, len + i_first - a.window + 1) / KT * KT : 0;
         const int steps = tile_end > tile_lo ? (tile_end - tile_lo + KT - 1) / KT : 0;
-        const int j0 = (int)((u64)steps * x0 / cost), j1 = (int)((u64)steps * x1 / cost);
+        const int j0 = units_before(steps, x0, cost), j1 = units_before(steps, x1, cost);
         // this wave's rows
         const int row0 = wave * 16 * RT, rows = min(16 * RT, valid - row0);             // (0 or fewer: none)
         const int wi_first = (t * QT + min(row0, valid - 1)) / group, wi_last = (t * QT + max(0, min(row0 + 16 * RT, valid) - 1)) / group;
@@ -707,7 +728,7 @@ __global__ __launch_bounds__(256, 2) void paged_many_kernel(PagedAttentionArgs a
         __syncthreads();                                              // the next tile's loads write what other waves may still read
         // ---- results
         const bool alone = x0 == 0 && x1 == cost;
-        const u64 item = pos - x0;
+        const unsigned item = pos - x0;
         const int wa = alone ? w : runs.of(item), wb = alone ? w : runs.of(item + cost - 1);
         constexpr int kSlot = QT * (D + 2);
         float *slot = pl.slots + (size_t)(2 * w + (w == wa)) * kSlot;
@@ -828,17 +849,30 @@ hipError_t launch_paged_attention(const PagedAttentionArgs &a, hipStream_t strea
     const int most = a.b.row_start ? std::max(1, a.b.n_rows - a.b.n_seqs + 1) : a.b.each;
     const bool few = most * pl.group <= kFewUpto, many = !few && (!a.b.row_start || a.b.n_seqs == 1);
     const int mean = (a.b.n_rows + a.b.n_seqs - 1) / a.b.n_seqs * pl.group;
-#define SPD_FEW(NT, C, D, RT)  hipLaunchKernelGGL((paged_few_kernel<NT, C, D, RT>), dim3(RT == 1 ? 512 : 256), dim3(256), 0, stream, a, pl)
+    // costs in 31 bits: the tiles of all heads, each of no more than this many keys
+    auto costs = [&](int QT, int keys) {
+        const u64 tiles = ((u64)a.b.n_rows * pl.group / QT + a.b.n_seqs) * a.c.n_kv, span = (u64)a.b.capacity + a.b.n_rows + 2 * QT + 64;
+        pl.shift = 0;
+        while (tiles * ((span >> pl.shift) + 2) >> 31) ++pl.shift;
+        pl.least = std::max(1, keys >> pl.shift);
+    };
+    const int wide = few ? std::min(most * pl.group, kFewUpto) : mean;
+#define SPD_FEW(NT, C, D, RT, NW)                                                                                            \
+    do {                                                                                                                     \
+        costs(16 * RT, 640);                                                                                                 \
+        hipLaunchKernelGGL((paged_few_kernel<NT, C, D, RT, NW>), dim3(256), dim3(NW * 64), 0, stream, a, pl);                \
+    } while (0)
 #define SPD_FEW_RT(NT, C, D)                                                                                                 \
     do {                                                                                                                     \
         if (!many) {                                                                                                         \
-            pl.above = 0; pl.upto = few ? 0x7fffffff : kFewUpto; pl.least = 192;                                             \
-            if (std::min(mean, kFewUpto) <= 16) SPD_FEW(NT, C, D, 1);                                                        \
-            else if (mean <= 32 || NT == 3) SPD_FEW(NT, C, D, 2);                                                            \
-            else SPD_FEW(NT, C, D, (NT == 3 ? 2 : 4));                                                                       \
+            pl.above = 0; pl.upto = few ? 0x7fffffff : kFewUpto;                                                             \
+            if (wide <= 16) SPD_FEW(NT, C, D, 1, 8);                                                                         \
+            else if (wide <= 32 || NT == 3) SPD_FEW(NT, C, D, 2, 4);                                                         \
+            else SPD_FEW(NT, C, D, (NT == 3 ? 2 : 4), 4);                                                                    \
         }                                                                                                                    \
         if (!few) {                                                                                                          \
-            pl.above = many ? 0 : kFewUpto; pl.upto = 0x7fffffff; pl.least = 512;                                            \
+            pl.above = many ? 0 : kFewUpto; pl.upto = 0x7fffffff;                                                            \
+            costs(128, 512);                                                                                                 \
             hipLaunchKernelGGL((paged_many_kernel<NT, C, D, 2>), dim3(kGroups), dim3(256), 0, stream, a, pl);                \
         }                                                                                                                    \
     } while (0)

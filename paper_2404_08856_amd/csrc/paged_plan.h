@@ -12,14 +12,10 @@ namespace spd {
 
 typedef unsigned long long u64;
 
-// lane l's value, in scalar registers
-__device__ __forceinline__ u64 lane_value(u64 x, int l) {
-    return (u64)(unsigned)__builtin_amdgcn_readlane((int)(x >> 32), l) << 32 | (unsigned)__builtin_amdgcn_readlane((int)x, l);
-}
-
 struct PagedPlan {
     u64 number;              // of the call: what a flag of this call carries
-    u64 least;               // cost of a workgroup at least
+    unsigned least;          // cost of a workgroup at least
+    int shift;               // a cost counts 2^shift keys, so that the whole fits 31 bits
     int group;               // query heads of a key head
     int above, upto;         // takes the sequences with so many packed rows: above < rows <= upto
     u64 *flags;              // [2 * workgroups]
@@ -29,10 +25,8 @@ struct PagedPlan {
 // A sequence as one kernel sees it
 template <int QT>
 struct PagedSeq {
-    static constexpr int kStart = 64;      // cost of a tile besides its keys
     int first, n, len, tiles, rising;
-    unsigned rows;                         // rows a tile covers, rounded up
-    u64 most;
+    unsigned base, rows, most, whole;      // cost of tile t: min(base + (t + 1) rows, most) + 1; of all tiles: whole
     __device__ __forceinline__ void init(const PagedAttentionArgs &a, const PagedPlan &pl, int s) {
         int last;
         paged_rows(a.b, s, first, last);
@@ -40,16 +34,20 @@ struct PagedSeq {
         len = paged_len(a.b, s);
         const int packed = n * pl.group;
         tiles = packed > pl.above && packed <= pl.upto ? (packed + QT - 1) / QT : 0;
-        rows = (QT + pl.group - 1) / pl.group;
-        most = a.window ? (u64)a.window + rows : ~0ull >> 8;
-        rising = most > (u64)len ? (int)min((u64)tiles, (most - len) / rows) : 0;
+        const unsigned span = (QT + pl.group - 1) / pl.group;               // rows a tile covers, rounded up
+        base = (unsigned)(len + kStart) >> pl.shift;
+        rows = span >> pl.shift;
+        most = a.window ? ((unsigned)a.window + span + kStart) >> pl.shift : 0x7fffffffu;
+        rising = most < base ? 0 : (rows && a.window ? (int)min((unsigned)tiles, (most - base) / rows) : tiles);
+        whole = before(tiles);
     }
-    __device__ __forceinline__ u64 cost(int t) const { return min(len + (u64)(t + 1) * rows, most) + kStart; }
-    __device__ __forceinline__ u64 before(int t) const {       // sum of the costs of tiles 0 .. t - 1
-        const u64 c = min(t, rising);
-        return c * (len + kStart) + rows * (c * (c + 1) / 2) + (u64)(t - c) * (most + kStart);
+    static constexpr int kStart = 64;      // what a tile costs besides its keys
+    __device__ __forceinline__ unsigned cost(int t) const { return min(base + (unsigned)(t + 1) * rows, most) + 1; }
+    __device__ __forceinline__ unsigned before(int t) const {       // sum of the costs of tiles 0 .. t - 1
+        const unsigned c = min(t, rising);
+        return c * (base + 1) + rows * (c * (c + 1) / 2) + (unsigned)(t - (int)c) * (most + 1);
     }
-    __device__ __forceinline__ int tile_at(u64 x) const {      // the tile that the cost x < before(tiles) falls into
+    __device__ __forceinline__ int tile_at(unsigned x) const {      // the tile that the cost x < whole falls into
         int lo = 0, hi = tiles;
         while (hi - lo > 1) {
             const int mid = (lo + hi) / 2;
@@ -59,18 +57,23 @@ struct PagedSeq {
     }
 };
 
+// Of `units` units of a tile those before its cost x (the same for whoever asks; all of them at x = cost)
+__device__ __forceinline__ int units_before(int units, unsigned x, unsigned cost) {
+    return x >= cost ? units : min(units, (int)((float)x * ((float)units / (float)cost)));
+}
+
 // The runs: workgroup w takes [start(w), start(w + 1)) of the whole cost
 struct PagedRuns {
-    u64 each, more;
+    unsigned each, more;
     int n;                                 // workgroups
-    __device__ __forceinline__ void init(u64 total, u64 least, int groups) {
-        n = (int)max(1ull, min((u64)groups, total / least));
-        each = total / n;
+    __device__ __forceinline__ void init(unsigned total, unsigned least, int groups) {
+        n = (int)max(1u, min((unsigned)groups, total / least));
+        each = total / (unsigned)n;
         more = total - each * n;           // the first `more` workgroups take one more
     }
-    __device__ __forceinline__ u64 start(int w) const { return each * w + min((u64)w, more); }
-    __device__ __forceinline__ int of(u64 x) const {
-        const u64 line = more * (each + 1);
+    __device__ __forceinline__ unsigned start(int w) const { return each * w + min((unsigned)w, more); }
+    __device__ __forceinline__ int of(unsigned x) const {
+        const unsigned line = more * (each + 1);
         return (int)(x < line ? x / (each + 1) : more + (x - line) / each);
     }
 };
@@ -81,32 +84,37 @@ struct PagedMap {
     const PagedAttentionArgs &a;
     const PagedPlan &pl;
     __device__ __forceinline__ PagedMap(const PagedAttentionArgs &a_, const PagedPlan &p_) : a(a_), pl(p_) {}
-    __device__ __forceinline__ u64 cost_of(int s) const {
+    __device__ __forceinline__ unsigned cost_of(int s) const {
         if (s >= a.b.n_seqs) return 0;
         PagedSeq<QT> q;
         q.init(a, pl, s);
-        return q.tiles ? q.before(q.tiles) * a.c.n_kv : 0;
+        return q.whole * a.c.n_kv;
     }
-    __device__ __forceinline__ static u64 scan(u64 x, int lane) {
+    __device__ __forceinline__ static unsigned scan(unsigned x, int lane) {
 #pragma unroll
         for (int d = 1; d < 64; d *= 2) {
-            const u64 y = __shfl_up(x, d);
+            const unsigned y = __shfl_up(x, d);
             if (lane >= d) x += y;
         }
         return x;
     }
-    __device__ __forceinline__ u64 total(u64 &mine) const {      // mine: this lane's prefix over the first 64 sequences, itself included
+    __device__ __forceinline__ static unsigned lane_value(unsigned x, int l) { return (unsigned)__builtin_amdgcn_readlane((int)x, l); }
+    __device__ __forceinline__ unsigned total(unsigned &mine) const {      // mine: this lane's prefix over the first 64 sequences, itself included
+        if (a.b.n_seqs == 1) return mine = cost_of(0);
         const int lane = threadIdx.x & 63;
         mine = scan(cost_of(lane), lane);
-        u64 sum = lane_value(mine, 63);
+        unsigned sum = lane_value(mine, 63);
         for (int s = 64; s < a.b.n_seqs; s += 64) sum += lane_value(scan(cost_of(s + lane), lane), 63);
         return sum;
     }
-    __device__ __forceinline__ void at(u64 x, u64 mine, int &s, u64 &before) const {
+    __device__ __forceinline__ void at(unsigned x, unsigned mine, int &s, unsigned &before) const {
+        s = 0;
+        before = 0;
+        if (a.b.n_seqs == 1) return;
         const int lane = threadIdx.x & 63;
-        u64 base = 0;
+        unsigned base = 0;
         for (int s0 = 0;; s0 += 64) {
-            const u64 upto = (s0 ? scan(cost_of(s0 + lane), lane) : mine) + base;
+            const unsigned upto = (s0 ? scan(cost_of(s0 + lane), lane) : mine) + base;
             const u64 hit = __ballot(upto > x);
             if (hit || s0 + 64 >= a.b.n_seqs) {
                 const int l = hit ? __builtin_ctzll(hit) : 63;   // (x is below the total: there is a hit)
