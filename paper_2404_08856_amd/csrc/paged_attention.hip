@@ -110,29 +110,25 @@ __global__ __launch_bounds__(NW * 64, NW / 4) void paged_few_kernel(PagedAttenti
     constexpr int QT = 16 * RT, G = 16 / sizeof(C), UK = 4 * G, HALVES = G / 8, NK = 2 * HALVES;   // NK: score tiles of a unit
     constexpr int KS = D / 32, KL = D / (4 * G), DT = D / 16, PT = NT;                              // K-steps, loads a key row, output tiles, terms of a weight
     __shared__ float o_s[NW][QT][D + 4], m_s[NW][QT], l_s[NW][QT];
+    __shared__ uint4 q_s[RT][KS][NT][64];                             // the queries as operands, alike for all waves
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), r = lane & 15, g = lane >> 4;
     const int P = 1 << a.c.page_bits, group = pl.group;
     const size_t page_bytes = (size_t)a.c.n_kv * P * D * sizeof(C), head_bytes = (size_t)P * D * sizeof(C);
     const bool q_wide = (uintptr_t)a.q.p % 16 == 0 && (a.q.row | a.q.head) % 8 == 0, out_wide = (uintptr_t)a.out.p % 16 == 0 && (a.out.row | a.out.head) % 4 == 0;
-    const PagedMap<QT> map(a, pl);
-    PagedRuns runs;
-    unsigned mine;
-    const unsigned all = map.total(mine);
-    if (all == 0) return;
-    runs.init(all, pl.least, gridDim.x);
+    const PagedRuns<QT> runs(a, pl, gridDim.x);
     const int w = blockIdx.x;
     if (w >= runs.n) return;
     unsigned pos = runs.start(w), before;
     const unsigned end = runs.start(w + 1);
     int s;
-    map.at(pos, mine, s, before);
+    runs.at(pos, s, before);
     PagedSeq<QT> seq;
-    seq.init(a, pl, s);
+    seq.init(a, pl, s, runs.flat);
     while (pos < end) {
         const unsigned off = pos - before, head_cost = seq.whole;
         if (off >= head_cost * a.c.n_kv) {                          // the next sequence with rows for this kernel
             before += head_cost * a.c.n_kv;
-            do seq.init(a, pl, ++s); while (seq.tiles == 0 && s + 1 < a.b.n_seqs);
+            do seq.init(a, pl, ++s, runs.flat); while (seq.tiles == 0 && s + 1 < a.b.n_seqs);
             continue;
         }
         const int h = (int)(off / head_cost);
@@ -148,15 +144,11 @@ __global__ __launch_bounds__(NW * 64, NW / 4) void paged_few_kernel(PagedAttenti
         const int u0 = units_before(units, x0, cost), u1 = units_before(units, x1, cost);
         // a unit of keys all_lo .. all_hi - 1 is seen whole by every row
         const int all_hi = a.seen ? len : min(len + i_first + 1, a.b.capacity), all_lo = a.window ? max(0, len + i_last - a.window + 1) : 0;
-        uint4 q[RT][KS][NT];
         Sees sees[RT];
 #pragma unroll
         for (int rt = 0; rt < RT; ++rt) {
-            const int pr = min(16 * rt + r, valid - 1) + t * QT, i = pr / group, j = pr - i * group;      // (rows behind the last: the last again)
+            const int i = (min(16 * rt + r, valid - 1) + t * QT) / group;      // (rows behind the last: the last again)
             sees[rt].init(a, seq.first, len, i);
-            const size_t at = (size_t)(seq.first + i) * a.q.row + (size_t)(h * group + j) * a.q.head;
-#pragma unroll
-            for (int c = 0; c < KS; ++c) load_query<NT>(a, at + (HALVES == 1 ? 32 * c + 8 * g : ((c / 2 * 4 + g) * 16 + c % 2 * 8)), q_wide, q[rt][c]);
         }
         const float factor = a.scale * kLog2e * (sizeof(C) == 1 ? a.c.k_scale[h] : 1.0f);
         f32x4_t acc[RT][DT];
@@ -195,12 +187,21 @@ __global__ __launch_bounds__(NW * 64, NW / 4) void paged_few_kernel(PagedAttenti
             load_k(u);
             load_v(u);
         }
+        for (int x = wave; x < RT * KS; x += NW) {
+            const int rt = x / KS, c = x % KS, pr = min(16 * rt + r, valid - 1) + t * QT, i = pr / group, j = pr - i * group;
+            uint4 terms[NT];
+            load_query<NT>(a, (size_t)(seq.first + i) * a.q.row + (size_t)(h * group + j) * a.q.head + (HALVES == 1 ? 32 * c + 8 * g : ((c / 2 * 4 + g) * 16 + c % 2 * 8)), q_wide, terms);
+#pragma unroll
+            for (int k = 0; k < NT; ++k) q_s[rt][c][k][lane] = terms[k];
+        }
+        __syncthreads();
         bool there = v_page >= 0;                                   // this lane's granule of the unit at hand
         if (u + NW < u1) pages(u + NW);
         for (; u < u1; u += NW) {
             const bool more = u + NW < u1;
             const int key0 = tile_lo + u * UK, key = key0 + g * G;   // key: of this lane's weights
             f32x4_t sc[RT][NK];
+            asm volatile("" ::: "memory");                           // the queries are read again each time: as registers they leave room for too few waves
 #pragma unroll
             for (int n = 0; n < NK; ++n) {
 #pragma unroll
@@ -211,7 +212,7 @@ __global__ __launch_bounds__(NW * 64, NW / 4) void paged_few_kernel(PagedAttenti
 #pragma unroll
                     for (int rt = 0; rt < RT; ++rt)
 #pragma unroll
-                        for (int i = NT - 1; i >= 0; --i) sc[rt][n] = mfma(k, q[rt][c][i], sc[rt][n]);
+                        for (int i = NT - 1; i >= 0; --i) sc[rt][n] = mfma(k, q_s[rt][c][i][lane], sc[rt][n]);
                 }
             }
             if (more) load_k(u + NW);
@@ -455,26 +456,21 @@ __global__ __launch_bounds__(256, 2) void paged_many_kernel(PagedAttentionArgs a
     const int P = 1 << a.c.page_bits, group = pl.group;
     const size_t page_bytes = (size_t)a.c.n_kv * P * D * sizeof(C), head_bytes = (size_t)P * D * sizeof(C);
     const bool q_wide = (uintptr_t)a.q.p % 16 == 0 && (a.q.row | a.q.head) % 8 == 0, out_wide = (uintptr_t)a.out.p % 16 == 0 && (a.out.row | a.out.head) % 4 == 0;
-    const PagedMap<QT> map(a, pl);
-    PagedRuns runs;
-    unsigned mine;
-    const unsigned all = map.total(mine);
-    if (all == 0) return;
-    runs.init(all, pl.least, gridDim.x);
+    const PagedRuns<QT> runs(a, pl, gridDim.x);
     if ((int)blockIdx.x >= runs.n) return;
     const int eighth = runs.n / 8, w = (int)blockIdx.x < 8 * eighth ? (int)(blockIdx.x % 8 * eighth + blockIdx.x / 8) : (int)blockIdx.x;   // neighbours in the row of tiles on one XCD
     unsigned pos = runs.start(w), before;
     const unsigned end = runs.start(w + 1);
     int s;
-    map.at(pos, mine, s, before);
+    runs.at(pos, s, before);
     PagedSeq<QT> seq;
-    seq.init(a, pl, s);
+    seq.init(a, pl, s, runs.flat);
     const int my_key = (lane & 32) + ((lane & 15) >> 2) * 8 + (lane & 16 ? 4 : 0) + (lane & 3);        // the key of this lane's place
     while (pos < end) {
         const unsigned off = pos - before, head_cost = seq.whole;
         if (off >= head_cost * a.c.n_kv) {
             before += head_cost * a.c.n_kv;
-            do seq.init(a, pl, ++s); while (seq.tiles == 0 && s + 1 < a.b.n_seqs);
+            do seq.init(a, pl, ++s, runs.flat); while (seq.tiles == 0 && s + 1 < a.b.n_seqs);
             continue;
         }
         const int h = (int)(off / head_cost);
@@ -847,19 +843,20 @@ hipError_t launch_paged_attention(const PagedAttentionArgs &a, hipStream_t strea
     // Rows of a sequence at most, as far as the host can tell: all, or, as long as no sequence is without any, all but one of each other.  What it
     // says chooses kernels; a kernel that is alone takes every sequence.
     const int most = a.b.row_start ? std::max(1, a.b.n_rows - a.b.n_seqs + 1) : a.b.each;
-    const bool few = most * pl.group <= kFewUpto, many = !few && (!a.b.row_start || a.b.n_seqs == 1);
+    const bool few = most * pl.group <= kFewUpto || a.b.n_rows * pl.group <= 128, many = !few && (!a.b.row_start || a.b.n_seqs == 1);
     const int mean = (a.b.n_rows + a.b.n_seqs - 1) / a.b.n_seqs * pl.group;
     // costs in 31 bits: the tiles of all heads, each of no more than this many keys
-    auto costs = [&](int QT, int keys) {
+    auto costs = [&](int QT, int keys, int join) {
         const u64 tiles = ((u64)a.b.n_rows * pl.group / QT + a.b.n_seqs) * a.c.n_kv, span = (u64)a.b.capacity + a.b.n_rows + 2 * QT + 64;
         pl.shift = 0;
         while (tiles * ((span >> pl.shift) + 2) >> 31) ++pl.shift;
         pl.least = std::max(1, keys >> pl.shift);
+        pl.join = std::max(1, join >> pl.shift);
     };
-    const int wide = few ? std::min(most * pl.group, kFewUpto) : mean;
+    const int wide = mean;
 #define SPD_FEW(NT, C, D, RT, NW)                                                                                            \
     do {                                                                                                                     \
-        costs(16 * RT, 640);                                                                                                 \
+        costs(16 * RT, 512, 850);                                                                                                 \
         hipLaunchKernelGGL((paged_few_kernel<NT, C, D, RT, NW>), dim3(256), dim3(NW * 64), 0, stream, a, pl);                \
     } while (0)
 #define SPD_FEW_RT(NT, C, D)                                                                                                 \
@@ -867,12 +864,12 @@ hipError_t launch_paged_attention(const PagedAttentionArgs &a, hipStream_t strea
         if (!many) {                                                                                                         \
             pl.above = 0; pl.upto = few ? 0x7fffffff : kFewUpto;                                                             \
             if (wide <= 16) SPD_FEW(NT, C, D, 1, 8);                                                                         \
-            else if (wide <= 32 || NT == 3) SPD_FEW(NT, C, D, 2, 4);                                                         \
-            else SPD_FEW(NT, C, D, (NT == 3 ? 2 : 4), 4);                                                                    \
+            else if (wide <= 32 || NT == 3) SPD_FEW(NT, C, D, 2, (D == 64 ? 8 : 4));                                                         \
+            else SPD_FEW(NT, C, D, (NT == 3 ? 2 : 4), (NT == 3 && D == 64 ? 8 : 4));                                                                   \
         }                                                                                                                    \
         if (!few) {                                                                                                          \
             pl.above = many ? 0 : kFewUpto; pl.upto = 0x7fffffff;                                                            \
-            costs(128, 512);                                                                                                 \
+            costs(128, 512, 1024);                                                                                                 \
             hipLaunchKernelGGL((paged_many_kernel<NT, C, D, 2>), dim3(kGroups), dim3(256), 0, stream, a, pl);                \
         }                                                                                                                    \
     } while (0)

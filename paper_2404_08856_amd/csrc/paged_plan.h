@@ -15,6 +15,7 @@ typedef unsigned long long u64;
 struct PagedPlan {
     u64 number;              // of the call: what a flag of this call carries
     unsigned least;          // cost of a workgroup at least
+    unsigned join;           // what sharing a tile costs
     int shift;               // a cost counts 2^shift keys, so that the whole fits 31 bits
     int group;               // query heads of a key head
     int above, upto;         // takes the sequences with so many packed rows: above < rows <= upto
@@ -27,7 +28,8 @@ template <int QT>
 struct PagedSeq {
     int first, n, len, tiles, rising;
     unsigned base, rows, most, whole;      // cost of tile t: min(base + (t + 1) rows, most) + 1; of all tiles: whole
-    __device__ __forceinline__ void init(const PagedAttentionArgs &a, const PagedPlan &pl, int s) {
+    // flat: every tile costs 1
+    __device__ __forceinline__ void init(const PagedAttentionArgs &a, const PagedPlan &pl, int s, bool flat) {
         int last;
         paged_rows(a.b, s, first, last);
         n = last - first;
@@ -38,6 +40,7 @@ struct PagedSeq {
         base = (unsigned)(len + kStart) >> pl.shift;
         rows = span >> pl.shift;
         most = a.window ? ((unsigned)a.window + span + kStart) >> pl.shift : 0x7fffffffu;
+        if (flat) base = rows = 0;
         rising = most < base ? 0 : (rows && a.window ? (int)min((unsigned)tiles, (most - base) / rows) : tiles);
         whole = before(tiles);
     }
@@ -62,35 +65,26 @@ __device__ __forceinline__ int units_before(int units, unsigned x, unsigned cost
     return x >= cost ? units : min(units, (int)((float)x * ((float)units / (float)cost)));
 }
 
-// The runs: workgroup w takes [start(w), start(w + 1)) of the whole cost
-struct PagedRuns {
-    unsigned each, more;
-    int n;                                 // workgroups
-    __device__ __forceinline__ void init(unsigned total, unsigned least, int groups) {
-        n = (int)max(1u, min((unsigned)groups, total / least));
-        each = total / (unsigned)n;
-        more = total - each * n;           // the first `more` workgroups take one more
-    }
-    __device__ __forceinline__ unsigned start(int w) const { return each * w + min((unsigned)w, more); }
-    __device__ __forceinline__ int of(unsigned x) const {
-        const unsigned line = more * (each + 1);
-        return (int)(x < line ? x / (each + 1) : more + (x - line) / each);
-    }
-};
-
-// Called by whole waves.  total: cost of all sequences; at(x): the sequence that cost x falls into, and the cost before it.
+// The runs: workgroup w takes [start(w), start(w + 1)) of the whole cost.  Where the tiles are no more than the workgroups and the largest is not above the
+// mean of a workgroup by more than sharing costs, each workgroup takes one tile (flat).  Called by whole waves.
 template <int QT>
-struct PagedMap {
+struct PagedRuns {
     const PagedAttentionArgs &a;
     const PagedPlan &pl;
-    __device__ __forceinline__ PagedMap(const PagedAttentionArgs &a_, const PagedPlan &p_) : a(a_), pl(p_) {}
-    __device__ __forceinline__ unsigned cost_of(int s) const {
-        if (s >= a.b.n_seqs) return 0;
-        PagedSeq<QT> q;
-        q.init(a, pl, s);
-        return q.whole * a.c.n_kv;
+    unsigned each, more, mine;             // mine: this lane's sum of costs over the first 64 sequences, itself included
+    int n;                                 // workgroups
+    bool flat;
+
+    struct Add { __device__ __forceinline__ unsigned operator()(unsigned x, unsigned y) const { return x + y; } };
+    struct Max { __device__ __forceinline__ unsigned operator()(unsigned x, unsigned y) const { return max(x, y); } };
+    template <class Op>
+    __device__ __forceinline__ static unsigned over_lanes(unsigned x, Op op) {
+        x = xor_step<32>(x, op); x = xor_step<16>(x, op); x = xor_step<8>(x, op); x = xor_step<4>(x, op); x = xor_step<2>(x, op);
+        return value(xor_step<1>(x, op), 0);
     }
-    __device__ __forceinline__ static unsigned scan(unsigned x, int lane) {
+    __device__ __forceinline__ static unsigned value(unsigned x, int l) { return (unsigned)__builtin_amdgcn_readlane((int)x, l); }
+    __device__ __forceinline__ static unsigned scan(unsigned x) {
+        const int lane = threadIdx.x & 63;
 #pragma unroll
         for (int d = 1; d < 64; d *= 2) {
             const unsigned y = __shfl_up(x, d);
@@ -98,31 +92,62 @@ struct PagedMap {
         }
         return x;
     }
-    __device__ __forceinline__ static unsigned lane_value(unsigned x, int l) { return (unsigned)__builtin_amdgcn_readlane((int)x, l); }
-    __device__ __forceinline__ unsigned total(unsigned &mine) const {      // mine: this lane's prefix over the first 64 sequences, itself included
-        if (a.b.n_seqs == 1) return mine = cost_of(0);
-        const int lane = threadIdx.x & 63;
-        mine = scan(cost_of(lane), lane);
-        unsigned sum = lane_value(mine, 63);
-        for (int s = 64; s < a.b.n_seqs; s += 64) sum += lane_value(scan(cost_of(s + lane), lane), 63);
-        return sum;
+    __device__ __forceinline__ unsigned cost_of(int s) const {
+        if (s >= a.b.n_seqs) return 0;
+        PagedSeq<QT> q;
+        q.init(a, pl, s, flat);
+        return q.whole * a.c.n_kv;
     }
-    __device__ __forceinline__ void at(unsigned x, unsigned mine, int &s, unsigned &before) const {
+    __device__ __forceinline__ PagedRuns(const PagedAttentionArgs &a_, const PagedPlan &p_, int groups) : a(a_), pl(p_), flat(false) {
+        const int lane = threadIdx.x & 63;
+        unsigned total = 0, tiles = 0, largest = 0;
+        if (a.b.n_seqs == 1) {
+            PagedSeq<QT> q;
+            q.init(a, pl, 0, false);
+            tiles = q.tiles;
+            total = q.whole * a.c.n_kv;
+            largest = q.tiles ? q.cost(q.tiles - 1) : 0;
+        } else {
+            for (int s0 = 0; s0 < a.b.n_seqs; s0 += 64) {
+                PagedSeq<QT> q;
+                q.tiles = 0; q.whole = 0;
+                if (s0 + lane < a.b.n_seqs) q.init(a, pl, s0 + lane, false);
+                if (s0 == 0) mine = q.whole * a.c.n_kv;
+                total += over_lanes(q.whole * a.c.n_kv, Add());
+                tiles += over_lanes(q.tiles, Add());
+                largest = max(largest, over_lanes(q.tiles ? q.cost(q.tiles - 1) : 0u, Max()));
+            }
+        }
+        const unsigned items = tiles * a.c.n_kv;
+        flat = items <= (unsigned)groups && largest <= total / (unsigned)groups + pl.join;
+        if (flat) total = items;
+        n = total == 0 ? 0 : (flat ? (int)items : (int)max(1u, min((unsigned)groups, total / pl.least)));
+        each = n ? total / (unsigned)n : 1;
+        more = n ? total - each * n : 0;
+        if (a.b.n_seqs > 1 && n) mine = scan(flat ? cost_of(lane) : mine);
+    }
+    __device__ __forceinline__ unsigned start(int w) const { return each * w + min((unsigned)w, more); }
+    __device__ __forceinline__ int of(unsigned x) const {          // the workgroup whose run has x
+        const unsigned line = more * (each + 1);
+        return (int)(x < line ? x / (each + 1) : more + (x - line) / each);
+    }
+    // the sequence that cost x falls into, and the cost before it
+    __device__ __forceinline__ void at(unsigned x, int &s, unsigned &before) const {
         s = 0;
         before = 0;
         if (a.b.n_seqs == 1) return;
         const int lane = threadIdx.x & 63;
         unsigned base = 0;
         for (int s0 = 0;; s0 += 64) {
-            const unsigned upto = (s0 ? scan(cost_of(s0 + lane), lane) : mine) + base;
+            const unsigned upto = (s0 ? scan(cost_of(s0 + lane)) : mine) + base;
             const u64 hit = __ballot(upto > x);
             if (hit || s0 + 64 >= a.b.n_seqs) {
-                const int l = hit ? __builtin_ctzll(hit) : 63;   // (x is below the total: there is a hit)
+                const int l = hit ? __builtin_ctzll(hit) : 63;     // (x is below the whole: there is a hit)
                 s = s0 + l;
-                before = l ? lane_value(upto, l - 1) : base;
+                before = l ? value(upto, l - 1) : base;
                 return;
             }
-            base = lane_value(upto, 63);
+            base = value(upto, 63);
         }
     }
 };
