@@ -489,11 +489,9 @@ __global__ __launch_bounds__(256, 2) void paged_many_kernel(PagedAttentionArgs a
         const int all_hi = a.seen ? len : min(len + wi_first + 1, a.b.capacity), all_lo = a.window ? max(0, len + wi_last - a.window + 1) : 0;
         const int any_hi = a.seen ? tile_end : min(len + wi_last + 1, a.b.capacity), any_lo = a.window ? max(0, len + wi_first - a.window + 1) : 0;
         uint4 q[RT][KS][NT];
-        Sees sees[RT];
 #pragma unroll
         for (int rt = 0; rt < RT; ++rt) {
             const int pr = min(row0 + 16 * rt + r, valid - 1) + t * QT, i = pr / group, j = pr - i * group;
-            sees[rt].init(a, seq.first, len, i);
             const size_t at = (size_t)(seq.first + i) * a.q.row + (size_t)(h * group + j) * a.q.head;
 #pragma unroll
             for (int c = 0; c < KS; ++c) load_query<NT>(a, at + 32 * c + 8 * g, q_wide, q[rt][c]);
@@ -507,7 +505,7 @@ __global__ __launch_bounds__(256, 2) void paged_many_kernel(PagedAttentionArgs a
                     }
             }
         }
-        const float factor = fabsf(a.scale) * kLog2e * (WIDEN ? a.c.k_scale[h] : 1.0f);
+        const float factor = fmaxf(fabsf(a.scale) * kLog2e * (WIDEN ? a.c.k_scale[h] : 1.0f), 1e-37f);       // (0: positions that are not seen stay at -infinity)
         f32x4_t acc[RT][DT];
         float m[RT], l[RT];
 #pragma unroll
@@ -562,28 +560,28 @@ __global__ __launch_bounds__(256, 2) void paged_many_kernel(PagedAttentionArgs a
                 }
             }
         };
-        bool there = true, there_next = true;                        // whether all keys of the step have a place
+        bool there = true;                                           // whether all keys of the step that comes next have a place
         if (j0 < j1) {
             pages(j0);
-            there_next = __all(k_page >= 0);
+            there = __all(k_page >= 0);
             load(j0, 0);
             widen(0);
             if (j0 + 1 < j1) pages(j0 + 1);
         }
-        for (int j = j0; j < j1; ++j) {
-            const int buf = (j - j0) & 1;
+        // Step j's keys and values are in LDS after this, and those of step j + 1 on their way
+        auto enter = [&](int j, int buf) {
             asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");      // this wave's part of the step is in LDS, and its reads of the other buffer are done
             __syncthreads();
-            there = there_next;
-            const bool more = j + 1 < j1;
-            if (more) {
-                there_next = __all(k_page >= 0);
+            if (j + 1 < j1) {
+                there = __all(k_page >= 0);
                 load(j + 1, buf ^ 1);
                 if (j + 2 < j1) pages(j + 2);
             }
-            const int key0 = tile_lo + j * KT;
-            auto step = [&](auto whole_) {
-                constexpr bool WHOLE = decltype(whole_)::value;
+        };
+        auto whole_at = [&](int j) { return there && tile_lo + j * KT >= all_lo && tile_lo + j * KT + KT <= all_hi && rows > 0; };
+        auto step = [&](auto whole_, const int key0, const int buf) {
+            constexpr bool WHOLE = decltype(whole_)::value;
+            {
                 f32x4_t sc[RT][4];
 #pragma unroll
                 for (int n = 0; n < 4; ++n) {
@@ -599,50 +597,34 @@ __global__ __launch_bounds__(256, 2) void paged_many_kernel(PagedAttentionArgs a
                             for (int c = 0; c < KS; ++c) sc[rt][n] = mfma(kf[c], q[rt][c][i], sc[rt][n]);
                     }
                 }
-                uint32_t seen_bits[RT][2], keep[2][4];
-                bool odd_values = false;
+                uint32_t seen_bits[RT];                               // bit 8 u + e: key 32 u + 8 g + e of the step
                 if constexpr (!WHOLE) {
-                    uint32_t bad = 0;
+                    bool here[2];
 #pragma unroll
-                    for (int u = 0; u < 2; ++u) {
-                        const int key = key0 + 32 * u + 8 * g;
-                        const bool here = paged_page(a.b, a.c, s, key >> a.c.page_bits) >= 0;
+                    for (int u = 0; u < 2; ++u) here[u] = paged_page(a.b, a.c, s, (key0 + 32 * u + 8 * g) >> a.c.page_bits) >= 0;
 #pragma unroll
-                        for (int rt = 0; rt < RT; ++rt) seen_bits[rt][u] = here ? sees[rt].keys(key, 8, len, tile_end) : 0;
+                    for (int rt = 0; rt < RT; ++rt) {
+                        Sees sees;
+                        sees.init(a, seq.first, len, (min(row0 + 16 * rt + r, valid - 1) + t * QT) / group);
+                        seen_bits[rt] = 0;
 #pragma unroll
-                        for (int i = 0; i < 4; ++i) {
-                            const int n = here ? min(max(tile_end - key - 2 * i, 0), 2) : 0;
-                            keep[u][i] = n == 2 ? 0xffffffffu : (1u << (16 * n)) - 1;
-                        }
-                        for (int d = 0; d < DT; ++d) {
-                            const uint4 v = v_s[buf][4 * u + g][16 * d + r];
-                            bad |= (((v.x & keep[u][0]) & 0x7f807f80u) + 0x00800080u) | (((v.y & keep[u][1]) & 0x7f807f80u) + 0x00800080u) |
-                                   (((v.z & keep[u][2]) & 0x7f807f80u) + 0x00800080u) | (((v.w & keep[u][3]) & 0x7f807f80u) + 0x00800080u);
-                        }
+                        for (int u = 0; u < 2; ++u)
+                            if (here[u]) seen_bits[rt] |= sees.keys(key0 + 32 * u + 8 * g, 8, len, tile_end) << (8 * u);
+#pragma unroll
+                        for (int n = 0; n < 4; ++n)
+#pragma unroll
+                            for (int i = 0; i < 4; ++i) sc[rt][n][i] = seen_bits[rt] >> (4 * n + i) & 1 ? sc[rt][n][i] : -INFINITY;
                     }
-                    odd_values = __any((bad & 0x80008000u) != 0);
                 }
                 // weights: exponentials above the running maximum by up to 2^8 are let be, the sums are brought to a new maximum only beyond
 #pragma unroll
                 for (int rt = 0; rt < RT; ++rt) {
                     float top = -INFINITY;
-                    if constexpr (WHOLE) {
 #pragma unroll
-                        for (int n = 0; n < 4; ++n)
+                    for (int n = 0; n < 4; ++n)
 #pragma unroll
-                            for (int i = 0; i < 4; ++i) top = fmaxf(top, sc[rt][n][i]);
-                        top *= factor;
-                    } else {
-#pragma unroll
-                        for (int n = 0; n < 4; ++n)
-#pragma unroll
-                            for (int i = 0; i < 4; ++i) {
-                                const float z = seen_bits[rt][n / 2] >> (n % 2 * 4 + i) & 1 ? sc[rt][n][i] * factor : -INFINITY;
-                                sc[rt][n][i] = z;
-                                top = fmaxf(top, z);
-                            }
-                    }
-                    top = max_over_rows(top);
+                        for (int i = 0; i < 4; ++i) top = fmaxf(top, sc[rt][n][i]);
+                    top = max_over_rows(top) * factor;
                     if (__any(top > m[rt] + 8.0f)) {
                         top = top > m[rt] + 8.0f ? top : m[rt];           // (a row's result does not depend on the others')
                         const float shrink = __builtin_amdgcn_exp2f(m[rt] - (top > -INFINITY ? top : 0.f));
@@ -659,67 +641,117 @@ __global__ __launch_bounds__(256, 2) void paged_many_kernel(PagedAttentionArgs a
                     for (int n = 0; n < 4; ++n)
 #pragma unroll
                         for (int i = 0; i < 4; ++i) {
-                            sc[rt][n][i] = __builtin_amdgcn_exp2f(WHOLE ? __builtin_fmaf(sc[rt][n][i], factor, -use) : sc[rt][n][i] - use);
+                            sc[rt][n][i] = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[rt][n][i], factor, -use));
                             sum += sc[rt][n][i];
                         }
                     l[rt] += sum;
                 }
+                auto weights = [&](int rt, int u, uint4 (&p)[PT]) {
+                    uint32_t words[PT][4];
 #pragma unroll
-                for (int u = 0; u < 2; ++u) {
-                    uint4 p[RT][PT];
+                    for (int i = 0; i < 4; ++i) {
+                        float x = sc[rt][2 * u + i / 2][i % 2 * 2], y = sc[rt][2 * u + i / 2][i % 2 * 2 + 1];
 #pragma unroll
-                    for (int rt = 0; rt < RT; ++rt) {
-                        uint32_t words[PT][4];
-#pragma unroll
-                        for (int i = 0; i < 4; ++i) {
-                            float x = sc[rt][2 * u + i / 2][i % 2 * 2], y = sc[rt][2 * u + i / 2][i % 2 * 2 + 1];
-#pragma unroll
-                            for (int k = 0; k < PT; ++k) {
-                                words[k][i] = two_bf16(x, y);
-                                if (k + 1 < PT) {
-                                    x -= bf16_lo(words[k][i]);
-                                    y -= bf16_hi(words[k][i]);
-                                }
+                        for (int k = 0; k < PT; ++k) {
+                            words[k][i] = two_bf16(x, y);
+                            if (k + 1 < PT) {
+                                x -= bf16_lo(words[k][i]);
+                                y -= bf16_hi(words[k][i]);
                             }
                         }
-#pragma unroll
-                        for (int k = 0; k < PT; ++k) p[rt][k] = uint4{words[k][0], words[k][1], words[k][2], words[k][3]};
                     }
 #pragma unroll
-                    for (int d = 0; d < DT; ++d) {
-                        uint4 v = v_s[buf][4 * u + g][16 * d + r];
-                        if constexpr (!WHOLE) { v.x &= keep[u][0]; v.y &= keep[u][1]; v.z &= keep[u][2]; v.w &= keep[u][3]; }
-                        if (WHOLE || !odd_values) {
+                    for (int k = 0; k < PT; ++k) p[k] = uint4{words[k][0], words[k][1], words[k][2], words[k][3]};
+                };
+                if constexpr (WHOLE) {
+#pragma unroll
+                    for (int u = 0; u < 2; ++u) {
+                        uint4 p[RT][PT];
+#pragma unroll
+                        for (int rt = 0; rt < RT; ++rt) weights(rt, u, p[rt]);
+#pragma unroll
+                        for (int d = 0; d < DT; ++d) {
+                            const uint4 v = v_s[buf][4 * u + g][16 * d + r];
 #pragma unroll
                             for (int rt = 0; rt < RT; ++rt)
 #pragma unroll
                                 for (int k = PT - 1; k >= 0; --k) acc[rt][d] = mfma(v, p[rt][k], acc[rt][d]);
-                        } else {
+                        }
+                    }
+                } else {
+                    // values of places that do not exist may be anything: zeros; others that are not finite are kept from the rows that do not see them
 #pragma unroll
-                            for (int rt = 0; rt < RT; ++rt)
+                    for (int u = 0; u < 2; ++u) {
+                        const int key = key0 + 32 * u + 8 * g;
+                        const bool here = paged_page(a.b, a.c, s, key >> a.c.page_bits) >= 0;
+                        uint32_t keep[4], bad = 0;
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) {
+                            const int n = here ? min(max(tile_end - key - 2 * i, 0), 2) : 0;
+                            keep[i] = n == 2 ? 0xffffffffu : (1u << (16 * n)) - 1;
+                        }
+                        auto value = [&](int d) {
+                            uint4 v = v_s[buf][4 * u + g][16 * d + r];
+                            v.x &= keep[0]; v.y &= keep[1]; v.z &= keep[2]; v.w &= keep[3];
+                            return v;
+                        };
+#pragma unroll
+                        for (int d = 0; d < DT; ++d) {
+                            const uint4 v = value(d);
+                            bad |= ((v.x & 0x7f807f80u) + 0x00800080u) | ((v.y & 0x7f807f80u) + 0x00800080u) | ((v.z & 0x7f807f80u) + 0x00800080u) | ((v.w & 0x7f807f80u) + 0x00800080u);
+                        }
+                        const bool finite = !__any((bad & 0x80008000u) != 0);
+                        asm volatile("" ::: "memory");
+#pragma unroll
+                        for (int rt = 0; rt < RT; ++rt) {
+                            uint4 p[PT];
+                            weights(rt, u, p);
+                            if (finite) {
+#pragma unroll
+                                for (int d = 0; d < DT; ++d) {
+                                    const uint4 v = value(d);
+#pragma unroll
+                                    for (int k = PT - 1; k >= 0; --k) acc[rt][d] = mfma(v, p[k], acc[rt][d]);
+                                }
+                            } else {
 #pragma unroll 1
                                 for (int x = 0; x < 16; ++x) {               // one row at a time, with zeros where it does not see
-                                    const uint32_t bits = __shfl(seen_bits[rt][u], 16 * g + x);
-                                    uint4 y = v;
-                                    y.x &= (bits & 1 ? 0xffffu : 0u) | (bits & 2 ? 0xffff0000u : 0u);
-                                    y.y &= (bits & 4 ? 0xffffu : 0u) | (bits & 8 ? 0xffff0000u : 0u);
-                                    y.z &= (bits & 16 ? 0xffffu : 0u) | (bits & 32 ? 0xffff0000u : 0u);
-                                    y.w &= (bits & 64 ? 0xffffu : 0u) | (bits & 128 ? 0xffff0000u : 0u);
-                                    f32x4_t one = acc[rt][d];
+                                    asm volatile("" ::: "memory");
+                                    const uint32_t bits = (uint32_t)__shfl((int)seen_bits[rt], 16 * g + x) >> (8 * u);
+                                    uint32_t mine[4];
 #pragma unroll
-                                    for (int k = PT - 1; k >= 0; --k) one = mfma(y, p[rt][k], one);
+                                    for (int i = 0; i < 4; ++i) mine[i] = (bits >> (2 * i) & 1 ? 0xffffu : 0u) | (bits >> (2 * i) & 2 ? 0xffff0000u : 0u);
 #pragma unroll
-                                    for (int i = 0; i < 4; ++i) acc[rt][d][i] = r == x ? one[i] : acc[rt][d][i];
+                                    for (int d = 0; d < DT; ++d) {
+                                        uint4 v = value(d);
+                                        v.x &= mine[0]; v.y &= mine[1]; v.z &= mine[2]; v.w &= mine[3];
+                                        f32x4_t one = acc[rt][d];
+#pragma unroll
+                                        for (int k = PT - 1; k >= 0; --k) one = mfma(v, p[k], one);
+#pragma unroll
+                                        for (int i = 0; i < 4; ++i) acc[rt][d][i] = r == x ? one[i] : acc[rt][d][i];
+                                    }
                                 }
+                            }
                         }
                     }
                 }
-            };
-            if (rows > 0 && key0 < any_hi && key0 + KT > any_lo) {
-                if (there && key0 >= all_lo && key0 + KT <= all_hi) step(std::integral_constant<bool, true>());
-                else step(std::integral_constant<bool, false>());
             }
-            if (more) widen(buf ^ 1);
+        };
+        // (a loop of its own for the steps that every row of the wave sees whole: one loop with both kinds spills in both)
+        for (int j = j0; j < j1;) {
+            for (; j < j1 && whole_at(j); ++j) {
+                const int buf = (j - j0) & 1;
+                enter(j, buf);
+                step(std::integral_constant<bool, true>(), tile_lo + j * KT, buf);
+                if (j + 1 < j1) widen(buf ^ 1);
+            }
+            for (; j < j1 && !whole_at(j); ++j) {
+                const int buf = (j - j0) & 1, key0 = tile_lo + j * KT;
+                enter(j, buf);
+                if (rows > 0 && key0 < any_hi && key0 + KT > any_lo) step(std::integral_constant<bool, false>(), key0, buf);
+                if (j + 1 < j1) widen(buf ^ 1);
+            }
         }
         __syncthreads();                                              // the next tile's loads write what other waves may still read
         // ---- results
