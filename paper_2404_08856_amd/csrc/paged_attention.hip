@@ -515,30 +515,36 @@ __global__ __launch_bounds__(256, 2) void paged_many_kernel(PagedAttentionArgs a
 #pragma unroll
             for (int d = 0; d < DT; ++d) acc[rt][d] = f32x4_t{0.f, 0.f, 0.f, 0.f};
         }
-        // pages of the step whose loads come next: of this lane's key, and of the granules of values that this wave (e4m3: thread) brings
+        // Pages of the steps whose loads come next: of this lane's key, and of the granules of values that this wave (e4m3: thread) brings
         constexpr int VG = WIDEN ? (D == 128 ? 2 : 1) : 2;
         int k_page = -1, v_page[VG];
         auto v_granule = [&](int i) { return WIDEN ? (tid + 256 * i) / D * 2 : wave * 2 + i; };        // of 8 keys
-        auto pages = [&](int j) {
-            const int key = tile_lo + j * KT;
-            k_page = paged_page(a.b, a.c, s, (key + my_key) >> a.c.page_bits);
+        auto k_pages = [&](int j) { k_page = paged_page(a.b, a.c, s, (tile_lo + j * KT + my_key) >> a.c.page_bits); };
+        auto v_pages = [&](int j) {
 #pragma unroll
-            for (int i = 0; i < VG; ++i) v_page[i] = paged_page(a.b, a.c, s, (key + v_granule(i) * 8) >> a.c.page_bits);
+            for (int i = 0; i < VG; ++i) v_page[i] = paged_page(a.b, a.c, s, (tile_lo + j * KT + v_granule(i) * 8) >> a.c.page_bits);
         };
         uint4 kr[WIDEN ? LOADS / 2 : 1], vr[WIDEN ? LOADS / 2 : 1];
-        auto load = [&](int j, int buf) {
-            const int key = tile_lo + j * KT;
+        auto load_k = [&](int j) {
+            const int key = tile_lo + j * KT, buf = j & 1;
             const char *kp = (const char *)a.c.k + (size_t)max(k_page, 0) * page_bytes + h * head_bytes + (size_t)((key + my_key) & (P - 1)) * 16;
             if constexpr (WIDEN) {
 #pragma unroll
+                for (int i = 0; i < LOADS / 2; ++i) kr[i] = *reinterpret_cast<const uint4 *>(kp + (size_t)(wave + 4 * i) * P * 16);
+            } else {
+#pragma unroll
+                for (int i = 0; i < D / 32; ++i) to_lds(kp + (size_t)(wave * (D / 32) + i) * P * 16, lds_place(&k_s[buf][wave * (D / 32) + i][0]));
+            }
+        };
+        auto load_v = [&](int j) {
+            const int key = tile_lo + j * KT, buf = j & 1;
+            if constexpr (WIDEN) {
+#pragma unroll
                 for (int i = 0; i < LOADS / 2; ++i) {
-                    kr[i] = *reinterpret_cast<const uint4 *>(kp + (size_t)(wave + 4 * i) * P * 16);
                     const int d = (tid + 256 * i) % D, slot = (key + v_granule(i) * 8) & (P - 1);
                     vr[i] = *reinterpret_cast<const uint4 *>((const char *)a.c.v + (size_t)max(v_page[i], 0) * page_bytes + h * head_bytes + (size_t)(slot / G * D + d) * 16);
                 }
             } else {
-#pragma unroll
-                for (int i = 0; i < D / 32; ++i) to_lds(kp + (size_t)(wave * (D / 32) + i) * P * 16, lds_place(&k_s[buf][wave * (D / 32) + i][0]));
 #pragma unroll
                 for (int i = 0; i < 2; ++i) {
                     const int slot = (key + v_granule(i) * 8) & (P - 1);
@@ -548,55 +554,94 @@ __global__ __launch_bounds__(256, 2) void paged_many_kernel(PagedAttentionArgs a
                 }
             }
         };
-        auto widen = [&](int buf) {
+        auto widen_k = [&](int j) {
             if constexpr (WIDEN) {
 #pragma unroll
                 for (int i = 0; i < LOADS / 2; ++i) {
-                    const int c = wave + 4 * i, d = (tid + 256 * i) % D, gv = v_granule(i);
-                    k_s[buf][2 * c][lane] = operand<C>(kr[i], 0);
-                    k_s[buf][2 * c + 1][lane] = operand<C>(kr[i], 1);
-                    v_s[buf][gv][d] = operand<C>(vr[i], 0);
-                    v_s[buf][gv + 1][d] = operand<C>(vr[i], 1);
+                    const int c = wave + 4 * i;
+                    k_s[j & 1][2 * c][lane] = operand<C>(kr[i], 0);
+                    k_s[j & 1][2 * c + 1][lane] = operand<C>(kr[i], 1);
                 }
             }
         };
-        bool there = true;                                           // whether all keys of the step that comes next have a place
-        if (j0 < j1) {
-            pages(j0);
-            there = __all(k_page >= 0);
-            load(j0, 0);
-            widen(0);
-            if (j0 + 1 < j1) pages(j0 + 1);
-        }
-        // Step j's keys and values are in LDS after this, and those of step j + 1 on their way
-        auto enter = [&](int j, int buf) {
-            asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");      // this wave's part of the step is in LDS, and its reads of the other buffer are done
-            __syncthreads();
-            if (j + 1 < j1) {
-                there = __all(k_page >= 0);
-                load(j + 1, buf ^ 1);
-                if (j + 2 < j1) pages(j + 2);
+        auto widen_v = [&](int j) {
+            if constexpr (WIDEN) {
+#pragma unroll
+                for (int i = 0; i < LOADS / 2; ++i) {
+                    const int d = (tid + 256 * i) % D, gv = v_granule(i);
+                    v_s[j & 1][gv][d] = operand<C>(vr[i], 0);
+                    v_s[j & 1][gv + 1][d] = operand<C>(vr[i], 1);
+                }
             }
+        };
+        // The scores of step j + 1 are multiplied while the weights of step j are made, so keys are brought two steps ahead, values one.
+        bool there = true, there_next = true;                        // whether all keys of steps j and j + 1 have a place
+        f32x4_t sc[RT][4];
+        auto scores = [&](int j, f32x4_t (&x)[RT][4]) {
+#pragma unroll
+            for (int n = 0; n < 4; ++n)
+#pragma unroll
+                for (int rt = 0; rt < RT; ++rt) x[rt][n] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int c = 0; c < KS; ++c) {
+                uint4 kf[4];
+#pragma unroll
+                for (int n = 0; n < 4; ++n) kf[n] = k_s[j & 1][c * 4 + g][16 * n + r];
+#pragma unroll
+                for (int i = NT - 1; i >= 0; --i)
+#pragma unroll
+                    for (int n = 0; n < 4; ++n)
+#pragma unroll
+                        for (int rt = 0; rt < RT; ++rt) x[rt][n] = mfma(kf[n], q[rt][c][i], x[rt][n]);
+            }
+        };
+        auto arrived = [] {                                          // this wave's loads are in LDS and its reads done, then everybody's
+            asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+            __syncthreads();
+        };
+        if (j0 < j1) {
+            k_pages(j0);
+            v_pages(j0);
+            there = __all(k_page >= 0);
+            load_k(j0);
+            load_v(j0);
+            widen_k(j0);
+            widen_v(j0);
+            if (j0 + 1 < j1) {
+                k_pages(j0 + 1);
+                there_next = __all(k_page >= 0);
+                load_k(j0 + 1);
+                widen_k(j0 + 1);
+                v_pages(j0 + 1);
+                if (j0 + 2 < j1) k_pages(j0 + 2);
+            }
+            arrived();
+            scores(j0, sc);
+        }
+        bool there_after = true;
+        auto enter = [&](int j) {                                    // step j's values and step j + 1's keys are in LDS after this
+            arrived();
+            if (j + 2 < j1) {
+                there_after = __all(k_page >= 0);
+                load_k(j + 2);
+            }
+            if (j + 1 < j1) load_v(j + 1);
+            if (j + 3 < j1) k_pages(j + 3);
+            if (j + 2 < j1) v_pages(j + 2);
+        };
+        auto leave = [&](int j) {
+            if (j + 2 < j1) widen_k(j + 2);
+            if (j + 1 < j1) widen_v(j + 1);
+            there = there_next;
+            there_next = there_after;
         };
         auto whole_at = [&](int j) { return there && tile_lo + j * KT >= all_lo && tile_lo + j * KT + KT <= all_hi && rows > 0; };
-        auto step = [&](auto whole_, const int key0, const int buf) {
+        auto step = [&](auto whole_, const int j) {
             constexpr bool WHOLE = decltype(whole_)::value;
+            const int key0 = tile_lo + j * KT, buf = j & 1;
+            f32x4_t next[RT][4];
+            scores(j + 1, next);                                      // (behind the last step: of whatever is there, for nobody)
             {
-                f32x4_t sc[RT][4];
-#pragma unroll
-                for (int n = 0; n < 4; ++n) {
-                    uint4 kf[KS];
-#pragma unroll
-                    for (int c = 0; c < KS; ++c) kf[c] = k_s[buf][c * 4 + g][16 * n + r];
-#pragma unroll
-                    for (int rt = 0; rt < RT; ++rt) {
-                        sc[rt][n] = f32x4_t{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-                        for (int i = NT - 1; i >= 0; --i)
-#pragma unroll
-                            for (int c = 0; c < KS; ++c) sc[rt][n] = mfma(kf[c], q[rt][c][i], sc[rt][n]);
-                    }
-                }
                 uint32_t seen_bits[RT];                               // bit 8 u + e: key 32 u + 8 g + e of the step
                 if constexpr (!WHOLE) {
                     bool here[2];
@@ -616,17 +661,52 @@ __global__ __launch_bounds__(256, 2) void paged_many_kernel(PagedAttentionArgs a
                             for (int i = 0; i < 4; ++i) sc[rt][n][i] = seen_bits[rt] >> (4 * n + i) & 1 ? sc[rt][n][i] : -INFINITY;
                     }
                 }
-                // weights: exponentials above the running maximum by up to 2^8 are let be, the sums are brought to a new maximum only beyond
+                // Weights: exponentials above a row's reference, which is the maximum at the time it was set.  It is set again only where a lane's sum
+                // passes 2^10 (or nothing was seen before): the steps in between need no maximum.
+                uint4 p[RT][2][PT];
+                float sum[RT];
+                auto weights = [&](int rt) {
+                    const float use = m[rt] > -INFINITY ? m[rt] : 0.f;
+                    sum[rt] = 0.f;
+#pragma unroll
+                    for (int u = 0; u < 2; ++u) {
+                        uint32_t words[PT][4];
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) {
+                            const f32x4_t &z = sc[rt][2 * u + i / 2];
+                            float x = __builtin_amdgcn_exp2f(__builtin_fmaf(z[i % 2 * 2], factor, -use)), y = __builtin_amdgcn_exp2f(__builtin_fmaf(z[i % 2 * 2 + 1], factor, -use));
+                            sum[rt] += x;
+                            sum[rt] += y;
+#pragma unroll
+                            for (int k = 0; k < PT; ++k) {
+                                words[k][i] = two_bf16(x, y);
+                                if (k + 1 < PT) {
+                                    x -= bf16_lo(words[k][i]);
+                                    y -= bf16_hi(words[k][i]);
+                                }
+                            }
+                        }
+#pragma unroll
+                        for (int k = 0; k < PT; ++k) p[rt][u][k] = uint4{words[k][0], words[k][1], words[k][2], words[k][3]};
+                    }
+                };
+                bool set = false;
 #pragma unroll
                 for (int rt = 0; rt < RT; ++rt) {
-                    float top = -INFINITY;
+                    weights(rt);
+                    set |= sum[rt] > 1024.f || m[rt] == -INFINITY;
+                }
+                if (__any(set)) {
 #pragma unroll
-                    for (int n = 0; n < 4; ++n)
+                    for (int rt = 0; rt < RT; ++rt) {
+                        float top = -INFINITY;
 #pragma unroll
-                        for (int i = 0; i < 4; ++i) top = fmaxf(top, sc[rt][n][i]);
-                    top = max_over_rows(top) * factor;
-                    if (__any(top > m[rt] + 8.0f)) {
-                        top = top > m[rt] + 8.0f ? top : m[rt];           // (a row's result does not depend on the others')
+                        for (int n = 0; n < 4; ++n)
+#pragma unroll
+                            for (int i = 0; i < 4; ++i) top = fmaxf(top, sc[rt][n][i]);
+                        top = max_over_rows(top) * factor;
+                        const bool mine = max_over_rows(sum[rt]) > 1024.f || m[rt] == -INFINITY;      // (a row's result does not depend on the others')
+                        top = mine ? fmaxf(top, m[rt]) : m[rt];
                         const float shrink = __builtin_amdgcn_exp2f(m[rt] - (top > -INFINITY ? top : 0.f));
                         m[rt] = top;
                         l[rt] *= shrink;
@@ -634,50 +714,22 @@ __global__ __launch_bounds__(256, 2) void paged_many_kernel(PagedAttentionArgs a
                         for (int d = 0; d < DT; ++d)
 #pragma unroll
                             for (int i = 0; i < 4; ++i) acc[rt][d][i] *= shrink;
+                        weights(rt);
                     }
-                    const float use = m[rt] > -INFINITY ? m[rt] : 0.f;
-                    float sum = 0.f;
-#pragma unroll
-                    for (int n = 0; n < 4; ++n)
-#pragma unroll
-                        for (int i = 0; i < 4; ++i) {
-                            sc[rt][n][i] = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[rt][n][i], factor, -use));
-                            sum += sc[rt][n][i];
-                        }
-                    l[rt] += sum;
                 }
-                auto weights = [&](int rt, int u, uint4 (&p)[PT]) {
-                    uint32_t words[PT][4];
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        float x = sc[rt][2 * u + i / 2][i % 2 * 2], y = sc[rt][2 * u + i / 2][i % 2 * 2 + 1];
-#pragma unroll
-                        for (int k = 0; k < PT; ++k) {
-                            words[k][i] = two_bf16(x, y);
-                            if (k + 1 < PT) {
-                                x -= bf16_lo(words[k][i]);
-                                y -= bf16_hi(words[k][i]);
-                            }
-                        }
-                    }
-#pragma unroll
-                    for (int k = 0; k < PT; ++k) p[k] = uint4{words[k][0], words[k][1], words[k][2], words[k][3]};
-                };
+                for (int rt = 0; rt < RT; ++rt) l[rt] += sum[rt];
                 if constexpr (WHOLE) {
 #pragma unroll
-                    for (int u = 0; u < 2; ++u) {
-                        uint4 p[RT][PT];
-#pragma unroll
-                        for (int rt = 0; rt < RT; ++rt) weights(rt, u, p[rt]);
+                    for (int u = 0; u < 2; ++u)
 #pragma unroll
                         for (int d = 0; d < DT; ++d) {
                             const uint4 v = v_s[buf][4 * u + g][16 * d + r];
 #pragma unroll
                             for (int rt = 0; rt < RT; ++rt)
 #pragma unroll
-                                for (int k = PT - 1; k >= 0; --k) acc[rt][d] = mfma(v, p[rt][k], acc[rt][d]);
+                                for (int k = PT - 1; k >= 0; --k) acc[rt][d] = mfma(v, p[rt][u][k], acc[rt][d]);
                         }
-                    }
                 } else {
                     // values of places that do not exist may be anything: zeros; others that are not finite are kept from the rows that do not see them
 #pragma unroll
@@ -704,14 +756,12 @@ __global__ __launch_bounds__(256, 2) void paged_many_kernel(PagedAttentionArgs a
                         asm volatile("" ::: "memory");
 #pragma unroll
                         for (int rt = 0; rt < RT; ++rt) {
-                            uint4 p[PT];
-                            weights(rt, u, p);
                             if (finite) {
 #pragma unroll
                                 for (int d = 0; d < DT; ++d) {
                                     const uint4 v = value(d);
 #pragma unroll
-                                    for (int k = PT - 1; k >= 0; --k) acc[rt][d] = mfma(v, p[k], acc[rt][d]);
+                                    for (int k = PT - 1; k >= 0; --k) acc[rt][d] = mfma(v, p[rt][u][k], acc[rt][d]);
                                 }
                             } else {
 #pragma unroll 1
@@ -727,7 +777,7 @@ __global__ __launch_bounds__(256, 2) void paged_many_kernel(PagedAttentionArgs a
                                         v.x &= mine[0]; v.y &= mine[1]; v.z &= mine[2]; v.w &= mine[3];
                                         f32x4_t one = acc[rt][d];
 #pragma unroll
-                                        for (int k = PT - 1; k >= 0; --k) one = mfma(v, p[k], one);
+                                        for (int k = PT - 1; k >= 0; --k) one = mfma(v, p[rt][u][k], one);
 #pragma unroll
                                         for (int i = 0; i < 4; ++i) acc[rt][d][i] = r == x ? one[i] : acc[rt][d][i];
                                     }
@@ -737,20 +787,24 @@ __global__ __launch_bounds__(256, 2) void paged_many_kernel(PagedAttentionArgs a
                     }
                 }
             }
+#pragma unroll
+            for (int n = 0; n < 4; ++n)
+#pragma unroll
+                for (int rt = 0; rt < RT; ++rt) sc[rt][n] = next[rt][n];
         };
         // (a loop of its own for the steps that every row of the wave sees whole: one loop with both kinds spills in both)
         for (int j = j0; j < j1;) {
             for (; j < j1 && whole_at(j); ++j) {
-                const int buf = (j - j0) & 1;
-                enter(j, buf);
-                step(std::integral_constant<bool, true>(), tile_lo + j * KT, buf);
-                if (j + 1 < j1) widen(buf ^ 1);
+                enter(j);
+                step(std::integral_constant<bool, true>(), j);
+                leave(j);
             }
             for (; j < j1 && !whole_at(j); ++j) {
-                const int buf = (j - j0) & 1, key0 = tile_lo + j * KT;
-                enter(j, buf);
-                if (rows > 0 && key0 < any_hi && key0 + KT > any_lo) step(std::integral_constant<bool, false>(), key0, buf);
-                if (j + 1 < j1) widen(buf ^ 1);
+                const int key0 = tile_lo + j * KT;
+                enter(j);
+                if (rows > 0 && key0 < any_hi && key0 + KT > any_lo) step(std::integral_constant<bool, false>(), j);
+                else scores(j + 1, sc);
+                leave(j);
             }
         }
         __syncthreads();                                              // the next tile's loads write what other waves may still read
@@ -901,8 +955,8 @@ hipError_t launch_paged_attention(const PagedAttentionArgs &a, hipStream_t strea
         }                                                                                                                    \
         if (!few) {                                                                                                          \
             pl.above = many ? 0 : kFewUpto; pl.upto = 0x7fffffff;                                                            \
-            costs(128, 512, 1024);                                                                                                 \
-            hipLaunchKernelGGL((paged_many_kernel<NT, C, D, 2>), dim3(kGroups), dim3(256), 0, stream, a, pl);                \
+            costs(NT == 3 ? 64 : 128, 512, 1024);                                                                                                 \
+            hipLaunchKernelGGL((paged_many_kernel<NT, C, D, (NT == 3 ? 1 : 2)>), dim3(kGroups), dim3(256), 0, stream, a, pl);                \
         }                                                                                                                    \
     } while (0)
 #define SPD_FEW_D(NT, C) do { if (a.c.dim == 64) SPD_FEW_RT(NT, C, 64); else SPD_FEW_RT(NT, C, 128); } while (0)

@@ -44,7 +44,7 @@ struct PagedSeq {
         rising = most < base ? 0 : (rows && a.window ? (int)min((unsigned)tiles, (most - base) / rows) : tiles);
         whole = before(tiles);
     }
-    static constexpr int kStart = 64;      // what a tile costs besides its keys
+    static constexpr int kStart = QT >= 64 ? 160 : 64;      // what a tile costs besides its keys
     __device__ __forceinline__ unsigned cost(int t) const { return min(base + (unsigned)(t + 1) * rows, most) + 1; }
     __device__ __forceinline__ unsigned before(int t) const {       // sum of the costs of tiles 0 .. t - 1
         const unsigned c = min(t, rising);
