@@ -505,6 +505,14 @@ __global__ __launch_bounds__(256, 2) void paged_many_kernel(PagedAttentionArgs a
                     }
             }
         }
+        // The queries have to be there before the loop: the compiler does not count the loads into LDS, and a wait for the queries inside it would be one
+        // for those loads.
+#pragma unroll
+        for (int rt = 0; rt < RT; ++rt)
+#pragma unroll
+            for (int c = 0; c < KS; ++c)
+#pragma unroll
+                for (int k = 0; k < NT; ++k) asm volatile("" : "+v"(q[rt][c][k].x), "+v"(q[rt][c][k].y), "+v"(q[rt][c][k].z), "+v"(q[rt][c][k].w));
         const float factor = fmaxf(fabsf(a.scale) * kLog2e * (WIDEN ? a.c.k_scale[h] : 1.0f), 1e-37f);       // (0: positions that are not seen stay at -infinity)
         f32x4_t acc[RT][DT];
         float m[RT], l[RT];
@@ -639,8 +647,8 @@ __global__ __launch_bounds__(256, 2) void paged_many_kernel(PagedAttentionArgs a
         auto step = [&](auto whole_, const int j) {
             constexpr bool WHOLE = decltype(whole_)::value;
             const int key0 = tile_lo + j * KT, buf = j & 1;
-            f32x4_t next[RT][4];
-            scores(j + 1, next);                                      // (behind the last step: of whatever is there, for nobody)
+            f32x4_t next[RT][4];                                      // (behind the last step: of whatever is there, for nobody)
+            if constexpr (!WHOLE) scores(j + 1, next);
             {
                 uint32_t seen_bits[RT];                               // bit 8 u + e: key 32 u + 8 g + e of the step
                 if constexpr (!WHOLE) {
@@ -665,37 +673,76 @@ __global__ __launch_bounds__(256, 2) void paged_many_kernel(PagedAttentionArgs a
                 // passes 2^10 (or nothing was seen before): the steps in between need no maximum.
                 uint4 p[RT][2][PT];
                 float sum[RT];
-                auto weights = [&](int rt) {
+                // half a row tile's: 32 keys
+                auto weights = [&](int rt, int u) {
                     const float use = m[rt] > -INFINITY ? m[rt] : 0.f;
-                    sum[rt] = 0.f;
+                    if (u == 0) sum[rt] = 0.f;
+                    uint32_t words[PT][4];
 #pragma unroll
-                    for (int u = 0; u < 2; ++u) {
-                        uint32_t words[PT][4];
+                    for (int i = 0; i < 4; ++i) {
+                        const f32x4_t &z = sc[rt][2 * u + i / 2];
+                        float x = __builtin_amdgcn_exp2f(__builtin_fmaf(z[i % 2 * 2], factor, -use)), y = __builtin_amdgcn_exp2f(__builtin_fmaf(z[i % 2 * 2 + 1], factor, -use));
+                        sum[rt] += x;
+                        sum[rt] += y;
 #pragma unroll
-                        for (int i = 0; i < 4; ++i) {
-                            const f32x4_t &z = sc[rt][2 * u + i / 2];
-                            float x = __builtin_amdgcn_exp2f(__builtin_fmaf(z[i % 2 * 2], factor, -use)), y = __builtin_amdgcn_exp2f(__builtin_fmaf(z[i % 2 * 2 + 1], factor, -use));
-                            sum[rt] += x;
-                            sum[rt] += y;
-#pragma unroll
-                            for (int k = 0; k < PT; ++k) {
-                                words[k][i] = two_bf16(x, y);
-                                if (k + 1 < PT) {
-                                    x -= bf16_lo(words[k][i]);
-                                    y -= bf16_hi(words[k][i]);
-                                }
+                        for (int k = 0; k < PT; ++k) {
+                            words[k][i] = two_bf16(x, y);
+                            if (k + 1 < PT) {
+                                x -= bf16_lo(words[k][i]);
+                                y -= bf16_hi(words[k][i]);
                             }
                         }
-#pragma unroll
-                        for (int k = 0; k < PT; ++k) p[rt][u][k] = uint4{words[k][0], words[k][1], words[k][2], words[k][3]};
                     }
+#pragma unroll
+                    for (int k = 0; k < PT; ++k) p[rt][u][k] = uint4{words[k][0], words[k][1], words[k][2], words[k][3]};
                 };
+                // The operands in LDS are read two groups of products ahead, and the order is held: left to itself the compiler reads each just
+                // before its use, and the wave waits for LDS at every second product.
+                constexpr int VB = 4, NB = 2 * DT / VB;               // operands a group, groups of the second product
+                uint4 vb[2][VB];
+                auto read_v = [&](int x) {
+#pragma unroll
+                    for (int i = 0; i < VB; ++i) vb[x & 1][i] = v_s[buf][4 * ((x * VB + i) / DT) + g][16 * ((x * VB + i) % DT) + r];
+                };
+                if constexpr (WHOLE) {
+                    uint4 kf[2][4];
+                    auto read_k = [&](int c) {
+#pragma unroll
+                        for (int n = 0; n < 4; ++n) kf[c & 1][n] = k_s[(j + 1) & 1][c * 4 + g][16 * n + r];
+                    };
+                    read_k(0);
+                    read_k(1);
+#pragma unroll
+                    for (int n = 0; n < 4; ++n)
+#pragma unroll
+                        for (int rt = 0; rt < RT; ++rt) next[rt][n] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                    for (int c = 0; c < KS; ++c) {
+                        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+                        for (int i = NT - 1; i >= 0; --i)
+#pragma unroll
+                            for (int n = 0; n < 4; ++n)
+#pragma unroll
+                                for (int rt = 0; rt < RT; ++rt) next[rt][n] = mfma(kf[c & 1][n], q[rt][c][i], next[rt][n]);
+                        if (c + 2 < KS) read_k(c + 2);
+                        else read_v(c + 2 - KS);
+#pragma unroll
+                        for (int x = c * 2 * RT / KS; x < (c + 1) * 2 * RT / KS; ++x) weights(x / 2, x % 2);
+#pragma unroll
+                        for (int i = 0; i < 4 * RT * NT; ++i) {       // in turn
+                            __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+                            __builtin_amdgcn_sched_group_barrier(0x002, 5, 0);
+                        }
+                    }
+                    __builtin_amdgcn_sched_barrier(0);
+                } else {
+#pragma unroll
+                    for (int x = 0; x < 2 * RT; ++x) weights(x / 2, x % 2);
+                }
                 bool set = false;
 #pragma unroll
-                for (int rt = 0; rt < RT; ++rt) {
-                    weights(rt);
-                    set |= sum[rt] > 1024.f || m[rt] == -INFINITY;
-                }
+                for (int rt = 0; rt < RT; ++rt) set |= sum[rt] > 1024.f || m[rt] == -INFINITY;
                 if (__any(set)) {
 #pragma unroll
                     for (int rt = 0; rt < RT; ++rt) {
@@ -714,22 +761,28 @@ __global__ __launch_bounds__(256, 2) void paged_many_kernel(PagedAttentionArgs a
                         for (int d = 0; d < DT; ++d)
 #pragma unroll
                             for (int i = 0; i < 4; ++i) acc[rt][d][i] *= shrink;
-                        weights(rt);
+                        weights(rt, 0);
+                        weights(rt, 1);
                     }
                 }
 #pragma unroll
                 for (int rt = 0; rt < RT; ++rt) l[rt] += sum[rt];
                 if constexpr (WHOLE) {
 #pragma unroll
-                    for (int u = 0; u < 2; ++u)
+                    for (int x = 0; x < NB; ++x) {
+                        __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-                        for (int d = 0; d < DT; ++d) {
-                            const uint4 v = v_s[buf][4 * u + g][16 * d + r];
+                        for (int i = 0; i < VB; ++i)
 #pragma unroll
                             for (int rt = 0; rt < RT; ++rt)
 #pragma unroll
-                                for (int k = PT - 1; k >= 0; --k) acc[rt][d] = mfma(v, p[rt][u][k], acc[rt][d]);
-                        }
+                                for (int k = PT - 1; k >= 0; --k) {
+                                    const int d = (x * VB + i) % DT, u = (x * VB + i) / DT;
+                                    acc[rt][d] = mfma(vb[x & 1][i], p[rt][u][k], acc[rt][d]);
+                                }
+                        if (x + 2 < NB) read_v(x + 2);
+                    }
+                    __builtin_amdgcn_sched_barrier(0);
                 } else {
                     // values of places that do not exist may be anything: zeros; others that are not finite are kept from the rows that do not see them
 #pragma unroll
