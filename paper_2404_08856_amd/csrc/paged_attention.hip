@@ -39,6 +39,7 @@ __device__ __forceinline__ uint4 operand(const uint4 &x, int e) {
 __device__ __forceinline__ void agent_store(float *p, float x) { __hip_atomic_store(p, x, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
 __device__ __forceinline__ float agent_load(const float *p) { return __hip_atomic_load(p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
 
+constexpr int kGroups = 512;                 // workgroups that share tiles, at most
 constexpr float kLn2 = 0.693147180559945309f, kLog2e = 1.44269504088896341f;
 
 // 8 neighbouring elements of a query as bf16 terms; flip: the sign bits to turn
@@ -115,7 +116,7 @@ __global__ __launch_bounds__(NW * 64, NW / 4) void paged_few_kernel(PagedAttenti
     const int P = 1 << a.c.page_bits, group = pl.group;
     const size_t page_bytes = (size_t)a.c.n_kv * P * D * sizeof(C), head_bytes = (size_t)P * D * sizeof(C);
     const bool q_wide = (uintptr_t)a.q.p % 16 == 0 && (a.q.row | a.q.head) % 8 == 0, out_wide = (uintptr_t)a.out.p % 16 == 0 && (a.out.row | a.out.head) % 4 == 0;
-    const PagedRuns<QT> runs(a, pl, gridDim.x);
+    const PagedRuns<QT> runs(a, pl, gridDim.x, gridDim.x);
     const int w = blockIdx.x;
     if (w >= runs.n) return;
     unsigned pos = runs.start(w), before;
@@ -131,10 +132,10 @@ __global__ __launch_bounds__(NW * 64, NW / 4) void paged_few_kernel(PagedAttenti
             do seq.init(a, pl, ++s, runs.flat); while (seq.tiles == 0 && s + 1 < a.b.n_seqs);
             continue;
         }
-        const int h = (int)(off / head_cost);
-        const unsigned in_head = off - h * head_cost;
-        const int t = seq.tile_at(in_head);
-        const unsigned cost = seq.cost(t), x0 = in_head - seq.before(t), x1 = min(cost, x0 + (end - pos));
+        int h, t;
+        unsigned first_cost;
+        seq.at(off, a.c.n_kv, runs.flat, h, t, first_cost);
+        const unsigned cost = seq.cost(t), x0 = off - first_cost, x1 = min(cost, x0 + (end - pos));
         // ---- the tile: packed rows t * QT .. , keys of all its rows
         const int packed = seq.n * group, valid = min(QT, packed - t * QT);
         const int i_first = t * QT / group, i_last = (t * QT + valid - 1) / group, len = seq.len;
@@ -456,9 +457,10 @@ __global__ __launch_bounds__(256, 2) void paged_many_kernel(PagedAttentionArgs a
     const int P = 1 << a.c.page_bits, group = pl.group;
     const size_t page_bytes = (size_t)a.c.n_kv * P * D * sizeof(C), head_bytes = (size_t)P * D * sizeof(C);
     const bool q_wide = (uintptr_t)a.q.p % 16 == 0 && (a.q.row | a.q.head) % 8 == 0, out_wide = (uintptr_t)a.out.p % 16 == 0 && (a.out.row | a.out.head) % 4 == 0;
-    const PagedRuns<QT> runs(a, pl, gridDim.x);
+    const PagedRuns<QT> runs(a, pl, kGroups, gridDim.x);
     if ((int)blockIdx.x >= runs.n) return;
-    const int eighth = runs.n / 8, w = (int)blockIdx.x < 8 * eighth ? (int)(blockIdx.x % 8 * eighth + blockIdx.x / 8) : (int)blockIdx.x;   // neighbours in the row of tiles on one XCD
+    // Workgroups on one XCD have neighbours in the row of tiles, which read the same keys; one by one the heads alternate, and with them the XCDs
+    const int eighth = runs.n / 8, w = !runs.flat && (int)blockIdx.x < 8 * eighth ? (int)(blockIdx.x % 8 * eighth + blockIdx.x / 8) : (int)blockIdx.x;
     unsigned pos = runs.start(w), before;
     const unsigned end = runs.start(w + 1);
     int s;
@@ -473,10 +475,10 @@ __global__ __launch_bounds__(256, 2) void paged_many_kernel(PagedAttentionArgs a
             do seq.init(a, pl, ++s, runs.flat); while (seq.tiles == 0 && s + 1 < a.b.n_seqs);
             continue;
         }
-        const int h = (int)(off / head_cost);
-        const unsigned in_head = off - h * head_cost;
-        const int t = seq.tile_at(in_head);
-        const unsigned cost = seq.cost(t), x0 = in_head - seq.before(t), x1 = min(cost, x0 + (end - pos));
+        int h, t;
+        unsigned first_cost;
+        seq.at(off, a.c.n_kv, runs.flat, h, t, first_cost);
+        const unsigned cost = seq.cost(t), x0 = off - first_cost, x1 = min(cost, x0 + (end - pos));
         const int packed = seq.n * group, valid = min(QT, packed - t * QT), len = seq.len;
         const int i_first = t * QT / group, i_last = (t * QT + valid - 1) / group;
         const int tile_end = a.seen ? min(len + min(seq.n, 64), a.b.capacity) : min(len + i_last + 1, a.b.capacity);
@@ -955,7 +957,6 @@ __global__ __launch_bounds__(256, 2) void paged_many_kernel(PagedAttentionArgs a
 
 // ---- launches -----------------------------------------------------------------------
 
-constexpr int kGroups = 512;                 // workgroups at most
 constexpr int kFewUpto = 64;                 // packed rows of a sequence that the kernel of few rows takes at most
 static size_t slot_floats(int QT, int dim) { return (size_t)QT * (dim + 2); }
 
@@ -993,6 +994,7 @@ hipError_t launch_paged_attention(const PagedAttentionArgs &a, hipStream_t strea
         pl.join = std::max(1, join >> pl.shift);
     };
     const int wide = mean;
+    auto many_grid = [&](int QT) { return (unsigned)std::min<u64>(std::max<u64>(kGroups, ((u64)a.b.n_rows * pl.group / QT + a.b.n_seqs) * a.c.n_kv), 1 << 20); };
 #define SPD_FEW(NT, C, D, RT, NW)                                                                                            \
     do {                                                                                                                     \
         costs(16 * RT, 512, 850);                                                                                                 \
@@ -1009,7 +1011,7 @@ hipError_t launch_paged_attention(const PagedAttentionArgs &a, hipStream_t strea
         if (!few) {                                                                                                          \
             pl.above = many ? 0 : kFewUpto; pl.upto = 0x7fffffff;                                                            \
             costs(NT == 3 ? 64 : 128, 512, 1024);                                                                                                 \
-            hipLaunchKernelGGL((paged_many_kernel<NT, C, D, (NT == 3 ? 1 : 2)>), dim3(kGroups), dim3(256), 0, stream, a, pl);                \
+            hipLaunchKernelGGL((paged_many_kernel<NT, C, D, (NT == 3 ? 1 : 2)>), dim3(many_grid(NT == 3 ? 64 : 128)), dim3(256), 0, stream, a, pl); \
         }                                                                                                                    \
     } while (0)
 #define SPD_FEW_D(NT, C) do { if (a.c.dim == 64) SPD_FEW_RT(NT, C, 64); else SPD_FEW_RT(NT, C, 128); } while (0)

@@ -45,6 +45,18 @@ struct PagedSeq {
         whole = before(tiles);
     }
     static constexpr int kStart = QT >= 64 ? 160 : 64;      // what a tile costs besides its keys
+    // the tile at cost x < whole * heads of the sequence: head, tile, and the cost before it
+    __device__ __forceinline__ void at(unsigned x, int heads, bool flat, int &h, int &t, unsigned &first_cost) const {
+        if (flat) {
+            t = tiles - 1 - (int)(x / (unsigned)heads);
+            h = (int)(x % (unsigned)heads);
+            first_cost = x;
+        } else {
+            h = (int)(x / whole);
+            t = tile_at(x - h * whole);
+            first_cost = h * whole + before(t);
+        }
+    }
     __device__ __forceinline__ unsigned cost(int t) const { return min(base + (unsigned)(t + 1) * rows, most) + 1; }
     __device__ __forceinline__ unsigned before(int t) const {       // sum of the costs of tiles 0 .. t - 1
         const unsigned c = min(t, rising);
@@ -65,13 +77,15 @@ __device__ __forceinline__ int units_before(int units, unsigned x, unsigned cost
     return x >= cost ? units : min(units, (int)((float)x * ((float)units / (float)cost)));
 }
 
-// The runs: workgroup w takes [start(w), start(w + 1)) of the whole cost.  Where the tiles are no more than the workgroups and the largest is not above the
-// mean of a workgroup by more than sharing costs, each workgroup takes one tile (flat).  Called by whole waves.
+// The runs: workgroup w < n takes [start(w), start(w + 1)) of the whole cost.  Where the tiles taken one by one, a sequence's longest first, are expected to be
+// done no later than even runs and what sharing tiles costs, each workgroup takes one tile (flat): the expectation is a full round for tiles of about
+// the same cost, and, where a sequence's costs fall to half or less, that the short ones fill the gaps.  Called by whole waves.
+// side: workgroups that run side by side; grid: all.
 template <int QT>
 struct PagedRuns {
     const PagedAttentionArgs &a;
     const PagedPlan &pl;
-    unsigned each, more, mine;             // mine: this lane's sum of costs over the first 64 sequences, itself included
+    unsigned each, more, mine = 0;         // mine: this lane's sum of costs over the first 64 sequences, itself included
     int n;                                 // workgroups
     bool flat;
 
@@ -98,15 +112,17 @@ struct PagedRuns {
         q.init(a, pl, s, flat);
         return q.whole * a.c.n_kv;
     }
-    __device__ __forceinline__ PagedRuns(const PagedAttentionArgs &a_, const PagedPlan &p_, int groups) : a(a_), pl(p_), flat(false) {
+    struct Min { __device__ __forceinline__ unsigned operator()(unsigned x, unsigned y) const { return min(x, y); } };
+    __device__ __forceinline__ PagedRuns(const PagedAttentionArgs &a_, const PagedPlan &p_, unsigned side, unsigned grid) : a(a_), pl(p_), flat(false) {
         const int lane = threadIdx.x & 63;
-        unsigned total = 0, tiles = 0, largest = 0;
+        unsigned total = 0, tiles = 0, largest = 0, least = 0xffffffffu;
         if (a.b.n_seqs == 1) {
             PagedSeq<QT> q;
             q.init(a, pl, 0, false);
             tiles = q.tiles;
             total = q.whole * a.c.n_kv;
             largest = q.tiles ? q.cost(q.tiles - 1) : 0;
+            least = q.cost(0);
         } else {
             for (int s0 = 0; s0 < a.b.n_seqs; s0 += 64) {
                 PagedSeq<QT> q;
@@ -116,12 +132,15 @@ struct PagedRuns {
                 total += over_lanes(q.whole * a.c.n_kv, Add());
                 tiles += over_lanes(q.tiles, Add());
                 largest = max(largest, over_lanes(q.tiles ? q.cost(q.tiles - 1) : 0u, Max()));
+                least = min(least, over_lanes(q.tiles ? q.cost(0) : 0xffffffffu, Min()));
             }
         }
         const unsigned items = tiles * a.c.n_kv;
-        flat = items <= (unsigned)groups && largest <= total / (unsigned)groups + pl.join;
+        const unsigned even = total / side, rounds = (items + side - 1) / side;
+        const unsigned expected = rounds > 1 && 2 * least <= largest ? max(largest, even + least) : rounds * largest;
+        flat = items <= grid && expected <= even + pl.join;
         if (flat) total = items;
-        n = total == 0 ? 0 : (flat ? (int)items : (int)max(1u, min((unsigned)groups, total / pl.least)));
+        n = total == 0 ? 0 : (flat ? (int)items : (int)max(1u, min(side, total / pl.least)));
         each = n ? total / (unsigned)n : 1;
         more = n ? total - each * n : 0;
         if (a.b.n_seqs > 1 && n) mine = scan(flat ? cost_of(lane) : mine);
