@@ -39,25 +39,16 @@ __device__ __forceinline__ uint32_t pack_bf16(float a, float b) {
     return __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2_t{a, b}), bf16x2_t));
 }
 // N neighbouring elements; 8 of them by loads and stores of 16 bytes
-template <int N>
-__device__ __forceinline__ void load_n(const float *p, float (&x)[N]) {
+template <int N, class T>
+__device__ __forceinline__ void load_n(const T *p, T (&x)[N]) {
     if constexpr (N == 8) {
-        const float4 a = reinterpret_cast<const float4 *>(p)[0], b = reinterpret_cast<const float4 *>(p)[1];
-        x[0] = a.x; x[1] = a.y; x[2] = a.z; x[3] = a.w; x[4] = b.x; x[5] = b.y; x[6] = b.z; x[7] = b.w;
+        uint4 q[sizeof(T) / 2];
+#pragma unroll
+        for (int i = 0; i < (int)sizeof(T) / 2; ++i) q[i] = reinterpret_cast<const uint4 *>(p)[i];
+        __builtin_memcpy(x, q, sizeof(x));
     } else {
 #pragma unroll
         for (int i = 0; i < N; ++i) x[i] = p[i];
-    }
-}
-template <int N>
-__device__ __forceinline__ void load_n(const uint16_t *p, float (&x)[N]) {
-    if constexpr (N == 8) {
-        const uint4 a = *reinterpret_cast<const uint4 *>(p);
-        x[0] = bf16_lo(a.x); x[1] = bf16_hi(a.x); x[2] = bf16_lo(a.y); x[3] = bf16_hi(a.y);
-        x[4] = bf16_lo(a.z); x[5] = bf16_hi(a.z); x[6] = bf16_lo(a.w); x[7] = bf16_hi(a.w);
-    } else {
-#pragma unroll
-        for (int i = 0; i < N; ++i) x[i] = bf16_bits_to_f32(p[i]);
     }
 }
 template <int N>
@@ -92,10 +83,12 @@ struct Part {
     bool turned;
     // parts of a head; without the rest where it stays in place
     static __host__ __device__ int count(int R, int dim, bool rest) { return (IL ? R : R / 2) / E + (rest ? (dim - R) / ET : 0); }
-    __device__ __forceinline__ void init(int part, int position, const RopeRef &r, bool inverse) {
+    __device__ __forceinline__ void init(int part, const RopeRef &r) {
         const int n = (IL ? r.R : r.R / 2) / E;
         turned = part < n;
         at = turned ? part * E : r.R + (part - n) * ET;
+    }
+    __device__ __forceinline__ void angles(int position, const RopeRef &r, bool inverse) {
         if (!turned) return;
         const float m = *reinterpret_cast<const float *>(r.table);
         const uint64_t *turn = reinterpret_cast<const uint64_t *>((const char *)r.table + kRopeHeader) + (IL ? at / 2 : at);
@@ -106,35 +99,45 @@ struct Part {
             cs[i] *= m;
         }
     }
+    // What the thread reads of a head, as it lies there: loads may be under way while something else is found out
+    template <class T>
+    struct Raw { T a[E], b[IL ? 1 : E], rest[ET]; };
+    template <class T>
+    __device__ __forceinline__ void load(const T *x, int R, Raw<T> &raw) const {
+        if (!turned) {
+            load_n<ET>(x + at, raw.rest);
+        } else {
+            load_n<E>(x + at, raw.a);
+            if constexpr (!IL) load_n<E>(x + at + R / 2, raw.b);
+        }
+    }
     // store(element, values of a run)
     template <class T, class Store>
-    __device__ __forceinline__ void apply(const T *x, int R, Store store) const {
+    __device__ __forceinline__ void apply(const Raw<T> &raw, int R, Store store) const {
         if (!turned) {
             float v[ET];
-            load_n<ET>(x + at, v);
+#pragma unroll
+            for (int i = 0; i < ET; ++i) v[i] = to_f32(raw.rest[i]);
             store(at, v);
         } else if constexpr (IL) {
             float v[E];
-            load_n<E>(x + at, v);
 #pragma unroll
             for (int i = 0; i < NP; ++i) {
-                const float a = v[2 * i], b = v[2 * i + 1];
+                const float a = to_f32(raw.a[2 * i]), b = to_f32(raw.a[2 * i + 1]);
                 v[2 * i] = __builtin_fmaf(a, cs[i], -(b * sn[i]));
                 v[2 * i + 1] = __builtin_fmaf(a, sn[i], b * cs[i]);
             }
             store(at, v);
         } else {
-            float a[E], b[E];
-            load_n<E>(x + at, a);
-            load_n<E>(x + at + R / 2, b);
+            float v[E], w[E];
 #pragma unroll
             for (int i = 0; i < NP; ++i) {
-                const float u = a[i], w = b[i];
-                a[i] = __builtin_fmaf(u, cs[i], -(w * sn[i]));
-                b[i] = __builtin_fmaf(u, sn[i], w * cs[i]);
+                const float a = to_f32(raw.a[i]), b = to_f32(raw.b[i]);
+                v[i] = __builtin_fmaf(a, cs[i], -(b * sn[i]));
+                w[i] = __builtin_fmaf(a, sn[i], b * cs[i]);
             }
-            store(at, a);
-            store(at + R / 2, b);
+            store(at, v);
+            store(at + R / 2, w);
         }
     }
 };
@@ -148,30 +151,45 @@ __global__ __launch_bounds__(kRopeThreads) void rope_kernel(RopeArgs a, int part
     const unsigned row = i / (unsigned)parts;
     if (row >= (unsigned)a.n_rows) return;
     Part<WIDE, IL> part;
-    part.init(i - row * parts, a.positions[row], a.rope, a.inverse);
+    part.init(i - row * parts, a.rope);
     const int h0 = blockIdx.y * per, h1 = min(h0 + per, a.n_heads);
     const T *x = (const T *)a.x.p + row * a.x.row;
     T *out = (T *)a.out.p + row * a.out.row;
-    for (int h = h0; h < h1; ++h)
-        part.apply(x + h * a.x.head, a.rope.R, [&](int at, const auto &v) { store_n(out + h * a.out.head + at, v); });
+    typename Part<WIDE, IL>::template Raw<T> raw;
+    part.load(x + h0 * a.x.head, a.rope.R, raw);
+    part.angles(a.positions[row], a.rope, a.inverse);
+    for (int h = h0; h < h1; ++h) {
+        const auto now = raw;
+        if (h + 1 < h1) part.load(x + (h + 1) * a.x.head, a.rope.R, raw);
+        part.apply(now, a.rope.R, [&](int at, const auto &v) { store_n(out + h * a.out.head + at, v); });
+    }
 }
 
 // ---- append -----------------------------------------------------------------------
 
-// the sequence that `row` belongs to; n_seqs: none
-__device__ __forceinline__ int seq_of(const PagedBatchArgs &b, int row) {
-    if (!b.row_start) return row / b.each;
-    int lo = 0, hi = b.n_seqs;                               // the last sequence that starts at or before the row
-    while (hi - lo > 1) {
-        const int mid = (lo + hi) / 2;
-        if (b.row_start[mid] <= row) lo = mid; else hi = mid;
+// The batch's rows and lengths: in LDS where they fit
+struct BatchRows {
+    const int32_t *starts, *lens;
+    // the sequence that `row` belongs to, its first row and the one behind its last; n_seqs: none
+    __device__ __forceinline__ int find(const PagedBatchArgs &b, int row, int &first, int &last) const {
+        if (!b.row_start) {
+            const int seq = row / b.each;
+            first = seq * b.each;
+            last = first + b.each;
+            return seq;
+        }
+        int lo = 0, hi = b.n_seqs;                           // the last sequence that starts at or before the row
+        while (hi - lo > 1) {
+            const int mid = (lo + hi) / 2;
+            if (starts[mid] <= row) lo = mid; else hi = mid;
+        }
+        first = min(max(starts[lo], 0), b.n_rows);
+        last = min(max(starts[lo + 1], first), b.n_rows);
+        return row >= first && row < last ? lo : b.n_seqs;
     }
-    int first, last;
-    paged_rows(b, lo, first, last);
-    return row >= first && row < last ? lo : b.n_seqs;
-}
+    __device__ __forceinline__ int len(const PagedBatchArgs &b, int seq) const { return min(max(lens[seq], 0), b.capacity); }
+};
 
-struct E4m3 { uint8_t x; };
 __device__ __forceinline__ float to_held(float x, float scale) {       // x / scale within e4m3's range, NaN kept
     return __builtin_elementwise_minimum(__builtin_elementwise_maximum(x / scale, -448.0f), 448.0f);
 }
@@ -194,51 +212,116 @@ __device__ __forceinline__ void put_held(uint8_t *p, const float (&x)[N], float 
     }
 }
 
-// grid: parts of all rows / 256, groups of `per` heads: of the queries, then of the keys, then of the values
-template <class T, class C, bool WIDE, bool IL>
-__global__ __launch_bounds__(kRopeThreads) void paged_append_kernel(PagedAppendArgs a, int parts, int per, int q_groups, int k_groups) {
+constexpr int kStartsInLds = 1024;
+
+// Values: a wave takes a head of `block` rows, a lane D / 64 dims of it.  Where a granule's slots are all of this call, the lane has the granule together
+// and writes its 16 bytes (rows of 64 lanes side by side); a part of one is written element by element, so that the slots beside it stay as they are.
+// 7100 rows of 32 + 8 + 8 heads: see launch_paged_append.
+template <class T, class C, int N>
+__device__ __forceinline__ void append_values(const PagedAppendArgs &a, const BatchRows &rows, int unit, int block) {
     constexpr int G = 16 / sizeof(C);
-    const unsigned i = blockIdx.x * kRopeThreads + threadIdx.x;
-    const unsigned row = i / (unsigned)parts;
-    if (row >= (unsigned)a.b.n_rows) return;
-    const int seq = seq_of(a.b, row);
-    if (seq >= a.b.n_seqs) return;
-    int first, last;
-    paged_rows(a.b, seq, first, last);
-    const int p = paged_len(a.b, seq) + ((int)row - first), P = 1 << a.c.page_bits, slot = p & (P - 1);
-    const int group = blockIdx.y, kind = group < q_groups ? 0 : (group < q_groups + k_groups ? 1 : 2);
-    const int h0 = (group - (kind == 0 ? 0 : (kind == 1 ? q_groups : q_groups + k_groups))) * per, h1 = min(h0 + per, kind == 0 ? a.n_heads : a.c.n_kv);
-    Part<WIDE, IL> part;
-    RopeRef rope = a.rope;
-    if (kind == 2) rope.R = 0;
-    if ((int)(i - row * parts) >= Part<WIDE, IL>::count(rope.R, a.c.dim, true)) return;      // turned heads have fewer parts
-    part.init(i - row * parts, a.positions ? a.positions[row] : p, rope, false);
-    if (kind == 0) {
-        for (int h = h0; h < h1; ++h)
-            part.apply((const T *)a.q.p + row * a.q.row + h * a.q.head, rope.R,
-                       [&](int at, const auto &v) { store_n((T *)a.q_out.p + row * a.q_out.row + h * a.q_out.head + at, v); });
+    const int lane = threadIdx.x & 63, h = unit % a.c.n_kv, row0 = unit / a.c.n_kv * block, P = 1 << a.c.page_bits;
+    // a lane per row: which rows begin a granule (or their sequence)
+    const int row = row0 + lane;
+    int seq = a.b.n_seqs, first = 0, last = 0, p = 0;
+    if (lane < block && row < a.b.n_rows) seq = rows.find(a.b, row, first, last);
+    if (seq < a.b.n_seqs) p = rows.len(a.b, seq) + (row - first);
+    unsigned long long begins = __ballot(seq < a.b.n_seqs && (row == first || p % G == 0));
+    const float scale = a.c.v_scale ? a.c.v_scale[h] : 1.0f;
+    while (begins) {
+        const int l = __builtin_ctzll(begins);
+        begins &= begins - 1;
+        const int s = __builtin_amdgcn_readlane(seq, l), pos = __builtin_amdgcn_readlane(p, l), end = __builtin_amdgcn_readlane(last, l);
+        const int r0 = row0 + l, slot = pos & (P - 1), n = min(G - slot % G, end - r0);
+        const T *src = (const T *)a.v.p + h * a.v.head + lane * N;
+        T raw[G][N];                                             // on their way together with the page
+#pragma unroll
+        for (int i = 0; i < G; ++i)
+#pragma unroll
+            for (int e = 0; e < N; ++e) raw[i][e] = src[(size_t)(r0 + min(i, n - 1)) * a.v.row + e];
+        const int page = paged_page(a.b, a.c, s, pos >> a.c.page_bits);
+        if (page < 0) continue;                                  // a granule lies in one page
+        float x[G][N];
+#pragma unroll
+        for (int i = 0; i < G; ++i)
+#pragma unroll
+            for (int e = 0; e < N; ++e) x[i][e] = to_f32(raw[i][e]);
+        C *dst = (C *)a.c.v + (((size_t)page * a.c.n_kv + h) * (P / G) + slot / G) * a.c.dim * G + lane * N * G;
+        if (n == G) {
+#pragma unroll
+            for (int e = 0; e < N; ++e)
+#pragma unroll
+                for (int i = 0; i < G; i += 8) {
+                    float y[8];
+#pragma unroll
+                    for (int k = 0; k < 8; ++k) y[k] = x[i + k][e];
+                    put_held(dst + e * G + i, y, scale);
+                }
+        } else {
+#pragma unroll
+            for (int i = 0; i < G; ++i)
+                if (i < n) {
+#pragma unroll
+                    for (int e = 0; e < N; ++e) {
+                        const float one[1] = {x[i][e]};
+                        put_held(dst + e * G + slot % G + i, one, scale);
+                    }
+                }
+        }
+    }
+}
+
+struct AppendGrid { int parts, per, q_groups, groups, across, block; };   // parts of a row's head, heads a thread, groups of heads (of q; all), workgroups a group, rows a wave of values
+
+// grid: groups of `per` heads, of the queries and then of the keys, by the parts of all rows / 256; then the values, four waves a workgroup
+template <class T, class C, bool WIDE, bool IL>
+__global__ __launch_bounds__(kRopeThreads) void paged_append_kernel(PagedAppendArgs a, AppendGrid g) {
+    constexpr int G = 16 / sizeof(C);
+    __shared__ int32_t starts[kStartsInLds + 1], lens[kStartsInLds];
+    BatchRows rows{a.b.row_start, a.b.lens};
+    const bool in_lds = a.b.row_start && a.b.n_seqs <= kStartsInLds;
+    if (in_lds)
+        for (int i = threadIdx.x; i <= a.b.n_seqs; i += kRopeThreads) {
+            starts[i] = a.b.row_start[i];
+            if (i < a.b.n_seqs) lens[i] = a.b.lens[i];
+        }
+    if ((int)blockIdx.x >= g.groups * g.across) {
+        const int unit = (blockIdx.x - g.groups * g.across) * 4 + (threadIdx.x >> 6);
+        if (in_lds) { __syncthreads(); rows = BatchRows{starts, lens}; }
+        if (unit / a.c.n_kv * g.block >= a.b.n_rows) return;
+        if (a.c.dim == 64) append_values<T, C, 1>(a, rows, unit, g.block);
+        else append_values<T, C, 2>(a, rows, unit, g.block);
         return;
     }
-    const int page = paged_page(a.b, a.c, seq, p >> a.c.page_bits);
+    const int group = blockIdx.x / g.across;
+    const unsigned i = (blockIdx.x - group * g.across) * kRopeThreads + threadIdx.x, row = i / (unsigned)g.parts;
+    const bool keys = group >= g.q_groups, mine = row < (unsigned)a.b.n_rows;
+    const int h0 = (keys ? group - g.q_groups : group) * g.per, h1 = min(h0 + g.per, keys ? a.c.n_kv : a.n_heads);
+    const HeadsArgs &src = keys ? a.k : a.q;
+    const T *x = (const T *)src.p + row * src.row;
+    Part<WIDE, IL> part;
+    part.init(i - row * g.parts, a.rope);
+    typename Part<WIDE, IL>::template Raw<T> raw;
+    if (mine) part.load(x + h0 * src.head, a.rope.R, raw);
+    if (in_lds) { __syncthreads(); rows = BatchRows{starts, lens}; }
+    if (!mine) return;
+    int first, last;
+    const int seq = rows.find(a.b, row, first, last);
+    if (seq >= a.b.n_seqs) return;
+    const int p = rows.len(a.b, seq) + ((int)row - first), page = keys ? paged_page(a.b, a.c, seq, p >> a.c.page_bits) : 0;
     if (page < 0) return;
-    const HeadsArgs &src = kind == 1 ? a.k : a.v;
-    const float *scales = kind == 1 ? a.c.k_scale : a.c.v_scale;
+    part.angles(a.positions ? a.positions[row] : p, a.rope, false);
+    const int P = 1 << a.c.page_bits, slot = p & (P - 1);
     for (int h = h0; h < h1; ++h) {
-        C *dst = (C *)(kind == 1 ? a.c.k : a.c.v) + ((size_t)page * a.c.n_kv + h) * a.c.dim * P;
-        const float scale = scales ? scales[h] : 1.0f;
-        part.apply((const T *)src.p + row * src.row + h * src.head, rope.R, [&](int at, const auto &v) {
-            if (kind == 1) {
-                put_held(dst + ((size_t)(at / G) * P + slot) * G + at % G, v, scale);
-            } else {
-                constexpr int N = sizeof(v) / sizeof(float);
-                C *to = dst + ((size_t)(slot / G) * a.c.dim + at) * G + slot % G;
-#pragma unroll
-                for (int e = 0; e < N; ++e) {
-                    const float one[1] = {v[e]};
-                    put_held(to + e * G, one, scale);
-                }
-            }
-        });
+        const auto now = raw;
+        if (h + 1 < h1) part.load(x + (h + 1) * src.head, a.rope.R, raw);
+        if (keys) {
+            C *dst = (C *)a.c.k + ((size_t)page * a.c.n_kv + h) * a.c.dim * P;
+            const float scale = a.c.k_scale ? a.c.k_scale[h] : 1.0f;
+            part.apply(now, a.rope.R, [&](int at, const auto &v) { put_held(dst + ((size_t)(at / G) * P + slot) * G + at % G, v, scale); });
+        } else {
+            part.apply(now, a.rope.R, [&](int at, const auto &v) { store_n((T *)a.q_out.p + row * a.q_out.row + h * a.q_out.head + at, v); });
+        }
     }
 }
 
@@ -280,13 +363,20 @@ hipError_t launch_rope(const RopeArgs &a, hipStream_t stream) {
 hipError_t launch_paged_append(const PagedAppendArgs &a, hipStream_t stream) {
     const int size = a.bf16 ? 2 : 4;
     const bool wide = (!a.rope.table || wide_rope(a.rope, a.c.dim)) && wide_heads(a.k, size) && wide_heads(a.v, size) && (!a.q.p || (wide_heads(a.q, size) && wide_heads(a.q_out, size)));
+    // Rows of values a wave: a granule's where that leaves enough waves, else one (the wave of a granule's first row takes all of it)
+    const int granule = a.c.e4m3 ? 16 : 8;
+    AppendGrid g;
+    g.block = (size_t)a.b.n_rows * a.c.n_kv >= (size_t)granule * 256 ? granule : 1;
+    const unsigned value_groups = (unsigned)(((size_t)((a.b.n_rows + g.block - 1) / g.block) * a.c.n_kv + 3) / 4);
 #define SPD_APPEND(T, C, W, I)                                                                                               \
     do {                                                                                                                     \
-        const int parts = std::max(Part<W, I>::count(a.rope.R, a.c.dim, true), Part<W, I>::count(0, a.c.dim, true));         \
-        const size_t threads = (size_t)parts * a.b.n_rows;                                                                   \
-        const int per = heads_per_thread(threads, a.n_heads + 2 * a.c.n_kv);                                                 \
-        const int qg = a.q.p ? (a.n_heads + per - 1) / per : 0, kg = (a.c.n_kv + per - 1) / per;                             \
-        hipLaunchKernelGGL((paged_append_kernel<T, C, W, I>), dim3((threads + kRopeThreads - 1) / kRopeThreads, qg + 2 * kg), dim3(kRopeThreads), 0, stream, a, parts, per, qg, kg); \
+        g.parts = Part<W, I>::count(a.rope.R, a.c.dim, true);                                                                \
+        const size_t threads = (size_t)g.parts * a.b.n_rows;                                                                 \
+        g.per = heads_per_thread(threads, a.n_heads + a.c.n_kv);                                                             \
+        g.q_groups = a.q.p ? (a.n_heads + g.per - 1) / g.per : 0;                                                            \
+        g.groups = g.q_groups + (a.c.n_kv + g.per - 1) / g.per;                                                              \
+        g.across = (int)((threads + kRopeThreads - 1) / kRopeThreads);                                                       \
+        hipLaunchKernelGGL((paged_append_kernel<T, C, W, I>), dim3((unsigned)(g.groups * g.across) + value_groups), dim3(kRopeThreads), 0, stream, a, g); \
     } while (0)
 #define SPD_APPEND_I(T, C, W) do { if (a.rope.interleaved) SPD_APPEND(T, C, W, true); else SPD_APPEND(T, C, W, false); } while (0)
 #define SPD_APPEND_W(T, C) do { if (wide) SPD_APPEND_I(T, C, true); else SPD_APPEND_I(T, C, false); } while (0)
