@@ -271,9 +271,10 @@ __device__ __forceinline__ void append_values(const PagedAppendArgs &a, const Ba
     }
 }
 
-struct AppendGrid { int parts, per, q_groups, groups, across, block; };   // parts of a row's head, heads a thread, groups of heads (of q; all), workgroups a group, rows a wave of values
+// workgroups of values; rows a wave of them; parts of a row's head, heads a thread, groups of heads (of q; all), workgroups a group
+struct AppendGrid { int values_first, value_groups, block, parts, per, q_groups, groups, across; };
 
-// grid: groups of `per` heads, of the queries and then of the keys, by the parts of all rows / 256; then the values, four waves a workgroup
+// grid: the values, four waves a workgroup, and groups of `per` heads, of the queries and of the keys, by the parts of all rows / 256
 template <class T, class C, bool WIDE, bool IL>
 __global__ __launch_bounds__(kRopeThreads) void paged_append_kernel(PagedAppendArgs a, AppendGrid g) {
     constexpr int G = 16 / sizeof(C);
@@ -285,16 +286,17 @@ __global__ __launch_bounds__(kRopeThreads) void paged_append_kernel(PagedAppendA
             starts[i] = a.b.row_start[i];
             if (i < a.b.n_seqs) lens[i] = a.b.lens[i];
         }
-    if ((int)blockIdx.x >= g.groups * g.across) {
-        const int unit = (blockIdx.x - g.groups * g.across) * 4 + (threadIdx.x >> 6);
+    const int turned = g.groups * g.across, in_values = (int)blockIdx.x - (g.values_first ? 0 : turned);
+    if (in_values >= 0 && in_values < g.value_groups) {
+        const int unit = in_values * 4 + (threadIdx.x >> 6);
         if (in_lds) { __syncthreads(); rows = BatchRows{starts, lens}; }
         if (unit / a.c.n_kv * g.block >= a.b.n_rows) return;
         if (a.c.dim == 64) append_values<T, C, 1>(a, rows, unit, g.block);
         else append_values<T, C, 2>(a, rows, unit, g.block);
         return;
     }
-    const int group = blockIdx.x / g.across;
-    const unsigned i = (blockIdx.x - group * g.across) * kRopeThreads + threadIdx.x, row = i / (unsigned)g.parts;
+    const int block = (int)blockIdx.x - (g.values_first ? g.value_groups : 0), group = block / g.across;
+    const unsigned i = (block - group * g.across) * kRopeThreads + threadIdx.x, row = i / (unsigned)g.parts;
     const bool keys = group >= g.q_groups, mine = row < (unsigned)a.b.n_rows;
     const int h0 = (keys ? group - g.q_groups : group) * g.per, h1 = min(h0 + g.per, keys ? a.c.n_kv : a.n_heads);
     const HeadsArgs &src = keys ? a.k : a.q;
@@ -334,10 +336,10 @@ hipError_t launch_rope_table(const RopeTableArgs &a, void *table, hipStream_t st
 
 static bool wide_heads(const HeadsArgs &h, int size) { return (uintptr_t)h.p % 16 == 0 && h.row * size % 16 == 0 && h.head * size % 16 == 0; }
 static bool wide_rope(const RopeRef &r, int dim) { return dim % 8 == 0 && r.R % (r.interleaved ? 8 : 16) == 0; }
-// heads a thread takes: more share the sines and cosines, fewer fill the CUs
+// heads a thread takes: more share the sines and cosines, fewer fill the CUs (2400 rows of 16 + 4 + 4 heads of 64: 10.0 us with 256 Ki threads asked for, 9.5 with 64 Ki)
 static int heads_per_thread(size_t threads, int heads) {
     int per = 8;
-    while (per > 1 && threads * ((heads + per - 1) / per) < 256 * 1024) per /= 2;
+    while (per > 1 && threads * ((heads + per - 1) / per) < 64 * 1024) per /= 2;
     return per;
 }
 
@@ -367,7 +369,10 @@ hipError_t launch_paged_append(const PagedAppendArgs &a, hipStream_t stream) {
     const int granule = a.c.e4m3 ? 16 : 8;
     AppendGrid g;
     g.block = (size_t)a.b.n_rows * a.c.n_kv >= (size_t)granule * 256 ? granule : 1;
-    const unsigned value_groups = (unsigned)(((size_t)((a.b.n_rows + g.block - 1) / g.block) * a.c.n_kv + 3) / 4);
+    g.value_groups = (int)(((size_t)((a.b.n_rows + g.block - 1) / g.block) * a.c.n_kv + 3) / 4);
+    // Few of them start first, as a wave of values waits longest; many would hold the others up: 2400 rows of 16 + 4 + 4 heads of 64 in e4m3, 155 workgroups,
+    // 9.7 us first and 11.5 last; 7100 rows of 32 + 8 + 8 heads of 128, 1775 workgroups, 46 and 41.
+    g.values_first = g.value_groups <= 512;
 #define SPD_APPEND(T, C, W, I)                                                                                               \
     do {                                                                                                                     \
         g.parts = Part<W, I>::count(a.rope.R, a.c.dim, true);                                                                \
@@ -376,7 +381,7 @@ hipError_t launch_paged_append(const PagedAppendArgs &a, hipStream_t stream) {
         g.q_groups = a.q.p ? (a.n_heads + g.per - 1) / g.per : 0;                                                            \
         g.groups = g.q_groups + (a.c.n_kv + g.per - 1) / g.per;                                                              \
         g.across = (int)((threads + kRopeThreads - 1) / kRopeThreads);                                                       \
-        hipLaunchKernelGGL((paged_append_kernel<T, C, W, I>), dim3((unsigned)(g.groups * g.across) + value_groups), dim3(kRopeThreads), 0, stream, a, g); \
+        hipLaunchKernelGGL((paged_append_kernel<T, C, W, I>), dim3((unsigned)(g.groups * g.across) + (unsigned)g.value_groups), dim3(kRopeThreads), 0, stream, a, g); \
     } while (0)
 #define SPD_APPEND_I(T, C, W) do { if (a.rope.interleaved) SPD_APPEND(T, C, W, true); else SPD_APPEND(T, C, W, false); } while (0)
 #define SPD_APPEND_W(T, C) do { if (wide) SPD_APPEND_I(T, C, true); else SPD_APPEND_I(T, C, false); } while (0)
