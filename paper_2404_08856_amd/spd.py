@@ -509,12 +509,15 @@ def spd_q4_matmul(matrix, x, y, workspace=None):
 _U64 = torch.int64
 
 
-def _heads(t, device, dtype, dim):
-    """spd_heads of a [rows, heads, dim] tensor on the current device whose heads' elements are neighbours (any strides between rows and heads)."""
-    shape, (row, head, step) = t.shape, t.stride()
-    assert t.dtype == dtype and t.get_device() == device and shape[2] == dim and (step == 1 or dim == 1), \
-        f"expected {dtype} [rows, heads, {dim}] on device {device} with contiguous heads, got {t.dtype} {tuple(shape)} with strides {t.stride()} on {t.device}"
-    return spd_heads(t.data_ptr(), row, head)
+def _heads(t, device, dtype):
+    """Address of an spd_heads of a [rows, heads, dim] tensor on the current device whose heads' elements are neighbours (any strides between rows and heads)."""
+    row, head, step = t.stride()
+    assert t.dtype == dtype and t.get_device() == device and (step == 1 or t.shape[2] == 1), \
+        f"expected {dtype} [rows, heads, dim] on device {device} with contiguous heads, got {t.dtype} {tuple(t.shape)} with strides {t.stride()} on {t.device}"
+    return _byref(spd_heads(t.data_ptr(), row, head))
+
+
+_byref = ctypes.byref
 
 
 def _row_type(t):
@@ -536,20 +539,20 @@ class Rope:
         self.table = torch.empty(b.value, dtype=torch.uint8, device=device)
         here = _current_device()
         _check(_lib.spd_rope_table(ctypes.byref(cfg), *_scratch(self.table, here), _raw_stream(here)))
-        self.rotary_dim, self.interleaved = int(rotary_dim), bool(interleaved)
+        self.rotary_dim, self.interleaved, self.device = int(rotary_dim), bool(interleaved), here
         self._struct = spd_rope(self.table.data_ptr(), self.rotary_dim, int(self.interleaved))
         self._at = ctypes.addressof(self._struct)
 
 
 def spd_rope_apply(rope, x, positions, out, inverse=False):
     """out [rows, heads, dim] (x itself will do) = x turned by positions [rows] int32."""
-    rows, heads, dim = x.shape
+    shape = x.shape
+    rows, heads, dim = shape
     here = _current_device()
     dtype, flags = _row_type(x)
-    assert out.shape == x.shape and rope.table.get_device() == here, f"expected an output of {tuple(x.shape)}, and the table on device {here}"
-    a, b = _heads(x, here, dtype, dim), _heads(out, here, dtype, dim)
-    _check(_lib.spd_rope_apply(rope._at, ctypes.byref(a), ctypes.byref(b), _own(positions, here, _I32, (rows,)), rows, heads, dim,
-                               flags | (SPD_ROPE_INVERSE if inverse else 0), _raw_stream(here)))
+    assert out.shape == shape and rope.device == here, f"expected an output of {tuple(shape)}, and the table on device {here}"
+    _check(_lib.spd_rope_apply(rope._at, _heads(x, here, dtype), _heads(out, here, dtype), _own(positions, here, _I32, (rows,)), rows, heads, dim,
+                               flags | SPD_ROPE_INVERSE if inverse else flags, _raw_stream(here)))
 
 
 def paged_cache_shapes(n_pages, page_size, n_kv_heads, head_dim, e4m3=False):
@@ -603,13 +606,18 @@ def spd_paged_append(cache, batch, k, v, rope=None, positions=None, q=None, q_ou
     here = _paged_here(cache, batch)
     rows, dim = batch.n_rows, cache.head_dim
     dtype, flags = _row_type(k)
-    assert k.shape == v.shape == (rows, cache.n_kv_heads, dim), f"expected keys and values {(rows, cache.n_kv_heads, dim)}, got {tuple(k.shape)} and {tuple(v.shape)}"
-    assert (q is None) == (q_out is None) and (q is None or q.shape == q_out.shape and q.shape[0] == rows), "q and q_out go together, with a row each"
-    assert rope is None or rope.table.get_device() == here, "the table is on the current device"
-    heads = [_heads(t, here, dtype, dim) for t in (k, v) + (() if q is None else (q, q_out))]
-    at = [ctypes.addressof(h) for h in heads] + [None, None]
-    _check(_lib.spd_paged_append(cache._at, batch._at, *at[:4], 0 if q is None else q.shape[1], None if rope is None else rope._at,
-                                 _own(positions, here, _I32, (rows,)), flags, _raw_stream(here)))
+    shape = (rows, cache.n_kv_heads, dim)
+    assert k.shape == shape and v.shape == shape, f"expected keys and values {shape}, got {tuple(k.shape)} and {tuple(v.shape)}"
+    qh = oh = None
+    heads = 0
+    if q is not None or q_out is not None:
+        assert q is not None and q_out is not None, "q and q_out go together"
+        heads = q.shape[1]
+        assert q.shape == (rows, heads, dim) and q_out.shape == q.shape, f"expected queries [{rows}, heads, {dim}] and an output like them, got {tuple(q.shape)} and {tuple(q_out.shape)}"
+        qh, oh = _heads(q, here, dtype), _heads(q_out, here, dtype)
+    assert rope is None or rope.device == here, "the table is on the current device"
+    _check(_lib.spd_paged_append(cache._at, batch._at, _heads(k, here, dtype), _heads(v, here, dtype), qh, oh, heads, None if rope is None else rope._at,
+                                 None if positions is None else _own(positions, here, _I32, (rows,)), flags, _raw_stream(here)))
 
 
 def spd_paged_attention_workspace_bytes(cache, batch, n_heads):
@@ -623,11 +631,11 @@ def spd_paged_attention(cache, batch, q, out, scale=None, window=0, seen=None, l
     here = _paged_here(cache, batch)
     rows, heads, dim = q.shape
     dtype, flags = _row_type(q)
-    assert rows == batch.n_rows and out.shape == q.shape, f"expected {batch.n_rows} rows and an output of {tuple(q.shape)}, got {tuple(out.shape)}"
+    assert rows == batch.n_rows and dim == cache.head_dim and out.shape == q.shape, \
+        f"expected queries [{batch.n_rows}, heads, {cache.head_dim}] and an output like them, got {tuple(q.shape)} and {tuple(out.shape)}"
     if workspace is None:
         workspace = torch.empty(spd_paged_attention_workspace_bytes(cache, batch, heads), dtype=torch.uint8, device=q.device)
-    a, b = _heads(q, here, dtype, cache.head_dim), _heads(out, here, dtype, cache.head_dim)
-    _check(_lib.spd_paged_attention(cache._at, batch._at, ctypes.byref(a), ctypes.byref(b), heads, dim ** -0.5 if scale is None else scale, window,
+    _check(_lib.spd_paged_attention(cache._at, batch._at, _heads(q, here, dtype), _heads(out, here, dtype), heads, dim ** -0.5 if scale is None else scale, window,
                                     _own(seen, here, _U64, (rows,)), _own(lse_out, here, _F32, (rows, heads)), flags, *_scratch(workspace, here), _raw_stream(here)))
 
 
