@@ -444,6 +444,18 @@ int32_t spd_paged_attention(const spd_paged_cache *h_cache, const spd_paged_batc
                             int32_t n_heads, float scale, int32_t window, const uint64_t *seen, float *lse_out, uint32_t flags,
                             void *workspace, size_t workspace_bytes, void *stream);
 
+/* spd_verify_forward over pages instead of the model's own cache: one forward of the new rows of a batch (ragged ones too, up to SPD_MAX_ROWS
+ * together), whose keys and values go into layers[l] of layer l (host array of n_layers; heads and head size those of the model, pages alike in
+ * all layers) and whose attention reads them, causal or, with `seen`, over a tree of drafted tokens (then with `positions`: what a token's place in
+ * its branch says).  tokens: int32 [n_rows].  logits_out: float32 [n_rows, vocab]; those of rows behind the last sequence say nothing.  rope: the
+ * model's positions (rotary_dim head_dim, its theta) or others, e.g. stretched for contexts beyond the model's; max_positions bounds nothing here.
+ * The model's own cache and lengths stay as they are, the lengths of the batch are the caller's to advance.  Prompts go in pieces of up to SPD_MAX_ROWS rows.
+ * Works for models in 4 bits too.  Errors as spd_paged_append and spd_paged_attention; SPD_ERR_SHAPE for other heads or more rows. */
+int32_t spd_verify_paged_workspace_bytes(const spd_model *model, const spd_paged_cache *h_layers, const spd_paged_batch *h_batch, size_t *h_bytes);
+int32_t spd_verify_forward_paged(spd_model *model, const int32_t *tokens, const spd_paged_cache *h_layers, const spd_paged_batch *h_batch,
+                                 const spd_rope *h_rope, const int32_t *positions, const uint64_t *seen, float *logits_out,
+                                 void *workspace, size_t workspace_bytes, void *stream);
+
 /* ---- the block loop without the host (Section 2.1, one block = gamma draft steps, one
  * target call, accept / resample, commit) ---------------------------------------------
  *

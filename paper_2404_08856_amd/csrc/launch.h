@@ -93,6 +93,8 @@ struct CommitArgs {
     int n_seqs, gamma, out_capacity;
 };
 hipError_t launch_block_commit(const CommitArgs &a, hipStream_t stream);
+// float32 rows [rows][K] (K % 8 == 0) as packed activations
+hipError_t launch_pack_rows(const float *x, int rows, int K, void *xpack, hipStream_t stream);
 hipError_t launch_fill_zero(void *p, size_t bytes, hipStream_t stream);
 // K and V of positions pos0 .. pos0 + n - 1 of one (layer, sequence) as float32 [n][H][dh] (k_cache / v_cache: that pair's slices)
 hipError_t launch_kv_export(const void *k_cache, const void *v_cache, int H, int dh, int max_positions, int pos0, int n,

@@ -594,11 +594,20 @@ int32_t run_chain(spd_model *m, const AttnArgs &lens, int seq0, int n_seqs, int 
     return SPD_OK;
 }
 
+// A forward over pages: the rows' keys and values go into them, and the rows' attention reads them.
+struct PagedLayers {
+    PagedAppendArgs append;              // of a layer but for its cache; queries are turned where they are
+    PagedAttentionArgs attention;
+    const spd_paged_cache *cache;        // [n_layers]
+    float *rows;                         // float32 [rows][n_heads * head_dim]: the attention's results
+};
+
 // Layers first .. of the decoder for M new rows of each of sequences seq0 .. seq0 + n_seqs - 1, and the LM head (logits_out may be NULL).
 // The input rows are in place: h, packed (h * attn_norm[first]) and their sums of squares (one part per row); `at` has the
 // KV lengths; longest: the longest of them as far as the host can tell.  kv_cached (a prompt's last row): layer
 // `first`'s key and value of the row are in the cache, and the length counts them; the sums are as exact as the prompt kernels'.
-int32_t run_layers(spd_model *m, int first, AttnArgs &at, int seq0, int n_seqs, int M, int longest, bool kv_cached, float *logits_out, hipStream_t st) {
+// pages (else NULL): see PagedLayers; `at` has nothing to say then.
+int32_t run_layers(spd_model *m, int first, AttnArgs &at, int seq0, int n_seqs, int M, int longest, bool kv_cached, float *logits_out, hipStream_t st, PagedLayers *pages = nullptr) {
     const spd_model_config &c = m->cfg;
     const Layout &L = m->L;
     const int rows = n_seqs * M;
@@ -621,8 +630,8 @@ int32_t run_layers(spd_model *m, int first, AttnArgs &at, int seq0, int n_seqs, 
 
     // Small models, few rows: a projection lasts about as long as its first loads take, so the weights of the next ones are
     // brought into L2 meanwhile.
-    const bool prefetch = !m->q4_group && rows <= 2 * kGroupRows && layer_weight_bytes(c) <= kSmallLayer;
-    const bool fused = m->fuse_qa && n_seqs == 1 && (rows <= kGroupRows || (rows <= 8 && m->fuse_qa2));   // shapes checked at creation
+    const bool prefetch = !pages && !m->q4_group && rows <= 2 * kGroupRows && layer_weight_bytes(c) <= kSmallLayer;
+    const bool fused = !pages && m->fuse_qa && n_seqs == 1 && (rows <= kGroupRows || (rows <= 8 && m->fuse_qa2));   // shapes checked at creation
     for (int l = first; l < c.n_layers; ++l) {
         // RMSNorm is folded into the projections: the producer of h (input rows / O / down
         // epilogue) leaves packed (h * gain) and per-tile sums of squares; the consumer
@@ -654,7 +663,18 @@ int32_t run_layers(spd_model *m, int first, AttnArgs &at, int seq0, int n_seqs, 
                 add(L.wdown[l], d, F);
                 if (l + 1 < c.n_layers) add(L.wqkv[l + 1], 3 * HD, d);
             }
-            for (int m0 = 0; m0 < M; m0 += 8) {         // at most 8 queries per sequence and launch
+            if (pages) {
+                auto in_pages = [&]() -> hipError_t {
+                    pages->append.c.k = pages->attention.c.k = pages->cache[l].k; pages->append.c.v = pages->attention.c.v = pages->cache[l].v;
+                    pages->append.c.k_scale = pages->attention.c.k_scale = pages->cache[l].k_scale; pages->append.c.v_scale = pages->attention.c.v_scale = pages->cache[l].v_scale;
+                    hipError_t rc = launch_paged_append(pages->append, st);
+                    if (rc == hipSuccess) rc = launch_paged_attention(pages->attention, st);
+                    if (rc == hipSuccess && !m->q4_group) rc = launch_pack_rows(pages->rows, rows, HD, xo, st);
+                    return rc;
+                };
+                PROF_TRY(PK_ATTENTION, in_pages());
+            }
+            for (int m0 = 0; m0 < M && !pages; m0 += 8) {         // at most 8 queries per sequence and launch
                 at.m0 = m0; at.Mq = std::min(8, M - m0);
                 PROF_TRY(PK_ATTENTION, launch_attention(at, longest, m0 == 0 ? pf : WeightPrefetch{}, st));
             }
@@ -662,6 +682,7 @@ int32_t run_layers(spd_model *m, int first, AttnArgs &at, int seq0, int n_seqs, 
         g = GemmArgs{};
         g.batch_partials = (float *)(m->ws + L.part); g.batch_arrive = (unsigned *)(m->ws + L.arrive); g.batch_zero = m->ws + L.zero; g.fold = kv_cached;
         g.W = m->packed + L.wo[l]; g.X = xo; g.N = d; g.K = HD; g.rows = rows; g.Y = h; g.ldy = d;
+        if (pages && m->q4_group) { g.X = pages->rows; g.x_rows = true; }
         g.gain_next = gain_of(L.mlp_norm[l]); g.Xnext = xn; g.ssq_out = ssq_a;
         PROF_GEMM(PK_O, g, EPI_RESIDUAL, m->t_o);
         g = GemmArgs{};
@@ -1332,6 +1353,61 @@ int32_t spd_paged_attention(const spd_paged_cache *cache, const spd_paged_batch 
     a.bf16 = flags & SPD_X_IS_BF16; a.workspace = workspace;
     HIP_TRY(launch_paged_attention(a, (hipStream_t)stream));
     return SPD_OK;
+}
+
+// what spd_verify_forward_paged needs behind the attention's own workspace
+static int32_t check_verify_paged(const spd_model *m, const spd_paged_cache *layers, const spd_paged_batch *batch, PagedCacheArgs &c, PagedBatchArgs &b) {
+    if (!m || !layers) return fail(SPD_ERR_INVALID_ARG, "NULL argument to spd_verify_forward_paged");
+    for (int l = 0; l < m->cfg.n_layers; ++l) {
+        const int32_t rc = check_paged(layers + l, batch, c, b);
+        if (rc) return rc;
+        if (c.n_kv != m->cfg.n_heads || c.dim != m->cfg.head_dim) return fail(SPD_ERR_SHAPE, "pages of layer %d have %d heads of %d, the model %d of %d", l, c.n_kv, c.dim, m->cfg.n_heads, m->cfg.head_dim);
+        if (layers[l].page_size != layers[0].page_size || layers[l].n_pages != layers[0].n_pages || layers[l].e4m3 != layers[0].e4m3) return fail(SPD_ERR_SHAPE, "the layers' pages differ");
+    }
+    if (b.n_rows > SPD_MAX_ROWS) return fail(SPD_ERR_SHAPE, "n_rows = %d must be in 1..%d", b.n_rows, SPD_MAX_ROWS);
+    return SPD_OK;
+}
+
+int32_t spd_verify_paged_workspace_bytes(const spd_model *m, const spd_paged_cache *layers, const spd_paged_batch *batch, size_t *bytes) {
+    if (!bytes) return fail(SPD_ERR_INVALID_ARG, "NULL argument to spd_verify_paged_workspace_bytes");
+    PagedCacheArgs c;
+    PagedBatchArgs b;
+    const int32_t rc = check_verify_paged(m, layers, batch, c, b);
+    if (rc) return rc;
+    *bytes = align_up(paged_attention_workspace_bytes(c, b, m->cfg.n_heads), 256) + (size_t)b.n_rows * c.n_kv * c.dim * sizeof(float);
+    return SPD_OK;
+}
+
+int32_t spd_verify_forward_paged(spd_model *m, const int32_t *tokens, const spd_paged_cache *layers, const spd_paged_batch *batch, const spd_rope *rope, const int32_t *positions,
+                                 const uint64_t *seen, float *logits_out, void *workspace, size_t workspace_bytes, void *stream) {
+    if (!tokens || !rope || !logits_out) return fail(SPD_ERR_INVALID_ARG, "NULL argument to spd_verify_forward_paged");
+    PagedLayers pages{};
+    PagedAppendArgs &ap = pages.append;
+    PagedAttentionArgs &pa = pages.attention;
+    int32_t rc = check_verify_paged(m, layers, batch, ap.c, ap.b);
+    if (!rc) rc = check_rope(rope, ap.c.dim);
+    if (rc) return rc;
+    const spd_model_config &c = m->cfg;
+    const Layout &L = m->L;
+    const int rows = ap.b.n_rows, dim = c.head_dim, HD = c.n_heads * dim;
+    const size_t attention_bytes = align_up(paged_attention_workspace_bytes(ap.c, ap.b, c.n_heads), 256);
+    if ((uintptr_t)workspace & 255) return fail(SPD_ERR_INVALID_ARG, "workspace must be 256-byte aligned");
+    if (!workspace || workspace_bytes < attention_bytes + (size_t)rows * HD * sizeof(float)) return fail(SPD_ERR_CAPACITY, "workspace smaller than spd_verify_paged_workspace_bytes reports");
+    float *qkv = (float *)(m->ws + L.qkv);
+    pages.cache = layers;
+    pages.rows = (float *)((char *)workspace + attention_bytes);
+    auto heads = [&](float *p) { return HeadsArgs{p, (size_t)3 * HD, (size_t)dim}; };
+    ap.q = ap.q_out = heads(qkv); ap.k = heads(qkv + HD); ap.v = heads(qkv + 2 * HD);
+    ap.n_heads = c.n_heads; ap.rope = {rope->table, rope->rotary_dim, rope->interleaved != 0}; ap.positions = positions; ap.bf16 = false;
+    pa.c = ap.c; pa.b = ap.b; pa.q = ap.q_out; pa.out = {pages.rows, (size_t)HD, (size_t)dim};
+    pa.n_heads = c.n_heads; pa.window = 0; pa.scale = 1.0f / sqrtf((float)dim); pa.seen = seen; pa.lse = nullptr; pa.bf16 = false; pa.workspace = workspace;
+    hipStream_t st = (hipStream_t)stream;
+    // rows behind the last sequence have no attention: zeros, so that what follows works on numbers
+    if (ap.b.row_start) HIP_TRY(launch_fill_zero(pages.rows, (size_t)rows * HD * sizeof(float), st));
+    PROF_TRY(PK_EMBED, launch_input_rows(m->packed + L.embed, tokens, rows, rows, nullptr, rows, c.d_model, c.vocab, (const float *)(m->packed + L.attn_norm[0]),
+                                         (float *)(m->ws + L.h), m->ws + L.xn, (float *)(m->ws + L.ssq_b), st));
+    AttnArgs at{};
+    return run_layers(m, 0, at, 0, 1, rows, 0, false, logits_out, st, &pages);
 }
 
 }  // extern "C"

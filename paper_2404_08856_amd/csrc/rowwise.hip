@@ -159,6 +159,24 @@ hipError_t launch_kv_export(const void *k_cache, const void *v_cache, int H, int
     return hipGetLastError();
 }
 
+// a thread packs 8 neighbouring values of a row: one slot of each term's operand
+__global__ void pack_rows_kernel(const float *__restrict__ x, int rows, int K, uint16_t *__restrict__ xpack) {
+    const int i = blockIdx.x * blockDim.x + threadIdx.x, row = i / (K / 8), k = i % (K / 8) * 8;
+    if (row >= rows) return;
+    const float4 a = *reinterpret_cast<const float4 *>(x + (size_t)row * K + k), b = *reinterpret_cast<const float4 *>(x + (size_t)row * K + k + 4);
+    uint32_t w[4][kTerms];
+    split3_pair(a.x, a.y, w[0]);
+    split3_pair(a.z, a.w, w[1]);
+    split3_pair(b.x, b.y, w[2]);
+    split3_pair(b.z, b.w, w[3]);
+#pragma unroll
+    for (int t = 0; t < kTerms; ++t) *reinterpret_cast<uint4 *>(xpack + xpack_index(row, k, K / 32, t)) = uint4{w[0][t], w[1][t], w[2][t], w[3][t]};
+}
+hipError_t launch_pack_rows(const float *x, int rows, int K, void *xpack, hipStream_t stream) {
+    hipLaunchKernelGGL(pack_rows_kernel, dim3((rows * (K / 8) + 255) / 256), dim3(256), 0, stream, x, rows, K, (uint16_t *)xpack);
+    return hipGetLastError();
+}
+
 __global__ void fill_zero_kernel(uint4 *p, size_t n16) {
     size_t i = (size_t)blockIdx.x * blockDim.x + threadIdx.x;
     size_t stride = (size_t)gridDim.x * blockDim.x;

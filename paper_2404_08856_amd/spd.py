@@ -33,7 +33,8 @@ EXPORTS = ["spd_last_error", "spd_model_bytes", "spd_model_create", "spd_model_d
            "spd_block_finish", "spd_device_status", "spd_speculative_accept_static", "spd_kv_export", "spd_probe_read_chain",
            "spd_model_bytes_q4", "spd_model_create_q4", "spd_q4_bytes", "spd_q4_quantize", "spd_q4_dequantize", "spd_q4_pack",
            "spd_q4_matmul_workspace_bytes", "spd_q4_matmul", "spd_logprobs_workspace_bytes", "spd_token_logprobs",
-           "spd_rope_table_bytes", "spd_rope_table", "spd_rope_apply", "spd_paged_append", "spd_paged_attention_workspace_bytes", "spd_paged_attention"]
+           "spd_rope_table_bytes", "spd_rope_table", "spd_rope_apply", "spd_paged_append", "spd_paged_attention_workspace_bytes", "spd_paged_attention",
+           "spd_verify_paged_workspace_bytes", "spd_verify_forward_paged"]
 TRACE_KINDS = ["qkv", "o", "gate_up", "down", "lm_head", "attention", "embed"]
 PROJECTIONS = ["qkv", "o", "gate_up", "down", "lm_head"]
 
@@ -148,6 +149,8 @@ _lib.spd_rope_apply.argtypes = [_vp, _vp, _vp, _vp, _i32, _i32, _i32, _u32, _vp]
 _lib.spd_paged_append.argtypes = [_vp, _vp, _vp, _vp, _vp, _vp, _i32, _vp, _vp, _u32, _vp]
 _lib.spd_paged_attention_workspace_bytes.argtypes = [_vp, _vp, _i32, _szp]
 _lib.spd_paged_attention.argtypes = [_vp, _vp, _vp, _vp, _i32, _f32, _i32, _vp, _vp, _u32, _vp, _sz, _vp]
+_lib.spd_verify_paged_workspace_bytes.argtypes = [_vp, _vp, _vp, _szp]
+_lib.spd_verify_forward_paged.argtypes = [_vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _sz, _vp]
 for _name in EXPORTS:
     if _name != "spd_last_error":
         getattr(_lib, _name).restype = _i32
@@ -341,6 +344,19 @@ class Model:
         assert logits_out.shape == (n_seqs, M, self.cfg.vocab)
         _check(_lib.spd_verify_forward(self.handle, _ptr(tokens, torch.int32), n_seqs, M,
                                        _ptr(logits_out, torch.float32), _stream()))
+
+    def spd_verify_forward_paged(self, tokens, layers, batch, rope, logits_out, positions=None, seen=None, workspace=None):
+        """tokens [batch.n_rows] through the model over pages: layers is a PagedCache per layer, logits_out [batch.n_rows, vocab]."""
+        here = _current_device()
+        assert len(layers) == self.cfg.n_layers, f"expected {self.cfg.n_layers} layers, got {len(layers)}"
+        assert all(c.device == here for c in layers) and batch.device == here and rope.device == here, f"pages, batch and table are on the current device {here}"
+        pages, rows = (spd_paged_cache * len(layers))(*[c._struct for c in layers]), (batch.n_rows,)
+        if workspace is None:
+            b = ctypes.c_size_t()
+            _check(_lib.spd_verify_paged_workspace_bytes(self.handle, pages, batch._at, ctypes.byref(b)))
+            workspace = torch.empty(b.value, dtype=torch.uint8, device=tokens.device)
+        _check(_lib.spd_verify_forward_paged(self.handle, _own(tokens, here, _I32, rows), pages, batch._at, rope._at, _own(positions, here, _I32, rows),
+                                             _own(seen, here, _U64, rows), _own(logits_out, here, _F32, (batch.n_rows, self.cfg.vocab)), *_scratch(workspace, here), _raw_stream(here)))
 
     def spd_draft_step(self, tokens_in, temperature, u_draft, D_row_out, token_out):
         n_seqs, n_in = tokens_in.shape

@@ -169,3 +169,12 @@ def test_attentions():
     c, b = structs({}, {})
     expect(bad, "spd_paged_attention_workspace_bytes", by(c), by(b), i32(2), null)
     expect(shape, "spd_paged_attention_workspace_bytes", by(c), by(b), i32(3), ctypes.byref(n))
+
+
+def test_forwards_without_a_model():
+    spd, _ = lib()
+    c, b = structs({}, {})
+    r, n = spd.spd_rope(4096, 64, 0), sz()
+    expect(spd.SPD_ERR_INVALID_ARG, "spd_verify_forward_paged", null, some, by(c), by(b), by(r), null, null, some, some, sz(1 << 40), null)
+    expect(spd.SPD_ERR_INVALID_ARG, "spd_verify_paged_workspace_bytes", null, by(c), by(b), ctypes.byref(n))
+    expect(spd.SPD_ERR_INVALID_ARG, "spd_verify_paged_workspace_bytes", some, by(c), by(b), null)
