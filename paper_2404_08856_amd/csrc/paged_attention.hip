@@ -39,7 +39,7 @@ __device__ __forceinline__ uint4 operand(const uint4 &x, int e) {
 __device__ __forceinline__ void agent_store(float *p, float x) { __hip_atomic_store(p, x, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
 __device__ __forceinline__ float agent_load(const float *p) { return __hip_atomic_load(p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
 
-constexpr int kGroups = 512;                 // workgroups that share tiles, at most
+constexpr int kFewGroups = 256, kGroups = 512;        // workgroups that share tiles, at most: one or two a CU
 constexpr float kLn2 = 0.693147180559945309f, kLog2e = 1.44269504088896341f;
 
 // 8 neighbouring elements of a query as bf16 terms; flip: the sign bits to turn
@@ -116,7 +116,7 @@ __global__ __launch_bounds__(NW * 64, NW / 4) void paged_few_kernel(PagedAttenti
     const int P = 1 << a.c.page_bits, group = pl.group;
     const size_t page_bytes = (size_t)a.c.n_kv * P * D * sizeof(C), head_bytes = (size_t)P * D * sizeof(C);
     const bool q_wide = (uintptr_t)a.q.p % 16 == 0 && (a.q.row | a.q.head) % 8 == 0, out_wide = (uintptr_t)a.out.p % 16 == 0 && (a.out.row | a.out.head) % 4 == 0;
-    const PagedRuns<QT> runs(a, pl, gridDim.x, gridDim.x);
+    const PagedRuns<QT> runs(a, pl, kFewGroups, gridDim.x);
     const int w = blockIdx.x;
     if (w >= runs.n) return;
     unsigned pos = runs.start(w), before;
@@ -204,17 +204,22 @@ __global__ __launch_bounds__(NW * 64, NW / 4) void paged_few_kernel(PagedAttenti
             f32x4_t sc[RT][NK];
             asm volatile("" ::: "memory");                           // the queries are read again each time: as registers they leave room for too few waves
 #pragma unroll
-            for (int n = 0; n < NK; ++n) {
+            for (int n = 0; n < NK; ++n)
 #pragma unroll
                 for (int rt = 0; rt < RT; ++rt) sc[rt][n] = f32x4_t{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-                for (int c = 0; c < KS; ++c) {
-                    const uint4 k = operand<C>(kf[n][c / HALVES], c % HALVES);
+            for (int c = 0; c < KS; ++c) {
+                uint4 k[NK];
 #pragma unroll
-                    for (int rt = 0; rt < RT; ++rt)
+                for (int n = 0; n < NK; ++n) k[n] = operand<C>(kf[n][c / HALVES], c % HALVES);
 #pragma unroll
-                        for (int i = NT - 1; i >= 0; --i) sc[rt][n] = mfma(k, q_s[rt][c][i][lane], sc[rt][n]);
-                }
+                for (int i = NT - 1; i >= 0; --i)
+#pragma unroll
+                    for (int rt = 0; rt < RT; ++rt) {
+                        const uint4 q = q_s[rt][c][i][lane];
+#pragma unroll
+                        for (int n = 0; n < NK; ++n) sc[rt][n] = mfma(k[n], q, sc[rt][n]);
+                    }
             }
             if (more) load_k(u + NW);
             const bool whole = key0 >= all_lo && key0 + UK <= all_hi && __all(there);
@@ -292,14 +297,18 @@ __global__ __launch_bounds__(NW * 64, NW / 4) void paged_few_kernel(PagedAttenti
             }
             if (!odd_values) {
 #pragma unroll
-                for (int d = 0; d < DT; ++d)
+                for (int d0 = 0; d0 < DT; d0 += 4)                    // four outputs at a time: a product does not wait for the one before it
 #pragma unroll
                     for (int hv = 0; hv < HALVES; ++hv) {
-                        const uint4 v = operand<C>(vf[d], hv);
+                        uint4 v[4];
 #pragma unroll
-                        for (int rt = 0; rt < RT; ++rt)
+                        for (int i = 0; i < 4; ++i) v[i] = operand<C>(vf[d0 + i], hv);
 #pragma unroll
-                            for (int k = PT - 1; k >= 0; --k) acc[rt][d] = mfma(v, p[rt][hv][k], acc[rt][d]);
+                        for (int k = PT - 1; k >= 0; --k)
+#pragma unroll
+                            for (int rt = 0; rt < RT; ++rt)
+#pragma unroll
+                                for (int i = 0; i < 4; ++i) acc[rt][d0 + i] = mfma(v[i], p[rt][hv][k], acc[rt][d0 + i]);
                     }
             } else {                                                 // one row at a time, with zeros where it does not see
 #pragma unroll
@@ -774,11 +783,11 @@ __global__ __launch_bounds__(256, 2) void paged_many_kernel(PagedAttentionArgs a
                     for (int x = 0; x < NB; ++x) {
                         __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-                        for (int i = 0; i < VB; ++i)
+                        for (int k = PT - 1; k >= 0; --k)             // (terms outside: a product does not wait for the one before it)
 #pragma unroll
-                            for (int rt = 0; rt < RT; ++rt)
+                            for (int i = 0; i < VB; ++i)
 #pragma unroll
-                                for (int k = PT - 1; k >= 0; --k) {
+                                for (int rt = 0; rt < RT; ++rt) {
                                     const int d = (x * VB + i) % DT, u = (x * VB + i) / DT;
                                     acc[rt][d] = mfma(vb[x & 1][i], p[rt][u][k], acc[rt][d]);
                                 }
@@ -994,11 +1003,12 @@ hipError_t launch_paged_attention(const PagedAttentionArgs &a, hipStream_t strea
         pl.join = std::max(1, join >> pl.shift);
     };
     const int wide = mean;
-    auto many_grid = [&](int QT) { return (unsigned)std::min<u64>(std::max<u64>(kGroups, ((u64)a.b.n_rows * pl.group / QT + a.b.n_seqs) * a.c.n_kv), 1 << 20); };
+    // as many workgroups as there can be tiles, so that each may be taken by one
+    auto tiles_grid = [&](int QT, u64 least) { return (unsigned)std::min<u64>(std::max(least, ((u64)a.b.n_rows * pl.group / QT + a.b.n_seqs) * a.c.n_kv), 1 << 20); };
 #define SPD_FEW(NT, C, D, RT, NW)                                                                                            \
     do {                                                                                                                     \
-        costs(16 * RT, 512, 850);                                                                                                 \
-        hipLaunchKernelGGL((paged_few_kernel<NT, C, D, RT, NW>), dim3(256), dim3(NW * 64), 0, stream, a, pl);                \
+        costs(16 * RT, 512, 1100);                                                                                                 \
+        hipLaunchKernelGGL((paged_few_kernel<NT, C, D, RT, NW>), dim3(tiles_grid(16 * RT, kFewGroups)), dim3(NW * 64), 0, stream, a, pl);                \
     } while (0)
 #define SPD_FEW_RT(NT, C, D)                                                                                                 \
     do {                                                                                                                     \
@@ -1011,7 +1021,7 @@ hipError_t launch_paged_attention(const PagedAttentionArgs &a, hipStream_t strea
         if (!few) {                                                                                                          \
             pl.above = many ? 0 : kFewUpto; pl.upto = 0x7fffffff;                                                            \
             costs(NT == 3 ? 64 : 128, 512, 1024);                                                                                                 \
-            hipLaunchKernelGGL((paged_many_kernel<NT, C, D, (NT == 3 ? 1 : 2)>), dim3(many_grid(NT == 3 ? 64 : 128)), dim3(256), 0, stream, a, pl); \
+            hipLaunchKernelGGL((paged_many_kernel<NT, C, D, (NT == 3 ? 1 : 2)>), dim3(tiles_grid(NT == 3 ? 64 : 128, kGroups)), dim3(256), 0, stream, a, pl); \
         }                                                                                                                    \
     } while (0)
 #define SPD_FEW_D(NT, C) do { if (a.c.dim == 64) SPD_FEW_RT(NT, C, 64); else SPD_FEW_RT(NT, C, 128); } while (0)

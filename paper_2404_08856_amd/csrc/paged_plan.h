@@ -44,7 +44,7 @@ struct PagedSeq {
         rising = most < base ? 0 : (rows && a.window ? (int)min((unsigned)tiles, (most - base) / rows) : tiles);
         whole = before(tiles);
     }
-    static constexpr int kStart = QT >= 64 ? 160 : 64;      // what a tile costs besides its keys
+    static constexpr int kStart = QT >= 64 ? 160 : 256;      // what a tile costs besides its keys
     // the tile at cost x < whole * heads of the sequence: head, tile, and the cost before it
     __device__ __forceinline__ void at(unsigned x, int heads, bool flat, int &h, int &t, unsigned &first_cost) const {
         if (flat) {
@@ -79,7 +79,7 @@ __device__ __forceinline__ int units_before(int units, unsigned x, unsigned cost
 
 // The runs: workgroup w < n takes [start(w), start(w + 1)) of the whole cost.  Where the tiles taken one by one, a sequence's longest first, are expected to be
 // done no later than even runs and what sharing tiles costs, each workgroup takes one tile (flat): the expectation is a full round for tiles of about
-// the same cost, and, where a sequence's costs fall to half or less, that the short ones fill the gaps.  Called by whole waves.
+// the same cost, and, where every sequence's costs fall to half or less, that the short ones fill the gaps.  Called by whole waves.
 // side: workgroups that run side by side; grid: all.
 template <int QT>
 struct PagedRuns {
@@ -116,6 +116,7 @@ struct PagedRuns {
     __device__ __forceinline__ PagedRuns(const PagedAttentionArgs &a_, const PagedPlan &p_, unsigned side, unsigned grid) : a(a_), pl(p_), flat(false) {
         const int lane = threadIdx.x & 63;
         unsigned total = 0, tiles = 0, largest = 0, least = 0xffffffffu;
+        bool falls = true;                 // in every sequence
         if (a.b.n_seqs == 1) {
             PagedSeq<QT> q;
             q.init(a, pl, 0, false);
@@ -123,6 +124,7 @@ struct PagedRuns {
             total = q.whole * a.c.n_kv;
             largest = q.tiles ? q.cost(q.tiles - 1) : 0;
             least = q.cost(0);
+            falls = 2 * least <= largest;
         } else {
             for (int s0 = 0; s0 < a.b.n_seqs; s0 += 64) {
                 PagedSeq<QT> q;
@@ -133,11 +135,12 @@ struct PagedRuns {
                 tiles += over_lanes(q.tiles, Add());
                 largest = max(largest, over_lanes(q.tiles ? q.cost(q.tiles - 1) : 0u, Max()));
                 least = min(least, over_lanes(q.tiles ? q.cost(0) : 0xffffffffu, Min()));
+                falls = falls && __all(q.tiles == 0 || 2 * q.cost(0) <= q.cost(q.tiles - 1));
             }
         }
         const unsigned items = tiles * a.c.n_kv;
         const unsigned even = total / side, rounds = (items + side - 1) / side;
-        const unsigned expected = rounds > 1 && 2 * least <= largest ? max(largest, even + least) : rounds * largest;
+        const unsigned expected = rounds > 1 && falls ? max(largest, even + least) : rounds * largest;
         flat = items <= grid && expected <= even + pl.join;
         if (flat) total = items;
         n = total == 0 ? 0 : (flat ? (int)items : (int)max(1u, min(side, total / pl.least)));
