@@ -23,4 +23,13 @@ __device__ __forceinline__ int paged_page(const PagedBatchArgs &b, const PagedCa
     return (unsigned)page < (unsigned)c.n_pages ? page : -1;
 }
 
+// The same in two parts: the table's entry, whose load may be under way while other things are done, and what it says.  (Looked at in the step that loads it,
+// an entry makes that step wait for every load before it.)
+__device__ __forceinline__ int paged_entry(const PagedBatchArgs &b, const PagedCacheArgs &c, int seq, int position) {
+    return b.page_table[(size_t)seq * b.table_stride + min(position >> c.page_bits, b.max_pages - 1)];
+}
+__device__ __forceinline__ int paged_entry_page(const PagedBatchArgs &b, const PagedCacheArgs &c, int entry, int position) {
+    return position < b.capacity && (unsigned)entry < (unsigned)c.n_pages ? entry : -1;
+}
+
 }  // namespace spd

@@ -162,14 +162,14 @@ __global__ __launch_bounds__(NW * 64, NW / 4) void paged_few_kernel(PagedAttenti
             for (int d = 0; d < DT; ++d) acc[rt][d] = f32x4_t{0.f, 0.f, 0.f, 0.f};
         }
         uint4 kf[NK][KL], vf[DT];
-        int k_page = -1, v_page = -1;                               // of the unit whose loads come next
-        auto pages = [&](int u) {
+        int k_entry = 0, v_entry = 0, v_page = -1;                  // of the unit whose loads come next
+        auto entries = [&](int u) {
             const int key = tile_lo + u * UK;
-            k_page = paged_page(a.b, a.c, s, (key + (r >> 2) * G) >> a.c.page_bits);
-            v_page = paged_page(a.b, a.c, s, (key + g * G) >> a.c.page_bits);
+            k_entry = paged_entry(a.b, a.c, s, key + (r >> 2) * G);
+            v_entry = paged_entry(a.b, a.c, s, key + g * G);
         };
         auto load_k = [&](int u) {
-            const int slot = ((tile_lo + u * UK + (r >> 2) * G) & (P - 1)) + (r & 3);
+            const int at = tile_lo + u * UK + (r >> 2) * G, slot = (at & (P - 1)) + (r & 3), k_page = paged_entry_page(a.b, a.c, k_entry, at);
             const char *p = (const char *)a.c.k + (size_t)max(k_page, 0) * page_bytes + h * head_bytes + (size_t)(g * P + slot) * 16;
 #pragma unroll
             for (int n = 0; n < NK; ++n)
@@ -177,14 +177,15 @@ __global__ __launch_bounds__(NW * 64, NW / 4) void paged_few_kernel(PagedAttenti
                 for (int c = 0; c < KL; ++c) kf[n][c] = *reinterpret_cast<const uint4 *>(p + (size_t)c * 64 * P + n * 64);
         };
         auto load_v = [&](int u) {
-            const int slot = (tile_lo + u * UK + g * G) & (P - 1);
+            const int at = tile_lo + u * UK + g * G, slot = at & (P - 1);
+            v_page = paged_entry_page(a.b, a.c, v_entry, at);
             const char *p = (const char *)a.c.v + (size_t)max(v_page, 0) * page_bytes + h * head_bytes + (size_t)(slot / G * D + r) * 16;
 #pragma unroll
             for (int d = 0; d < DT; ++d) vf[d] = *reinterpret_cast<const uint4 *>(p + d * 256);
         };
         int u = u0 + wave;
         if (u < u1) {
-            pages(u);
+            entries(u);
             load_k(u);
             load_v(u);
         }
@@ -197,7 +198,7 @@ __global__ __launch_bounds__(NW * 64, NW / 4) void paged_few_kernel(PagedAttenti
         }
         __syncthreads();
         bool there = v_page >= 0;                                   // this lane's granule of the unit at hand
-        if (u + NW < u1) pages(u + NW);
+        if (u + NW < u1) entries(u + NW);
         for (; u < u1; u += NW) {
             const bool more = u + NW < u1;
             const int key0 = tile_lo + u * UK, key = key0 + g * G;   // key: of this lane's weights
@@ -336,9 +337,9 @@ __global__ __launch_bounds__(NW * 64, NW / 4) void paged_few_kernel(PagedAttenti
                         }
                     }
             }
-            there = v_page >= 0;
             if (more) load_v(u + NW);
-            if (u + 2 * NW < u1) pages(u + 2 * NW);
+            there = v_page >= 0;
+            if (u + 2 * NW < u1) entries(u + 2 * NW);
         }
         // ---- the waves' parts
 #pragma unroll
@@ -516,14 +517,6 @@ __global__ __launch_bounds__(256, 2) void paged_many_kernel(PagedAttentionArgs a
                     }
             }
         }
-        // The queries have to be there before the loop: the compiler does not count the loads into LDS, and a wait for the queries inside it would be one
-        // for those loads.
-#pragma unroll
-        for (int rt = 0; rt < RT; ++rt)
-#pragma unroll
-            for (int c = 0; c < KS; ++c)
-#pragma unroll
-                for (int k = 0; k < NT; ++k) asm volatile("" : "+v"(q[rt][c][k].x), "+v"(q[rt][c][k].y), "+v"(q[rt][c][k].z), "+v"(q[rt][c][k].w));
         const float factor = fmaxf(fabsf(a.scale) * kLog2e * (WIDEN ? a.c.k_scale[h] : 1.0f), 1e-37f);       // (0: positions that are not seen stay at -infinity)
         f32x4_t acc[RT][DT];
         float m[RT], l[RT];
@@ -534,19 +527,26 @@ __global__ __launch_bounds__(256, 2) void paged_many_kernel(PagedAttentionArgs a
 #pragma unroll
             for (int d = 0; d < DT; ++d) acc[rt][d] = f32x4_t{0.f, 0.f, 0.f, 0.f};
         }
-        // Pages of the steps whose loads come next: of this lane's key, and of the granules of values that this wave (e4m3: thread) brings
+        // Entries of the page table for the steps whose loads come next: of this lane's key, and of the granules of values that this wave (e4m3: thread) brings.
+        // Keys behind the tile's last are nobody's: their place need not exist.
         constexpr int VG = WIDEN ? (D == 128 ? 2 : 1) : 2;
-        int k_page = -1, v_page[VG];
+        int k_entry = 0, v_entry[VG];
         auto v_granule = [&](int i) { return WIDEN ? (tid + 256 * i) / D * 2 : wave * 2 + i; };        // of 8 keys
-        auto k_pages = [&](int j) { k_page = paged_page(a.b, a.c, s, (tile_lo + j * KT + my_key) >> a.c.page_bits); };
-        auto v_pages = [&](int j) {
+        auto k_at = [&](int j) { return tile_lo + j * KT + my_key; };
+        auto v_at = [&](int j, int i) { return tile_lo + j * KT + v_granule(i) * 8; };
+        auto page_of = [&](int entry, int key) { return key < tile_end ? paged_entry_page(a.b, a.c, entry, key) : 0; };
+        auto page_at = [&](int key) { return page_of(paged_entry(a.b, a.c, s, key), key); };
+        auto v_entries = [&](int j, int (&to)[VG]) {
 #pragma unroll
-            for (int i = 0; i < VG; ++i) v_page[i] = paged_page(a.b, a.c, s, (tile_lo + j * KT + v_granule(i) * 8) >> a.c.page_bits);
+            for (int i = 0; i < VG; ++i) to[i] = paged_entry(a.b, a.c, s, v_at(j, i));
         };
+        auto k_entries = [&](int j) { return paged_entry(a.b, a.c, s, k_at(j)); };
         uint4 kr[WIDEN ? LOADS / 2 : 1], vr[WIDEN ? LOADS / 2 : 1];
+        bool k_there = true;                                         // whether all keys of the step loaded last have a place
         auto load_k = [&](int j) {
-            const int key = tile_lo + j * KT, buf = j & 1;
-            const char *kp = (const char *)a.c.k + (size_t)max(k_page, 0) * page_bytes + h * head_bytes + (size_t)((key + my_key) & (P - 1)) * 16;
+            const int key = tile_lo + j * KT, buf = j & 1, page = page_of(k_entry, k_at(j));
+            k_there = __all(page >= 0);
+            const char *kp = (const char *)a.c.k + (size_t)max(page, 0) * page_bytes + h * head_bytes + (size_t)((key + my_key) & (P - 1)) * 16;
             if constexpr (WIDEN) {
 #pragma unroll
                 for (int i = 0; i < LOADS / 2; ++i) kr[i] = *reinterpret_cast<const uint4 *>(kp + (size_t)(wave + 4 * i) * P * 16);
@@ -561,13 +561,13 @@ __global__ __launch_bounds__(256, 2) void paged_many_kernel(PagedAttentionArgs a
 #pragma unroll
                 for (int i = 0; i < LOADS / 2; ++i) {
                     const int d = (tid + 256 * i) % D, slot = (key + v_granule(i) * 8) & (P - 1);
-                    vr[i] = *reinterpret_cast<const uint4 *>((const char *)a.c.v + (size_t)max(v_page[i], 0) * page_bytes + h * head_bytes + (size_t)(slot / G * D + d) * 16);
+                    vr[i] = *reinterpret_cast<const uint4 *>((const char *)a.c.v + (size_t)max(page_of(v_entry[i], v_at(j, i)), 0) * page_bytes + h * head_bytes + (size_t)(slot / G * D + d) * 16);
                 }
             } else {
 #pragma unroll
                 for (int i = 0; i < 2; ++i) {
                     const int slot = (key + v_granule(i) * 8) & (P - 1);
-                    const char *vp = (const char *)a.c.v + (size_t)max(v_page[i], 0) * page_bytes + h * head_bytes + (size_t)(slot / G * D + lane) * 16;
+                    const char *vp = (const char *)a.c.v + (size_t)max(page_of(v_entry[i], v_at(j, i)), 0) * page_bytes + h * head_bytes + (size_t)(slot / G * D + lane) * 16;
 #pragma unroll
                     for (int x = 0; x < D / 64; ++x) to_lds(vp + x * 1024, lds_place(&v_s[buf][wave * 2 + i][64 * x]));
                 }
@@ -619,21 +619,34 @@ __global__ __launch_bounds__(256, 2) void paged_many_kernel(PagedAttentionArgs a
             __syncthreads();
         };
         if (j0 < j1) {
-            k_pages(j0);
-            v_pages(j0);
-            there = __all(k_page >= 0);
+            // all entries that the first steps need on their way at once, with the queries; then the keys and values
+            int v_next[VG];
+            k_entry = k_entries(j0);
+            const int k_second = k_entries(min(j0 + 1, j1 - 1)), k_third = k_entries(min(j0 + 2, j1 - 1));
+            v_entries(j0, v_entry);
+            v_entries(min(j0 + 1, j1 - 1), v_next);
             load_k(j0);
+            there = k_there;
             load_v(j0);
             widen_k(j0);
             widen_v(j0);
             if (j0 + 1 < j1) {
-                k_pages(j0 + 1);
-                there_next = __all(k_page >= 0);
+                k_entry = k_second;
                 load_k(j0 + 1);
+                there_next = k_there;
                 widen_k(j0 + 1);
-                v_pages(j0 + 1);
-                if (j0 + 2 < j1) k_pages(j0 + 2);
             }
+            k_entry = k_third;
+#pragma unroll
+            for (int i = 0; i < VG; ++i) v_entry[i] = v_next[i];
+            // The queries have to be there before the loop: the compiler does not count the loads into LDS, and a wait for the queries inside it would be one
+            // for those loads.
+#pragma unroll
+            for (int rt = 0; rt < RT; ++rt)
+#pragma unroll
+                for (int c = 0; c < KS; ++c)
+#pragma unroll
+                    for (int k = 0; k < NT; ++k) asm volatile("" : "+v"(q[rt][c][k].x), "+v"(q[rt][c][k].y), "+v"(q[rt][c][k].z), "+v"(q[rt][c][k].w));
             arrived();
             scores(j0, sc);
         }
@@ -641,12 +654,12 @@ __global__ __launch_bounds__(256, 2) void paged_many_kernel(PagedAttentionArgs a
         auto enter = [&](int j) {                                    // step j's values and step j + 1's keys are in LDS after this
             arrived();
             if (j + 2 < j1) {
-                there_after = __all(k_page >= 0);
                 load_k(j + 2);
+                there_after = k_there;
             }
             if (j + 1 < j1) load_v(j + 1);
-            if (j + 3 < j1) k_pages(j + 3);
-            if (j + 2 < j1) v_pages(j + 2);
+            if (j + 3 < j1) k_entry = k_entries(j + 3);
+            if (j + 2 < j1) v_entries(j + 2, v_entry);
         };
         auto leave = [&](int j) {
             if (j + 2 < j1) widen_k(j + 2);
@@ -665,7 +678,7 @@ __global__ __launch_bounds__(256, 2) void paged_many_kernel(PagedAttentionArgs a
                 if constexpr (!WHOLE) {
                     bool here[2];
 #pragma unroll
-                    for (int u = 0; u < 2; ++u) here[u] = paged_page(a.b, a.c, s, (key0 + 32 * u + 8 * g) >> a.c.page_bits) >= 0;
+                    for (int u = 0; u < 2; ++u) here[u] = there || page_at(key0 + 32 * u + 8 * g) >= 0;
 #pragma unroll
                     for (int rt = 0; rt < RT; ++rt) {
                         Sees sees;
@@ -799,7 +812,7 @@ __global__ __launch_bounds__(256, 2) void paged_many_kernel(PagedAttentionArgs a
 #pragma unroll
                     for (int u = 0; u < 2; ++u) {
                         const int key = key0 + 32 * u + 8 * g;
-                        const bool here = paged_page(a.b, a.c, s, key >> a.c.page_bits) >= 0;
+                        const bool here = there || page_at(key) >= 0;
                         uint32_t keep[4], bad = 0;
 #pragma unroll
                         for (int i = 0; i < 4; ++i) {
