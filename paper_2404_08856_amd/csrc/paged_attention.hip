@@ -625,18 +625,22 @@ __global__ __launch_bounds__(256, 2) void paged_many_kernel(PagedAttentionArgs a
             const int k_second = k_entries(min(j0 + 1, j1 - 1)), k_third = k_entries(min(j0 + 2, j1 - 1));
             v_entries(j0, v_entry);
             v_entries(min(j0 + 1, j1 - 1), v_next);
+            int k_next = k_second, k_after = k_third;
+            asm volatile("" : "+v"(k_entry), "+v"(k_next), "+v"(k_after));
+#pragma unroll
+            for (int i = 0; i < VG; ++i) asm volatile("" : "+v"(v_entry[i]), "+v"(v_next[i]));
             load_k(j0);
             there = k_there;
             load_v(j0);
             widen_k(j0);
             widen_v(j0);
             if (j0 + 1 < j1) {
-                k_entry = k_second;
+                k_entry = k_next;
                 load_k(j0 + 1);
                 there_next = k_there;
                 widen_k(j0 + 1);
             }
-            k_entry = k_third;
+            k_entry = k_after;
 #pragma unroll
             for (int i = 0; i < VG; ++i) v_entry[i] = v_next[i];
             // The queries have to be there before the loop: the compiler does not count the loads into LDS, and a wait for the queries inside it would be one
@@ -653,6 +657,10 @@ __global__ __launch_bounds__(256, 2) void paged_many_kernel(PagedAttentionArgs a
         bool there_after = true;
         auto enter = [&](int j) {                                    // step j's values and step j + 1's keys are in LDS after this
             arrived();
+            // the entries are there as well, and have to be so for the compiler: its wait for them behind the loads below would be one for those
+            asm volatile("" : "+v"(k_entry));
+#pragma unroll
+            for (int i = 0; i < VG; ++i) asm volatile("" : "+v"(v_entry[i]));
             if (j + 2 < j1) {
                 load_k(j + 2);
                 there_after = k_there;
