@@ -987,7 +987,13 @@ __global__ __launch_bounds__(256, 2) void paged_many_kernel(PagedAttentionArgs a
 
 // ---- launches -----------------------------------------------------------------------
 
-constexpr int kFewUpto = 64;                 // packed rows of a sequence that the kernel of few rows takes at most
+// Which kernel takes what, by packed rows.  Up to a mean of kFewMean a sequence the kernel of few rows, but for sequences of more than kFewMost, which the
+// kernel of many rows takes in a launch of its own (not needed if there can be none); beyond that mean the kernel of many rows takes all.  Both / few alone /
+// many alone, us: 16 x 16 rows, 4 heads a key head, 4000 keys (mean 64) 91 / 89 / 112; 33 x 1 to 20, 500 to 8000 keys (42) 210 / 169 / 164; 64 x 1 to 4
+// (10) 205 / 202 / 245; 8 x 8 (32) 46 / 43 / 79; pieces of prompts of up to 700 rows (2450) 57 / - / 44; 17 x 1 to 481, short (241) 74 / 158 / 56.
+constexpr int kFewMean = 64, kFewMost = 256;
+// row tiles of a wave of the kernel of many rows
+constexpr int many_tiles(int NT, int held, int D) { return NT == 3 || (held == 1 && D == 128) ? 1 : 2; }
 static size_t slot_floats(int QT, int dim) { return (size_t)QT * (dim + 2); }
 
 size_t paged_attention_workspace_bytes(const PagedCacheArgs &c, const PagedBatchArgs &, int) {
@@ -1010,11 +1016,11 @@ hipError_t launch_paged_attention(const PagedAttentionArgs &a, hipStream_t strea
     pl.group = a.n_heads / a.c.n_kv;
     pl.flags = (u64 *)a.workspace;
     pl.slots = (float *)(pl.flags + 2 * kGroups);
-    // Rows of a sequence at most, as far as the host can tell: all, or, as long as no sequence is without any, all but one of each other.  What it
-    // says chooses kernels; a kernel that is alone takes every sequence.
+    // Rows of a sequence at most: all, or, as long as no sequence is without any, all but one of each other.  What that says chooses kernels; one that is
+    // alone takes every sequence.
     const int most = a.b.row_start ? std::max(1, a.b.n_rows - a.b.n_seqs + 1) : a.b.each;
-    const bool few = most * pl.group <= kFewUpto || a.b.n_rows * pl.group <= 128, many = !few && (!a.b.row_start || a.b.n_seqs == 1);
     const int mean = (a.b.n_rows + a.b.n_seqs - 1) / a.b.n_seqs * pl.group;
+    const bool few = mean <= kFewMean, both = few && most * pl.group > kFewMost;
     // costs in 31 bits: the tiles of all heads, each of no more than this many keys
     auto costs = [&](int QT, int keys, int join) {
         const u64 tiles = ((u64)a.b.n_rows * pl.group / QT + a.b.n_seqs) * a.c.n_kv, span = (u64)a.b.capacity + a.b.n_rows + 2 * QT + 64;
@@ -1023,7 +1029,6 @@ hipError_t launch_paged_attention(const PagedAttentionArgs &a, hipStream_t strea
         pl.least = std::max(1, keys >> pl.shift);
         pl.join = std::max(1, join >> pl.shift);
     };
-    const int wide = mean;
     // as many workgroups as there can be tiles, so that each may be taken by one
     auto tiles_grid = [&](int QT, u64 least) { return (unsigned)std::min<u64>(std::max(least, ((u64)a.b.n_rows * pl.group / QT + a.b.n_seqs) * a.c.n_kv), 1 << 20); };
 #define SPD_FEW(NT, C, D, RT, NW)                                                                                            \
@@ -1033,16 +1038,17 @@ hipError_t launch_paged_attention(const PagedAttentionArgs &a, hipStream_t strea
     } while (0)
 #define SPD_FEW_RT(NT, C, D)                                                                                                 \
     do {                                                                                                                     \
-        if (!many) {                                                                                                         \
-            pl.above = 0; pl.upto = few ? 0x7fffffff : kFewUpto;                                                             \
-            if (wide <= 16) SPD_FEW(NT, C, D, 1, 8);                                                                         \
-            else if (wide <= 32 || NT == 3) SPD_FEW(NT, C, D, 2, (D == 64 ? 8 : 4));                                                         \
-            else SPD_FEW(NT, C, D, (NT == 3 ? 2 : 4), (NT == 3 && D == 64 ? 8 : 4));                                                                   \
+        if (few) {                                                                                                           \
+            pl.above = 0; pl.upto = both ? kFewMost : 0x7fffffff;                                                            \
+            if (mean <= 16) SPD_FEW(NT, C, D, 1, 8);                                                                         \
+            else if (mean <= 32 || NT == 3) SPD_FEW(NT, C, D, 2, (D == 64 ? 8 : 4));                                         \
+            else SPD_FEW(NT, C, D, (NT == 3 ? 2 : 4), (NT == 3 && D == 64 ? 8 : 4));                                         \
         }                                                                                                                    \
-        if (!few) {                                                                                                          \
-            pl.above = many ? 0 : kFewUpto; pl.upto = 0x7fffffff;                                                            \
-            costs(NT == 3 ? 64 : 128, 512, 1024);                                                                                                 \
-            hipLaunchKernelGGL((paged_many_kernel<NT, C, D, (NT == 3 ? 1 : 2)>), dim3(tiles_grid(NT == 3 ? 64 : 128, kGroups)), dim3(256), 0, stream, a, pl); \
+        if (!few || both) {                                                                                                  \
+            constexpr int RT = many_tiles(NT, sizeof(C), D);                                                                 \
+            pl.above = few ? kFewMost : 0; pl.upto = 0x7fffffff;                                                             \
+            costs(64 * RT, 512, 1024);                                                                                       \
+            hipLaunchKernelGGL((paged_many_kernel<NT, C, D, RT>), dim3(tiles_grid(64 * RT, kGroups)), dim3(256), 0, stream, a, pl); \
         }                                                                                                                    \
     } while (0)
 #define SPD_FEW_D(NT, C) do { if (a.c.dim == 64) SPD_FEW_RT(NT, C, 64); else SPD_FEW_RT(NT, C, 128); } while (0)
