@@ -73,6 +73,7 @@ extern "C" {
 #define SPD_MAX_PAGED_ROWS   (1 << 20)  /* rows per paged call, and of spd_rope_apply  */
 #define SPD_MAX_PAGED_HEADS  1024  /* heads of a row                              */
 #define SPD_MAX_PAGED_POSITIONS (1 << 30)  /* positions a row of a page table reaches */
+#define SPD_MAX_PAGED_ROW_HEADS (1 << 27)  /* spd_paged_append: rows times heads of q, k and v together */
 
 typedef struct spd_model spd_model;
 

@@ -1312,6 +1312,7 @@ int32_t spd_paged_append(const spd_paged_cache *cache, const spd_paged_batch *ba
             rc = fail(SPD_ERR_INVALID_ARG, "q_out in the place of q has the strides of q");
     }
     if (rc) return rc;
+    if ((int64_t)rows * ((q ? n_heads : 0) + 2 * cache->n_kv_heads) > SPD_MAX_PAGED_ROW_HEADS) return fail(SPD_ERR_SHAPE, "rows times heads of q, k and v exceed %d", SPD_MAX_PAGED_ROW_HEADS);
     a.k = heads_args(k); a.v = heads_args(v);
     if (q) { a.q = heads_args(q); a.q_out = heads_args(q_out); a.n_heads = n_heads; }
     if (rope) a.rope = {rope->table, rope->rotary_dim, rope->interleaved != 0};

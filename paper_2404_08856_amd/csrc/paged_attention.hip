@@ -129,6 +129,7 @@ __global__ __launch_bounds__(NW * 64, NW / 4) void paged_few_kernel(PagedAttenti
         const unsigned off = pos - before, head_cost = seq.whole;
         if (off >= head_cost * a.c.n_kv) {                          // the next sequence with rows for this kernel
             before += head_cost * a.c.n_kv;
+            if (s + 1 >= a.b.n_seqs) break;
             do seq.init(a, pl, ++s, runs.flat); while (seq.tiles == 0 && s + 1 < a.b.n_seqs);
             continue;
         }
@@ -482,6 +483,7 @@ __global__ __launch_bounds__(256, 2) void paged_many_kernel(PagedAttentionArgs a
         const unsigned off = pos - before, head_cost = seq.whole;
         if (off >= head_cost * a.c.n_kv) {
             before += head_cost * a.c.n_kv;
+            if (s + 1 >= a.b.n_seqs) break;
             do seq.init(a, pl, ++s, runs.flat); while (seq.tiles == 0 && s + 1 < a.b.n_seqs);
             continue;
         }
@@ -996,8 +998,17 @@ constexpr int kFewMean = 64, kFewMost = 256;
 constexpr int many_tiles(int NT, int held, int D) { return NT == 3 || (held == 1 && D == 128) ? 1 : 2; }
 static size_t slot_floats(int QT, int dim) { return (size_t)QT * (dim + 2); }
 
-size_t paged_attention_workspace_bytes(const PagedCacheArgs &c, const PagedBatchArgs &, int) {
-    return 2 * kGroups * sizeof(u64) + 2 * kGroups * slot_floats(128, c.dim) * sizeof(float);
+// Rows of a sequence at most: all, or, as long as no sequence is without any, all but one of each other.  What that says chooses kernels; one that is
+// alone takes every sequence.
+struct Kernels { int mean; bool few, many; };
+static Kernels paged_kernels(const PagedBatchArgs &b, int group) {
+    const int most = b.row_start ? std::max(1, b.n_rows - b.n_seqs + 1) : b.each, mean = (b.n_rows + b.n_seqs - 1) / b.n_seqs * group;
+    const bool few = mean <= kFewMean;
+    return {mean, few, !few || most * group > kFewMost};
+}
+size_t paged_attention_workspace_bytes(const PagedCacheArgs &c, const PagedBatchArgs &b, int n_heads) {
+    const bool many = paged_kernels(b, n_heads / c.n_kv).many;
+    return 2 * kGroups * sizeof(u64) + 2 * (many ? kGroups * slot_floats(128, c.dim) : kFewGroups * slot_floats(64, c.dim)) * sizeof(float);
 }
 
 // A number that no workspace holds by chance, another one each call
@@ -1016,14 +1027,12 @@ hipError_t launch_paged_attention(const PagedAttentionArgs &a, hipStream_t strea
     pl.group = a.n_heads / a.c.n_kv;
     pl.flags = (u64 *)a.workspace;
     pl.slots = (float *)(pl.flags + 2 * kGroups);
-    // Rows of a sequence at most: all, or, as long as no sequence is without any, all but one of each other.  What that says chooses kernels; one that is
-    // alone takes every sequence.
-    const int most = a.b.row_start ? std::max(1, a.b.n_rows - a.b.n_seqs + 1) : a.b.each;
-    const int mean = (a.b.n_rows + a.b.n_seqs - 1) / a.b.n_seqs * pl.group;
-    const bool few = mean <= kFewMean, both = few && most * pl.group > kFewMost;
+    const Kernels use = paged_kernels(a.b, pl.group);
+    const int mean = use.mean;
+    const bool few = use.few, both = use.few && use.many;
     // costs in 31 bits: the tiles of all heads, each of no more than this many keys
     auto costs = [&](int QT, int keys, int join) {
-        const u64 tiles = ((u64)a.b.n_rows * pl.group / QT + a.b.n_seqs) * a.c.n_kv, span = (u64)a.b.capacity + a.b.n_rows + 2 * QT + 64;
+        const u64 tiles = ((u64)a.b.n_rows * pl.group / QT + a.b.n_seqs) * a.c.n_kv, span = (u64)a.b.capacity + (u64)a.b.n_rows * (pl.group / QT + 1) + 2 * QT + 256;
         pl.shift = 0;
         while (tiles * ((span >> pl.shift) + 2) >> 31) ++pl.shift;
         pl.least = std::max(1, keys >> pl.shift);

@@ -24,7 +24,7 @@ SPD_ROWS_ARE_PROBS = SPD_W_IS_BF16 = SPD_X_IS_BF16 = 1
 SPD_ROPE_INVERSE = 2
 SPD_ROPE_NONE, SPD_ROPE_LINEAR, SPD_ROPE_RAMP, SPD_ROPE_LOG_RAMP = range(4)
 SPD_MAX_ROWS, SPD_MAX_M, SPD_MAX_TOP = 64, 8, 32
-SPD_MAX_HEAD_DIM, SPD_MAX_PAGED_SEQS, SPD_MAX_PAGED_ROWS, SPD_MAX_PAGED_HEADS, SPD_MAX_PAGED_POSITIONS = 256, 4096, 1 << 20, 1024, 1 << 30
+SPD_MAX_HEAD_DIM, SPD_MAX_PAGED_SEQS, SPD_MAX_PAGED_ROWS, SPD_MAX_PAGED_HEADS, SPD_MAX_PAGED_POSITIONS, SPD_MAX_PAGED_ROW_HEADS = 256, 4096, 1 << 20, 1024, 1 << 30, 1 << 27
 
 EXPORTS = ["spd_last_error", "spd_model_bytes", "spd_model_create", "spd_model_destroy", "spd_kv_set_len",
            "spd_kv_get_len", "spd_prefill", "spd_prefill_tokens", "spd_verify_forward", "spd_draft_step",

@@ -119,6 +119,14 @@ def test_rows_of_equal_numbers_without_row_start(dtype, is_e4m3):
     check(Paged(3, [5] * 7, [0, 11, 16, 31, 32, 100, 63], 2, 64, 32, is_e4m3, fill=0.5), 4, dtype, 64, with_row_start=False)
 
 
+@pytest.mark.parametrize("dtype,is_e4m3", [(torch.float32, False), (torch.bfloat16, True)])
+@pytest.mark.parametrize("seqs", [65, 1024, 1025, 1500])
+def test_many_sequences(dtype, is_e4m3, seqs):
+    g = torch.Generator().manual_seed(seqs)
+    new = torch.randint(0, 4, (seqs,), generator=g).tolist()
+    check(Paged(seqs, new, torch.randint(0, 20, (seqs,), generator=g).tolist(), 1, 64, 16, is_e4m3, fill=0.5), 1, dtype, 64)
+
+
 @pytest.mark.parametrize("pad", [0, 1])
 @pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
 def test_rows_behind_the_last_sequence_and_queries_in_place(dtype, pad):

@@ -41,6 +41,30 @@ def test_against_64_bits(dtype, is_e4m3, new, lens, heads, kv_heads, dim, page):
 
 
 @pytest.mark.parametrize("dtype,is_e4m3", KINDS)
+@pytest.mark.parametrize("new,lens,heads,kv_heads,dim,page", [
+    ([1], [5000], 4, 1, 128, 16),                          # one head's keys over many workgroups
+    ([2, 1], [1, 4100], 2, 2, 64, 64),
+    ([3, 1, 0, 2], [2000, 40, 7, 900], 20, 2, 64, 256),    # several tiles a head
+    ([100], [1700], 4, 2, 64, 16),                         # many rows, keys shared by workgroups
+    ([66, 70], [900, 1500], 1, 1, 128, 128),
+    ([5, 300], [1200, 90], 3, 1, 64, 32),                  # few and many rows in a batch
+    ([1] * 9 + [290], [33] * 9 + [20], 2, 2, 64, 32),      # one that the mean does not tell of
+])
+def test_long_caches(dtype, is_e4m3, new, lens, heads, kv_heads, dim, page):
+    check(Paged(sum(new) + sum(lens) + dim, new, lens, kv_heads, dim, page, is_e4m3), heads, dtype)
+
+
+@pytest.mark.parametrize("dtype,is_e4m3", [(torch.float32, False), (torch.bfloat16, True)])
+@pytest.mark.parametrize("seqs,most_new,most_len,kv_heads", [(65, 1, 300, 1), (100, 2, 900, 4), (130, 1, 3, 2), (70, 40, 60, 1), (1300, 1, 5, 1)])
+def test_many_sequences(dtype, is_e4m3, seqs, most_new, most_len, kv_heads):
+    g = torch.Generator().manual_seed(seqs)
+    new = torch.randint(0, most_new + 1, (seqs,), generator=g).tolist()
+    new[-1] = most_new
+    lens = torch.randint(0, most_len + 1, (seqs,), generator=g).tolist()
+    check(Paged(seqs, new, lens, kv_heads, 64, 16, is_e4m3), kv_heads, dtype)
+
+
+@pytest.mark.parametrize("dtype,is_e4m3", KINDS)
 @pytest.mark.parametrize("window", [1, 2, 17, 64, 1000])
 def test_windows(dtype, is_e4m3, window):
     check(Paged(window, [1, 5, 90], [200, 31, 60], 2, 64, 16, is_e4m3), 6, dtype, window=window)

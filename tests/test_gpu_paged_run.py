@@ -190,3 +190,34 @@ def test_refusals_of_models_over_pages():
     refused(spd.SPD_ERR_SHAPE, rows=65)
     refused(spd.SPD_ERR_SHAPE, rope=spd.Rope(shape.head_dim + 2))
     refused(spd.SPD_ERR_CAPACITY, ws=torch.empty(256, dtype=torch.uint8, device="cuda"))
+
+
+@pytest.mark.parametrize("new", [[1, 3], [150, 9]])
+def test_offsets_beyond_32_bits(new):
+    """Pages of 512 KiB behind the first 4 GiB: append and attention there give the bits that they give in the first pages."""
+    spd = spd_mod()
+    HK, D, P, H, n_pages = 8, 128, 256, 16, 8600
+    ks, vs = spd.paged_cache_shapes(n_pages, P, HK, D)
+    cache = spd.PagedCache(torch.empty(ks, dtype=torch.bfloat16, device="cuda"), torch.empty(vs, dtype=torch.bfloat16, device="cuda"))
+    assert cache.k.numel() * 2 > 1 << 32
+    g = torch.Generator().manual_seed(6)
+    rows, lens = sum(new), torch.tensor([700, 90], dtype=torch.int32).cuda()
+    start = torch.tensor([0, new[0], rows], dtype=torch.int32).cuda()
+    qkv = torch.randn((rows, H + 2 * HK, D), generator=g).bfloat16().cuda()
+    old = torch.randn((790, 2, HK, D), generator=g).bfloat16().cuda()
+    rope, results = spd.Rope(D), []
+    for first in (0, n_pages - 8):
+        table = torch.arange(first, first + 8, dtype=torch.int32).view(2, 4).flip(0).contiguous().cuda()
+        for s, (a, b) in enumerate(((0, 700), (700, 790))):
+            spd.spd_paged_append(cache, spd.PagedBatch(table[s : s + 1], torch.zeros(1, dtype=torch.int32, device="cuda"), b - a), old[a:b, 0], old[a:b, 1])
+        q, k, v = qkv.split([H, HK, HK], 1)
+        turned, out, lse = torch.empty_like(q, memory_format=torch.contiguous_format), torch.empty((rows, H, D), dtype=torch.bfloat16, device="cuda"), torch.empty((rows, H), device="cuda")
+        batch = spd.PagedBatch(table, lens, rows, start)
+        spd.spd_paged_append(cache, batch, k, v, rope=rope, q=q, q_out=turned)
+        spd.spd_paged_attention(cache, batch, turned, out, lse_out=lse)
+        results.append((turned, out, lse, cache.k[first : first + 8].clone(), cache.v[first : first + 8].clone()))
+    torch.cuda.synchronize()
+    for x, y in zip(*[r[:3] for r in results]):
+        assert torch.equal(x, y) and torch.isfinite(x).all()
+    for page in (4, 5):                                    # two that the first sequence fills
+        assert torch.equal(results[0][3][page], results[1][3][page]) and torch.equal(results[0][4][page], results[1][4][page])

@@ -148,6 +148,13 @@ def test_appends():
     append(shape, rope=(4096, 66, 0)); append(bad, rope=(4098, 64, 0)); append(bad, flags=2)
 
 
+def test_appends_of_too_many_rows_and_heads():
+    spd, _ = lib()
+    c, b = structs({"n_kv_heads": 1024}, {"n_seqs": 1, "n_rows": 1 << 20})
+    h = spd.spd_heads(4096, 1 << 20, 64)
+    expect(spd.SPD_ERR_SHAPE, "spd_paged_append", by(c), by(b), by(h), by(h), null, null, i32(0), null, null, u32(0), null)
+
+
 def attention(code, q=(4096, 128, 64), out=(8192, 128, 64), heads=2, scale=1.0, window=0, seen=null, flags=0, ws=some, size=1 << 40):
     spd, _ = lib()
     c, b = structs({}, {})
