@@ -4,7 +4,9 @@
 //   softmax  running maximum and sum per row, in base 2
 //   output   O[d, row] = sum_key V[key, d] p[row, key]    A = 16 dims x 32 keys, B = p
 //
-// float32 rows: q and p as three bf16 terms each, exact to float32's roundings.  e4m3 keys and values are bf16 values, their scales one factor
+// float32 rows: q and p as three bf16 terms each, exact to float32's roundings.  bfloat16 rows: p, unnormalised, is rounded to bfloat16 once (each weight
+// within 2^-8 of itself, independent of the others; the output's own rounding is as large, and does not average out), its sum taken in float32 before that.
+// Sums, maxima and statistics are float32 throughout.  e4m3 keys and values are bf16 values, their scales one factor
 // of a head's scores and of its output.  The rows of the score tiles are keys in such an order that a lane ends with the weights of a whole granule
 // of keys, the 16 bytes of V that it reads for the second product: no data moves between lanes, and every load is 16 bytes of one granule.
 #include <algorithm>
@@ -42,7 +44,7 @@ __device__ __forceinline__ float agent_load(const float *p) { return __hip_atomi
 constexpr int kFewGroups = 256, kGroups = 512;        // workgroups that share tiles, at most: one or two a CU
 constexpr float kLn2 = 0.693147180559945309f, kLog2e = 1.44269504088896341f;
 
-// 8 neighbouring elements of a query as bf16 terms; flip: the sign bits to turn
+// 8 neighbouring elements of a query as bf16 terms
 template <int NT>
 __device__ __forceinline__ void load_query(const PagedAttentionArgs &a, size_t at, bool wide, uint4 (&t)[NT]) {
     if constexpr (NT == 1) {
@@ -104,8 +106,14 @@ struct Sees {
 };
 
 // ---- few rows: the waves of a workgroup share a tile's keys ----------------------------------------
-// A wave takes units of four granules of keys (32 in bf16, 64 in e4m3), one in four of the workgroup's run.  The registers of K and V are filled again for the
-// wave's next unit as soon as the product has read them.
+// A wave takes units of four granules of keys (32 in bf16, 64 in e4m3), one in NW of the workgroup's run.  The registers of K and V are filled again for the
+// wave's next unit as soon as the product has read them, straight from memory: 16 KiB a wave and 128 KiB a CU are under way at any time.
+//
+// Bound by memory: 64 sequences of 100 to 8000 keys, 32 heads on 8 of 128, one row each, bf16, 189 us, 5.6 TB/s; trees of 9 to 16 rows of 8 sequences of 1500
+// to 2047 keys, 32 heads, float32, 49.5 us, 4.8 TB/s; 4 sequences of 60000 to 131000 keys in e4m3 160 us, 4.9 TB/s.  A single row of 640 keys is a chain of
+// latencies, 11.8 us: a start of 1.2, entries of the page table and first keys 3, three rounds of units 4, joining the waves 2.
+// Eight waves of at most 256 registers: with the queries in registers instead of LDS, four waves a workgroup and two of these a CU, the trees took 59 us.
+// 32 rows a tile (RT = 2) at dims of 128 do not fit them, and take four waves: 8 x 8 rows of 32 heads on 8, 4000 keys, 43 us against 50 in two tiles of 16.
 template <int NT, class C, int D, int RT, int NW>
 __global__ __launch_bounds__(NW * 64, NW / 4) void paged_few_kernel(PagedAttentionArgs a, PagedPlan pl) {
     constexpr int QT = 16 * RT, G = 16 / sizeof(C), UK = 4 * G, HALVES = G / 8, NK = 2 * HALVES;   // NK: score tiles of a unit
@@ -446,9 +454,17 @@ __global__ __launch_bounds__(NW * 64, NW / 4) void paged_few_kernel(PagedAttenti
 }
 
 // ---- many rows: the waves of a workgroup share tiles of 64 keys in LDS -----------------------------
-// Each wave has 16 RT rows of the tile.  Keys and values come straight into LDS (e4m3: through registers, widened on the way) one tile ahead, in
+// Each wave has 16 RT rows of the tile.  Keys and values come straight into LDS (e4m3: through registers, widened on the way) ahead of their use, in
 // such an order that every operand of the matrix cores is 16 neighbouring granules: place 32 u + 16 n + r of a tile of keys holds key
 // 32 u + 8 (r / 4) + 4 n + r % 4, the row r of score tile n of unit u.
+//
+// A prompt of 4096 rows, 32 heads on 8 of 128, bf16: 163 to 188 us over runs, 730 to 840 TFLOP/s (a large bf16 product of the library reaches 1242).  A SIMD's matrix core has a
+// third of the cycles, other vector instructions about as much, and the two waves of a SIMD overlap them only in part; a tile's first loads and its results are
+// about 10 us beside 33 steps of 1.6.  Steps, one after another: scores and weights in turn on one path 422 us; a loop of its own for steps seen whole (the registers
+// of masks spilled in all) 261; the scores a step ahead, no maximum in between and operands read two groups ahead 255; tiles one by one instead of runs 188.
+// Tried: RT = 1, 201 us where RT = 2 takes 169; workgroups of eight waves, 166 there and 322 for 512 rows over 32000 keys (355), but 83 for 2 x 1351 rows of 32 heads (69);
+// a load into LDS a group of products instead of all at once, 202 (193).  Pieces of 1 to 700 rows, 14 heads on 2 of 64, window 1000, float32: 43 us, a chain of 17
+// steps of 1.4 us on CUs with one workgroup each.
 #pragma clang diagnostic push
 #pragma clang diagnostic ignored "-Winline-asm"
 __device__ __forceinline__ unsigned lds_place(const void *p) { return (unsigned)(uintptr_t)(const __attribute__((address_space(3))) void *)p; }
@@ -1031,6 +1047,7 @@ hipError_t launch_paged_attention(const PagedAttentionArgs &a, hipStream_t strea
     const int mean = use.mean;
     const bool few = use.few, both = use.few && use.many;
     // costs in 31 bits: the tiles of all heads, each of no more than this many keys
+    // keys: what a workgroup takes at least; join: what sharing costs, in keys: with 350 the pieces of prompts (above) took 56 us, with 1024 47.
     auto costs = [&](int QT, int keys, int join) {
         const u64 tiles = ((u64)a.b.n_rows * pl.group / QT + a.b.n_seqs) * a.c.n_kv, span = (u64)a.b.capacity + (u64)a.b.n_rows * (pl.group / QT + 1) + 2 * QT + 256;
         pl.shift = 0;

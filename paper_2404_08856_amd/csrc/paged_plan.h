@@ -4,7 +4,11 @@
 // (sequence, key head) make a tile.  A tile's cost is about the number of keys that its last row sees, so that the sum over a sequence's tiles has a closed
 // form; all tiles in a row (sequences, key heads, tiles) are cut into W runs of equal cost.  A workgroup takes the tiles or parts of tiles of its run.  A tile
 // that several workgroups share is joined by the last of them to arrive: each leaves its unnormalised sums and its maximum in a slot of the
-// workspace, then puts the call's number on the slot's flag, then looks whether all flags of the tile carry it.  Nobody waits.
+// workspace, then puts the call's number on the slot's flag, then looks whether all flags of the tile carry it.  Nobody waits.  (Two may find them all there: both write
+// the same.)  The flags are cleared by who has joined, so that a replay of the same call begins with none.
+//
+// A shared tile costs about 5 us with few rows and 10 with many, beside what it divides: so tiles are shared only where that is expected to pay (PagedRuns).  One token of
+// 640 keys in 32 heads 25.6 us shared over 120 workgroups, 19.1 over 36, 12.5 by a workgroup a head; 64 uneven sequences 190 us shared and 230 by a workgroup a tile.
 #pragma once
 #include "paged.h"
 
