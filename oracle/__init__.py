@@ -19,4 +19,5 @@ spec_sampling  softmax, accept test, residual distribution, fixed-point
                inverse-CDF sampler, one speculative block, whole generation
                loops (speculative and plain autoregressive).
 metrics        block efficiency and memory-bound speed-up.
+paged          rotary positions, places in a paged cache, attention over it.
 """
