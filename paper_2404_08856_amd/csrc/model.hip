@@ -1344,6 +1344,7 @@ int32_t spd_paged_attention(const spd_paged_cache *cache, const spd_paged_batch 
     rc = check_heads("q", q, a.b.n_rows, n_heads, a.c.dim, size);
     if (!rc) rc = check_heads("out", out, a.b.n_rows, n_heads, a.c.dim, size);
     if (rc) return rc;
+    if (q->data == out->data) return fail(SPD_ERR_INVALID_ARG, "out must not overlap q");
     if (!std::isfinite(scale)) return fail(SPD_ERR_INVALID_ARG, "scale must be finite");
     if (window < 0) return fail(SPD_ERR_INVALID_ARG, "window must not be negative");
     if (window && seen) return fail(SPD_ERR_INVALID_ARG, "a window and a tree of rows do not go together");

@@ -162,6 +162,10 @@ def attention(code, q=(4096, 128, 64), out=(8192, 128, 64), heads=2, scale=1.0, 
     expect(code, "spd_paged_attention", by(c), by(b), by(a), by(o), i32(heads), f32(scale), i32(window), seen, null, u32(flags), ws, sz(size), null)
 
 
+def test_attention_in_the_place_of_its_queries():
+    attention(lib()[0].SPD_ERR_INVALID_ARG, out=(4096, 128, 64))
+
+
 def test_attentions():
     spd, _ = lib()
     bad, shape = spd.SPD_ERR_INVALID_ARG, spd.SPD_ERR_SHAPE
