@@ -25,6 +25,11 @@ __device__ __forceinline__ uint32_t two_bf16(float a, float b) {
     typedef __attribute__((ext_vector_type(2))) __bf16 bf16x2_t;
     return __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2_t{a, b}), bf16x2_t));
 }
+// c + the two bf16 of x
+__device__ __forceinline__ float add_two(uint32_t x, float c) {
+    typedef __attribute__((ext_vector_type(2))) __bf16 bf16x2_t;
+    return __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2_t, x), __builtin_bit_cast(bf16x2_t, 0x3f803f80u), c, false);
+}
 // four e4m3 as four bf16, exactly
 __device__ __forceinline__ uint2 wider(uint32_t x) {
     typedef __attribute__((ext_vector_type(2))) __bf16 bf16x2_t;
@@ -41,6 +46,8 @@ __device__ __forceinline__ uint4 operand(const uint4 &x, int e) {
 __device__ __forceinline__ void agent_store(float *p, float x) { __hip_atomic_store(p, x, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
 __device__ __forceinline__ float agent_load(const float *p) { return __hip_atomic_load(p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
 
+// a slot of the workspace: QT rows' sums, then their maxima, sums of weights, and of rounded weights
+constexpr int slot_floats(int QT, int dim) { return QT * (dim + 3); }
 constexpr int kFewGroups = 256, kGroups = 512;        // workgroups that share tiles, at most: one or two a CU
 constexpr float kLn2 = 0.693147180559945309f, kLog2e = 1.44269504088896341f;
 
@@ -118,7 +125,8 @@ template <int NT, class C, int D, int RT, int NW>
 __global__ __launch_bounds__(NW * 64, NW / 4) void paged_few_kernel(PagedAttentionArgs a, PagedPlan pl) {
     constexpr int QT = 16 * RT, G = 16 / sizeof(C), UK = 4 * G, HALVES = G / 8, NK = 2 * HALVES;   // NK: score tiles of a unit
     constexpr int KS = D / 32, KL = D / (4 * G), DT = D / 16, PT = NT;                              // K-steps, loads a key row, output tiles, terms of a weight
-    __shared__ float o_s[NW][QT][D + 4], m_s[NW][QT], l_s[NW][QT];
+    constexpr bool ROUNDED = PT == 1;                                 // weights have a divisor of their own
+    __shared__ float o_s[NW][QT][D + 4], m_s[NW][QT], l_s[NW][QT], n_s[ROUNDED ? NW : 1][QT];
     __shared__ uint4 q_s[RT][KS][NT][64];                             // the queries as operands, alike for all waves
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), r = lane & 15, g = lane >> 4;
     const int P = 1 << a.c.page_bits, group = pl.group;
@@ -162,11 +170,11 @@ __global__ __launch_bounds__(NW * 64, NW / 4) void paged_few_kernel(PagedAttenti
         }
         const float factor = a.scale * kLog2e * (sizeof(C) == 1 ? a.c.k_scale[h] : 1.0f);
         f32x4_t acc[RT][DT];
-        float m[RT], l[RT];
+        float m[RT], l[RT], n[RT];                                  // maximum, sum of the weights, and as they are multiplied (ROUNDED)
 #pragma unroll
         for (int rt = 0; rt < RT; ++rt) {
             m[rt] = -INFINITY;
-            l[rt] = 0.f;
+            l[rt] = n[rt] = 0.f;
 #pragma unroll
             for (int d = 0; d < DT; ++d) acc[rt][d] = f32x4_t{0.f, 0.f, 0.f, 0.f};
         }
@@ -284,6 +292,7 @@ __global__ __launch_bounds__(NW * 64, NW / 4) void paged_few_kernel(PagedAttenti
                     sum += z[e];
                 }
                 l[rt] = __builtin_fmaf(l[rt], shrink, sum);
+                if constexpr (ROUNDED) n[rt] *= shrink;
 #pragma unroll
                 for (int d = 0; d < DT; ++d)
 #pragma unroll
@@ -300,6 +309,7 @@ __global__ __launch_bounds__(NW * 64, NW / 4) void paged_few_kernel(PagedAttenti
                             x -= bf16_lo(words[k][i]);
                             y -= bf16_hi(words[k][i]);
                         }
+                        if constexpr (ROUNDED) n[rt] = add_two(words[0][i], n[rt]);
                     }
 #pragma unroll
                     for (int k = 0; k < PT; ++k) p[rt][hv][k] = uint4{words[k][0], words[k][1], words[k][2], words[k][3]};
@@ -354,7 +364,12 @@ __global__ __launch_bounds__(NW * 64, NW / 4) void paged_few_kernel(PagedAttenti
 #pragma unroll
         for (int rt = 0; rt < RT; ++rt) {
             l[rt] = xor_reduce<32, 16>(l[rt], AddOp());
-            if (g == 0) { m_s[wave][16 * rt + r] = m[rt]; l_s[wave][16 * rt + r] = l[rt]; }
+            if constexpr (ROUNDED) n[rt] = xor_reduce<32, 16>(n[rt], AddOp());
+            if (g == 0) {
+                m_s[wave][16 * rt + r] = m[rt];
+                l_s[wave][16 * rt + r] = l[rt];
+                if constexpr (ROUNDED) n_s[wave][16 * rt + r] = n[rt];
+            }
 #pragma unroll
             for (int d = 0; d < DT; ++d) *reinterpret_cast<float4 *>(&o_s[wave][16 * rt + r][16 * d + 4 * g]) = float4{acc[rt][d][0], acc[rt][d][1], acc[rt][d][2], acc[rt][d][3]};
         }
@@ -362,13 +377,13 @@ __global__ __launch_bounds__(NW * 64, NW / 4) void paged_few_kernel(PagedAttenti
         const bool alone = x0 == 0 && x1 == cost;
         const unsigned item = pos - x0;
         const int wa = alone ? w : runs.of(item), wb = alone ? w : runs.of(item + cost - 1);
-        constexpr int kSlot = QT * (D + 2);
+        constexpr int kSlot = slot_floats(QT, D);
         float *slot = pl.slots + (size_t)(2 * w + (w == wa)) * kSlot;
         const float v_scale = sizeof(C) == 1 ? a.c.v_scale[h] : 1.0f;
-        auto finish = [&](int row, int d, float top, float sum, float (&o)[4]) {
+        auto finish = [&](int row, int d, float top, float sum, float rounded, float (&o)[4]) {
             const int pr = t * QT + row, i = pr / group, j = pr - i * group;
             const bool empty = top == -INFINITY && sum == 0.f;
-            const float by = empty ? 0.f : v_scale / sum;
+            const float by = empty ? 0.f : v_scale / (ROUNDED ? rounded : sum);
 #pragma unroll
             for (int k = 0; k < 4; ++k) o[k] = empty ? 0.f : o[k] * by;
             store_output<NT>(a, (size_t)(seq.first + i) * a.out.row + (size_t)(h * group + j) * a.out.head + d, out_wide, o);
@@ -376,7 +391,7 @@ __global__ __launch_bounds__(NW * 64, NW / 4) void paged_few_kernel(PagedAttenti
         };
         for (int idx = tid; idx < valid * (D / 4); idx += NW * 64) {
             const int row = idx / (D / 4), d = idx % (D / 4) * 4;
-            float top = m_s[0][row], sum = 0.f, o[4] = {0.f, 0.f, 0.f, 0.f};
+            float top = m_s[0][row], sum = 0.f, rounded = 0.f, o[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
             for (int k = 1; k < NW; ++k) top = fmaxf(top, m_s[k][row]);
             const float use = top > -INFINITY ? top : 0.f;
@@ -385,13 +400,14 @@ __global__ __launch_bounds__(NW * 64, NW / 4) void paged_few_kernel(PagedAttenti
                 const float f = __builtin_amdgcn_exp2f(m_s[k][row] - use);
                 const float4 x = *reinterpret_cast<const float4 *>(&o_s[k][row][d]);
                 sum = __builtin_fmaf(l_s[k][row], f, sum);
+                if constexpr (ROUNDED) rounded = __builtin_fmaf(n_s[k][row], f, rounded);
                 o[0] = __builtin_fmaf(x.x, f, o[0]);
                 o[1] = __builtin_fmaf(x.y, f, o[1]);
                 o[2] = __builtin_fmaf(x.z, f, o[2]);
                 o[3] = __builtin_fmaf(x.w, f, o[3]);
             }
             if (alone) {
-                finish(row, d, top, sum, o);
+                finish(row, d, top, sum, rounded, o);
             } else {
 #pragma unroll
                 for (int k = 0; k < 2; ++k)
@@ -399,6 +415,7 @@ __global__ __launch_bounds__(NW * 64, NW / 4) void paged_few_kernel(PagedAttenti
                 if (d == 0) {
                     agent_store(slot + QT * D + row, top);
                     agent_store(slot + QT * D + QT + row, sum);
+                    if constexpr (ROUNDED) agent_store(slot + QT * D + 2 * QT + row, rounded);
                 }
             }
         }
@@ -417,10 +434,10 @@ __global__ __launch_bounds__(NW * 64, NW / 4) void paged_few_kernel(PagedAttenti
             if (__syncthreads_and(all_there)) {                     // (two may find so: they write the same)
                 for (int idx = tid; idx < valid * (D / 4); idx += NW * 64) {
                     const int row = idx / (D / 4), d = idx % (D / 4) * 4;
-                    float top = -INFINITY, sum = 0.f, o[4] = {0.f, 0.f, 0.f, 0.f};
+                    float top = -INFINITY, sum = 0.f, rounded = 0.f, o[4] = {0.f, 0.f, 0.f, 0.f};
                     constexpr int B = 4;                              // parts whose loads are on their way together
                     for (int k0 = wa; k0 <= wb; k0 += B) {
-                        float pm[B], ps[B];
+                        float pm[B], ps[B], pn[B];
                         u64 po[B][2];
 #pragma unroll
                         for (int k = 0; k < B; ++k) {
@@ -428,6 +445,7 @@ __global__ __launch_bounds__(NW * 64, NW / 4) void paged_few_kernel(PagedAttenti
                             const float *part = pl.slots + (size_t)(2 * from + (from == wa)) * kSlot;
                             pm[k] = agent_load(part + QT * D + row);
                             ps[k] = agent_load(part + QT * D + QT + row);
+                            if constexpr (ROUNDED) pn[k] = agent_load(part + QT * D + 2 * QT + row);
 #pragma unroll
                             for (int e = 0; e < 2; ++e) po[k][e] = __hip_atomic_load(reinterpret_cast<const u64 *>(part + row * D + d) + e, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
                         }
@@ -438,11 +456,12 @@ __global__ __launch_bounds__(NW * 64, NW / 4) void paged_few_kernel(PagedAttenti
                             top = higher;
                             if (k0 + k > wb) continue;
                             sum = __builtin_fmaf(ps[k], f, sum * shrink);
+                            if constexpr (ROUNDED) rounded = __builtin_fmaf(pn[k], f, rounded * shrink);
 #pragma unroll
                             for (int e = 0; e < 4; ++e) o[e] = __builtin_fmaf(__uint_as_float((unsigned)(po[k][e / 2] >> (e % 2 * 32))), f, o[e] * shrink);
                         }
                     }
-                    finish(row, d, top, sum, o);
+                    finish(row, d, top, sum, rounded, o);
                 }
                 for (int k = wa + tid; k <= wb; k += NW * 64)            // for the next call that carries this number (a replay)
                     __hip_atomic_store(pl.flags + 2 * k + (k == wa), 0ull, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
@@ -477,6 +496,7 @@ __device__ __forceinline__ void to_lds(const void *src, unsigned dst) {
 template <int NT, class C, int D, int RT>
 __global__ __launch_bounds__(256, 2) void paged_many_kernel(PagedAttentionArgs a, PagedPlan pl) {
     constexpr int QT = 64 * RT, G = 16 / sizeof(C), KT = 64, KS = D / 32, DT = D / 16, PT = NT;
+    constexpr bool ROUNDED = PT == 1;                                 // weights have a divisor of their own
     constexpr bool WIDEN = sizeof(C) == 1;
     constexpr int LOADS = D / 8 * KT / 256;                          // granules of 16 bytes a thread brings of K, and of V (bf16)
     __shared__ uint4 k_s[2][D / 8][KT], v_s[2][KT / 8][D];
@@ -537,11 +557,11 @@ __global__ __launch_bounds__(256, 2) void paged_many_kernel(PagedAttentionArgs a
         }
         const float factor = fmaxf(fabsf(a.scale) * kLog2e * (WIDEN ? a.c.k_scale[h] : 1.0f), 1e-37f);       // (0: positions that are not seen stay at -infinity)
         f32x4_t acc[RT][DT];
-        float m[RT], l[RT];
+        float m[RT], l[RT], n[RT];                                  // maximum, sum of the weights, and as they are multiplied (ROUNDED)
 #pragma unroll
         for (int rt = 0; rt < RT; ++rt) {
             m[rt] = -INFINITY;
-            l[rt] = 0.f;
+            l[rt] = n[rt] = 0.f;
 #pragma unroll
             for (int d = 0; d < DT; ++d) acc[rt][d] = f32x4_t{0.f, 0.f, 0.f, 0.f};
         }
@@ -722,11 +742,11 @@ __global__ __launch_bounds__(256, 2) void paged_many_kernel(PagedAttentionArgs a
                 // Weights: exponentials above a row's reference, which is the maximum at the time it was set.  It is set again only where a lane's sum
                 // passes 2^10 (or nothing was seen before): the steps in between need no maximum.
                 uint4 p[RT][2][PT];
-                float sum[RT];
+                float sum[RT], rounded[RT];
                 // half a row tile's: 32 keys
                 auto weights = [&](int rt, int u) {
                     const float use = m[rt] > -INFINITY ? m[rt] : 0.f;
-                    if (u == 0) sum[rt] = 0.f;
+                    if (u == 0) sum[rt] = rounded[rt] = 0.f;
                     uint32_t words[PT][4];
 #pragma unroll
                     for (int i = 0; i < 4; ++i) {
@@ -742,6 +762,7 @@ __global__ __launch_bounds__(256, 2) void paged_many_kernel(PagedAttentionArgs a
                                 y -= bf16_hi(words[k][i]);
                             }
                         }
+                        if constexpr (ROUNDED) rounded[rt] = add_two(words[0][i], rounded[rt]);
                     }
 #pragma unroll
                     for (int k = 0; k < PT; ++k) p[rt][u][k] = uint4{words[k][0], words[k][1], words[k][2], words[k][3]};
@@ -807,6 +828,7 @@ __global__ __launch_bounds__(256, 2) void paged_many_kernel(PagedAttentionArgs a
                         const float shrink = __builtin_amdgcn_exp2f(m[rt] - (top > -INFINITY ? top : 0.f));
                         m[rt] = top;
                         l[rt] *= shrink;
+                        if constexpr (ROUNDED) n[rt] *= shrink;
 #pragma unroll
                         for (int d = 0; d < DT; ++d)
 #pragma unroll
@@ -816,7 +838,10 @@ __global__ __launch_bounds__(256, 2) void paged_many_kernel(PagedAttentionArgs a
                     }
                 }
 #pragma unroll
-                for (int rt = 0; rt < RT; ++rt) l[rt] += sum[rt];
+                for (int rt = 0; rt < RT; ++rt) {
+                    l[rt] += sum[rt];
+                    if constexpr (ROUNDED) n[rt] += rounded[rt];
+                }
                 if constexpr (WHOLE) {
 #pragma unroll
                     for (int x = 0; x < NB; ++x) {
@@ -915,14 +940,14 @@ __global__ __launch_bounds__(256, 2) void paged_many_kernel(PagedAttentionArgs a
         const bool alone = x0 == 0 && x1 == cost;
         const unsigned item = pos - x0;
         const int wa = alone ? w : runs.of(item), wb = alone ? w : runs.of(item + cost - 1);
-        constexpr int kSlot = QT * (D + 2);
+        constexpr int kSlot = slot_floats(QT, D);
         float *slot = pl.slots + (size_t)(2 * w + (w == wa)) * kSlot;
         const float v_scale = WIDEN ? a.c.v_scale[h] : 1.0f;
         auto finish = [&](int rt) {
             if (16 * rt + r >= rows) return;
             const int pr = t * QT + row0 + 16 * rt + r, i = pr / group, j = pr - i * group;
             const bool empty = m[rt] == -INFINITY && l[rt] == 0.f;
-            const float by = empty ? 0.f : v_scale / l[rt];
+            const float by = empty ? 0.f : v_scale / (ROUNDED ? n[rt] : l[rt]);
             const size_t at = (size_t)(seq.first + i) * a.out.row + (size_t)(h * group + j) * a.out.head + 4 * g;
 #pragma unroll
             for (int d = 0; d < DT; ++d) {
@@ -936,6 +961,7 @@ __global__ __launch_bounds__(256, 2) void paged_many_kernel(PagedAttentionArgs a
 #pragma unroll
         for (int rt = 0; rt < RT; ++rt) {
             l[rt] = xor_reduce<32, 16>(l[rt], AddOp());
+            if constexpr (ROUNDED) n[rt] = xor_reduce<32, 16>(n[rt], AddOp());
             if (alone) {
                 finish(rt);
             } else if (16 * rt + r < rows) {
@@ -950,6 +976,7 @@ __global__ __launch_bounds__(256, 2) void paged_many_kernel(PagedAttentionArgs a
                 if (g == 0) {
                     agent_store(slot + QT * D + row, m[rt]);
                     agent_store(slot + QT * D + QT + row, l[rt]);
+                    if constexpr (ROUNDED) agent_store(slot + QT * D + 2 * QT + row, n[rt]);
                 }
             }
         }
@@ -969,7 +996,7 @@ __global__ __launch_bounds__(256, 2) void paged_many_kernel(PagedAttentionArgs a
                 for (int rt = 0; rt < RT; ++rt) {
                     if (16 * rt + r >= rows) continue;
                     const int row = row0 + 16 * rt + r;
-                    float top = -INFINITY, sum = 0.f;
+                    float top = -INFINITY, sum = 0.f, rounded = 0.f;
                     for (int k = wa; k <= wb; ++k) top = fmaxf(top, agent_load(pl.slots + (size_t)(2 * k + (k == wa)) * kSlot + QT * D + row));
                     const float use = top > -INFINITY ? top : 0.f;
 #pragma unroll
@@ -978,6 +1005,7 @@ __global__ __launch_bounds__(256, 2) void paged_many_kernel(PagedAttentionArgs a
                         const float *part = pl.slots + (size_t)(2 * k + (k == wa)) * kSlot;
                         const float f = __builtin_amdgcn_exp2f(agent_load(part + QT * D + row) - use);
                         sum = __builtin_fmaf(agent_load(part + QT * D + QT + row), f, sum);
+                        if constexpr (ROUNDED) rounded = __builtin_fmaf(agent_load(part + QT * D + 2 * QT + row), f, rounded);
                         u64 x[DT][2];
 #pragma unroll
                         for (int d = 0; d < DT; ++d)
@@ -994,6 +1022,7 @@ __global__ __launch_bounds__(256, 2) void paged_many_kernel(PagedAttentionArgs a
                     }
                     m[rt] = top;
                     l[rt] = sum;
+                    n[rt] = rounded;
                     finish(rt);
                 }
                 for (int k = wa + tid; k <= wb; k += 256) __hip_atomic_store(pl.flags + 2 * k + (k == wa), 0ull, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
@@ -1012,7 +1041,6 @@ __global__ __launch_bounds__(256, 2) void paged_many_kernel(PagedAttentionArgs a
 constexpr int kFewMean = 64, kFewMost = 256;
 // row tiles of a wave of the kernel of many rows
 constexpr int many_tiles(int NT, int held, int D) { return NT == 3 || (held == 1 && D == 128) ? 1 : 2; }
-static size_t slot_floats(int QT, int dim) { return (size_t)QT * (dim + 2); }
 
 // Rows of a sequence at most: all, or, as long as no sequence is without any, all but one of each other.  What that says chooses kernels; one that is
 // alone takes every sequence.
@@ -1024,7 +1052,7 @@ static Kernels paged_kernels(const PagedBatchArgs &b, int group) {
 }
 size_t paged_attention_workspace_bytes(const PagedCacheArgs &c, const PagedBatchArgs &b, int n_heads) {
     const bool many = paged_kernels(b, n_heads / c.n_kv).many;
-    return 2 * kGroups * sizeof(u64) + 2 * (many ? kGroups * slot_floats(128, c.dim) : kFewGroups * slot_floats(64, c.dim)) * sizeof(float);
+    return 2 * kGroups * sizeof(u64) + 2 * (size_t)(many ? kGroups * slot_floats(128, c.dim) : kFewGroups * slot_floats(64, c.dim)) * sizeof(float);
 }
 
 // A number that no workspace holds by chance, another one each call

@@ -24,7 +24,7 @@ struct PagedPlan {
     int group;               // query heads of a key head
     int above, upto;         // takes the sequences with so many packed rows: above < rows <= upto
     u64 *flags;              // [2 * workgroups]
-    float *slots;            // [2 * workgroups][QT * (dim + 2)]
+    float *slots;            // [2 * workgroups][QT * (dim + 3)]
 };
 
 // A sequence as one kernel sees it
