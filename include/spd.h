@@ -435,7 +435,8 @@ int32_t spd_paged_append(const spd_paged_cache *h_cache, const spd_paged_batch *
  * lse_out: float32 [n_rows][n_heads] or NULL, log sum exp of the scores (-infinity for a row that sees nothing): with it, parts of
  * a softmax over several caches can be joined.
  * q, out: float32, or bfloat16 with SPD_X_IS_BF16; out must not overlap q.  Sums and statistics are float32.  Products of float32 rows are exact to float32's roundings; with
- * bfloat16 rows the softmax's weights, whose sum is taken before, are rounded to bfloat16 for the product with v.
+ * bfloat16 rows the softmax's weights are taken to 16 bits for the product with v, or, where sequences have many rows (a mean of more than 32 rows times n_heads / n_kv_heads,
+ * or more than 256 in one), to bfloat16's 8, and divided by the sum of what they were rounded to: out is off by at most 2^-8 of sum_p softmax_p |v[p] - out| before its own rounding.
  * workspace: spd_paged_attention_workspace_bytes bytes, 256-byte aligned; it may hold anything before the call, and nothing in it has to survive
  * it.  Calls that share one must not overlap; the results of calls that do are undefined, those of later calls are not, with one exception: a call captured
  * in a graph that overlapped with another needs the workspace cleared before its next replay.

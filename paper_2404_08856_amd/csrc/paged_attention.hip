@@ -4,9 +4,12 @@
 //   softmax  running maximum and sum per row, in base 2
 //   output   O[d, row] = sum_key V[key, d] p[row, key]    A = 16 dims x 32 keys, B = p
 //
-// float32 rows: q and p as three bf16 terms each, exact to float32's roundings.  bfloat16 rows: p, unnormalised, is rounded to bfloat16 once (each weight
-// within 2^-8 of itself, independent of the others; the output's own rounding is as large, and does not average out), its sum taken in float32 before that.
-// Sums, maxima and statistics are float32 throughout.  e4m3 keys and values are bf16 values, their scales one factor
+// float32 rows: q and p as three bf16 terms each, exact to float32's roundings.  bfloat16 rows: p, unnormalised, as two terms where tiles have up to 32 rows (each
+// weight within 2^-16 of itself; that kernel waits for memory, and the second product costs it nothing: 8 x 8 rows of 32 heads on 8, 4000 keys, 43 us with either), and as one
+// (within 2^-8) where they have more: there the second takes registers or the matrix core's time (16 x 16 rows, 4000 e4m3 keys, 76 us and 100; a prompt of 4096 rows 173 and
+// 213).  The roundings of a row's weights need not be independent: one key may outweigh the others, or all scores be equal.  So results of one term are divided by the sum of
+// the rounded weights, and are off by at most 2^-8 of the weighted mean of |v - result|, less than their own rounding unless the values scatter widely; lse has the sum from before
+// the rounding.  Sums, maxima and statistics are float32 throughout.  e4m3 keys and values are bf16 values, their scales one factor
 // of a head's scores and of its output.  The rows of the score tiles are keys in such an order that a lane ends with the weights of a whole granule
 // of keys, the 16 bytes of V that it reads for the second product: no data moves between lanes, and every load is 16 bytes of one granule.
 #include <algorithm>
@@ -46,7 +49,7 @@ __device__ __forceinline__ uint4 operand(const uint4 &x, int e) {
 __device__ __forceinline__ void agent_store(float *p, float x) { __hip_atomic_store(p, x, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
 __device__ __forceinline__ float agent_load(const float *p) { return __hip_atomic_load(p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
 
-// a slot of the workspace: QT rows' sums, then their maxima, sums of weights, and of rounded weights
+// A slot of the workspace: QT rows' sums, then their maxima, sums of weights, and of the weights as they are multiplied
 constexpr int slot_floats(int QT, int dim) { return QT * (dim + 3); }
 constexpr int kFewGroups = 256, kGroups = 512;        // workgroups that share tiles, at most: one or two a CU
 constexpr float kLn2 = 0.693147180559945309f, kLog2e = 1.44269504088896341f;
@@ -124,7 +127,7 @@ struct Sees {
 template <int NT, class C, int D, int RT, int NW>
 __global__ __launch_bounds__(NW * 64, NW / 4) void paged_few_kernel(PagedAttentionArgs a, PagedPlan pl) {
     constexpr int QT = 16 * RT, G = 16 / sizeof(C), UK = 4 * G, HALVES = G / 8, NK = 2 * HALVES;   // NK: score tiles of a unit
-    constexpr int KS = D / 32, KL = D / (4 * G), DT = D / 16, PT = NT;                              // K-steps, loads a key row, output tiles, terms of a weight
+    constexpr int KS = D / 32, KL = D / (4 * G), DT = D / 16, PT = NT == 1 && RT <= 2 ? 2 : NT;     // K-steps, loads a key row, output tiles, terms of a weight
     constexpr bool ROUNDED = PT == 1;                                 // weights have a divisor of their own
     __shared__ float o_s[NW][QT][D + 4], m_s[NW][QT], l_s[NW][QT], n_s[ROUNDED ? NW : 1][QT];
     __shared__ uint4 q_s[RT][KS][NT][64];                             // the queries as operands, alike for all waves

@@ -1,8 +1,8 @@
 """Attention over pages with bfloat16 rows: what the rounding of the softmax's weights may do to a result.
 
-The weights of the product with v are rounded to bfloat16 (a relative error of up to 2^-8 each, r_i = w_i (1 + e_i)), and the result is divided by the sum of the
-rounded ones:  sum r_i v_i / sum r_i - o = sum p_i e_i (v_i - o) / sum p_i (1 + e_i),  at most 2^-8 / (1 - 2^-8) of sum p_i |v_i - o|.  So what all keys of a row agree
-on, or one key outweighs, is exact to float32's roundings: those of check_attention, with the result's own rounding, 2^-8 of it."""
+Many packed rows a sequence: the weights of the product with v are rounded to bfloat16 (a relative error of up to 2^-8 each, r_i = w_i (1 + e_i)), and the result is
+divided by the sum of the rounded ones:  sum r_i v_i / sum r_i - o = sum p_i e_i (v_i - o) / sum p_i (1 + e_i),  at most 2^-8 / (1 - 2^-8) of sum p_i |v_i - o|.  So what all
+keys of a row agree on, or one key outweighs, is exact to float32's roundings, those of check_attention.  Few: two terms of bfloat16, 2^-16 of each weight."""
 import numpy as np
 import pytest
 import torch
@@ -46,7 +46,9 @@ def check(p, q, window=0):
     want, want_lse, spread, apart, work, count = exact(p, q, scale, window)
     d = (p.dim + 24) * U * work
     sums = (count[:, None] / 16 + 100) * U
-    wide = spread * (2 * d + 2 * sums)[..., None] + apart * 2.0 ** -8 * (1 + 2.0 ** -7)        # before the result's own rounding, which keeps an order
+    many = -(-q.shape[0] // len(p.new)) * (q.shape[1] // p.kv_heads) > 32
+    # before the result's own rounding, which keeps an order
+    wide = spread * (2 * d + 2 * sums)[..., None] + (apart * 2.0 ** -8 * (1 + 2.0 ** -7) if many else spread * 2.0 ** -16)
     low, high = (f64(torch.from_numpy(t).float().bfloat16()) for t in (want - wide, want + wide))
     got = f64(out)
     wrong = (got < low) | (got > high)
