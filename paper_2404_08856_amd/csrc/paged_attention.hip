@@ -171,7 +171,7 @@ __global__ __launch_bounds__(NW * 64, NW / 4) void paged_few_kernel(PagedAttenti
             const int i = (min(16 * rt + r, valid - 1) + t * QT) / group;      // (rows behind the last: the last again)
             sees[rt].init(a, seq.first, len, i);
         }
-        const float factor = a.scale * kLog2e * (sizeof(C) == 1 ? a.c.k_scale[h] : 1.0f);
+        const float factor = a.scale == 0.f ? 1.f : a.scale * kLog2e * (sizeof(C) == 1 ? a.c.k_scale[h] : 1.0f);      // (0: the queries are zeros)
         f32x4_t acc[RT][DT];
         float m[RT], l[RT], n[RT];                                  // maximum, sum of the weights, and as they are multiplied (ROUNDED)
 #pragma unroll
@@ -214,7 +214,7 @@ __global__ __launch_bounds__(NW * 64, NW / 4) void paged_few_kernel(PagedAttenti
             uint4 terms[NT];
             load_query<NT>(a, (size_t)(seq.first + i) * a.q.row + (size_t)(h * group + j) * a.q.head + (HALVES == 1 ? 32 * c + 8 * g : ((c / 2 * 4 + g) * 16 + c % 2 * 8)), q_wide, terms);
 #pragma unroll
-            for (int k = 0; k < NT; ++k) q_s[rt][c][k][lane] = terms[k];
+            for (int k = 0; k < NT; ++k) q_s[rt][c][k][lane] = a.scale == 0.f ? uint4{0, 0, 0, 0} : terms[k];
         }
         __syncthreads();
         bool there = v_page >= 0;                                   // this lane's granule of the unit at hand
@@ -281,7 +281,7 @@ __global__ __launch_bounds__(NW * 64, NW / 4) void paged_few_kernel(PagedAttenti
 #pragma unroll
                 for (int e = 0; e < G; ++e) {
                     z[e] = sc[rt][e / 4][e % 4] * factor;
-                    if (!whole && !(seen_bits[rt] >> e & 1)) z[e] = -INFINITY;            // (a factor of 0 or below)
+                    if (!whole && !(seen_bits[rt] >> e & 1)) z[e] = -INFINITY;            // (a factor below 0, or one that float32 does not hold)
                     top = fmaxf(top, z[e]);
                 }
                 top = fmaxf(max_over_rows(top), m[rt]);
@@ -548,17 +548,19 @@ __global__ __launch_bounds__(256, 2) void paged_many_kernel(PagedAttentionArgs a
             const size_t at = (size_t)(seq.first + i) * a.q.row + (size_t)(h * group + j) * a.q.head;
 #pragma unroll
             for (int c = 0; c < KS; ++c) load_query<NT>(a, at + 32 * c + 8 * g, q_wide, q[rt][c]);
-            if (a.scale < 0.f) {
+            if (a.scale <= 0.f) {
 #pragma unroll
                 for (int c = 0; c < KS; ++c)
 #pragma unroll
                     for (int i2 = 0; i2 < NT; ++i2) {
                         uint4 &x = q[rt][c][i2];
-                        x.x ^= 0x80008000u; x.y ^= 0x80008000u; x.z ^= 0x80008000u; x.w ^= 0x80008000u;
+                        if (a.scale == 0.f) x = uint4{0, 0, 0, 0};    // (a product beyond float32's range has no 0 to become)
+                        else { x.x ^= 0x80008000u; x.y ^= 0x80008000u; x.z ^= 0x80008000u; x.w ^= 0x80008000u; }
                     }
             }
         }
-        const float factor = fmaxf(fabsf(a.scale) * kLog2e * (WIDEN ? a.c.k_scale[h] : 1.0f), 1e-37f);       // (0: positions that are not seen stay at -infinity)
+        // (not 0, so that positions that are not seen stay at -infinity: with a scale of 0 the queries are zeros, others are float32's least at least)
+        const float factor = a.scale == 0.f ? 1.f : fmaxf(fabsf(a.scale) * kLog2e * (WIDEN ? a.c.k_scale[h] : 1.0f), __FLT_DENORM_MIN__);
         f32x4_t acc[RT][DT];
         float m[RT], l[RT], n[RT];                                  // maximum, sum of the weights, and as they are multiplied (ROUNDED)
 #pragma unroll
