@@ -448,7 +448,7 @@ int32_t spd_paged_attention(const spd_paged_cache *h_cache, const spd_paged_batc
 
 /* spd_verify_forward over pages instead of the model's own cache: one forward of the new rows of a batch (ragged ones too, up to SPD_MAX_ROWS
  * together), whose keys and values go into layers[l] of layer l (host array of n_layers; heads and head size those of the model, pages alike in
- * all layers) and whose attention reads them, causal or, with `seen`, over a tree of drafted tokens (then with `positions`: what a token's place in
+ * all layers) and whose attention reads them, causal or, with `seen`, over a tree of drafted tokens (then with `positions`, and refused without: what a token's place in
  * its branch says).  tokens: int32 [n_rows].  logits_out: float32 [n_rows, vocab]; those of rows behind the last sequence say nothing.  rope: the
  * model's positions (rotary_dim head_dim, its theta) or others, e.g. stretched for contexts beyond the model's; max_positions bounds nothing here.
  * The model's own cache and lengths stay as they are, the lengths of the batch are the caller's to advance.  Prompts go in pieces of up to SPD_MAX_ROWS rows.

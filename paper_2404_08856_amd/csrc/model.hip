@@ -1383,6 +1383,7 @@ int32_t spd_verify_paged_workspace_bytes(const spd_model *m, const spd_paged_cac
 int32_t spd_verify_forward_paged(spd_model *m, const int32_t *tokens, const spd_paged_cache *layers, const spd_paged_batch *batch, const spd_rope *rope, const int32_t *positions,
                                  const uint64_t *seen, float *logits_out, void *workspace, size_t workspace_bytes, void *stream) {
     if (!tokens || !rope || !logits_out) return fail(SPD_ERR_INVALID_ARG, "NULL argument to spd_verify_forward_paged");
+    if (seen && !positions) return fail(SPD_ERR_INVALID_ARG, "a tree of rows needs positions: its branches share them, which the rows' own do not say");
     PagedLayers pages{};
     PagedAppendArgs &ap = pages.append;
     PagedAttentionArgs &pa = pages.attention;
