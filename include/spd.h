@@ -451,7 +451,9 @@ int32_t spd_paged_attention(const spd_paged_cache *h_cache, const spd_paged_batc
  * all layers) and whose attention reads them, causal or, with `seen`, over a tree of drafted tokens (then with `positions`, and refused without: what a token's place in
  * its branch says).  tokens: int32 [n_rows].  logits_out: float32 [n_rows, vocab]; those of rows behind the last sequence say nothing.  rope: the
  * model's positions (rotary_dim head_dim, its theta) or others, e.g. stretched for contexts beyond the model's; max_positions bounds nothing here.
- * The model's own cache and lengths stay as they are, the lengths of the batch are the caller's to advance.  Prompts go in pieces of up to SPD_MAX_ROWS rows.
+ * The model's own cache and lengths stay as they are, the lengths of the batch are the caller's to advance: by the rows that are kept, as long as they are the first ones
+ * (everyone sees the positions below a length).  Of an accepted branch of a tree that is not so, the length takes the tokens up to the first gap, and the others go again as the
+ * first rows of the next call, which puts their keys and values where they belong.  Prompts go in pieces of up to SPD_MAX_ROWS rows.
  * Works for models in 4 bits too.  Errors as spd_paged_append and spd_paged_attention; SPD_ERR_SHAPE for other heads or more rows. */
 int32_t spd_verify_paged_workspace_bytes(const spd_model *model, const spd_paged_cache *h_layers, const spd_paged_batch *h_batch, size_t *h_bytes);
 int32_t spd_verify_forward_paged(spd_model *model, const int32_t *tokens, const spd_paged_cache *h_layers, const spd_paged_batch *h_batch,
