@@ -171,7 +171,7 @@ __global__ __launch_bounds__(NW * 64, NW / 4) void paged_few_kernel(PagedAttenti
             const int i = (min(16 * rt + r, valid - 1) + t * QT) / group;      // (rows behind the last: the last again)
             sees[rt].init(a, seq.first, len, i);
         }
-        const float factor = a.scale == 0.f ? 1.f : a.scale * kLog2e * (sizeof(C) == 1 ? a.c.k_scale[h] : 1.0f);      // (0: the queries are zeros)
+        const float factor = a.scale * kLog2e * (sizeof(C) == 1 ? a.c.k_scale[h] : 1.0f);
         f32x4_t acc[RT][DT];
         float m[RT], l[RT], n[RT];                                  // maximum, sum of the weights, and as they are multiplied (ROUNDED)
 #pragma unroll
@@ -214,7 +214,7 @@ __global__ __launch_bounds__(NW * 64, NW / 4) void paged_few_kernel(PagedAttenti
             uint4 terms[NT];
             load_query<NT>(a, (size_t)(seq.first + i) * a.q.row + (size_t)(h * group + j) * a.q.head + (HALVES == 1 ? 32 * c + 8 * g : ((c / 2 * 4 + g) * 16 + c % 2 * 8)), q_wide, terms);
 #pragma unroll
-            for (int k = 0; k < NT; ++k) q_s[rt][c][k][lane] = a.scale == 0.f ? uint4{0, 0, 0, 0} : terms[k];
+            for (int k = 0; k < NT; ++k) q_s[rt][c][k][lane] = terms[k];
         }
         __syncthreads();
         bool there = v_page >= 0;                                   // this lane's granule of the unit at hand
@@ -281,7 +281,7 @@ __global__ __launch_bounds__(NW * 64, NW / 4) void paged_few_kernel(PagedAttenti
 #pragma unroll
                 for (int e = 0; e < G; ++e) {
                     z[e] = sc[rt][e / 4][e % 4] * factor;
-                    if (!whole && !(seen_bits[rt] >> e & 1)) z[e] = -INFINITY;            // (a factor below 0, or one that float32 does not hold)
+                    if (!whole && !(seen_bits[rt] >> e & 1)) z[e] = -INFINITY;            // (a factor of 0 or below)
                     top = fmaxf(top, z[e]);
                 }
                 top = fmaxf(max_over_rows(top), m[rt]);
@@ -548,19 +548,17 @@ __global__ __launch_bounds__(256, 2) void paged_many_kernel(PagedAttentionArgs a
             const size_t at = (size_t)(seq.first + i) * a.q.row + (size_t)(h * group + j) * a.q.head;
 #pragma unroll
             for (int c = 0; c < KS; ++c) load_query<NT>(a, at + 32 * c + 8 * g, q_wide, q[rt][c]);
-            if (a.scale <= 0.f) {
+            if (a.scale < 0.f) {
 #pragma unroll
                 for (int c = 0; c < KS; ++c)
 #pragma unroll
                     for (int i2 = 0; i2 < NT; ++i2) {
                         uint4 &x = q[rt][c][i2];
-                        if (a.scale == 0.f) x = uint4{0, 0, 0, 0};    // (a product beyond float32's range has no 0 to become)
-                        else { x.x ^= 0x80008000u; x.y ^= 0x80008000u; x.z ^= 0x80008000u; x.w ^= 0x80008000u; }
+                        x.x ^= 0x80008000u; x.y ^= 0x80008000u; x.z ^= 0x80008000u; x.w ^= 0x80008000u;
                     }
             }
         }
-        // (not 0, so that positions that are not seen stay at -infinity: with a scale of 0 the queries are zeros, others are float32's least at least)
-        const float factor = a.scale == 0.f ? 1.f : fmaxf(fabsf(a.scale) * kLog2e * (WIDEN ? a.c.k_scale[h] : 1.0f), __FLT_DENORM_MIN__);
+        const float factor = fmaxf(fabsf(a.scale) * kLog2e * (WIDEN ? a.c.k_scale[h] : 1.0f), __FLT_DENORM_MIN__);       // (0: positions that are not seen stay at -infinity)
         f32x4_t acc[RT][DT];
         float m[RT], l[RT], n[RT];                                  // maximum, sum of the weights, and as they are multiplied (ROUNDED)
 #pragma unroll
@@ -1055,9 +1053,10 @@ static Kernels paged_kernels(const PagedBatchArgs &b, int group) {
     const bool few = mean <= kFewMean;
     return {mean, few, !few || most * group > kFewMost};
 }
+// flags, slots, a head of zeros
+static size_t zeros_at(bool many, int dim) { return 2 * kGroups * sizeof(u64) + 2 * (size_t)(many ? kGroups * slot_floats(128, dim) : kFewGroups * slot_floats(64, dim)) * sizeof(float); }
 size_t paged_attention_workspace_bytes(const PagedCacheArgs &c, const PagedBatchArgs &b, int n_heads) {
-    const bool many = paged_kernels(b, n_heads / c.n_kv).many;
-    return 2 * kGroups * sizeof(u64) + 2 * (size_t)(many ? kGroups * slot_floats(128, c.dim) : kFewGroups * slot_floats(64, c.dim)) * sizeof(float);
+    return zeros_at(paged_kernels(b, n_heads / c.n_kv).many, c.dim) + c.dim * sizeof(float);
 }
 
 // A number that no workspace holds by chance, another one each call
@@ -1070,7 +1069,8 @@ static u64 call_number() {
     return x ? x : 1;
 }
 
-hipError_t launch_paged_attention(const PagedAttentionArgs &a, hipStream_t stream) {
+hipError_t launch_paged_attention(const PagedAttentionArgs &args, hipStream_t stream) {
+    PagedAttentionArgs a = args;
     PagedPlan pl;
     pl.number = call_number();
     pl.group = a.n_heads / a.c.n_kv;
@@ -1079,6 +1079,11 @@ hipError_t launch_paged_attention(const PagedAttentionArgs &a, hipStream_t strea
     const Kernels use = paged_kernels(a.b, pl.group);
     const int mean = use.mean;
     const bool few = use.few, both = use.few && use.many;
+    if (a.scale == 0.f) {                  // all queries are one head of zeros: a product beyond float32's range would have no 0 to become
+        a.q = {(char *)a.workspace + zeros_at(use.many, a.c.dim), 0, 0};
+        const hipError_t rc = launch_fill_zero(a.q.p, a.c.dim * sizeof(float), stream);
+        if (rc != hipSuccess) return rc;
+    }
     // costs in 31 bits: the tiles of all heads, each of no more than this many keys
     // keys: what a workgroup takes at least; join: what sharing costs, in keys: with 350 the pieces of prompts (above) took 56 us, with 1024 47.
     auto costs = [&](int QT, int keys, int join) {
