@@ -355,7 +355,9 @@ int32_t spd_q4_matmul(const void *packed, int32_t N, int32_t K, int32_t group, c
  *     SPD_ROPE_LOG_RAMP  the same with r = (ln t_i - ln low) / (ln high - ln low)
  *   m = magnitude (1 if the model states none).
  * Positions are any int32, negative ones too: a frequency is held as a 64-bit fraction of a turn, so that the angle's place within its
- * turn is exact to 2^-32 turns however far the position.
+ * turn is exact to 2^-32 turns however far the position (of frequencies of up to a turn a position, 2 pi; one of 2^n turns loses n of its 64 bits).
+ * SPD_ROPE_LOG_RAMP is linear in the pair's index i between the indices where t_i is high and low.  Models that round those two to whole indices get the same by
+ * the low and high that belong to the whole ones: t_i = original_positions theta^(-2 i / rotary_dim) / (2 pi).
  * spd_rope_table makes the frequencies' table (spd_rope_table_bytes bytes, 16-byte aligned) once; spd_rope names it in the calls. */
 #define SPD_ROPE_NONE     0
 #define SPD_ROPE_LINEAR   1
@@ -416,8 +418,8 @@ typedef struct {
     const int32_t *page_table, *lens, *row_start;
 } spd_paged_batch;
 
-/* Appends the rows' keys and values (n_kv_heads heads of head_dim; rounded once to bfloat16, or x / scale to the nearest e4m3, ties to
- * even, limited to +-448; NaN stays NaN).  h_rope not NULL: keys are turned first, by positions[r] (int32 [n_rows]) or, if that is NULL, by the rows' own.
+/* Appends the rows' keys and values (n_kv_heads heads of head_dim; rounded once to bfloat16, or the float32 quotient x / scale to the nearest e4m3,
+ * ties to even, limited to +-448; NaN stays NaN).  h_rope not NULL: keys are turned first, by positions[r] (int32 [n_rows]) or, if that is NULL, by the rows' own.
  * h_q not NULL: n_heads heads of queries are turned in the same launch into h_q_out (which may be h_q itself).
  * Rows float32, or bfloat16 with SPD_X_IS_BF16.  Places that two rows share (a page that two sequences append to) hold either's.
  * Errors: SPD_ERR_INVALID_ARG, SPD_ERR_SHAPE; nothing is launched then. */
@@ -431,7 +433,7 @@ int32_t spd_paged_append(const spd_paged_cache *h_cache, const spd_paged_batch *
  * positions p < lens[s], and of the sequence's new rows those whose bit is set (bit j: row j; at most 64 rows of a sequence
  * can be seen): a tree of drafted tokens, whose rows have the bits of the tokens that they continue, and their own.
  * Positions that a row does not see weigh nothing, whatever they hold; so do scores of -infinity.  A row that sees nothing: out 0.
- * A key that is not finite and seen may leave its head's row NaN, such a value its element not finite.
+ * A key that is not finite and seen may leave its head's row NaN, such a value its element not finite.  A scale of 0 weighs all keys that are seen alike, whatever q holds.
  * lse_out: float32 [n_rows][n_heads] or NULL, log sum exp of the scores (-infinity for a row that sees nothing): with it, parts of
  * a softmax over several caches can be joined.
  * q, out: float32, or bfloat16 with SPD_X_IS_BF16; out must not overlap q.  Sums and statistics are float32.  Products of float32 rows are exact to float32's roundings; with

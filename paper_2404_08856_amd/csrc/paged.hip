@@ -376,7 +376,8 @@ hipError_t launch_paged_append(const PagedAppendArgs &a, hipStream_t stream) {
     g.block = (size_t)a.b.n_rows * a.c.n_kv >= (size_t)granule * 256 ? granule : 1;
     g.value_groups = (int)(((size_t)((a.b.n_rows + g.block - 1) / g.block) * a.c.n_kv + 3) / 4);
     // Few of them start first, as a wave of values waits longest; many would hold the others up: 2400 rows of 16 + 4 + 4 heads of 64 in e4m3, 155 workgroups,
-    // 9.7 us first and 11.5 last; 7100 rows of 32 + 8 + 8 heads of 128, 1775 workgroups, 46 and 41.
+    // 9.7 us first and 11.5 last; 7100 rows of 32 + 8 + 8 heads of 128, 1775 workgroups, 46 and 41.  The border is no sharp one: 2100 rows of the latter, 524 workgroups,
+    // 15.3 and 14.0, 1400 rows, 350, 12.0 and 11.3, and in e4m3, 174, 16.0 and 13.5; 700 rows, 86, 11.4 and 11.8.
     g.values_first = g.value_groups <= 512;
 #define SPD_APPEND(T, C, W, I)                                                                                               \
     do {                                                                                                                     \

@@ -119,11 +119,11 @@ struct Sees {
 // A wave takes units of four granules of keys (32 in bf16, 64 in e4m3), one in NW of the workgroup's run.  The registers of K and V are filled again for the
 // wave's next unit as soon as the product has read them, straight from memory: 16 KiB a wave and 128 KiB a CU are under way at any time.
 //
-// Bound by memory: 64 sequences of 100 to 8000 keys, 32 heads on 8 of 128, one row each, bf16, 189 us, 5.6 TB/s; trees of 9 to 16 rows of 8 sequences of 1500
-// to 2047 keys, 32 heads, float32, 49.5 us, 4.8 TB/s; 4 sequences of 60000 to 131000 keys in e4m3 160 us, 4.9 TB/s.  A single row of 640 keys is a chain of
+// Bound by memory: 64 sequences of 100 to 8000 keys, 32 heads on 8 of 128, one row each, bf16, 190 us, 5.6 TB/s; trees of 9 to 16 rows of 8 sequences of 1500
+// to 2047 keys, 32 heads, float32, 50 us, 4.7 TB/s; 4 sequences of 60000 to 131000 keys in e4m3 163 us, 4.8 TB/s.  A single row of 640 keys is a chain of
 // latencies, 11.8 us: a start of 1.2, entries of the page table and first keys 3, three rounds of units 4, joining the waves 2.
 // Eight waves of at most 256 registers: with the queries in registers instead of LDS, four waves a workgroup and two of these a CU, the trees took 59 us.
-// 32 rows a tile (RT = 2) at dims of 128 do not fit them, and take four waves: 8 x 8 rows of 32 heads on 8, 4000 keys, 43 us against 50 in two tiles of 16.
+// 32 rows a tile (RT = 2) at dims of 128 do not fit them, and take four waves: 8 x 8 rows of 32 heads on 8, 4000 keys, 43.5 us against 50 in two tiles of 16.
 template <int NT, class C, int D, int RT, int NW>
 __global__ __launch_bounds__(NW * 64, NW / 4) void paged_few_kernel(PagedAttentionArgs a, PagedPlan pl) {
     constexpr int QT = 16 * RT, G = 16 / sizeof(C), UK = 4 * G, HALVES = G / 8, NK = 2 * HALVES;   // NK: score tiles of a unit
@@ -480,10 +480,11 @@ __global__ __launch_bounds__(NW * 64, NW / 4) void paged_few_kernel(PagedAttenti
 // such an order that every operand of the matrix cores is 16 neighbouring granules: place 32 u + 16 n + r of a tile of keys holds key
 // 32 u + 8 (r / 4) + 4 n + r % 4, the row r of score tile n of unit u.
 //
-// A prompt of 4096 rows, 32 heads on 8 of 128, bf16: 163 to 188 us over runs, 730 to 840 TFLOP/s (a large bf16 product of the library reaches 1242).  A SIMD's matrix core has a
-// third of the cycles, other vector instructions about as much, and the two waves of a SIMD overlap them only in part; a tile's first loads and its results are
+// A prompt of 4096 rows, 32 heads on 8 of 128, bf16: 169 to 187 us, as the clock has it, 730 to 810 TFLOP/s (a large bf16 product of the library reaches 1242).  A SIMD's matrix
+// core has a third of the cycles, other vector instructions about as much, and the two waves of a SIMD overlap them only in part; a tile's first loads and its results are
 // about 10 us beside 33 steps of 1.6.  Steps, one after another: scores and weights in turn on one path 422 us; a loop of its own for steps seen whole (the registers
-// of masks spilled in all) 261; the scores a step ahead, no maximum in between and operands read two groups ahead 255; tiles one by one instead of runs 188.
+// of masks spilled in all) 261; the scores a step ahead, no maximum in between and operands read two groups ahead 255; tiles one by one instead of runs 188 (168 where the same
+// was timed with others); the sum of the rounded weights, an instruction for two of them, 174 there.
 // Tried: RT = 1, 201 us where RT = 2 takes 169; workgroups of eight waves, 166 there and 322 for 512 rows over 32000 keys (355), but 83 for 2 x 1351 rows of 32 heads (69);
 // a load into LDS a group of products instead of all at once, 202 (193).  Pieces of 1 to 700 rows, 14 heads on 2 of 64, window 1000, float32: 43 us: 390 tiles in
 // one round on 256 CUs, each a chain of 17 steps of 1.4 us behind the plan and first loads.
@@ -1038,9 +1039,9 @@ __global__ __launch_bounds__(256, 2) void paged_many_kernel(PagedAttentionArgs a
 // ---- launches -----------------------------------------------------------------------
 
 // Which kernel takes what, by packed rows.  Up to a mean of kFewMean a sequence the kernel of few rows, but for sequences of more than kFewMost, which the
-// kernel of many rows takes in a launch of its own (not needed if there can be none); beyond that mean the kernel of many rows takes all.  Both / few alone /
-// many alone, us: 16 x 16 rows, 4 heads a key head, 4000 keys (mean 64) 91 / 89 / 112; 33 x 1 to 20, 500 to 8000 keys (42) 210 / 169 / 164; 64 x 1 to 4
-// (10) 205 / 202 / 245; 8 x 8 (32) 46 / 43 / 79; pieces of prompts of up to 700 rows (2450) 57 / - / 44; 17 x 1 to 481, short (241) 74 / 158 / 56.
+// kernel of many rows takes in a launch of its own (not needed if there can be none); beyond that mean the kernel of many rows takes all.  As it is / few alone /
+// many alone, us: 16 x 16 rows, 4 heads a key head, 4000 keys (mean 64) 96 / 92 / 122; 33 x 1 to 20, 500 to 8000 keys (42) 178 / 175 / 172; 64 x 1 to 4
+// (10) 209 / 203 / 258; 8 x 8 (32) 45 / 44 / 85; pieces of prompts of up to 700 rows (2450) 42 / 71 / 41; 17 x 1 to 481, short (241) 53 / 148 / 53.
 constexpr int kFewMean = 64, kFewMost = 256;
 // row tiles of a wave of the kernel of many rows
 constexpr int many_tiles(int NT, int held, int D) { return NT == 3 || (held == 1 && D == 128) ? 1 : 2; }
@@ -1085,7 +1086,9 @@ hipError_t launch_paged_attention(const PagedAttentionArgs &args, hipStream_t st
         if (rc != hipSuccess) return rc;
     }
     // costs in 31 bits: the tiles of all heads, each of no more than this many keys
-    // keys: what a workgroup takes at least; join: what sharing costs, in keys: with 350 the pieces of prompts (above) took 56 us, with 1024 47.
+    // keys: what a workgroup takes at least (of sixteen batches none is more than 5 % off with half or twice as many).  join: what sharing costs, in keys: with 350 the pieces of
+    // prompts (above) took 56 us, with 1024 47; with half of what stands below one token of 640 keys takes 16.5 us (11), 17 short prompts 71 (53); with twice as much 16 x 16
+    // rows over 4000 keys 115 (96).
     auto costs = [&](int QT, int keys, int join) {
         const u64 tiles = ((u64)a.b.n_rows * pl.group / QT + a.b.n_seqs) * a.c.n_kv, span = (u64)a.b.capacity + (u64)a.b.n_rows * (pl.group / QT + 1) + 2 * QT + 256;
         pl.shift = 0;

@@ -48,7 +48,9 @@ struct PagedSeq {
         rising = most < base ? 0 : (rows && a.window ? (int)min((unsigned)tiles, (most - base) / rows) : tiles);
         whole = before(tiles);
     }
-    static constexpr int kStart = QT >= 64 ? 160 : 256;      // what a tile costs besides its keys
+    // What a tile costs besides its keys (its start and its results, in keys).  With 0 uneven batches take more (64 x 1 row 205 us, 191; 33 x 1 to 20 rows 190, 178), with
+    // twice as much 17 short prompts 69 (53).
+    static constexpr int kStart = QT >= 64 ? 160 : 256;
     // the tile at cost x < whole * heads of the sequence: head, tile, and the cost before it
     __device__ __forceinline__ void at(unsigned x, int heads, bool flat, int &h, int &t, unsigned &first_cost) const {
         if (flat) {

@@ -346,7 +346,7 @@ class Model:
                                        _ptr(logits_out, torch.float32), _stream()))
 
     def spd_verify_forward_paged(self, tokens, layers, batch, rope, logits_out, positions=None, seen=None, workspace=None):
-        """tokens [batch.n_rows] through the model over pages: layers is a PagedCache per layer, logits_out [batch.n_rows, vocab]."""
+        """tokens [batch.n_rows] through the model over pages: layers is a PagedCache per layer, logits_out [batch.n_rows, vocab]; seen (a tree) goes with positions."""
         here = _current_device()
         assert len(layers) == self.cfg.n_layers, f"expected {self.cfg.n_layers} layers, got {len(layers)}"
         assert all(c.device == here for c in layers) and batch.device == here and rope.device == here, f"pages, batch and table are on the current device {here}"
